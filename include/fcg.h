@@ -274,6 +274,147 @@ fcg_status fcg_decode_noalloc(fcg_cache* cache, int32_t layer, int32_t n_seqs, c
                               const void* q, const void* k, const void* v, void* out,
                               int32_t* positions_out, void* stream);
 
+/* ------------------------- rotary forms, appending, attention over a shared prefix */
+
+/* The cache's own rotary form (rotate-half over the whole head, theta of the
+ * descriptor) is what fcg_graft, fcg_patch_prefill and fcg_decode use.  For
+ * models of another form, a rotary handle describes it, and the calls of this
+ * section take the handle: fcg_rope_apply encodes the keys of a library
+ * segment, fcg_graft_rope grafts them, fcg_append places fresh tokens and
+ * encodes their queries, fcg_prefix_attend attends.
+ *
+ * Tensors of this section are given with strides, so that slices of a fused
+ * projection need no copy.  Strides count elements of the storage dtype; the
+ * head_dim elements of a row are adjacent.  A row may start at any element. */
+typedef struct {
+  void* data;    /* device; null = not given, where that is allowed */
+  int64_t layer; /* from a layer's tensor to the next (calls of several layers) */
+  int64_t token; /* from a token to the next; >= 0 */
+  int64_t head;  /* from a head to the next; >= 0 */
+} fcg_tensor;
+
+typedef struct fcg_rope fcg_rope;
+
+/* layout: which dimensions turn together, for pair i < rotary_dim / 2 */
+#define FCG_ROPE_HALF 0  /* i and i + rotary_dim / 2 */
+#define FCG_ROPE_PAIRS 1 /* 2i and 2i + 1 (interleaved) */
+/* scaling of the frequencies w_i = theta^(-2i / rotary_dim) for long contexts */
+#define FCG_ROPE_PLAIN 0  /* none */
+#define FCG_ROPE_LINEAR 1 /* w_i / factor (positions interpolated) */
+#define FCG_ROPE_NTK 2    /* theta * factor^(R / (R - 2)) in place of theta, R = rotary_dim (>= 4 by its rule) */
+#define FCG_ROPE_PARTS 3  /* by parts: with r = orig_tokens * w_i / (2 pi) turns over the trained length and
+                             c = (r - low_turns) / (high_turns - low_turns) clamped to [0, 1]:
+                             w_i ((1 - c) / factor + c) */
+#define FCG_ROPE_GIVEN 4  /* freqs[i] */
+
+typedef struct {
+  int32_t rotary_dim;   /* R: a multiple of 16; dimensions >= R of a head pass unturned */
+  int32_t layout;       /* FCG_ROPE_HALF or FCG_ROPE_PAIRS */
+  int32_t scaling;      /* FCG_ROPE_PLAIN .. FCG_ROPE_GIVEN; the fields below that a kind does not name are ignored */
+  double theta;         /* > 1 (not FCG_ROPE_GIVEN) */
+  double factor;        /* >= 1 (LINEAR, NTK, PARTS) */
+  double orig_tokens;   /* > 0 (PARTS) */
+  double low_turns;     /* 0 <= low_turns < high_turns (PARTS) */
+  double high_turns;
+  double attn_factor;   /* m > 0: the rotated dimensions of encoded queries and keys are multiplied by it */
+  const double* freqs;  /* host [R / 2], finite, in radians per position (GIVEN), read by the call */
+} fcg_rope_desc;
+
+/* Create a rotary handle: host memory only, usable on every device and from
+ * several threads and streams at once.
+ * Errors: EINVAL (null argument, rotary_dim not a multiple of 16 in [16, 128],
+ * a field out of its range), ENOMEM. */
+fcg_status fcg_rope_create(const fcg_rope_desc* desc, fcg_rope** out);
+/* freqs [R / 2] (host) receives the frequencies after scaling.  Errors: EINVAL. */
+fcg_status fcg_rope_frequencies(const fcg_rope* rope, double* freqs);
+fcg_status fcg_rope_destroy(fcg_rope* rope);
+
+/* Encode n_tok tokens of n_layers layers at their positions: with p = pos[t]
+ * (device int32 [n_tok], any value, shared by the layers) and m the attention
+ * factor, the pair (a, b) of every head becomes
+ *   (m (a cos(p w_i) - b sin(p w_i)), m (b cos(p w_i) + a sin(p w_i))),
+ * the angle taken in 64 bits, the turn in 32, rounded once to dtype; dimensions
+ * past rotary_dim are copied.  FCG_ROPE_BACKWARD: the gradient of that map (the
+ * angle negated, the factor kept), from the gradient of its result to that of
+ * its input.  q [n_layers][n_tok][n_q_heads][head_dim] and k alike, each with
+ * an output of its own shape; either may be left out (null pointer or zero
+ * heads).  An output may be its input (the same data and strides), and must not
+ * overlap it otherwise; rows of an output must not overlap each other, rows of
+ * an input may (stride 0).  Nothing is allocated or uploaded: the call can be
+ * captured into a graph, whose replays read pos, q and k anew.
+ * Errors: EINVAL (null rope, pos or tensor, dtype, head_dim not 64 or 128 or
+ * below rotary_dim, negative counts, flags or strides, overlapping output
+ * rows), EHIP. */
+#define FCG_ROPE_BACKWARD 1u
+fcg_status fcg_rope_apply(const fcg_rope* rope, int32_t dtype, int32_t head_dim, int32_t n_layers, int32_t n_tok,
+                          const int32_t* pos, int32_t n_q_heads, const fcg_tensor* q, const fcg_tensor* q_out,
+                          int32_t n_k_heads, const fcg_tensor* k, const fcg_tensor* k_out, uint32_t flags,
+                          void* stream);
+
+/* Cache-stitching as fcg_graft, for segments whose keys carry the rotary form
+ * of `rope`: keys turn by the angles of delta = dst[i] - src_pos0 (without the
+ * attention factor, which the encoded keys hold already), dimensions past
+ * rotary_dim and values are copied bit for bit.  Errors as fcg_graft, and
+ * EINVAL (null rope, rotary_dim above the head). */
+fcg_status fcg_graft_rope(fcg_cache* cache, const fcg_lib* lib, const fcg_rope* rope, int32_t n_items,
+                          const int32_t* seq, const int32_t* seg, const int32_t* dst, void* stream);
+
+/* Append without attending: token t (host seq[t], pos[t]) has its key encoded
+ * at pos[t] and rounded to storage, and key and value stored at pos[t], in the
+ * layers layer .. layer + n_layers - 1; with q, its query is encoded as
+ * well and written to q_out.  rope null: the cache's own rotary form, the same
+ * bits fcg_patch_prefill stores.  k, v [n_layers][n_tok][Hkv][D], q and q_out
+ * [n_layers][n_tok][Hq][D]; q_out may be q (the same data and strides), and
+ * must not overlap q otherwise, nor its own rows.  k and v both null reserve
+ * the positions only (pages mapped, positions written, their rows' content
+ * whatever the memory holds; q must be null then).  Tokens come in any
+ * order, and positions may leave holes, which fcg_patch_prefill and fcg_decode
+ * refuse to attend over and fcg_prefix_attend fills from its prefix.
+ * FCG_REPLACE: positions already written are written over (a retried span, a
+ * rejected draft) instead of refused.
+ * A call can be captured into a graph if it maps no page and the tokens form at
+ * most 64 runs (consecutive positions of one sequence at consecutive indices)
+ * on at most 384 pages; replays write the same places.
+ * Errors: EINVAL (null arrays or tensors, negative counts or strides, flags,
+ * rotary_dim above the head, overlapping rows of q_out), ERANGE (layers,
+ * sequence, position), EOVERLAP (a position given twice; one written in one of
+ * the layers, without FCG_REPLACE), ESTATE (with FCG_REPLACE: a position whose
+ * value is read from the library, FCG_ALIAS_V; a capture that would need an
+ * upload), ENOMEM (pages), EHIP. */
+#define FCG_REPLACE 1u
+fcg_status fcg_append(fcg_cache* cache, int32_t layer, int32_t n_layers, int32_t n_tok, const int32_t* seq,
+                      const int32_t* pos, const fcg_rope* rope, const fcg_tensor* q, const fcg_tensor* q_out,
+                      const fcg_tensor* k, const fcg_tensor* v, uint32_t flags, void* stream);
+
+/* Attention of a batch over one shared prefix, read once for all of it.  The
+ * prefix is positions [0, prefix_len) of sequence prefix_seq; token t (host
+ * seq[t], pos[t]) attends to it and to positions prefix_len .. pos[t] of its own
+ * sequence at one layer:
+ *   out[t] = softmax(q k^T / sqrt(D)) v,  lse[t] = ln sum exp(q k^T / sqrt(D))
+ * over these keys, query head h reading kv head h / (Hq / Hkv).  q is encoded
+ * already (fcg_append's q_out, fcg_rope_apply); nothing is written to the
+ * cache.  Positions of seq[t] below prefix_len, if any are written, are not
+ * read.  pos[t] = prefix_len - 1 attends to the prefix only; with prefix_len = 0
+ * as well there is no key, out[t] is 0 and lse[t] -inf.  prefix_len = 0 is
+ * attention over each token's own sequence (prefix_seq is then ignored).
+ * Tokens come in any order, several of a sequence, the same position twice.
+ * q, out [n_tok][Hq][D] with strides (layer strides ignored); lse fp32
+ * [n_tok][Hq], contiguous, may be null.  out may be q (the same data and
+ * strides).
+ * The split partials sit in a workspace of the cache, enlarged when a call
+ * needs more.  A call can be captured into a graph if a call as large ran
+ * before and it has at most 64 tokens of at most 16 / (Hq / Hkv) per sequence (and
+ * bf16 caches); a workspace that a capture used is kept until the cache is
+ * destroyed.
+ * Errors: EINVAL (null arrays or tensors, negative counts or strides,
+ * overlapping rows of out), ERANGE (layer, sequences, prefix_len outside [0,
+ * max_tokens], pos[t] outside [prefix_len - 1, max_tokens)), EHOLE (an attended
+ * position is not written), ESTATE (a capture that would need an upload or a
+ * larger workspace), ENOMEM, EHIP. */
+fcg_status fcg_prefix_attend(fcg_cache* cache, int32_t layer, int32_t prefix_seq, int32_t prefix_len, int32_t n_tok,
+                             const int32_t* seq, const int32_t* pos, const fcg_tensor* q, const fcg_tensor* out,
+                             float* lse, void* stream);
+
 /* ------------------------------------------------- code-cache management */
 
 /* Locality score of the cache entries (Sec. 4.1, Eq. 3; App. B.1, Eq. 8-10;

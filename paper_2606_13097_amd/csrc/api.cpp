@@ -18,6 +18,7 @@
 #include "fcg.h"
 #include "kernels.hpp"
 #include "locality.hpp"
+#include "objects.hpp"
 #include "planner.hpp"
 
 using namespace fcg;
@@ -35,19 +36,11 @@ fcg_status fail(fcg_status s, const std::string& msg) {
 
 fcg_status fcg::report(fcg_status s, const std::string& msg) { return fail(s, msg); }
 
-namespace {
-
-fcg_status hip_fail(hipError_t e, const char* what) {
+fcg_status fcg::hip_fail(hipError_t e, const char* what) {
   return fail(FCG_EHIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
-#define HIP_TRY(expr, what)                          \
-  do {                                               \
-    hipError_t e_ = (expr);                          \
-    if (e_ != hipSuccess) return hip_fail(e_, what); \
-  } while (0)
-
-size_t esize(int32_t dtype) { return dtype == FCG_F32 ? 4 : 2; }
+namespace {
 
 fcg_status check_desc(const fcg_model_desc* d) {
   if (!d) return fail(FCG_EINVAL, "null model descriptor");
@@ -77,202 +70,7 @@ fcg_status upload_inv_freq(const fcg_model_desc& d, double** out) {
   return FCG_OK;
 }
 
-// Staging of per-call plans: a pinned host ring mirrored by a device ring.  A
-// call packs its arrays into one blob, which one kernel on the call's stream
-// takes from the host ring (upload), and records an event after its last kernel;
-// a region is reused only after its event.
-struct Ring {
-  char* host = nullptr;
-  char* dev = nullptr;
-  size_t cap = 0, head = 0;
-  std::deque<std::tuple<size_t, size_t, hipEvent_t>> inflight;
-  std::vector<hipEvent_t> spare;
-
-  ~Ring() { release(); }
-  void release() {
-    for (auto& f : inflight) {
-      hipEventSynchronize(std::get<2>(f));
-      hipEventDestroy(std::get<2>(f));
-    }
-    inflight.clear();
-    for (auto e : spare) hipEventDestroy(e);
-    spare.clear();
-    if (host) hipHostFree(host);
-    if (dev) hipFree(dev);
-    host = dev = nullptr;
-    cap = head = 0;
-  }
-  fcg_status reserve(size_t n) {
-    if (n <= cap) return FCG_OK;
-    size_t nc = std::max<size_t>(cap * 2, std::max<size_t>(n, 1 << 20));
-    release();
-    HIP_TRY(hipHostMalloc((void**)&host, nc, hipHostMallocDefault), "hipHostMalloc(staging)");
-    HIP_TRY(hipMalloc((void**)&dev, nc), "hipMalloc(staging)");
-    cap = nc;
-    return FCG_OK;
-  }
-  // Region [off, off + n) of both rings, free for writing.
-  fcg_status acquire(size_t n, size_t* off) {
-    fcg_status st = reserve(n);
-    if (st) return st;
-    if (head + n > cap) head = 0;
-    const size_t a = head, b = head + n;
-    for (auto it = inflight.begin(); it != inflight.end();) {
-      if (std::get<1>(*it) <= a || std::get<0>(*it) >= b) {
-        ++it;
-        continue;
-      }
-      HIP_TRY(hipEventSynchronize(std::get<2>(*it)), "hipEventSynchronize(staging)");
-      spare.push_back(std::get<2>(*it));
-      it = inflight.erase(it);
-    }
-    head = b;
-    *off = a;
-    return FCG_OK;
-  }
-  fcg_status retire(size_t off, size_t n, hipStream_t s) {
-    hipEvent_t e;
-    if (!spare.empty()) {
-      e = spare.back();
-      spare.pop_back();
-    } else {
-      HIP_TRY(hipEventCreateWithFlags(&e, hipEventDisableTiming), "hipEventCreate");
-    }
-    HIP_TRY(hipEventRecord(e, s), "hipEventRecord");
-    inflight.emplace_back(off, off + n, e);
-    return FCG_OK;
-  }
-};
-
-// Packs host arrays into one blob with 256-byte aligned members.
-struct Blob {
-  std::vector<char> bytes;
-  size_t add(const void* p, size_t n) {
-    size_t off = (bytes.size() + 255) & ~size_t(255);
-    bytes.resize(off + n);
-    if (n) std::memcpy(bytes.data() + off, p, n);
-    return off;
-  }
-};
-
 }  // namespace
-
-struct Segment {
-  int64_t tok_off;  // first token in the device slabs, -1 while offloaded
-  int32_t len, src_pos0;
-  int64_t host_off = -1;  // first token in the pinned host slabs, -1 without a host copy
-  mutable int32_t pins = 0;  // FCG_ALIAS_V caches reading this segment's values in place
-};
-
-struct fcg_lib {
-  fcg_model_desc desc;
-  int64_t cap = 0, used = 0;              // device slab tokens: capacity, high-water mark
-  std::map<int64_t, int64_t> free_tok;    // device token ranges below `used` freed by offloads (start -> length)
-  int32_t max_segments = 0;
-  uint32_t flags = 0;
-  std::vector<Segment> segs;
-  void* k = nullptr;
-  void* v = nullptr;
-  int device = 0;
-  // host tier (fcg_lib_host_reserve): pinned [L][Hkv][host_cap][D] slabs, filled once per segment
-  int64_t host_cap = 0, host_used = 0;
-  void* host_k = nullptr;
-  void* host_v = nullptr;
-  hipEvent_t freed = nullptr;  // after the copies that read the last freed device range
-  // Ordering across streams (offload / reload on a side stream beside grafts):
-  // a graft waits for the last reload; a reload or an ingest into a freed
-  // range waits for the last graft (which may still read that range) and the
-  // offload that freed it.
-  mutable hipEvent_t graft_done = nullptr;
-  hipEvent_t reload_done = nullptr;
-
-  // first fit among freed ranges, else past the high-water mark; -1 if nothing fits
-  int64_t alloc(int64_t len) {
-    for (auto it = free_tok.begin(); it != free_tok.end(); ++it)
-      if (it->second >= len) {
-        const int64_t off = it->first, rest = it->second - len;
-        free_tok.erase(it);
-        if (rest) free_tok[off + len] = rest;
-        return off;
-      }
-    if (used + len > cap) return -1;
-    used += len;
-    return used - len;
-  }
-  void release(int64_t off, int64_t len) {
-    auto it = free_tok.emplace(off, len).first;
-    auto nx = std::next(it);
-    if (nx != free_tok.end() && it->first + it->second == nx->first) {
-      it->second += nx->second;
-      free_tok.erase(nx);
-    }
-    if (it != free_tok.begin()) {
-      auto pv = std::prev(it);
-      if (pv->first + pv->second == it->first) {
-        pv->second += it->second;
-        free_tok.erase(it);
-        it = pv;
-      }
-    }
-    if (it->first + it->second == used) {  // the top range returns to the high-water mark
-      used = it->first;
-      free_tok.erase(it);
-    }
-  }
-};
-
-struct fcg_cache {
-  fcg_model_desc desc;
-  int32_t n_seqs, max_tokens, page_size, n_pages;
-  uint32_t flags;
-  Planner plan;
-  void* k = nullptr;
-  void* v = nullptr;
-  int64_t layer_stride = 0;
-  int32_t* d_page_table = nullptr;
-  double* d_inv_freq = nullptr;
-  float2* d_rope = nullptr;   // (cos, sin) per position and rotary pair [max_tokens][D/2]
-  int device = 0;
-  Ring ring;
-  // workspaces, grown on demand
-  void* qws = nullptr;
-  size_t qws_bytes = 0;
-  float* part = nullptr;
-  size_t part_bytes = 0;
-  float* dpart = nullptr;     // decode split partials
-  size_t dpart_bytes = 0;
-  const fcg_lib* alias_lib = nullptr;  // FCG_ALIAS_V: the library value pages map onto (bound by the first graft)
-  std::vector<std::vector<int32_t>> alias_segs;  // per sequence: segments it pins in alias_lib
-  int32_t* d_count = nullptr; // decode merge arrival counters [kMaxDecodeSeqs][Hkv] (kCountStride apart), zero between launches
-  // kernel timing (fcg_cache_timing): recorded (start, end) event pairs per kind
-  bool timing = false;
-  std::vector<std::pair<hipEvent_t, hipEvent_t>> spans[5];
-  std::vector<hipEvent_t> ev_pool;
-  std::unordered_map<hipEvent_t, int> ev_refs;
-
-  fcg_cache(const fcg_model_desc& d, int32_t ns, int32_t mt, int32_t ps, int32_t np, uint32_t fl)
-      : desc(d), n_seqs(ns), max_tokens(mt), page_size(ps), n_pages(np), flags(fl),
-        plan(d.n_layers, ns, mt, ps, np, (fl & FCG_ALIAS_V) != 0) {}
-  bool layout_only() const { return flags & FCG_LAYOUT_ONLY; }
-
-  CacheView view() const {
-    CacheView c;
-    c.k = k;
-    c.v = v;
-    c.layer_stride = layer_stride;
-    c.page_table = d_page_table;
-    c.v_alias = plan.alias_v() && d_page_table ? d_page_table + plan.n_logical_pages() : nullptr;
-    c.lib_v = alias_lib ? alias_lib->v : nullptr;
-    c.lib_cap = alias_lib ? alias_lib->cap : 0;
-    c.n_seqs = n_seqs;
-    c.max_tokens = max_tokens;
-    c.page_size = page_size;
-    c.n_lp = plan.n_logical_pages();
-    c.n_kv_heads = desc.n_kv_heads;
-    c.head_dim = desc.head_dim;
-    return c;
-  }
-};
 
 namespace {
 
@@ -325,7 +123,18 @@ void time_drop(fcg_cache* c, hipEvent_t e) {
   }
 }
 
-fcg_status grow(void** p, size_t* have, size_t need, const char* what) {
+// The device row of seq: its page row, then its value-alias row.
+size_t stage_row(const fcg_cache* c, int32_t seq, Blob* blob) {
+  const size_t nlp = c->plan.n_logical_pages();
+  std::vector<int32_t> row(2 * nlp);
+  std::memcpy(row.data(), c->plan.page_row(seq), nlp * sizeof(int32_t));
+  std::memcpy(row.data() + nlp, c->plan.alias_row(seq), nlp * sizeof(int32_t));
+  return blob->add(row.data(), row.size() * sizeof(int32_t));
+}
+
+}  // namespace
+
+fcg_status fcg::grow(void** p, size_t* have, size_t need, const char* what) {
   if (need <= *have) return FCG_OK;
   // at least twice the old size, so that a workload whose need creeps up (a
   // sequence crossing a split boundary every few decode steps) reallocates
@@ -343,20 +152,8 @@ fcg_status grow(void** p, size_t* have, size_t need, const char* what) {
   return FCG_OK;
 }
 
-// The device row of seq: its page row, then its value-alias row.
-size_t stage_row(const fcg_cache* c, int32_t seq, Blob* blob) {
-  const size_t nlp = c->plan.n_logical_pages();
-  std::vector<int32_t> row(2 * nlp);
-  std::memcpy(row.data(), c->plan.page_row(seq), nlp * sizeof(int32_t));
-  std::memcpy(row.data() + nlp, c->plan.alias_row(seq), nlp * sizeof(int32_t));
-  return blob->add(row.data(), row.size() * sizeof(int32_t));
-}
-
-// After a planner check: map the new pages, and prepare the device copies of
-// the page-table rows that change (appended to the blob): those of the new
-// pages' sequences and of `seqs`.
-void stage_pages(fcg_cache* c, const std::vector<std::pair<int32_t, int32_t>>& new_pages, Blob* blob,
-                 std::vector<std::pair<int32_t, size_t>>* rows, std::vector<int32_t> seqs = {}) {
+void fcg::stage_pages(fcg_cache* c, const std::vector<std::pair<int32_t, int32_t>>& new_pages, Blob* blob,
+                      std::vector<std::pair<int32_t, size_t>>* rows, std::vector<int32_t> seqs) {
   c->plan.map_pages(new_pages);
   for (auto& sl : new_pages)  // in (sequence, logical page) order
     if (seqs.empty() || seqs.back() != sl.first) seqs.push_back(sl.first);
@@ -365,12 +162,8 @@ void stage_pages(fcg_cache* c, const std::vector<std::pair<int32_t, int32_t>>& n
   for (int32_t s : seqs) rows->push_back({s, stage_row(c, s, blob)});
 }
 
-// Upload a plan: the staged page rows (at the front of the blob, in the order
-// staged) into the device page table, the rest of the blob into the device ring,
-// both read by one small kernel from the pinned ring.  *dev and *off_out receive
-// the blob's place in the device ring.
-fcg_status upload(fcg_cache* c, const Blob& blob, const std::vector<std::pair<int32_t, size_t>>& rows,
-                  hipStream_t s, char** dev, size_t* off_out) {
+fcg_status fcg::upload(fcg_cache* c, const Blob& blob, const std::vector<std::pair<int32_t, size_t>>& rows,
+                       hipStream_t s, char** dev, size_t* off_out) {
   const size_t n = std::max<size_t>((blob.bytes.size() + 255) & ~size_t(255), 256);
   size_t off;
   fcg_status st = c->ring.acquire(n, &off);
@@ -397,8 +190,6 @@ fcg_status upload(fcg_cache* c, const Blob& blob, const std::vector<std::pair<in
   *off_out = off;
   return FCG_OK;
 }
-
-}  // namespace
 
 extern "C" {
 
@@ -844,6 +635,7 @@ fcg_status fcg_cache_destroy(fcg_cache* c) {
     if (c->d_rope) hipFree(c->d_rope);
     if (c->qws) hipFree(c->qws);
     if (c->part) hipFree(c->part);
+    if (c->xpart) hipFree(c->xpart);
     if (c->dpart) hipFree(c->dpart);
     if (c->d_count) hipFree(c->d_count);
     for (auto& v : c->spans)
@@ -860,8 +652,11 @@ fcg_status fcg_cache_destroy(fcg_cache* c) {
 
 // ----------------------------------------------------------------- hot path
 
-fcg_status fcg_graft(fcg_cache* c, const fcg_lib* lib, int32_t n_items, const int32_t* seq, const int32_t* seg,
-                     const int32_t* dst, void* stream) {
+namespace {
+
+// rope null: the cache's own rotary form
+fcg_status graft(fcg_cache* c, const fcg_lib* lib, const fcg_rope* rope, int32_t n_items, const int32_t* seq,
+                 const int32_t* seg, const int32_t* dst, void* stream) {
   if (!c || !lib) return fail(FCG_EINVAL, "null cache or library");
   if (n_items < 0) return fail(FCG_EINVAL, "negative item count");
   if (n_items > 0 && (!seq || !seg || !dst)) return fail(FCG_EINVAL, "null item array");
@@ -935,8 +730,11 @@ fcg_status fcg_graft(fcg_cache* c, const fcg_lib* lib, int32_t n_items, const in
   if (!(lib->flags & FCG_LAYOUT_ONLY))  // segments reloaded on another stream are in place first
     HIP_TRY(hipStreamWaitEvent(s, lib->reload_done, 0), "hipStreamWaitEvent");
   const KTime tg{timing_event(c), timing_event(c)};
-  int rc = launch_graft(c->desc.dtype, by_value ? nullptr : (const GraftChunk*)(dev + o_chunks), args, (int)n_runs,
-                        lib->k, lib->v, lib->cap, c->view(), c->d_inv_freq, c->desc.n_layers, s, tg);
+  const GraftChunk* runs = by_value ? nullptr : (const GraftChunk*)(dev + o_chunks);
+  const int rc = rope ? launch_graft_rope(c->desc.dtype, rope->pairs(), runs, args, (int)n_runs, lib->k, lib->v, lib->cap,
+                                          c->view(), rope->args(), c->desc.n_layers, s, tg)
+                      : launch_graft(c->desc.dtype, runs, args, (int)n_runs, lib->k, lib->v, lib->cap, c->view(),
+                                     c->d_inv_freq, c->desc.n_layers, s, tg);
   time_open(c, FCG_TIME_GRAFT, tg.start);
   time_close(c, FCG_TIME_GRAFT, tg.stop);
   if (rc) return hip_fail((hipError_t)rc, "graft launch");
@@ -945,6 +743,20 @@ fcg_status fcg_graft(fcg_cache* c, const fcg_lib* lib, int32_t n_items, const in
     if (fcg_status st = c->ring.retire(off, blob.bytes.size(), s)) return st;
   for (auto& sp : spans) c->plan.mark_all_layers(sp.seq, sp.dst, sp.len);
   return FCG_OK;
+}
+
+}  // namespace
+
+fcg_status fcg_graft(fcg_cache* c, const fcg_lib* lib, int32_t n_items, const int32_t* seq, const int32_t* seg,
+                     const int32_t* dst, void* stream) {
+  return graft(c, lib, nullptr, n_items, seq, seg, dst, stream);
+}
+
+fcg_status fcg_graft_rope(fcg_cache* c, const fcg_lib* lib, const fcg_rope* rope, int32_t n_items, const int32_t* seq,
+                          const int32_t* seg, const int32_t* dst, void* stream) {
+  if (!rope) return fail(FCG_EINVAL, "null rope");
+  if (c && rope->rot > c->desc.head_dim) return fail(FCG_EINVAL, "rotary_dim exceeds head_dim");
+  return graft(c, lib, rope, n_items, seq, seg, dst, stream);
 }
 
 namespace {

@@ -220,4 +220,19 @@ __device__ __forceinline__ void rope_cs(double pos, double w, float* c, float* s
   *s = (float)sd;
 }
 
+// cos and sin of pos * w for a rotary pair, w given as `turns` = w / (2 pi) turns
+// per position: the product and its distance to the nearest whole turn are
+// float64 (exact after the product's rounding, 2^-53 of up to 2^31 turns), the
+// rest of the angle is at most half a turn and goes through the fp32 sincospi,
+// so each of the two is within about 2^-23 of the definition at any position.
+// The float64 sincos of rope_cs costs several times as much, most of it the
+// range reduction that one rint does here.
+__device__ __forceinline__ void rope_cs_turns(double pos, double turns, float* c, float* s) {
+  const double t = pos * turns;
+  sincospif(2.f * (float)(t - rint(t)), s, c);
+}
+
+// 16 and 8 bytes to any address
+__device__ __forceinline__ void st16_any(void* p, const uint4& v) { __builtin_memcpy(p, &v, 16); }
+
 }  // namespace fcg

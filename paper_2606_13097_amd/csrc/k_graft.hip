@@ -71,10 +71,31 @@ struct RunsInMemory {
   __device__ __forceinline__ GraftChunk get(int b) const { return p[b]; }
 };
 
-template <typename T, int D, bool PAGED, typename Runs>
+// The turn of a block's keys.  The cache's own form: rotate-half over the whole
+// head.  A form by value (RopeArgs): a lane's two vectors of a key row hold both
+// ends of VEC pairs in every form (k_rope.hip), or dimensions that pass unturned.
+struct OwnForm {
+  const double* inv_freq;
+  static constexpr bool kPairs = false;
+  __device__ __forceinline__ int turned(int half) const { return half; }
+  __device__ __forceinline__ void cs(int delta, int i, float* c, float* s) const {
+    rope_cs((double)delta, inv_freq[i], c, s);
+  }
+};
+template <bool PAIRS>
+struct GivenForm {
+  RopeArgs ra;
+  static constexpr bool kPairs = PAIRS;
+  __device__ __forceinline__ int turned(int) const { return ra.rot / 2; }
+  __device__ __forceinline__ void cs(int delta, int i, float* c, float* s) const {
+    rope_cs_turns((double)delta, ra.turns[i], c, s);
+  }
+};
+
+template <typename T, int D, bool PAGED, typename Runs, typename Form>
 __global__ void __launch_bounds__(256) graft_kernel(Runs runs, const T* __restrict__ lib_k,
                                                     const T* __restrict__ lib_v, int64_t cap, CacheView cv,
-                                                    const double* __restrict__ inv_freq) {
+                                                    Form form) {
   constexpr int VEC = Store<T>::VEC;
   constexpr int HALF = D / 2;
   constexpr int KT = HALF / VEC;            // lanes per key row (each owns a pair of vectors)
@@ -124,11 +145,15 @@ __global__ void __launch_bounds__(256) graft_kernel(Runs runs, const T* __restri
   // row (their stores are skipped), so the loads carry no branches
   uint4 klo[KP], khi[KP], vv[VP];
   const int kc = t % KT, kr = t / KT;
+  const int nturn = form.turned(HALF);          // turned pairs
+  const bool turn = kc * VEC < nturn;
+  const int lo = Form::kPairs || !turn ? 2 * kc * VEC : kc * VEC;
+  const int hi = Form::kPairs || !turn ? lo + VEC : nturn + kc * VEC;
 #pragma unroll
   for (int p = 0; p < KP; ++p) {
     const int j = min(p * KR + kr, ch.n - 1);
-    klo[p] = ld_lib<PAGED>(sk + (int64_t)j * D + kc * VEC);
-    khi[p] = ld_lib<PAGED>(sk + (int64_t)j * D + HALF + kc * VEC);
+    klo[p] = ld_lib<PAGED>(sk + (int64_t)j * D + lo);
+    khi[p] = ld_lib<PAGED>(sk + (int64_t)j * D + hi);
   }
   const int vc = t % VT, vr = t / VT;
   // values: not read or written on pages the segment covers entirely when
@@ -144,13 +169,13 @@ __global__ void __launch_bounds__(256) graft_kernel(Runs runs, const T* __restri
     }
   }
   // cos/sin of the run's delta, while the loads are in flight
-  if (t < HALF) rope_cs((double)ch.delta, inv_freq[t], &s_cos[t], &s_sin[t]);
+  if (t < nturn) form.cs(ch.delta, t, &s_cos[t], &s_sin[t]);
   __syncthreads();  // cos/sin ready
 
   float c[VEC], s[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
-    c[e] = s_cos[kc * VEC + e];
+    c[e] = s_cos[kc * VEC + e];  // not used by a lane past the turned pairs
     s[e] = s_sin[kc * VEC + e];
   }
 #pragma unroll
@@ -162,12 +187,20 @@ __global__ void __launch_bounds__(256) graft_kernel(Runs runs, const T* __restri
       Store<T>::unpack(khi[p], x2);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        y1[e] = fmaf(x1[e], c[e], -x2[e] * s[e]);
-        y2[e] = fmaf(x2[e], c[e], x1[e] * s[e]);
+        if (Form::kPairs) {  // pair kc VEC + e: elements 2e, 2e + 1 of the two vectors end to end
+          const int i = (2 * e) % VEC;
+          const float* x = e < VEC / 2 ? x1 : x2;
+          float* y = e < VEC / 2 ? y1 : y2;
+          y[i] = fmaf(x[i], c[e], -x[i + 1] * s[e]);
+          y[i + 1] = fmaf(x[i + 1], c[e], x[i] * s[e]);
+        } else {
+          y1[e] = fmaf(x1[e], c[e], -x2[e] * s[e]);
+          y2[e] = fmaf(x2[e], c[e], x1[e] * s[e]);
+        }
       }
       const int64_t off = dst_off(ch.dst + j);
-      st_cache<PAGED>(ck + off + kc * VEC, Store<T>::pack(y1));
-      st_cache<PAGED>(ck + off + HALF + kc * VEC, Store<T>::pack(y2));
+      st_cache<PAGED>(ck + off + lo, turn ? Store<T>::pack(y1) : klo[p]);
+      st_cache<PAGED>(ck + off + hi, turn ? Store<T>::pack(y2) : khi[p]);
     }
   }
   if (run_aliased) return;
@@ -265,14 +298,17 @@ int launch_upload(const UploadArgs& args, hipStream_t s) {
   return check(hipGetLastError());
 }
 
-int launch_graft(int dtype, const GraftChunk* runs, const GraftArgs& args, int n_runs, const void* lib_k,
-                 const void* lib_v, int64_t cap, const CacheView& cv, const double* inv_freq, int L, hipStream_t s,
-                 KTime tm) {
+namespace {
+
+template <typename Form>
+int launch_graft_form(int dtype, const GraftChunk* runs, const GraftArgs& args, int n_runs, const void* lib_k,
+                      const void* lib_v, int64_t cap, const CacheView& cv, const Form& form, int L, hipStream_t s,
+                      KTime tm) {
   if (n_runs == 0) return 0;
   dim3 grid(n_runs, cv.n_kv_heads, L);
 #define GRR(T, DD, PG, RU, RV)                                                                                 \
-  hipExtLaunchKernelGGL((graft_kernel<T, DD, PG, RU>), grid, dim3(256), 0, s, tm.start, tm.stop, 0, RV,        \
-                        (const T*)lib_k, (const T*)lib_v, cap, cv, inv_freq)
+  hipExtLaunchKernelGGL((graft_kernel<T, DD, PG, RU, Form>), grid, dim3(256), 0, s, tm.start, tm.stop, 0, RV,  \
+                        (const T*)lib_k, (const T*)lib_v, cap, cv, form)
 #define GR(T, DD, PG)                                                                                          \
   {                                                                                                            \
     if (runs) GRR(T, DD, PG, RunsInMemory, RunsInMemory{runs});                                                \
@@ -286,6 +322,21 @@ int launch_graft(int dtype, const GraftChunk* runs, const GraftArgs& args, int n
 #undef GR
 #undef GRR
   return check(hipGetLastError());
+}
+
+}  // namespace
+
+int launch_graft(int dtype, const GraftChunk* runs, const GraftArgs& args, int n_runs, const void* lib_k,
+                 const void* lib_v, int64_t cap, const CacheView& cv, const double* inv_freq, int L, hipStream_t s,
+                 KTime tm) {
+  return launch_graft_form(dtype, runs, args, n_runs, lib_k, lib_v, cap, cv, OwnForm{inv_freq}, L, s, tm);
+}
+
+int launch_graft_rope(int dtype, bool pairs, const GraftChunk* runs, const GraftArgs& args, int n_runs,
+                      const void* lib_k, const void* lib_v, int64_t cap, const CacheView& cv, const RopeArgs& ra, int L,
+                      hipStream_t s, KTime tm) {
+  return pairs ? launch_graft_form(dtype, runs, args, n_runs, lib_k, lib_v, cap, cv, GivenForm<true>{ra}, L, s, tm)
+               : launch_graft_form(dtype, runs, args, n_runs, lib_k, lib_v, cap, cv, GivenForm<false>{ra}, L, s, tm);
 }
 
 }  // namespace fcg

@@ -1,0 +1,261 @@
+// Rotary encoding of rows in any of the rotary forms, into a caller's tensor
+// (rope apply) or into a cache (append), for gfx950.
+//
+//   (a, b) -> (m (a cos - b sin), m (b cos + a sin)),  angle p w_i,
+// for the pairs (i, i + R/2) or (2i, 2i + 1) of the first R dimensions of a
+// head; the others are copied.  The backward pass negates the angle.
+//
+// A block owns up to 16 tokens at consecutive indices (and, appending, at
+// consecutive positions of one sequence) of one layer.  The (cos, sin) of its
+// tokens' pairs are computed once into LDS while the first rows' loads are in
+// flight, and shared by all heads.  A lane moves two 16-byte vectors of a row,
+// chosen so that they hold both ends of 16 / sizeof(T) pairs: vectors c and
+// c + R / 32 (bf16) for halves, 2c and 2c + 1 for neighbours and for the
+// dimensions past R; so every form turns registers only.  Caller rows start at
+// any element (unaligned 16-byte accesses); cache rows are aligned.
+//
+// What bounds it: many tokens, HBM; few, the chain of argument fetch, position,
+// rows and stores.
+#include "fcg_device.hpp"
+#include "kernels.hpp"
+
+namespace fcg {
+
+namespace {
+
+constexpr int kApply = 0, kAppendArgs = 1, kAppendList = 2;
+
+template <int MODE>
+struct Where {};
+template <>
+struct Where<kApply> {
+  const int32_t* pos;
+};
+template <>
+struct Where<kAppendArgs> {
+  AppendArgs a;
+  int32_t n_runs;
+};
+template <>
+struct Where<kAppendList> {
+  const AppendGroup* groups;
+};
+
+// group b of a plan by value: its run is the last one whose first group is at
+// most b; every lane of a wave holds one run, so one vector load finds it
+__device__ __forceinline__ AppendGroup find_group(const Where<kAppendArgs>& w, int b, int tb) {
+  static_assert(kAppRuns == 64, "one run per lane");
+  const int lane = threadIdx.x & 63;
+  const AppendRun mine = w.a.run[min(lane, w.n_runs - 1)];
+  const uint64_t below = __builtin_amdgcn_ballot_w64(lane < w.n_runs && mine.grp0 <= b);
+  const int r = 63 - __builtin_clzll(below);
+  const int tok0 = __builtin_amdgcn_readlane(mine.tok0, r), seq = __builtin_amdgcn_readlane(mine.seq, r);
+  const int pos0 = __builtin_amdgcn_readlane(mine.pos0, r), n = __builtin_amdgcn_readlane(mine.n, r);
+  const int grp0 = __builtin_amdgcn_readlane(mine.grp0, r), pg = __builtin_amdgcn_readlane(mine.page0, r);
+  const int j = (b - grp0) * tb;
+  AppendGroup g;
+  g.tok0 = tok0 + j;
+  g.seq = seq;
+  g.pos0 = pos0 + j;
+  g.n = min(tb, n - j);
+  g.enter = pg < 0;
+  const int e = (pg & 0x7FFFFFFF) + (g.pos0 >> 4) - (pos0 >> 4);
+  g.page_a = w.a.page[min(e, kAppPages - 1)];
+  g.page_b = w.a.page[min(e + 1, kAppPages - 1)];
+  g.pad = 0;
+  return g;
+}
+
+}  // namespace
+
+template <typename T, int D, bool PAIRS, int MODE, bool PAGED>
+__global__ void __launch_bounds__(256) rope_rows_kernel(Where<MODE> where, RopeRows rows, CacheView cv, int layer0,
+                                                        RopeArgs ra, const float2* __restrict__ tab) {
+  constexpr int VEC = Store<T>::VEC;
+  constexpr int NCH = D / (2 * VEC);  // vector pairs of a row
+  constexpr int U = 4;                // vector pairs of a lane in flight
+  __shared__ __align__(16) float2 s_cs[kAppMaxTb * kRopePairs];
+
+  const int t = threadIdx.x;
+  const int layer = blockIdx.z;
+  AppendGroup g;
+  if constexpr (MODE == kApply) {
+    g.tok0 = blockIdx.x * rows.tb;
+    g.n = min(rows.tb, rows.n_tok - g.tok0);
+  } else if constexpr (MODE == kAppendArgs) {
+    g = find_group(where, blockIdx.x, rows.tb);
+  } else {
+    g = where.groups[blockIdx.x];
+  }
+  const int half = ra.rot / 2;
+  const int H = rows.Hq + rows.Hk + rows.Hv;
+  const int r0 = blockIdx.y * rows.slice_rows;
+  const int nrow = min(rows.slice_rows, g.n * H - r0);  // rows of this block, token-major
+  const int total = nrow * NCH;
+  const int rchunks = half / VEC;  // vector pairs that turn
+
+  if constexpr (MODE != kApply && PAGED) {
+    if (g.enter && blockIdx.y == 0 && layer == 0 && t == 0) {
+      int32_t* row = const_cast<int32_t*>(cv.page_table) + (int64_t)g.seq * 2 * cv.n_lp + (g.pos0 >> 4);
+      row[0] = g.page_a;
+      row[cv.n_lp] = -1;
+      if (((g.pos0 + g.n - 1) >> 4) != (g.pos0 >> 4)) {
+        row[1] = g.page_b;
+        row[cv.n_lp + 1] = -1;
+      }
+    }
+  }
+
+  struct Item {
+    int tl, kind, head, c;  // token of the group, 0 q / 1 k / 2 v, head, vector pair
+  };
+  auto item_of = [&](int i) __attribute__((always_inline)) -> Item {
+    Item x;
+    x.c = i % NCH;
+    const int r = r0 + i / NCH;
+    x.tl = r / H;
+    const int h = r - x.tl * H;
+    x.kind = h < rows.Hq ? 0 : h < rows.Hq + rows.Hk ? 1 : 2;
+    x.head = h - (x.kind == 0 ? 0 : x.kind == 1 ? rows.Hq : rows.Hq + rows.Hk);
+    return x;
+  };
+  // element offsets of the lane's two vectors in the row
+  auto lo_of = [&](const Item& x) __attribute__((always_inline)) {
+    return (PAIRS || x.c >= rchunks || x.kind == 2 ? 2 * x.c : x.c) * VEC;
+  };
+  auto hi_of = [&](const Item& x) __attribute__((always_inline)) {
+    return (PAIRS || x.c >= rchunks || x.kind == 2 ? 2 * x.c + 1 : x.c + rchunks) * VEC;
+  };
+  auto row_of = [&](const RowView& v, const Item& x) __attribute__((always_inline)) {
+    return reinterpret_cast<const T*>(v.p) + (int64_t)layer * v.layer + (int64_t)(g.tok0 + x.tl) * v.token +
+           (int64_t)x.head * v.head;
+  };
+
+  for (int i0 = t; i0 - t < total; i0 += 256 * U) {
+    uint4 a[U], b[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + 256 * u;
+      if (i < total) {
+        const Item x = item_of(i);
+        const T* src = row_of(x.kind == 0 ? rows.q : x.kind == 1 ? rows.k : rows.v, x);
+        a[u] = ld16_any(src + lo_of(x));
+        b[u] = ld16_any(src + hi_of(x));
+      }
+    }
+    if (i0 == t) {  // (block-uniform) the (cos, sin) of the group's tokens, behind the first loads
+      for (int i = t; i < g.n * half; i += 256) {
+        const int tl = i / half, pr = i - tl * half;
+        float c, s;
+        if (MODE != kApply && tab) {
+          const float2 cs = tab[(int64_t)(g.pos0 + tl) * half + pr];
+          c = cs.x;
+          s = cs.y;
+        } else {
+          int pos;
+          if constexpr (MODE == kApply) pos = where.pos[g.tok0 + tl];
+          else pos = g.pos0 + tl;
+          rope_cs_turns((double)pos, ra.turns[pr], &c, &s);
+          c *= ra.m;
+          s *= ra.m * rows.sign;
+        }
+        s_cs[i] = make_float2(c, s);
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + 256 * u;
+      if (i >= total) continue;
+      const Item x = item_of(i);
+      uint4 ya = a[u], yb = b[u];
+      if (x.kind != 2 && x.c < rchunks) {
+        float xa[VEC], xb[VEC], za[VEC], zb[VEC];
+        Store<T>::unpack(ya, xa);
+        Store<T>::unpack(yb, xb);
+        const float2* cs = s_cs + x.tl * half + x.c * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float c = cs[e].x, s = cs[e].y;
+          if (PAIRS) {  // pair c VEC + e: elements 2e, 2e + 1 of the two vectors end to end
+            const float p = e < VEC / 2 ? xa[(2 * e) % VEC] : xb[(2 * e) % VEC];
+            const float q = e < VEC / 2 ? xa[(2 * e + 1) % VEC] : xb[(2 * e + 1) % VEC];
+            (e < VEC / 2 ? za : zb)[(2 * e) % VEC] = fmaf(p, c, -q * s);
+            (e < VEC / 2 ? za : zb)[(2 * e + 1) % VEC] = fmaf(q, c, p * s);
+          } else {
+            za[e] = fmaf(xa[e], c, -xb[e] * s);
+            zb[e] = fmaf(xb[e], c, xa[e] * s);
+          }
+        }
+        ya = Store<T>::pack(za);
+        yb = Store<T>::pack(zb);
+      }
+      if (MODE == kApply || x.kind == 0) {
+        T* dst = const_cast<T*>(row_of(x.kind == 0 ? rows.q_out : rows.k_out, x));
+        st16_any(dst + lo_of(x), ya);
+        st16_any(dst + hi_of(x), yb);
+      } else {
+        const int pos = g.pos0 + x.tl;
+        int64_t off = (int64_t)(layer0 + layer) * cv.layer_stride;
+        if (PAGED) {
+          const int page = (pos >> 4) == (g.pos0 >> 4) ? g.page_a : g.page_b;
+          off += (((int64_t)page * cv.n_kv_heads + x.head) * 16 + (pos & 15)) * D;
+        } else {
+          off += (((int64_t)g.seq * cv.n_kv_heads + x.head) * cv.max_tokens + pos) * D;
+        }
+        T* dst = reinterpret_cast<T*>(x.kind == 1 ? cv.k : cv.v) + off;
+        st16(dst + lo_of(x), ya);
+        st16(dst + hi_of(x), yb);
+      }
+    }
+  }
+}
+
+namespace {
+
+int check(hipError_t e) { return e == hipSuccess ? 0 : (int)e; }
+
+template <int MODE, bool PAGED>
+void launch_rows(int dtype, int D, bool pairs, dim3 grid, const Where<MODE>& where, const RopeRows& rows,
+                 const CacheView& cv, int layer0, const RopeArgs& ra, const float2* tab, hipStream_t s) {
+#define RR(T, DD, PR)                                                                                              \
+  hipLaunchKernelGGL((rope_rows_kernel<T, DD, PR, MODE, PAGED>), grid, dim3(256), 0, s, where, rows, cv, layer0, ra, \
+                     tab)
+#define RRP(T, DD) { if (pairs) RR(T, DD, true); else RR(T, DD, false); }
+  if (dtype == 0) { if (D == 64) RRP(float, 64) else RRP(float, 128) }
+  else { if (D == 64) RRP(bf16_t, 64) else RRP(bf16_t, 128) }
+#undef RRP
+#undef RR
+}
+
+}  // namespace
+
+int launch_rope_apply(int dtype, int D, bool pairs, const RopeRows& rows, const int32_t* pos, const RopeArgs& ra,
+                      hipStream_t s) {
+  const int H = rows.Hq + rows.Hk;
+  const dim3 grid((rows.n_tok + rows.tb - 1) / rows.tb, (rows.tb * H + rows.slice_rows - 1) / rows.slice_rows,
+                  rows.n_layers);
+  launch_rows<kApply, false>(dtype, D, pairs, grid, Where<kApply>{pos}, rows, CacheView{}, 0, ra, nullptr, s);
+  return check(hipGetLastError());
+}
+
+int launch_append(int dtype, bool pairs, const RopeRows& rows, const AppendArgs& args, int n_runs,
+                  const AppendGroup* groups, int n_groups, const CacheView& cv, int layer0, const RopeArgs& ra,
+                  const float2* tab, hipStream_t s) {
+  const int H = rows.Hq + rows.Hk + rows.Hv;
+  const dim3 grid(n_groups, (rows.tb * H + rows.slice_rows - 1) / rows.slice_rows, rows.n_layers);
+#define AP(PG)                                                                                                     \
+  {                                                                                                                \
+    if (groups)                                                                                                    \
+      launch_rows<kAppendList, PG>(dtype, cv.head_dim, pairs, grid, Where<kAppendList>{groups}, rows, cv, layer0, ra, \
+                                   tab, s);                                                                        \
+    else                                                                                                           \
+      launch_rows<kAppendArgs, PG>(dtype, cv.head_dim, pairs, grid, Where<kAppendArgs>{args, n_runs}, rows, cv, layer0, \
+                                   ra, tab, s);                                                                    \
+  }
+  if (cv.page_size) AP(true) else AP(false)
+#undef AP
+  return check(hipGetLastError());
+}
+
+}  // namespace fcg

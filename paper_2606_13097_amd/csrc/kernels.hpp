@@ -274,6 +274,99 @@ constexpr size_t kNoAllocPartBytes = (size_t)8 << 20;
 constexpr size_t kNoAllocScratchBytes = kNoAllocCountBytes + kNoAllocPartBytes;
 int noalloc_scratch(hipStream_t s, void** base);
 
+// A rotary form by value: frequencies in turns per position of the rot / 2
+// pairs, the factor on the turned dimensions.
+constexpr int kRopePairs = 64;  // head_dim <= 128
+struct RopeArgs {
+  double turns[kRopePairs];
+  float m;
+  int32_t rot;
+};
+
+// Rows of a caller's tensor: strides in elements between layers, tokens, heads.
+struct RowView {
+  const void* p;
+  int64_t layer, token, head;
+};
+
+// Tokens of one append launch.  A group is up to `tb` (<= 16) tokens at
+// consecutive caller indices and positions of one sequence; page_a holds its
+// first position, page_b that of the next logical page (paged caches).
+struct AppendGroup {
+  int32_t tok0, seq, pos0, n;
+  int32_t page_a, page_b;
+  int32_t enter;  // 1: enter the pages into the device page table
+  int32_t pad;
+};
+// By value: up to kAppRuns runs, each cut into groups of tb tokens; a run's
+// logical pages are page[page0 ..].
+struct AppendRun {
+  int32_t tok0, seq, pos0, n;
+  int32_t grp0;   // first group of the run
+  int32_t page0;  // its first entry of page[]; bit 31: enter the pages into the device page table
+};
+constexpr int kAppRuns = 64, kAppPages = 384, kAppMaxTb = 16;
+struct AppendArgs {
+  AppendRun run[kAppRuns];
+  int32_t page[kAppPages];
+};
+struct RopeRows {
+  RowView q, q_out, k, k_out, v;  // a null p: no rows of that kind
+  int32_t Hq, Hk, Hv;             // rows per token of each kind
+  int32_t n_tok, tb;              // tokens, tokens of a block
+  int32_t slice_rows;             // rows of a block (grid y cuts the rows of its tokens)
+  int32_t n_layers;
+  float sign;                     // of the angles
+};
+
+// Turn rows into caller tensors: q -> q_out, k -> k_out, token t at device pos[t].
+int launch_rope_apply(int dtype, int D, bool pairs, const RopeRows& rows, const int32_t* pos, const RopeArgs& ra,
+                      hipStream_t s);
+
+// Turn and append: q -> q_out, k and v -> the cache rows of layers layer0 ...  tab
+// non-null: the cache's rotary table (whole head, rotate-half) instead of ra.
+// groups null: the plan by value (n_groups groups of n_runs runs).
+int launch_append(int dtype, bool pairs, const RopeRows& rows, const AppendArgs& args, int n_runs,
+                  const AppendGroup* groups, int n_groups, const CacheView& cv, int layer0, const RopeArgs& ra,
+                  const float2* tab, hipStream_t s);
+
+// Graft of a rotary form; as launch_graft.
+int launch_graft_rope(int dtype, bool pairs, const GraftChunk* runs, const GraftArgs& args, int n_runs,
+                      const void* lib_k, const void* lib_v, int64_t cap, const CacheView& cv, const RopeArgs& ra, int L,
+                      hipStream_t s, KTime tm = {});
+
+// Attention over a shared prefix.  Query rows are sorted by rank (token) and,
+// per kv head, numbered rank * g + j; an item attends rows [row0, row0 + n_row)
+// over prefix positions [a0, a1) and then positions [b0, b1) of sequence seq,
+// the latter up to each row's own position, and leaves slot `slot`'s partial.
+struct PrefixItem {
+  int32_t row0, n_row, seq;
+  int32_t a0, a1, b0, b1;
+  int32_t slot;
+};
+// A rank: its token and position, and the slots its rows have partials in,
+// 0 .. na - 1 and b0 .. b0 + nb - 1.
+struct PrefixRank {
+  int32_t tok, pos;
+  uint16_t na, b0, nb, pad;
+};
+struct PrefixCall {
+  RowView q, out;
+  float* lse;
+  const PrefixItem* items;
+  const PrefixRank* ranks;
+  void* part_o;     // [slot][Hkv][rows][D], bf16 for bf16 caches
+  float* part_ml;   // [slot][Hkv][rows][2] (max, sum), base 2
+  int32_t n_items, n_rank, rows, g;
+  int32_t prefix_seq, layer;
+  int32_t direct;   // 1: every row has one slot, items write the output
+};
+constexpr int kPfxRows = 128;     // query rows of an item, bf16
+constexpr int kPfxRowsF32 = 64;   // fp32
+constexpr int kPfxTile = 64;      // keys of a tile
+int launch_prefix_attend(int dtype, const PrefixCall& call, const CacheView& cv, hipStream_t s);
+int launch_prefix_merge(int dtype, const PrefixCall& call, const CacheView& cv, hipStream_t s);
+
 // Merge split partials into out: part_o and out fp32 rows, or (mfma_part) both
 // bf16, part_o in the accumulator order of the MFMA prefill kernel.
 int launch_combine(const CombineArgs& args, const TokenMeta* meta, int Hq, int Hkv, int D,

@@ -1,0 +1,519 @@
+// Entry points around the cache that take a rotary handle or a shared prefix
+// (include/fcg.h): rotary handles, rope apply, append, prefix attention.
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "objects.hpp"
+
+using namespace fcg;
+
+namespace {
+
+fcg_status fail(fcg_status s, const std::string& msg) { return report(s, msg); }
+
+// Body of an entry point: host allocations that fail become a status.
+template <typename F>
+fcg_status guarded(F&& f) {
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    return fail(FCG_ENOMEM, "host allocation");
+  } catch (const std::exception& e) {
+    return fail(FCG_ENOMEM, e.what());
+  }
+}
+
+// The handle's device for the call, the caller's again afterwards.
+struct OnDevice {
+  int before = -1;
+  hipError_t err = hipSuccess;
+  explicit OnDevice(int device) {
+    err = hipGetDevice(&before);
+    if (err == hipSuccess && before != device) err = hipSetDevice(device);
+    else if (err == hipSuccess) before = -1;
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+bool capturing(hipStream_t s) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &st) == hipSuccess) return st != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();  // not this call's error
+  return false;
+}
+
+RowView view_of(const fcg_tensor* t) {
+  return t ? RowView{t->data, t->layer, t->token, t->head} : RowView{nullptr, 0, 0, 0};
+}
+
+// strides of a tensor [layers][tokens][heads][D]
+fcg_status check_strides(const fcg_tensor* t, const char* what) {
+  if (t && (t->layer < 0 || t->token < 0 || t->head < 0))
+    return fail(FCG_EINVAL, std::string(what) + ": negative stride");
+  return FCG_OK;
+}
+
+// Rows of an output must not meet: sorted by stride, each dimension steps over
+// what the smaller ones cover.
+fcg_status check_output(const fcg_tensor* t, int64_t layers, int64_t tokens, int64_t heads, int64_t D, const char* what) {
+  std::pair<int64_t, int64_t> dim[3] = {{t->layer, layers}, {t->token, tokens}, {t->head, heads}};  // stride, size
+  std::sort(dim, dim + 3);
+  int64_t extent = D;
+  for (auto& d : dim) {
+    if (d.second <= 1) continue;
+    if (d.first < extent) return fail(FCG_EINVAL, std::string(what) + ": rows of an output overlap");
+    extent = d.first * (d.second - 1) + extent;
+  }
+  return FCG_OK;
+}
+
+bool same_view(const fcg_tensor* a, const fcg_tensor* b) {
+  return a->data == b->data && a->layer == b->layer && a->token == b->token && a->head == b->head;
+}
+
+// an output that starts where its input does is that input in place, or an error
+fcg_status check_alias(const fcg_tensor* in, const fcg_tensor* out, const char* what) {
+  if (in->data == out->data && !same_view(in, out))
+    return fail(FCG_EINVAL, std::string(what) + ": an output in its input's place needs its strides");
+  return FCG_OK;
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------- rotary forms
+
+fcg_status fcg_rope_create(const fcg_rope_desc* d, fcg_rope** out) {
+  if (!d || !out) return fail(FCG_EINVAL, "null rope descriptor or output");
+  if (d->rotary_dim < 16 || d->rotary_dim > 2 * kRopePairs || d->rotary_dim % 16)
+    return fail(FCG_EINVAL, "rotary_dim must be a multiple of 16 in [16, 128]");
+  if (d->layout != FCG_ROPE_HALF && d->layout != FCG_ROPE_PAIRS) return fail(FCG_EINVAL, "unknown rope layout");
+  if (d->scaling < FCG_ROPE_PLAIN || d->scaling > FCG_ROPE_GIVEN) return fail(FCG_EINVAL, "unknown rope scaling");
+  if (!(d->attn_factor > 0.0) || !std::isfinite(d->attn_factor)) return fail(FCG_EINVAL, "attn_factor must be > 0");
+  const bool given = d->scaling == FCG_ROPE_GIVEN, scaled = d->scaling != FCG_ROPE_PLAIN && !given;
+  if (!given && (!(d->theta > 1.0) || !std::isfinite(d->theta))) return fail(FCG_EINVAL, "theta must be > 1");
+  if (scaled && (!(d->factor >= 1.0) || !std::isfinite(d->factor))) return fail(FCG_EINVAL, "factor must be >= 1");
+  if (d->scaling == FCG_ROPE_PARTS) {
+    if (!(d->orig_tokens > 0.0) || !std::isfinite(d->orig_tokens)) return fail(FCG_EINVAL, "orig_tokens must be > 0");
+    if (!(d->low_turns >= 0.0) || !(d->high_turns > d->low_turns) || !std::isfinite(d->high_turns))
+      return fail(FCG_EINVAL, "0 <= low_turns < high_turns is needed");
+  }
+  const int n = d->rotary_dim / 2;
+  if (given) {
+    if (!d->freqs) return fail(FCG_EINVAL, "null frequencies");
+    for (int i = 0; i < n; ++i)
+      if (!std::isfinite(d->freqs[i])) return fail(FCG_EINVAL, "a frequency is not finite");
+  }
+  return guarded([&]() -> fcg_status {
+    std::vector<double> w(n);
+    const double R = d->rotary_dim;
+    const double theta = d->scaling == FCG_ROPE_NTK ? d->theta * std::pow(d->factor, R / (R - 2.0)) : d->theta;
+    for (int i = 0; i < n; ++i) {
+      w[i] = given ? d->freqs[i] : std::pow(theta, -2.0 * i / R);
+      if (d->scaling == FCG_ROPE_LINEAR) w[i] /= d->factor;
+      if (d->scaling == FCG_ROPE_PARTS) {
+        const double r = d->orig_tokens * w[i] / 6.283185307179586477;
+        const double keep = std::min(1.0, std::max(0.0, (r - d->low_turns) / (d->high_turns - d->low_turns)));
+        w[i] *= (1.0 - keep) / d->factor + keep;
+      }
+    }
+    fcg_rope* r = new fcg_rope();
+    r->rot = d->rotary_dim;
+    r->layout = d->layout;
+    r->attn_factor = d->attn_factor;
+    r->freqs = std::move(w);
+    *out = r;
+    return FCG_OK;
+  });
+}
+
+fcg_status fcg_rope_frequencies(const fcg_rope* rope, double* freqs) {
+  if (!rope || !freqs) return fail(FCG_EINVAL, "null rope or output");
+  std::copy(rope->freqs.begin(), rope->freqs.end(), freqs);
+  return FCG_OK;
+}
+
+fcg_status fcg_rope_destroy(fcg_rope* rope) {
+  delete rope;
+  return FCG_OK;
+}
+
+namespace {
+
+// How the tokens' rows are cut into blocks: tokens of a block and, where there
+// are few tokens, rows of a block.
+void cut_rows(RopeRows* rows, int64_t n_tok, int64_t n_layers, int H, int nch) {
+  rows->tb = (int)std::max<int64_t>(1, std::min<int64_t>(kAppMaxTb, n_tok * n_layers / 2048));
+  rows->slice_rows = rows->tb * H;
+  const int pass = 256 / nch;  // rows that one pass of a block moves
+  if (n_tok * n_layers < 256) rows->slice_rows = std::min(rows->slice_rows, pass);
+}
+
+}  // namespace
+
+fcg_status fcg_rope_apply(const fcg_rope* rope, int32_t dtype, int32_t head_dim, int32_t n_layers, int32_t n_tok,
+                          const int32_t* pos, int32_t n_q_heads, const fcg_tensor* q, const fcg_tensor* q_out,
+                          int32_t n_k_heads, const fcg_tensor* k, const fcg_tensor* k_out, uint32_t flags,
+                          void* stream) {
+  if (!rope) return fail(FCG_EINVAL, "null rope");
+  if (dtype != FCG_F32 && dtype != FCG_BF16) return fail(FCG_EINVAL, "unknown dtype");
+  if (head_dim != 64 && head_dim != 128) return fail(FCG_EINVAL, "head_dim must be 64 or 128");
+  if (rope->rot > head_dim) return fail(FCG_EINVAL, "rotary_dim exceeds head_dim");
+  if (n_layers < 0 || n_layers > 65535 || n_tok < 0 || n_q_heads < 0 || n_k_heads < 0)
+    return fail(FCG_EINVAL, "a count is negative, or more than 65535 layers");
+  if (n_q_heads > 4096 || n_k_heads > 4096) return fail(FCG_EINVAL, "more than 4096 heads");
+  if (flags & ~FCG_ROPE_BACKWARD) return fail(FCG_EINVAL, "unknown flags");
+  const bool has_q = q && n_q_heads, has_k = k && n_k_heads;
+  if ((has_q && !q_out) || (has_k && !k_out)) return fail(FCG_EINVAL, "an input without its output");
+  struct {
+    const fcg_tensor *in, *out;
+    int32_t heads;
+    const char* name;
+  } both[2] = {{q, q_out, n_q_heads, "q"}, {k, k_out, n_k_heads, "k"}};
+  const bool work = n_layers > 0 && n_tok > 0 && (has_q || has_k);
+  if (work && !pos) return fail(FCG_EINVAL, "null positions");
+  for (int i = 0; i < 2; ++i) {
+    if (!(i ? has_k : has_q)) continue;
+    const auto& b = both[i];
+    if (work && (!b.in->data || !b.out->data)) return fail(FCG_EINVAL, std::string(b.name) + ": null tensor");
+    if (fcg_status st = check_strides(b.in, b.name)) return st;
+    if (fcg_status st = check_strides(b.out, b.name)) return st;
+    if (fcg_status st = check_output(b.out, n_layers, n_tok, b.heads, head_dim, b.name)) return st;
+    if (work)
+      if (fcg_status st = check_alias(b.in, b.out, b.name)) return st;
+  }
+  if (!work) return FCG_OK;
+  RopeRows rows{};
+  if (has_q) {
+    rows.q = view_of(q);
+    rows.q_out = view_of(q_out);
+    rows.Hq = n_q_heads;
+  }
+  if (has_k) {
+    rows.k = view_of(k);
+    rows.k_out = view_of(k_out);
+    rows.Hk = n_k_heads;
+  }
+  rows.n_tok = n_tok;
+  rows.n_layers = n_layers;
+  rows.sign = flags & FCG_ROPE_BACKWARD ? -1.f : 1.f;
+  cut_rows(&rows, n_tok, n_layers, rows.Hq + rows.Hk, head_dim * (int)esize(dtype) / 32);
+  if (int rc = launch_rope_apply(dtype, head_dim, rope->pairs(), rows, pos, rope->args(), (hipStream_t)stream))
+    return hip_fail((hipError_t)rc, "rope launch");
+  return FCG_OK;
+}
+
+// ---------------------------------------------------------------------- append
+
+fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_tok, const int32_t* seq,
+                      const int32_t* pos, const fcg_rope* rope, const fcg_tensor* q, const fcg_tensor* q_out,
+                      const fcg_tensor* k, const fcg_tensor* v, uint32_t flags, void* stream) {
+  if (!c) return fail(FCG_EINVAL, "null cache");
+  if (n_layers < 0 || n_tok < 0) return fail(FCG_EINVAL, "negative count");
+  if (n_tok > 0 && (!seq || !pos)) return fail(FCG_EINVAL, "null token array");
+  if (flags & ~FCG_REPLACE) return fail(FCG_EINVAL, "unknown flags");
+  const fcg_model_desc& d = c->desc;
+  if (rope && rope->rot > d.head_dim) return fail(FCG_EINVAL, "rotary_dim exceeds head_dim");
+  const bool has_k = k && k->data, has_v = v && v->data, has_q = q && q->data;
+  if (has_k != has_v) return fail(FCG_EINVAL, "k and v must both be given or both be null");
+  if (has_q && (!q_out || !q_out->data)) return fail(FCG_EINVAL, "q without q_out");
+  if (has_q && !has_k) return fail(FCG_EINVAL, "q without k and v");
+  if (has_k && c->layout_only()) return fail(FCG_EINVAL, "a layout-only cache takes no data");
+  for (const fcg_tensor* t : {has_k ? k : nullptr, has_v ? v : nullptr, has_q ? q : nullptr, has_q ? q_out : nullptr})
+    if (fcg_status st = check_strides(t, "append")) return st;
+  if (has_q) {
+    if (fcg_status st = check_output(q_out, n_layers, n_tok, d.n_q_heads, d.head_dim, "q_out")) return st;
+    if (fcg_status st = check_alias(q, q_out, "q")) return st;
+  }
+  return guarded([&]() -> fcg_status {
+    std::vector<std::pair<int32_t, int32_t>> new_pages;
+    std::vector<int32_t> order;
+    std::string msg;
+    if (fcg_status st = c->plan.check_place(layer, n_layers, n_tok, seq, pos, (flags & FCG_REPLACE) != 0, &order,
+                                            &new_pages, &msg))
+      return fail(st, msg);
+    if (n_tok == 0 || n_layers == 0) return FCG_OK;
+    auto commit = [&]() {
+      for (int32_t l = layer; l < layer + n_layers; ++l)
+        for (int32_t t = 0; t < n_tok; ++t) c->plan.mark(seq[t], l, pos[t]);
+    };
+    if (c->layout_only()) {
+      c->plan.map_pages(new_pages);
+      commit();
+      return FCG_OK;
+    }
+    OnDevice dev(c->device);
+    HIP_TRY(dev.err, "hipSetDevice");
+    hipStream_t s = (hipStream_t)stream;
+    RopeRows rows{};
+    rows.n_tok = n_tok;
+    rows.n_layers = n_layers;
+    rows.sign = 1.f;
+    if (has_q) {
+      rows.q = view_of(q);
+      rows.q_out = view_of(q_out);
+      rows.Hq = d.n_q_heads;
+    }
+    if (has_k) {
+      rows.k = view_of(k);
+      rows.v = view_of(v);
+      rows.Hk = rows.Hv = d.n_kv_heads;
+    }
+    const int H = rows.Hq + rows.Hk + rows.Hv;
+    cut_rows(&rows, n_tok, n_layers, std::max(H, 1), d.head_dim * (int)esize(d.dtype) / 32);
+    // runs: consecutive positions of one sequence at consecutive indices
+    std::vector<AppendRun> runs;
+    for (int32_t i = 0; i < n_tok;) {
+      const int32_t t0 = order[i];
+      int32_t j = i + 1;
+      while (j < n_tok && order[j] == t0 + (j - i) && seq[order[j]] == seq[t0] && pos[order[j]] == pos[t0] + (j - i)) ++j;
+      runs.push_back(AppendRun{t0, seq[t0], pos[t0], j - i, 0, 0});
+      i = j;
+    }
+    int64_t n_page = 0;
+    int32_t n_groups = 0;
+    for (auto& r : runs) {
+      r.grp0 = n_groups;
+      n_groups += (r.n + rows.tb - 1) / rows.tb;
+      if (c->page_size) {
+        r.page0 = (int32_t)n_page;
+        n_page += (r.pos0 + r.n - 1) / 16 - r.pos0 / 16 + 1;
+      }
+    }
+    const bool by_value = (int)runs.size() <= kAppRuns && n_page <= kAppPages && has_k;
+    // what needs an upload cannot be captured: its staging memory is used again
+    if ((!by_value || !new_pages.empty()) && capturing(s))
+      return fail(FCG_ESTATE, "this append maps pages or has too many runs to be captured into a graph");
+    const RopeArgs ra = rope ? rope->args() : [&] {
+      RopeArgs a{};
+      a.rot = d.head_dim;
+      return a;
+    }();
+    const bool pairs = rope && rope->pairs();
+    const float2* tab = rope ? nullptr : c->d_rope;
+    if (by_value) {
+      c->plan.map_pages(new_pages);
+      AppendArgs args;
+      size_t np = 0;  // new_pages is sorted by (sequence, logical page)
+      for (size_t i = 0; i < runs.size(); ++i) {
+        AppendRun& r = runs[i];
+        if (c->page_size) {
+          const int32_t lp0 = r.pos0 / 16, lp1 = (r.pos0 + r.n - 1) / 16;
+          std::copy(c->plan.page_row(r.seq) + lp0, c->plan.page_row(r.seq) + lp1 + 1, args.page + r.page0);
+          while (np < new_pages.size() && new_pages[np] < std::pair<int32_t, int32_t>(r.seq, lp0)) ++np;
+          if (np < new_pages.size() && new_pages[np] <= std::pair<int32_t, int32_t>(r.seq, lp1)) r.page0 |= INT32_MIN;
+        }
+        args.run[i] = r;
+      }
+      const int rc = launch_append(d.dtype, pairs, rows, args, (int)runs.size(), nullptr, n_groups, c->view(), layer, ra,
+                                   tab, s);
+      if (rc) return hip_fail((hipError_t)rc, "append launch");
+      commit();
+      return FCG_OK;
+    }
+    Blob blob;
+    std::vector<std::pair<int32_t, size_t>> page_rows;
+    stage_pages(c, new_pages, &blob, &page_rows);
+    std::vector<AppendGroup> groups;
+    if (has_k)
+      for (const auto& r : runs)
+        for (int32_t j = 0; j < r.n; j += rows.tb) {
+          AppendGroup g{r.tok0 + j, r.seq, r.pos0 + j, std::min(rows.tb, r.n - j), 0, 0, 0, 0};
+          if (c->page_size) {
+            g.page_a = c->plan.page_of(r.seq, g.pos0);
+            g.page_b = c->plan.page_of(r.seq, g.pos0 + g.n - 1);
+          }
+          groups.push_back(g);
+        }
+    const size_t o_groups = blob.add(groups.data(), groups.size() * sizeof(AppendGroup));
+    char* dplan = nullptr;
+    size_t off = 0;
+    if (fcg_status st = upload(c, blob, page_rows, s, &dplan, &off)) return st;
+    if (has_k) {
+      const int rc = launch_append(d.dtype, pairs, rows, AppendArgs{}, 0, (const AppendGroup*)(dplan + o_groups),
+                                   (int)groups.size(), c->view(), layer, ra, tab, s);
+      if (rc) return hip_fail((hipError_t)rc, "append launch");
+    }
+    commit();
+    return c->ring.retire(off, blob.bytes.size(), s);
+  });
+}
+
+// ------------------------------------------------------------ prefix attention
+
+namespace {
+
+struct PrefixPlan {
+  std::vector<PrefixItem> items;
+  std::vector<PrefixRank> ranks;
+  int slots = 0;
+  bool direct = false;
+};
+
+// Cut the call into items.  Tokens of one sequence whose rows fill a block by
+// themselves go over prefix and own keys in one item (no merge between the
+// two); the others share prefix items and have own items per sequence.
+PrefixPlan plan_prefix(const fcg_model_desc& d, int32_t prefix_len, int32_t n, const int32_t* seq, const int32_t* pos) {
+  PrefixPlan p;
+  const int g = d.n_q_heads / d.n_kv_heads;
+  const int block = d.dtype == FCG_F32 ? kPfxRowsF32 : kPfxRows;
+  const int P = prefix_len;
+  std::vector<int32_t> order(n);
+  for (int32_t t = 0; t < n; ++t) order[t] = t;
+  auto less = [&](int32_t a, int32_t b) { return seq[a] != seq[b] ? seq[a] < seq[b] : pos[a] < pos[b]; };
+  if (!std::is_sorted(order.begin(), order.end(), less)) std::stable_sort(order.begin(), order.end(), less);
+  struct Group {
+    int32_t first, n, seq, end;  // of `order`; end: one past the last attended position
+    bool big;
+  };
+  std::vector<Group> groups;
+  for (int32_t i = 0; i < n;) {
+    int32_t j = i;
+    while (j < n && seq[order[j]] == seq[order[i]]) ++j;
+    groups.push_back(Group{i, j - i, seq[order[i]], pos[order[j - 1]] + 1, (int64_t)(j - i) * g >= block});
+    i = j;
+  }
+  std::stable_partition(groups.begin(), groups.end(), [](const Group& x) { return !x.big; });
+  // ranks: small groups first
+  p.ranks.reserve(n);
+  std::vector<int32_t> rank0;
+  int32_t n_small = 0;
+  for (const Group& x : groups) {
+    rank0.push_back((int32_t)p.ranks.size());
+    for (int32_t i = 0; i < x.n; ++i) p.ranks.push_back(PrefixRank{order[x.first + i], pos[order[x.first + i]], 0, 0, 0, 0});
+    if (!x.big) n_small += x.n;
+  }
+  auto tiles = [](int64_t lo, int64_t hi) { return hi > lo ? (hi - 1) / kPfxTile - lo / kPfxTile + 1 : 0; };
+  // split length in tiles: the grid about two blocks per compute unit
+  const int64_t ta = tiles(0, P);
+  const int64_t small_rb = ((int64_t)n_small * g + block - 1) / block;
+  int64_t total = small_rb * ta, longest = 0;
+  for (const Group& x : groups) {
+    const int64_t own = tiles(P, x.end);
+    const int64_t rb = x.big ? ((int64_t)x.n * g + block - 1) / block : 1;
+    total += rb * (own + (x.big ? ta : 0));
+    longest = std::max(longest, own + ta);
+  }
+  const int64_t target = 512;
+  int64_t per = std::max<int64_t>({1, (total * d.n_kv_heads + target - 1) / target, (longest + 255) / 256});
+  // prefix items of the small groups
+  int pre_slots = 0;
+  if (n_small && P) {
+    pre_slots = (int)((ta + per - 1) / per);
+    for (int32_t r0 = 0; r0 < n_small * g; r0 += block)
+      for (int s = 0; s < pre_slots; ++s)
+        p.items.push_back(PrefixItem{r0, std::min(block, n_small * g - r0), 0, (int32_t)(s * per * kPfxTile),
+                                     (int32_t)std::min<int64_t>(P, (s + 1) * per * kPfxTile), 0, 0, s});
+    p.slots = pre_slots;
+  }
+  for (size_t gi = 0; gi < groups.size(); ++gi) {
+    const Group& x = groups[gi];
+    const int32_t row0 = rank0[gi] * g, rows = x.n * g;
+    if (!x.big) {
+      // own positions [P, end), cut at multiples of the split length
+      const int64_t t0 = P / kPfxTile, nt = tiles(P, x.end);
+      const int ns = (int)((nt + per - 1) / per);
+      for (int s = 0; s < ns; ++s) {
+        const int64_t lo = std::max<int64_t>(P, (t0 + s * per) * kPfxTile);
+        const int64_t hi = std::min<int64_t>(x.end, (t0 + (s + 1) * per) * kPfxTile);
+        p.items.push_back(PrefixItem{row0, rows, x.seq, 0, 0, (int32_t)lo, (int32_t)hi, pre_slots + s});
+      }
+      for (int32_t i = 0; i < x.n; ++i) {
+        PrefixRank& r = p.ranks[rank0[gi] + i];
+        r.na = (uint16_t)pre_slots;
+        r.b0 = (uint16_t)pre_slots;
+        r.nb = (uint16_t)ns;
+      }
+      p.slots = std::max(p.slots, pre_slots + ns);
+      continue;
+    }
+    // prefix tiles, then own tiles, one run of tiles cut every `per`
+    const int64_t tb = tiles(P, x.end), t0 = P / kPfxTile;
+    const int ns = (int)((ta + tb + per - 1) / per);
+    for (int32_t r0 = 0; r0 < rows; r0 += block)
+      for (int s = 0; s < ns; ++s) {
+        const int64_t a = s * per, b = std::min(ta + tb, (s + 1) * per);
+        PrefixItem it{row0 + r0, std::min(block, rows - r0), x.seq, 0, 0, 0, 0, s};
+        if (a < ta) {
+          it.a0 = (int32_t)(a * kPfxTile);
+          it.a1 = (int32_t)std::min<int64_t>(P, std::min(b, ta) * kPfxTile);
+        }
+        if (b > ta) {
+          // up to the item's last row: positions past it are masked for all of its rows
+          const int32_t last = p.ranks[(row0 + r0 + it.n_row - 1) / g].pos + 1;
+          it.b0 = (int32_t)std::max<int64_t>(P, (t0 + std::max<int64_t>(a - ta, 0)) * kPfxTile);
+          it.b1 = std::max(it.b0, (int32_t)std::min<int64_t>(last, (t0 + b - ta) * kPfxTile));
+        }
+        p.items.push_back(it);
+      }
+    for (int32_t i = 0; i < x.n; ++i) p.ranks[rank0[gi] + i].na = (uint16_t)ns;
+    p.slots = std::max(p.slots, ns);
+  }
+  p.direct = n > 0;
+  for (const PrefixRank& r : p.ranks) p.direct = p.direct && r.na + r.nb == 1;
+  return p;
+}
+
+}  // namespace
+
+fcg_status fcg_prefix_attend(fcg_cache* c, int32_t layer, int32_t prefix_seq, int32_t prefix_len, int32_t n_tok,
+                             const int32_t* seq, const int32_t* pos, const fcg_tensor* q, const fcg_tensor* out,
+                             float* lse, void* stream) {
+  if (!c) return fail(FCG_EINVAL, "null cache");
+  if (n_tok < 0) return fail(FCG_EINVAL, "negative token count");
+  if (n_tok > 0 && (!seq || !pos)) return fail(FCG_EINVAL, "null token array");
+  const fcg_model_desc& d = c->desc;
+  if (n_tok > 0 && !c->layout_only()) {
+    if (!q || !out || !q->data || !out->data) return fail(FCG_EINVAL, "null tensor");
+    if (fcg_status st = check_strides(q, "q")) return st;
+    if (fcg_status st = check_strides(out, "out")) return st;
+    if (fcg_status st = check_output(out, 1, n_tok, d.n_q_heads, d.head_dim, "out")) return st;
+    fcg_tensor a = *q, b = *out;
+    a.layer = b.layer = 0;
+    if (fcg_status st = check_alias(&a, &b, "out")) return st;
+  }
+  if ((int64_t)n_tok * d.n_q_heads > INT32_MAX / 2) return fail(FCG_EINVAL, "too many query rows for one call");
+  return guarded([&]() -> fcg_status {
+    std::string msg;
+    if (fcg_status st = c->plan.check_attend(layer, prefix_seq, prefix_len, n_tok, seq, pos, &msg)) return fail(st, msg);
+    if (n_tok == 0 || c->layout_only()) return FCG_OK;
+    OnDevice dev(c->device);
+    HIP_TRY(dev.err, "hipSetDevice");
+    hipStream_t s = (hipStream_t)stream;
+    const PrefixPlan p = plan_prefix(d, prefix_len, n_tok, seq, pos);
+    const int g = d.n_q_heads / d.n_kv_heads;
+    const size_t prow = (size_t)p.slots * d.n_kv_heads * n_tok * g;
+    const size_t o_bytes = (prow * d.head_dim * esize(d.dtype) + 255) & ~size_t(255);
+    const bool cap = capturing(s);
+    if (cap) return fail(FCG_ESTATE, "fcg_prefix_attend needs an upload here and cannot be captured into a graph");
+    if (!p.direct && p.slots)
+      if (fcg_status st = grow(&c->xpart, &c->xpart_bytes, o_bytes + prow * 8, "prefix partials")) return st;
+    Blob blob;
+    const size_t o_items = blob.add(p.items.data(), p.items.size() * sizeof(PrefixItem));
+    const size_t o_ranks = blob.add(p.ranks.data(), p.ranks.size() * sizeof(PrefixRank));
+    char* dplan = nullptr;
+    size_t off = 0;
+    if (fcg_status st = upload(c, blob, {}, s, &dplan, &off)) return st;
+    PrefixCall pc{};
+    pc.q = view_of(q);
+    pc.out = view_of(out);
+    pc.lse = lse;
+    pc.items = (const PrefixItem*)(dplan + o_items);
+    pc.ranks = (const PrefixRank*)(dplan + o_ranks);
+    pc.part_o = c->xpart;
+    pc.part_ml = (float*)((char*)c->xpart + o_bytes);
+    pc.n_items = (int32_t)p.items.size();
+    pc.n_rank = n_tok;
+    pc.rows = n_tok * g;
+    pc.g = g;
+    pc.prefix_seq = prefix_seq;
+    pc.layer = layer;
+    pc.direct = p.direct;
+    if (int rc = launch_prefix_attend(d.dtype, pc, c->view(), s)) return hip_fail((hipError_t)rc, "prefix attention launch");
+    if (!p.direct)
+      if (int rc = launch_prefix_merge(d.dtype, pc, c->view(), s)) return hip_fail((hipError_t)rc, "prefix merge launch");
+    return c->ring.retire(off, blob.bytes.size(), s);
+  });
+}

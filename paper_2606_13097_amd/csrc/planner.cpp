@@ -150,6 +150,83 @@ fcg_status Planner::check_append(int32_t layer, int32_t n, const int32_t* seq, c
   return collect_pages(touched, new_pages, msg);
 }
 
+fcg_status Planner::check_place(int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq, const int32_t* pos,
+                                bool replace, std::vector<int32_t>* order,
+                                std::vector<std::pair<int32_t, int32_t>>* new_pages, std::string* msg) const {
+  if (layer < 0 || (int64_t)layer + n_layers > L_) {
+    *msg = fmt("layers %lld .. %lld out of range", layer, (int64_t)layer + n_layers - 1);
+    return FCG_ERANGE;
+  }
+  for (int32_t t = 0; t < n; ++t) {
+    if (seq[t] < 0 || seq[t] >= S_) { *msg = fmt("sequence %lld out of range", seq[t]); return FCG_ERANGE; }
+    if (pos[t] < 0 || pos[t] >= T_) { *msg = fmt("position %lld out of range", pos[t]); return FCG_ERANGE; }
+  }
+  if (replace && AV_)
+    for (int32_t t = 0; t < n; ++t)
+      if (valias_[(size_t)seq[t] * NLP_ + pos[t] / P_] >= 0) {
+        *msg = fmt("the value at position %lld of sequence %lld is read from the library", pos[t], seq[t]);
+        return FCG_ESTATE;
+      }
+  order->resize(n);
+  bool sorted = true;
+  auto less = [&](int32_t a, int32_t b) { return seq[a] != seq[b] ? seq[a] < seq[b] : pos[a] < pos[b]; };
+  for (int32_t t = 0; t < n; ++t) {
+    (*order)[t] = t;
+    sorted = sorted && (t == 0 || less(t - 1, t));
+  }
+  if (!sorted) std::sort(order->begin(), order->end(), less);
+  for (int32_t i = 0; i < n; ++i) {
+    const int32_t t = (*order)[i], u = i ? (*order)[i - 1] : t;
+    if (i && seq[t] == seq[u] && pos[t] == pos[u]) {
+      *msg = fmt("position %lld of sequence %lld given twice", pos[t], seq[t]);
+      return FCG_EOVERLAP;
+    }
+  }
+  if (!replace)
+    for (int32_t l = layer; l < layer + n_layers; ++l)
+      for (int32_t t = 0; t < n; ++t)
+        if (written(seq[t], l, pos[t])) {
+          *msg = fmt("position %lld of sequence %lld already written in layer %lld", pos[t], seq[t], l);
+          return FCG_EOVERLAP;
+        }
+  std::vector<std::pair<int32_t, int32_t>> touched;
+  if (P_ && n_layers)
+    for (int32_t t : *order) {
+      const std::pair<int32_t, int32_t> sl{seq[t], pos[t] / P_};
+      if (touched.empty() || touched.back() != sl) touched.push_back(sl);
+    }
+  return collect_pages(touched, new_pages, msg);
+}
+
+fcg_status Planner::check_attend(int32_t layer, int32_t prefix_seq, int32_t prefix_len, int32_t n, const int32_t* seq,
+                                 const int32_t* pos, std::string* msg) const {
+  if (layer < 0 || layer >= L_) { *msg = fmt("layer %lld out of range", layer); return FCG_ERANGE; }
+  if (prefix_len < 0 || prefix_len > T_) { *msg = fmt("prefix length %lld out of range", prefix_len); return FCG_ERANGE; }
+  if (prefix_len && (prefix_seq < 0 || prefix_seq >= S_)) {
+    *msg = fmt("prefix sequence %lld out of range", prefix_seq);
+    return FCG_ERANGE;
+  }
+  for (int32_t t = 0; t < n; ++t) {
+    if (seq[t] < 0 || seq[t] >= S_) { *msg = fmt("sequence %lld out of range", seq[t]); return FCG_ERANGE; }
+    if (pos[t] < prefix_len - 1 || pos[t] >= T_) { *msg = fmt("position %lld out of range", pos[t]); return FCG_ERANGE; }
+  }
+  if (n && prefix_len && count_below(prefix_seq, layer, prefix_len) != prefix_len) {
+    *msg = fmt("sequence %lld has unwritten positions below %lld (layer %lld)", prefix_seq, prefix_len, layer);
+    return FCG_EHOLE;
+  }
+  // the furthest position of each run of tokens of one sequence covers the others
+  for (int32_t t = 0; t < n;) {
+    int32_t u = t, top = pos[t];
+    for (; u < n && seq[u] == seq[t]; ++u) top = std::max(top, pos[u]);
+    if (count_below(seq[t], layer, top + 1) - count_below(seq[t], layer, prefix_len) != top + 1 - prefix_len) {
+      *msg = fmt("sequence %lld has unwritten positions in %lld .. %lld", seq[t], prefix_len, top);
+      return FCG_EHOLE;
+    }
+    t = u;
+  }
+  return FCG_OK;
+}
+
 fcg_status Planner::check_decode(int32_t layer, int32_t n, const int32_t* seq, std::vector<int32_t>* pos_out,
                                  std::vector<std::pair<int32_t, int32_t>>* new_pages, std::string* msg) const {
   std::vector<int32_t> s(seq, seq + n);

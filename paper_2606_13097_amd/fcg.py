@@ -41,7 +41,13 @@ EXPORTS = [
     "fcg_cache_timing", "fcg_cache_timing_read",
     "fcg_locality_create", "fcg_locality_record", "fcg_locality_set_ppl", "fcg_locality_scores",
     "fcg_locality_residency", "fcg_locality_destroy",
+    "fcg_rope_create", "fcg_rope_frequencies", "fcg_rope_destroy", "fcg_rope_apply", "fcg_graft_rope", "fcg_append",
+    "fcg_prefix_attend",
 ]
+FCG_ROPE_HALF, FCG_ROPE_PAIRS = 0, 1
+FCG_ROPE_PLAIN, FCG_ROPE_LINEAR, FCG_ROPE_NTK, FCG_ROPE_PARTS, FCG_ROPE_GIVEN = range(5)
+FCG_ROPE_BACKWARD = 1
+FCG_REPLACE = 1
 FCG_TIME_GRAFT, FCG_TIME_PREFILL_ATTN, FCG_TIME_PREFILL, FCG_TIME_DECODE, FCG_TIME_DECODE_ATTN = range(5)
 
 
@@ -55,6 +61,17 @@ class ModelDesc(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("rope_theta", C.c_double), ("dtype", C.c_int32),
                 ("rope_style", C.c_int32)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("theta", C.c_double),
+                ("factor", C.c_double), ("orig_tokens", C.c_double), ("low_turns", C.c_double),
+                ("high_turns", C.c_double), ("attn_factor", C.c_double), ("freqs", C.c_void_p)]
+
+
+class TensorView(C.Structure):
+    """``fcg_tensor``: address and strides (elements) of layer, token and head."""
+    _fields_ = [("data", C.c_void_p), ("layer", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
 
 
 def model_desc(n_layers, n_q_heads, n_kv_heads, head_dim, rope_theta, dtype) -> ModelDesc:
@@ -100,6 +117,16 @@ def _load():
         "fcg_locality_residency": [P, I64, P, P],
         "fcg_locality_destroy": [P],
     }
+    PT = C.POINTER(TensorView)
+    sig.update({
+        "fcg_rope_create": [C.POINTER(RopeDesc), C.POINTER(P)],
+        "fcg_rope_frequencies": [P, P],
+        "fcg_rope_destroy": [P],
+        "fcg_rope_apply": [P, I32, I32, I32, I32, P, I32, PT, PT, I32, PT, PT, U32, P],
+        "fcg_graft_rope": [P, P, P, I32, P, P, P, P],
+        "fcg_append": [P, I32, I32, I32, P, P, P, PT, PT, PT, PT, U32, P],
+        "fcg_prefix_attend": [P, I32, I32, I32, I32, P, P, PT, PT, P, P],
+    })
     for name, args in sig.items():
         f = getattr(lib, name)
         f.argtypes = args
@@ -199,6 +226,8 @@ class Cache:
         self.h, self.desc = h, desc
         self._lib = _L   # kept for close(), which may run while the interpreter tears down globals
         self.n_seqs, self.max_tokens, self.page_size, self.n_pages = n_seqs, max_tokens, page_size, n_pages
+        # the device its memory is on (None: layout only)
+        self.device = None if flags & FCG_LAYOUT_ONLY else torch.cuda.current_device()
         self.n_lp = -(-max_tokens // page_size) if page_size else 0
 
     def close(self):
@@ -398,6 +427,149 @@ def fcg_locality_residency(loc: Locality, budget: int, cost) -> np.ndarray:
     out = np.zeros(loc.n_funcs, dtype=np.uint8)
     _check(_L.fcg_locality_residency(loc.h, int(budget), c.ctypes.data, out.ctypes.data))
     return out
+
+
+# ------------------------------------------- rotary forms, appending, attention over a shared prefix
+
+class Rope:
+    """Handle of a rotary form (``fcg_rope``); host memory, any device."""
+
+    h = None
+
+    def __init__(self, desc: RopeDesc):
+        h = C.c_void_p()
+        _check(_L.fcg_rope_create(C.byref(desc), C.byref(h)))
+        self.h, self.rotary_dim = h, desc.rotary_dim
+        self._lib = _L
+
+    def close(self):
+        if self.h:
+            self._lib.fcg_rope_destroy(self.h)
+            self.h = None
+
+    __del__ = close
+
+
+def fcg_rope_create(rotary_dim: int, theta: float = 10000.0, layout: int = FCG_ROPE_HALF,
+                    scaling: int = FCG_ROPE_PLAIN, factor: float = 1.0, orig_tokens: float = 0.0,
+                    low_turns: float = 1.0, high_turns: float = 32.0, attn_factor: float = 1.0, freqs=None) -> Rope:
+    w = None
+    if freqs is not None:
+        w = np.ascontiguousarray(freqs, dtype=np.float64)
+        if w.shape != (int(rotary_dim) // 2,):
+            raise ValueError("one frequency per rotary pair")
+    return Rope(RopeDesc(int(rotary_dim), int(layout), int(scaling), float(theta), float(factor), float(orig_tokens),
+                         float(low_turns), float(high_turns), float(attn_factor),
+                         None if w is None else w.ctypes.data))
+
+
+def fcg_rope_frequencies(rope: Rope) -> np.ndarray:
+    out = np.zeros(rope.rotary_dim // 2, dtype=np.float64)
+    _check(_L.fcg_rope_frequencies(rope.h, out.ctypes.data))
+    return out
+
+
+def fcg_rope_destroy(rope: Rope) -> None:
+    rope.close()
+
+
+_TORCH_DT = {torch.float32: FCG_F32, torch.bfloat16: FCG_BF16}
+
+
+def _view(t, n_layers: int, n_tok: int, n_heads: int, head_dim: int, dtype: int, device, what: str):
+    """fcg_tensor of a [n_layers][n_tok][n_heads][head_dim] tensor (three dimensions: one layer)."""
+    if t is None:
+        return None
+    if not t.is_cuda or _TORCH_DT.get(t.dtype) != dtype:
+        raise ValueError(f"{what}: not a GPU tensor of the expected type")
+    if device is not None and t.device.index != device:
+        raise ValueError(f"{what}: on device {t.device.index}, expected {device}")
+    shape, st = tuple(t.shape), t.stride()
+    if t.dim() == 3:
+        shape, st = (1,) + shape, (0,) + st
+    if shape != (n_layers, n_tok, n_heads, head_dim):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected "
+                         f"{(n_layers, n_tok, n_heads, head_dim)[0 if t.dim() == 4 else 1:]}")
+    if st[3] != 1 and t.numel():
+        raise ValueError(f"{what}: the elements of a row must be adjacent")
+    return TensorView(t.data_ptr(), st[0], st[1], st[2])
+
+
+def _ref(v: Optional[TensorView]):
+    return None if v is None else C.byref(v)
+
+
+def _stream_of(stream, device) -> Optional[int]:
+    """The given stream, or torch's current stream of ``device``."""
+    if stream is not None or device is None:
+        return _stream(stream) if stream is not None else None
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def fcg_rope_apply(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, flags: int = 0, stream=None) -> None:
+    """Encode q and k ([n][heads][head_dim], or with layers in front) at ``pos`` (int32 GPU tensor [n]) into q_out, k_out."""
+    if not pos.is_cuda or pos.dtype != torch.int32 or pos.dim() != 1 or not pos.is_contiguous():
+        raise ValueError("pos: a contiguous int32 GPU tensor [n_tok]")
+    like = q if q is not None else k
+    if like is None:
+        raise ValueError("neither q nor k")
+    if like.dtype not in _TORCH_DT or like.dim() not in (3, 4):
+        raise ValueError("a float32 or bfloat16 tensor of three or four dimensions")
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError("an input without its output, or an output without its input")
+    dt, dev, n, d = _TORCH_DT[like.dtype], pos.device.index, pos.numel(), like.shape[-1]
+    layers = like.shape[0] if like.dim() == 4 else 1
+    hq, hk = 0 if q is None else q.shape[-2], 0 if k is None else k.shape[-2]
+    views = [_view(t, layers, n, h, d, dt, dev, w) for t, h, w in
+             ((q, hq, "q"), (q_out, hq, "q_out"), (k, hk, "k"), (k_out, hk, "k_out"))]
+    vq, vqo, vk, vko = map(_ref, views)
+    with torch.cuda.device(dev):
+        _check(_L.fcg_rope_apply(rope.h, dt, d, layers, n, pos.data_ptr(), hq, vq, vqo, hk, vk, vko, int(flags),
+                                 _stream_of(stream, dev)))
+
+
+def fcg_graft_rope(cache: Cache, lib: Library, rope: Rope, seq: Sequence[int], seg: Sequence[int], dst: Sequence[int],
+                   stream=None) -> None:
+    s, g, d = _i32(seq), _i32(seg), _i32(dst)
+    if not (s.size == g.size == d.size):
+        raise ValueError("seq, seg and dst differ in length")
+    _check(_L.fcg_graft_rope(cache.h, lib.h, rope.h, int(s.size), _p(s), _p(g), _p(d), _stream(stream)))
+
+
+def fcg_append(cache: Cache, layer: int, seq, pos, k=None, v=None, rope: Optional[Rope] = None, q=None, q_out=None,
+               flags: int = 0, stream=None, n_layers: int = 1) -> None:
+    """Place k, v ([n][Hkv][D]: layer ``layer``; [L][n][Hkv][D]: the L layers from it) at (seq, pos), keys encoded;
+    with q, its encoding goes to q_out.  Without k and v the positions of ``n_layers`` layers are reserved."""
+    s, p = _i32(seq), _i32(pos)
+    if s.ndim != 1 or s.shape != p.shape:
+        raise ValueError("seq and pos differ in length")
+    if q is not None and q_out is None:
+        raise ValueError("q without q_out")
+    if k is not None:
+        n_layers = k.shape[0] if k.dim() == 4 else 1
+    d, n = cache.desc, int(s.size)
+    views = [_view(t, n_layers, n, h, d.head_dim, d.dtype, cache.device, w) for t, h, w in
+             ((q, d.n_q_heads, "q"), (q_out, d.n_q_heads, "q_out"), (k, d.n_kv_heads, "k"), (v, d.n_kv_heads, "v"))]
+    vq, vqo, vk, vv = map(_ref, views)
+    _check(_L.fcg_append(cache.h, int(layer), int(n_layers), n, _p(s), _p(p), None if rope is None else rope.h, vq, vqo,
+                         vk, vv, int(flags), _stream_of(stream, cache.device)))
+
+
+def fcg_prefix_attend(cache: Cache, layer: int, prefix_seq: int, prefix_len: int, seq, pos, q, out, lse=None,
+                      stream=None) -> None:
+    """Attention of tokens (seq, pos) over positions [0, prefix_len) of prefix_seq and their own from prefix_len on.
+    q (encoded) and out [n][Hq][D]; lse float32 [n][Hq] or None."""
+    s, p = _i32(seq), _i32(pos)
+    if s.ndim != 1 or s.shape != p.shape:
+        raise ValueError("seq and pos differ in length")
+    d, n = cache.desc, int(s.size)
+    vq, vo = (_view(t, 1, n, d.n_q_heads, d.head_dim, d.dtype, cache.device, w) for t, w in ((q, "q"), (out, "out")))
+    if lse is not None and (not lse.is_cuda or lse.dtype != torch.float32 or not lse.is_contiguous() or
+                            tuple(lse.shape) != (n, d.n_q_heads) or lse.device.index != cache.device):
+        raise ValueError("lse: a contiguous float32 GPU tensor [n_tok][Hq]")
+    _check(_L.fcg_prefix_attend(cache.h, int(layer), int(prefix_seq), int(prefix_len), n, _p(s), _p(p), _ref(vq),
+                                _ref(vo), _dptr(lse), _stream_of(stream, cache.device)))
 
 
 def fcg_status_string(status: int) -> str:
