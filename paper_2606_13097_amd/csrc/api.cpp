@@ -636,6 +636,7 @@ fcg_status fcg_cache_destroy(fcg_cache* c) {
     if (c->qws) hipFree(c->qws);
     if (c->part) hipFree(c->part);
     if (c->xpart) hipFree(c->xpart);
+    for (void* p : c->xkept) hipFree(p);
     if (c->dpart) hipFree(c->dpart);
     if (c->d_count) hipFree(c->d_count);
     for (auto& v : c->spans)

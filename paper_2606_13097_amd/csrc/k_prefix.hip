@@ -23,6 +23,8 @@
 // wave brings in lie on one page, whose entry is one scalar load.  Keys of a tile
 // outside the range re-read a key inside it and are masked; a position that is not
 // attended is never read.
+#include <type_traits>
+
 #include "fcg_device.hpp"
 #include "kernels.hpp"
 
@@ -54,35 +56,41 @@ struct Keys {
   int seq, lo, hi;
 };
 
-// Where the 16 keys from position p0 (a multiple of 16) of a sequence lie.
-// Positions are clamped into [lo, hi) by the caller, so the page is mapped.
-template <typename T, int D, bool PAGED>
-struct Rows16 {
-  const T *k, *v;  // row of position p0
+__device__ __forceinline__ int tiles_of(const Keys& ks, int len) {
+  return ks.hi > ks.lo ? (ks.hi - 1) / len - ks.lo / len + 1 : 0;
+}
+
+// The 16 positions from q0 (a multiple of 16) of a sequence: its page and the
+// library token its values are read from, wave-uniform, through the scalar cache.
+struct Entry {
+  int32_t page, alias;
 };
+template <bool PAGED>
+__device__ __forceinline__ Entry entry_of(const CacheView& cv, int seq, int pos) {
+  Entry e{0, -1};
+  if (PAGED) {
+    typedef const __attribute__((address_space(4))) int32_t* cptr;
+    const cptr row = (cptr)(uintptr_t)(cv.page_table + (int64_t)seq * 2 * cv.n_lp);
+    e.page = row[pos >> 4];
+    if (cv.v_alias) e.alias = row[cv.n_lp + (pos >> 4)];
+  }
+  return e;
+}
+template <int D, bool PAGED>
+__device__ __forceinline__ int64_t rows_off(const CacheView& cv, int layer, int seq, int hk, int q0, const Entry& e) {
+  if (PAGED) return (int64_t)layer * cv.layer_stride + ((int64_t)e.page * cv.n_kv_heads + hk) * 16 * D;
+  return kv_offset<false>(cv, layer, seq, hk, q0);
+}
 template <typename T, int D, bool PAGED>
-__device__ __forceinline__ Rows16<T, D, PAGED> rows16(const CacheView& cv, int layer, int seq, int hk, int p0) {
-  const T* ck = reinterpret_cast<const T*>(cv.k);
-  const T* cvv = reinterpret_cast<const T*>(cv.v);
-  Rows16<T, D, PAGED> r;
-  if (!PAGED) {
-    const int64_t off = kv_offset<false>(cv, layer, seq, hk, p0);
-    r.k = ck + off;
-    r.v = cvv + off;
-    return r;
-  }
-  typedef const __attribute__((address_space(4))) int32_t* cptr;  // wave-uniform: through the scalar cache
-  const cptr row = (cptr)(uintptr_t)(cv.page_table + (int64_t)seq * 2 * cv.n_lp);
-  const int page = row[p0 >> 4];
-  const int64_t off = (int64_t)layer * cv.layer_stride + ((int64_t)page * cv.n_kv_heads + hk) * 16 * D;
-  r.k = ck + off;
-  r.v = cvv + off;
-  if (cv.v_alias) {
-    const int a = row[cv.n_lp + (p0 >> 4)];
-    if (a >= 0)
-      r.v = reinterpret_cast<const T*>(cv.lib_v) + (((int64_t)layer * cv.n_kv_heads + hk) * cv.lib_cap + a) * D;
-  }
-  return r;
+__device__ __forceinline__ const T* key_rows(const CacheView& cv, int layer, int seq, int hk, int q0, const Entry& e) {
+  return (const T*)uniform_ptr(reinterpret_cast<const T*>(cv.k) + rows_off<D, PAGED>(cv, layer, seq, hk, q0, e));
+}
+template <typename T, int D, bool PAGED>
+__device__ __forceinline__ const T* value_rows(const CacheView& cv, int layer, int seq, int hk, int q0, const Entry& e) {
+  const T* p = reinterpret_cast<const T*>(cv.v) + rows_off<D, PAGED>(cv, layer, seq, hk, q0, e);
+  if (PAGED && e.alias >= 0)
+    p = reinterpret_cast<const T*>(cv.lib_v) + (((int64_t)layer * cv.n_kv_heads + hk) * cv.lib_cap + e.alias) * D;
+  return (const T*)uniform_ptr(p);
 }
 
 __device__ __forceinline__ const char* row_ptr(const RowView& v, int64_t esize, int tok, int head) {
@@ -102,108 +110,240 @@ __device__ __forceinline__ uint32_t finite2(uint32_t x, bool* bad) {
   return x & (hi ? 0x0000FFFFu : 0xFFFFFFFFu) & (lo ? 0xFFFF0000u : 0xFFFFFFFFu);
 }
 __device__ __forceinline__ float not_finite(float x) { return fabsf(x) < INFINITY ? 0.f : x; }
+__device__ __forceinline__ float finite_abs(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
+
+// max over each group of N lanes (16 or 32)
+template <int N>
+__device__ __forceinline__ float max_lanes(float v) {
+  if (N == 32) return max_lanes32(v);
+  v = fmaxf(v, dpp_f32<kDppXor1>(v));
+  v = fmaxf(v, dpp_f32<kDppXor2>(v));
+  v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
+  return fmaxf(v, dpp_f32<kDppMirror>(v));
+}
+
+// Where a row's result goes: the output, or the slot's partial.  bf16 caches keep
+// partial outputs in fp16, scaled per row by the power of two 2^up that brings the
+// row's largest to 2^14 .. 2^15 (so eleven significant bits in two bytes; bf16 ones
+// cost a rounding of the size of the result's own, 2.8e-3 off the definition
+// instead of 2.4e-3, and fp32 ones move twice the bytes); max, sum and up are
+// fp32.  fp32 caches keep fp32 partials, up = 0.
+typedef _Float16 px_f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 px_f16x8 __attribute__((ext_vector_type(8)));
+template <typename T, int D>
+struct Emit {
+  char* dst;
+  float* aux;  // lse, or the partial's (max, sum, up, -)
+  float scale, a0, a1, a2;
+  bool direct;
+  __device__ __forceinline__ Emit(const PrefixCall& pc, const PrefixItem& it, int hk, int Hkv, int r, int tok, int head,
+                                  float m, float l, float top) {
+    direct = pc.direct;
+    if (direct) {
+      scale = l == 0.f ? 0.f : 1.f / l;
+      dst = const_cast<char*>(row_ptr(pc.out, sizeof(T), tok, head));
+      a0 = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+      aux = pc.lse ? pc.lse + (int64_t)tok * (Hkv * pc.g) + head : nullptr;
+    } else {
+      const int up = sizeof(T) == 2 && top > 0.f ? max(-126, min(126, 15 - __builtin_amdgcn_frexp_expf(top))) : 0;
+      scale = __builtin_ldexpf(1.f, up);
+      const int64_t pr = ((int64_t)it.slot * Hkv + hk) * pc.rows + it.row0 + r;
+      dst = reinterpret_cast<char*>(pc.part_o) + pr * (D * (int)sizeof(T));
+      aux = pc.part_ml + pr * 4;
+      a0 = m;
+      a1 = l;
+      a2 = (float)up;
+    }
+  }
+  __device__ __forceinline__ void put(int dim, float x0, float x1, float x2, float x3) const {
+    if (dim == 0) {
+      if (!direct) *reinterpret_cast<float4*>(aux) = make_float4(a0, a1, a2, 0.f);
+      else if (aux) *aux = a0;
+    }
+    if (sizeof(T) == 4) {
+      const float4 y = make_float4(x0 * scale, x1 * scale, x2 * scale, x3 * scale);
+      __builtin_memcpy(dst + dim * 4, &y, 16);
+    } else if (direct) {
+      const uint2 y = make_uint2(px_cvt(x0 * scale, x1 * scale), px_cvt(x2 * scale, x3 * scale));
+      __builtin_memcpy(dst + dim * 2, &y, 8);
+    } else {
+      const px_f16x2 a = __builtin_convertvector((px_f32x2){x0 * scale, x1 * scale}, px_f16x2);
+      const px_f16x2 b = __builtin_convertvector((px_f32x2){x2 * scale, x3 * scale}, px_f16x2);
+      st8_nt(dst + dim * 2, __builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+    }
+  }
+};
+
+// The plan of a call: in device memory, or by value.
+template <bool VALUE>
+struct Plan {};
+template <>
+struct Plan<false> {
+  const PrefixItem* items;
+  const PrefixRank* ranks;
+  __device__ __forceinline__ PrefixItem item(int b) const { return items[b]; }
+  __device__ __forceinline__ PrefixRank rank(int r) const { return ranks[r]; }
+};
+template <>
+struct Plan<true> {
+  PrefixArgs a;
+  __device__ __forceinline__ PrefixItem item(int b) const {
+    PrefixItem it{};
+    if (b < a.n_pre) {
+      const int rb = b / a.pre_slots, s = b - rb * a.pre_slots;
+      it.row0 = rb * a.block;
+      it.n_row = min(a.block, a.pre_rows - it.row0);
+      it.a0 = s * a.per;
+      it.a1 = min(a.prefix_len, it.a0 + a.per);
+      it.slot = s;
+      return it;
+    }
+    // the group is the last one whose first item is at most b: one group per lane
+    static_assert(kPfxGroups == 64, "one group per lane");
+    const int lane = threadIdx.x & 63, x = b - a.n_pre;
+    const PrefixGroup mine = a.group[min(lane, a.n_group - 1)];
+    const uint64_t below = __builtin_amdgcn_ballot_w64(lane < a.n_group && mine.item0 <= x);
+    const int r = 63 - __builtin_clzll(below);
+    const int rows = __builtin_amdgcn_readlane(mine.rows, r), end = __builtin_amdgcn_readlane(mine.end, r);
+    it.seq = __builtin_amdgcn_readlane(mine.seq, r);
+    const int s = x - __builtin_amdgcn_readlane(mine.item0, r);
+    it.row0 = rows & 0xFFFF;
+    it.n_row = rows >> 16;
+    const int cut = a.prefix_len / kPfxTile * kPfxTile + s * a.per;  // splits are cut at multiples of a tile
+    it.b0 = max(a.prefix_len, cut);
+    it.b1 = min(end, cut + a.per);
+    it.slot = a.pre_slots + s;
+    return it;
+  }
+  __device__ __forceinline__ PrefixRank rank(int r) const {
+    const PrefixSmall m = a.rank[r];
+    return PrefixRank{m.tok, m.pos, (uint16_t)a.pre_slots, (uint16_t)a.pre_slots, m.nb, 0};
+  }
+};
 
 }  // namespace
 
 // ------------------------------------------------------------------ bf16
 
-template <int D, bool PAGED>
-__global__ void __launch_bounds__(256, 2) prefix_attend_kernel(PrefixCall pc, CacheView cv) {
-  constexpr int KS = D / 32;        // 32-deep steps over the head dimension
-  constexpr int DT = D / 16;        // 16-wide output tiles
-  constexpr int NC = D / 8;         // 16-byte chunks of a row
-  constexpr int RI = 64 / NC;       // rows of one DMA instruction
-  constexpr int KI = 16 / RI;       // instructions for 16 rows
-  constexpr int HALF_T = kPfxTile * D;  // elements of a tile's keys (values)
-  __shared__ __align__(16) bf16_t s_kv[2][2 * HALF_T];
-  __shared__ float s_wm[4][16], s_wl[4][16];
+// WAVES 4: 128 query rows, two tiles in LDS, two blocks per compute unit.  WAVES
+// 8: 256 rows, four tiles, one block.  VALUE: the plan comes by value.
+template <int D, bool PAGED, int WAVES, bool VALUE>
+__global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_kernel(PrefixCall pc, Plan<VALUE> plan,
+                                                                                       CacheView cv) {
+  constexpr int NT = WAVES * 64;
+  constexpr int NB = WAVES == 4 ? 2 : 4;  // tiles in LDS
+  constexpr int KS = D / 32;              // 32-deep steps over the head dimension
+  constexpr int DT = D / 16;              // 16-wide output tiles
+  constexpr int NC = D / 8;               // 16-byte chunks of a row
+  constexpr int RI = 64 / NC;             // rows of one DMA instruction
+  constexpr int KI = 16 / RI;             // instructions for 16 rows
+  constexpr int HALF_T = kPfxTile * D;    // elements of a tile's keys (values)
+  __shared__ __align__(16) bf16_t s_kv[NB][2 * HALF_T];
+  __shared__ float s_wm[WAVES][32], s_wl[WAVES][32];
+  __shared__ __align__(16) int s_bad[2][4];
 
-  const PrefixItem it = pc.items[blockIdx.x];
-  const int hk = blockIdx.y;
+  const PrefixItem it = plan.item(blockIdx.y);
+  const int hk = blockIdx.x;  // fastest: workgroups go to the eight XCDs in turn, so a head's blocks share an L2
   const int t = threadIdx.x, lane = t & 63, lr = lane & 15, lq = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int Hkv = cv.n_kv_heads;
   const int g = pc.g;
   const float qscale = 1.4426950408889634f / sqrtf((float)D);
+  const Keys ka{pc.prefix_seq, it.a0, it.a1}, kb{it.seq, it.b0, it.b1};
 
-  // lane offsets (bytes) of the DMA instructions for 16 rows, interior tiles
+  // byte offset of this lane's chunk in row r (of 16) for instruction j, and the
+  // chunk's swizzle: keys row % NC, values 2 (row % (NC / 2))
   auto k_off = [&](int j, int r) __attribute__((always_inline)) -> uint32_t {
-    const int rr = j * RI + lane / NC;
-    return (uint32_t)(r * D + ((lane % NC) ^ (rr % NC)) * 8) * 2;
+    return (uint32_t)(r * D + ((lane % NC) ^ ((j * RI + lane / NC) % NC)) * 8) * 2;
   };
   auto v_off = [&](int j, int r) __attribute__((always_inline)) -> uint32_t {
-    const int rr = j * RI + lane / NC;
-    return (uint32_t)(r * D + ((lane % NC) ^ (2 * (rr % (NC / 2)))) * 8) * 2;
+    return (uint32_t)(r * D + ((lane % NC) ^ (2 * ((j * RI + lane / NC) % (NC / 2)))) * 8) * 2;
   };
-  // 16 keys from position p0 of range ks into LDS, keys at lk, values at lv
-  auto issue16 = [&](const Keys& ks, int p0, uint32_t lk, uint32_t lv) __attribute__((always_inline)) {
-    // a group of 16 with no key inside the range re-reads the nearest one
-    const int q0 = min(max(p0, ks.lo & ~15), (ks.hi - 1) & ~15);
-    const Rows16<bf16_t, D, PAGED> b = rows16<bf16_t, D, PAGED>(cv, pc.layer, ks.seq, hk, q0);
+  // 16 rows from position q0 of range ks into LDS; rows outside the range re-read one inside it
+  auto issue_k = [&](const Keys& ks, int q0, const void* base, uint32_t lds) __attribute__((always_inline)) {
     const int rlo = max(ks.lo - q0, 0), rhi = min(ks.hi - 1 - q0, 15);
-    const void *bk = uniform_ptr(b.k), *bv = uniform_ptr(b.v);
 #pragma unroll
-    for (int j = 0; j < KI; ++j) dma16s(bk, k_off(j, min(max(j * RI + lane / NC, rlo), rhi)), lk + j * 1024);
-#pragma unroll
-    for (int j = 0; j < KI; ++j) dma16s(bv, v_off(j, min(max(j * RI + lane / NC, rlo), rhi)), lv + j * 1024);
+    for (int j = 0; j < KI; ++j) dma16s(base, k_off(j, min(max(j * RI + lane / NC, rlo), rhi)), lds + j * 1024);
   };
-  constexpr int DPT = 2 * KI;  // DMA instructions of one issue16
-
-  // the two ranges, tiles of `len` keys starting on multiples of len
-  const Keys ka{pc.prefix_seq, it.a0, it.a1}, kb{it.seq, it.b0, it.b1};
-  auto tiles_of = [&](const Keys& ks, int len) { return ks.hi > ks.lo ? (ks.hi - 1) / len - ks.lo / len + 1 : 0; };
-
-  // this lane's query row `r` of the item
-  auto load_q = [&](int r, uint4* qf, int* rpos, int* rtok, int* rhead) __attribute__((always_inline)) {
-    const int row = it.row0 + (r < it.n_row ? r : 0);
-    const PrefixRank m = pc.ranks[row / g];
-    *rpos = m.pos;
-    *rtok = m.tok;
-    *rhead = hk * g + row % g;
-    const char* src = row_ptr(pc.q, 2, m.tok, *rhead);
+  auto issue_v = [&](const Keys& ks, int q0, const void* base, uint32_t lds) __attribute__((always_inline)) {
+    const int rlo = max(ks.lo - q0, 0), rhi = min(ks.hi - 1 - q0, 15);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = ld16_any(src + (ks * 32 + lq * 8) * 2);
+    for (int j = 0; j < KI; ++j) dma16s(base, v_off(j, min(max(j * RI + lane / NC, rlo), rhi)), lds + j * 1024);
   };
-
-  // write a row's result: the output, or the slot's partial
-  auto emit8 = [&](int r, int rtok, int rhead, int dim, float x0, float x1, float x2, float x3, float m,
-                   float l) __attribute__((always_inline)) {
-    if (pc.direct) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const uint2 y = make_uint2(px_cvt(x0 * inv, x1 * inv), px_cvt(x2 * inv, x3 * inv));
-      char* dst = const_cast<char*>(row_ptr(pc.out, 2, rtok, rhead)) + dim * 2;
-      __builtin_memcpy(dst, &y, 8);
-      if (dim == 0 && pc.lse)
-        pc.lse[(int64_t)rtok * (Hkv * g) + rhead] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-    } else {
-      // partial outputs in bf16: the merge weights them in fp32, and its result is bf16
-      const int64_t pr = ((int64_t)it.slot * Hkv + hk) * pc.rows + it.row0 + r;
-      st8_nt(reinterpret_cast<bf16_t*>(pc.part_o) + pr * D + dim, px_cvt(x0, x1), px_cvt(x2, x3));
-      if (dim == 0) {
-        pc.part_ml[pr * 2 + 0] = m;
-        pc.part_ml[pr * 2 + 1] = l;
-      }
+  // a group of 16 positions with none inside the range stands for the nearest one that has
+  auto group_of = [&](const Keys& ks, int p0) __attribute__((always_inline)) {
+    return min(max(p0, ks.lo & ~15), (ks.hi - 1) & ~15);
+  };
+  // non-finite elements of 16 value rows in LDS to zeros; true if there were some
+  auto clean16 = [&](bf16_t* v) __attribute__((always_inline)) -> bool {
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < KI; ++j) {
+      uint4* p = reinterpret_cast<uint4*>(v) + j * 64 + lane;
+      uint4 x = *p;
+      bool b = false;
+      x = make_uint4(finite2(x.x, &b), finite2(x.y, &b), finite2(x.z, &b), finite2(x.w, &b));
+      if (b) *p = x;
+      bad = bad || b;
     }
+    return __builtin_amdgcn_ballot_w64(bad) != 0;
   };
 
-  if (it.n_row > 16) {
+  if (it.n_row > 32) {
     // ---------------------------------------------------------------- wide
     constexpr int RT = 2;
-    const int na = tiles_of(ka, kPfxTile), nb = tiles_of(kb, kPfxTile), nt = na + nb;
-    // tile ti: its range and first position
-    auto issue = [&](int ti) __attribute__((always_inline)) {
-      const bool own = ti >= na;
-      const Keys ks = own ? kb : ka;
-      const int p0 = (ks.lo / kPfxTile + (own ? ti - na : ti)) * kPfxTile + 16 * w;
-      bf16_t* buf = s_kv[ti & 1];
-      issue16(ks, p0, lds_addr(buf) + w * (16 * D * 2), lds_addr(buf + HALF_T) + w * (16 * D * 2));
+    constexpr int DPT = 8 * KI / WAVES;  // DMA instructions of this wave for a tile
+    const int ta0 = ka.lo / kPfxTile, tb0 = kb.lo / kPfxTile;
+    const int na = tiles_of(ka, kPfxTile), nt = na + tiles_of(kb, kPfxTile);
+    const int grp = w & 3;               // the 16 keys this wave brings in
+    auto first_of = [&](int ti) __attribute__((always_inline)) {
+      return (ti >= na ? tb0 + ti - na : ta0 + ti) * kPfxTile;
     };
+    Entry ent;
+    auto fetch = [&](int ti) __attribute__((always_inline)) {  // the page of this wave's rows of tile ti
+      if (ti >= nt) return;
+      const Keys& ks = ti >= na ? kb : ka;
+      ent = entry_of<PAGED>(cv, ks.seq, group_of(ks, first_of(ti) + 16 * grp));
+    };
+    auto issue = [&](int ti) __attribute__((always_inline)) {
+      const Keys ks = ti >= na ? kb : ka;
+      const int q0 = group_of(ks, first_of(ti) + 16 * grp);
+      bf16_t* buf = s_kv[ti & (NB - 1)];
+      if (WAVES == 4 || w < 4)
+        issue_k(ks, q0, key_rows<bf16_t, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, ent), lds_addr(buf) + grp * (16 * D * 2));
+      if (WAVES == 4 || w >= 4)
+        issue_v(ks, q0, value_rows<bf16_t, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, ent),
+                lds_addr(buf + HALF_T) + grp * (16 * D * 2));
+    };
+    fetch(0);
     if (nt) issue(0);
     uint4 qf[RT][KS];
     int rpos[RT], rtok[RT], rhead[RT];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-      load_q(16 * (RT * w + rt) + lr, qf[rt], &rpos[rt], &rtok[rt], &rhead[rt]);
+    for (int rt = 0; rt < RT; ++rt) {
+      const int r = 16 * (RT * w + rt) + lr;
+      const int row = it.row0 + (r < it.n_row ? r : 0);
+      const PrefixRank m = plan.rank(row / g);
+      rpos[rt] = m.pos;
+      rtok[rt] = m.tok;
+      rhead[rt] = hk * g + row % g;
+      const char* src = row_ptr(pc.q, 2, m.tok, rhead[rt]);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) qf[rt][ks] = ld16_any(src + (ks * 32 + lq * 8) * 2);
+    }
+    // the compiler cannot see the tile loads: its wait for these must not fall into the loop
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) asm volatile("" ::"v"(__builtin_bit_cast(u32x4_t, qf[rt][s])));
+      asm volatile("" ::"v"(rpos[rt]), "v"(rtok[rt]));
+    }
+#pragma unroll
+    for (int i = 1; i < NB - 1; ++i) {
+      fetch(i);
+      if (i < nt) issue(i);
+    }
+    fetch(NB - 1);
     float mrow[RT], lsum[RT];
     px_f32x4 acc[RT][DT];
 #pragma unroll
@@ -214,24 +354,28 @@ __global__ void __launch_bounds__(256, 2) prefix_attend_kernel(PrefixCall pc, Ca
       for (int dt = 0; dt < DT; ++dt) acc[rt][dt] = px_f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const bool busy = 16 * RT * w < it.n_row;  // some row of this wave
-    // the compiler cannot see the tile loads: its wait for these must not fall into the loop
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-      for (int s = 0; s < KS; ++s) asm volatile("" ::"v"(__builtin_bit_cast(u32x4_t, qf[rt][s])));
-      asm volatile("" ::"v"(rpos[rt]), "v"(rtok[rt]));
-    }
-#pragma unroll 1
-    for (int ti = 0; ti < nt; ++ti) {
-      wait_vm<0>();   // this wave's loads of the tile have landed ...
-      lds_barrier();  // ... and every wave's; every wave is done with the tile before
-      if (ti + 1 < nt) issue(ti + 1);
-      if (!busy) continue;
+
+    auto step = [&](int ti, auto buf) __attribute__((always_inline)) {
+      bf16_t* K = s_kv[buf];
+      bf16_t* V = K + HALF_T;
       const bool own = ti >= na;
-      const Keys ks = own ? kb : ka;
-      const int p0 = (ks.lo / kPfxTile + (own ? ti - na : ti)) * kPfxTile;
-      const bf16_t* K = s_kv[ti & 1];
-      const bf16_t* V = K + HALF_T;
+      const int lo = own ? kb.lo : ka.lo, hi = own ? kb.hi : ka.hi;
+      const int p0 = first_of(ti);
+      const bool edge = own || p0 < lo || p0 + kPfxTile > hi;  // masked keys: block-uniform
+      // this wave's loads of the tile have landed (up to NB - 2 later tiles may be in flight) ...
+      const int ahead = min(NB - 2, nt - 1 - ti);
+      if (ahead >= 2) wait_vm<2 * DPT>();
+      else if (ahead == 1) wait_vm<DPT>();
+      else wait_vm<0>();
+      if (edge && (WAVES == 4 || w >= 4))
+      {
+        const bool bad = clean16(V + grp * 16 * D);
+        if (lane == 0) s_bad[buf & 1][grp] = bad;
+      }
+      lds_barrier();  // ... and every wave's; every wave is done with the tile before
+      if (ti + NB - 1 < nt) issue(ti + NB - 1);
+      fetch(ti + NB);
+      if (!busy) return;
       px_f32x4 st[RT][4];
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) {
@@ -246,18 +390,17 @@ __global__ void __launch_bounds__(256, 2) prefix_attend_kernel(PrefixCall pc, Ca
           st[rt][kt] = c;
         }
       }
-      const bool edge = own || p0 < ks.lo || p0 + kPfxTile > ks.hi;  // masked keys: block-uniform
       if (edge) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          // key p0 + 16 kt + 4 lq + e is visible iff lo <= 16 kt + e <= hi
-          const int lo = ks.lo - p0 - 4 * lq;
-          const int hi = (own ? min(rpos[rt], ks.hi - 1) : ks.hi - 1) - p0 - 4 * lq;
+          // key p0 + 16 kt + 4 lq + e is visible iff a <= 16 kt + e <= b
+          const int a = lo - p0 - 4 * lq;
+          const int b = (own ? min(rpos[rt], hi - 1) : hi - 1) - p0 - 4 * lq;
 #pragma unroll
           for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              st[rt][kt][e] = 16 * kt + e >= lo && 16 * kt + e <= hi ? st[rt][kt][e] : -INFINITY;
+              st[rt][kt][e] = 16 * kt + e >= a && 16 * kt + e <= b ? st[rt][kt][e] : -INFINITY;
         }
       }
       uint4 pb[RT][2];
@@ -300,177 +443,220 @@ __global__ void __launch_bounds__(256, 2) prefix_attend_kernel(PrefixCall pc, Ca
       auto vfrag = [&](int i) __attribute__((always_inline)) -> uint4 {
         const int vc = (2 * (i >> 1) + ((lr & 3) >> 1)) ^ vsw;
         const bf16_t* row = &V[((32 * (i & 1) + vr) * NC + vc) * 8 + (lr & 1) * 4];
-        const uint2 lo = ld_tr8(row), hi = ld_tr8(row + 16 * D);
-        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+        const uint2 lo2 = ld_tr8(row), hi2 = ld_tr8(row + 16 * D);
+        return make_uint4(lo2.x, lo2.y, hi2.x, hi2.y);
       };
-      if (!edge) {
-        uint4 va = vfrag(0);
+      uint4 va = vfrag(0);
 #pragma unroll
-        for (int i = 0; i < 2 * DT; ++i) {
-          const uint4 vn = i + 1 < 2 * DT ? vfrag(i + 1) : va;
+      for (int i = 0; i < 2 * DT; ++i) {
+        const uint4 vn = i + 1 < 2 * DT ? vfrag(i + 1) : va;
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) acc[rt][i >> 1] = mma32(va, pb[rt][i & 1], acc[rt][i >> 1]);
-          va = vn;
-        }
-      } else {
-        bool bad = false;
-#pragma unroll
-        for (int i = 0; i < 2 * DT; ++i) {
-          uint4 va = vfrag(i);
-          va = make_uint4(finite2(va.x, &bad), finite2(va.y, &bad), finite2(va.z, &bad), finite2(va.w, &bad));
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) acc[rt][i >> 1] = mma32(va, pb[rt][i & 1], acc[rt][i >> 1]);
-        }
-        if (__builtin_amdgcn_ballot_w64(bad)) {
+        for (int rt = 0; rt < RT; ++rt) acc[rt][i >> 1] = mma32(va, pb[rt][i & 1], acc[rt][i >> 1]);
+        va = vn;
+      }
+      const int* sb = s_bad[buf & 1];
+      if (edge && (sb[0] | sb[1] | sb[2] | sb[3])) {
+        const int seq = own ? kb.seq : ka.seq;
 #pragma unroll 1
-          for (int p = max(p0, ks.lo); p < min(p0 + kPfxTile, ks.hi); ++p) {
-            const int kk = p - p0, sw = 2 * (kk % (NC / 2));
+        for (int p = max(p0, lo); p < min(p0 + kPfxTile, hi); ++p) {
+          const bf16_t* row = value_rows<bf16_t, D, PAGED>(cv, pc.layer, seq, hk, p & ~15, entry_of<PAGED>(cv, seq, p)) +
+                              (p & 15) * D + lq * 4;
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-              const uint2 x = *reinterpret_cast<const uint2*>(&V[(kk * NC + ((2 * dt + (lq >> 1)) ^ sw)) * 8 + (lq & 1) * 4]);
-              const float v[4] = {lo_bf16(x.x), hi_bf16(x.x), lo_bf16(x.y), hi_bf16(x.y)};
+          for (int dt = 0; dt < DT; ++dt) {
+            const uint2 x = *reinterpret_cast<const uint2*>(row + dt * 16);
+            const float v[4] = {lo_bf16(x.x), hi_bf16(x.x), lo_bf16(x.y), hi_bf16(x.y)};
 #pragma unroll
-              for (int rt = 0; rt < RT; ++rt)
+            for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[rt][dt][e] += !own || p <= rpos[rt] ? not_finite(v[e]) : 0.f;
-            }
+              for (int e = 0; e < 4; ++e) acc[rt][dt][e] += !own || p <= rpos[rt] ? not_finite(v[e]) : 0.f;
           }
         }
+      }
+    };
+    // unrolled by the ring, so that every LDS address is a constant past a lane's base
+    for (int ti = 0; ti < nt; ti += NB) {
+      step(ti, std::integral_constant<int, 0>{});
+      if (ti + 1 >= nt) break;
+      step(ti + 1, std::integral_constant<int, 1>{});
+      if constexpr (NB == 4) {
+        if (ti + 2 >= nt) break;
+        step(ti + 2, std::integral_constant<int, 2>{});
+        if (ti + 3 >= nt) break;
+        step(ti + 3, std::integral_constant<int, 3>{});
       }
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const float l = sum_rows4(lsum[rt]);
       const int r = 16 * (RT * w + rt) + lr;
+      float top = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, finite_abs(acc[rt][dt][e]));
+      const Emit<bf16_t, D> em(pc, it, hk, Hkv, r, rtok[rt], rhead[rt], mrow[rt], l, max_rows4(top));
       if (r >= it.n_row) continue;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
-        emit8(r, rtok[rt], rhead[rt], dt * 16 + lq * 4, acc[rt][dt][0], acc[rt][dt][1], acc[rt][dt][2], acc[rt][dt][3],
-              mrow[rt], l);
+        em.put(dt * 16 + lq * 4, acc[rt][dt][0], acc[rt][dt][1], acc[rt][dt][2], acc[rt][dt][3]);
     }
     return;
   }
 
   // ------------------------------------------------------------------ narrow
   constexpr int TILE = 16 * D * 2 * 2;  // bytes of a 16-key tile: keys, then values
-  static_assert(4 * 2 * TILE == sizeof(s_kv), "a ring of two per wave");
+  constexpr int DPT = 2 * KI;
+  static_assert(WAVES * 2 * TILE == sizeof(s_kv) || WAVES == 8, "a ring of two per wave");
+  static_assert(WAVES * 2 * TILE <= sizeof(s_kv) && 32 * D * 4 <= 2 * TILE, "rings and results fit");
   char* ring = reinterpret_cast<char*>(s_kv) + w * 2 * TILE;
-  const uint32_t ring_lds = lds_addr(ring);
-  const int na = tiles_of(ka, 16), nb = tiles_of(kb, 16);
-  const int n = (na + nb - w + 3) >> 2;  // this wave's tiles: w, w + 4, ...
-  auto issue = [&](int i) __attribute__((always_inline)) {
-    const int ti = w + 4 * i;
-    const bool own = ti >= na;
-    const Keys ks = own ? kb : ka;
-    const int p0 = ((ks.lo >> 4) + (own ? ti - na : ti)) * 16;
-    issue16(ks, p0, ring_lds + (i & 1) * TILE, ring_lds + (i & 1) * TILE + 16 * D * 2);
-  };
-  if (n > 0) issue(0);
-  uint4 qf[KS];
-  int rpos, rtok, rhead;
-  load_q(lr, qf, &rpos, &rtok, &rhead);
-  float mref = -INFINITY, lsum = 0.f;
-  px_f32x4 acc[DT];
+  auto narrow = [&](auto row_tiles) __attribute__((always_inline)) {
+    constexpr int RT = decltype(row_tiles)::value;
+    const uint32_t ring_lds = lds_addr(ring);
+    const int na = tiles_of(ka, 16), nb = tiles_of(kb, 16);
+    const int n = (na + nb - w + WAVES - 1) / WAVES;  // this wave's tiles: w, w + WAVES, ...
+    auto first_of = [&](int i) __attribute__((always_inline)) {
+      const int ti = w + WAVES * i;
+      return (ti >= na ? (kb.lo >> 4) + ti - na : (ka.lo >> 4) + ti) * 16;
+    };
+    auto own_of = [&](int i) __attribute__((always_inline)) { return w + WAVES * i >= na; };
+    Entry ent;
+    auto fetch = [&](int i) __attribute__((always_inline)) {
+      if (i < n) ent = entry_of<PAGED>(cv, own_of(i) ? kb.seq : ka.seq, first_of(i));
+    };
+    auto issue = [&](int i) __attribute__((always_inline)) {
+      const Keys ks = own_of(i) ? kb : ka;
+      const int q0 = first_of(i);
+      issue_k(ks, q0, key_rows<bf16_t, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, ent), ring_lds + (i & 1) * TILE);
+      issue_v(ks, q0, value_rows<bf16_t, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, ent),
+              ring_lds + (i & 1) * TILE + 16 * D * 2);
+    };
+    fetch(0);
+    if (n > 0) issue(0);
+    fetch(1);
+    uint4 qf[RT][KS];
+    int rpos[RT];
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) acc[dt] = px_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int rt = 0; rt < RT; ++rt) {
+      const int r = 16 * rt + lr;
+      const int row = it.row0 + (r < it.n_row ? r : 0);
+      const PrefixRank m = plan.rank(row / g);
+      rpos[rt] = m.pos;
+      const char* src = row_ptr(pc.q, 2, m.tok, hk * g + row % g);
 #pragma unroll
-  for (int s = 0; s < KS; ++s) asm volatile("" ::"v"(__builtin_bit_cast(u32x4_t, qf[s])));  // landed before the next tile
+      for (int ks = 0; ks < KS; ++ks) qf[rt][ks] = ld16_any(src + (ks * 32 + lq * 8) * 2);
+    }
+    float mref[RT], lsum[RT];
+    px_f32x4 acc[RT][DT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      mref[rt] = -INFINITY;
+      lsum[rt] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) acc[rt][dt] = px_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) asm volatile("" ::"v"(__builtin_bit_cast(u32x4_t, qf[rt][s])));
+      asm volatile("" ::"v"(rpos[rt]));
+    }
 #pragma unroll 1
-  for (int i = 0; i < n; ++i) {
-    if (i + 1 < n) {
-      wait_lds();  // the reads of the buffer's tile before have returned
-      issue(i + 1);
-      wait_vm<DPT>();
-    } else {
-      wait_vm<0>();
-    }
-    const int ti = w + 4 * i;
-    const bool own = ti >= na;
-    const Keys ks = own ? kb : ka;
-    const int p0 = ((ks.lo >> 4) + (own ? ti - na : ti)) * 16;
-    const bf16_t* K = reinterpret_cast<const bf16_t*>(ring + (i & 1) * TILE);
-    uint4 kf[KS];
+    for (int i = 0; i < n; ++i) {
+      if (i + 1 < n) {
+        wait_lds();  // the reads of the buffer's tile before have returned
+        issue(i + 1);
+        fetch(i + 2);
+        wait_vm<DPT>();
+      } else {
+        wait_vm<0>();
+      }
+      const bool own = own_of(i);
+      const int lo = own ? kb.lo : ka.lo, hi = own ? kb.hi : ka.hi;
+      const int p0 = first_of(i);
+      bf16_t* K = reinterpret_cast<bf16_t*>(ring + (i & 1) * TILE);
+      const bool edge = (own && it.n_row > g) || p0 < lo || p0 + 16 > hi;  // masked keys: wave-uniform
+      const bool bad = edge && clean16(K + 16 * D);
+      uint4 kf[KS];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) kf[s] = ld16(&K[(lr * NC + ((s * 4 + lq) ^ (lr % NC))) * 8]);
-    uint2 va[DT];
-    const int vr = 4 * lq + (lr >> 2), vsw = 2 * (vr % (NC / 2));
+      for (int s = 0; s < KS; ++s) kf[s] = ld16(&K[(lr * NC + ((s * 4 + lq) ^ (lr % NC))) * 8]);
+      uint2 va[DT];
+      const int vr = 4 * lq + (lr >> 2), vsw = 2 * (vr % (NC / 2));
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-      va[dt] = ld_tr8(&K[16 * D + (vr * NC + ((2 * dt + ((lr & 3) >> 1)) ^ vsw)) * 8 + (lr & 1) * 4]);
-    px_f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+      for (int dt = 0; dt < DT; ++dt)
+        va[dt] = ld_tr8(&K[16 * D + (vr * NC + ((2 * dt + ((lr & 3) >> 1)) ^ vsw)) * 8 + (lr & 1) * 4]);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) sc = mma32(kf[s], qf[s], sc);
-    const int lo = ks.lo - p0 - 4 * lq, hi = (own ? min(rpos, ks.hi - 1) : ks.hi - 1) - p0 - 4 * lq;
-    float x[4], lmax = -INFINITY;
+      for (int rt = 0; rt < RT; ++rt) {
+        px_f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[e] = e >= lo && e <= hi ? sc[e] * qscale : -INFINITY;
-      lmax = fmaxf(lmax, x[e]);
-    }
-    if (__builtin_amdgcn_ballot_w64(lmax > mref + 8.f)) {
-      const float mn = max_rows4(fmaxf(mref, lmax));
-      const float f = mref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mref - mn);
-      lsum *= f;
+        for (int s = 0; s < KS; ++s) sc = mma32(kf[s], qf[rt][s], sc);
+        const int a = lo - p0 - 4 * lq, b = (own ? min(rpos[rt], hi - 1) : hi - 1) - p0 - 4 * lq;
+        float x[4], lmax = -INFINITY;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) acc[dt] *= f;
-      mref = mn;
-    }
-    const float mr = mref == -INFINITY ? 0.f : mref;
-    float p[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(x[e] - mr);
-      lsum += p[e];
-    }
-    const uint2 pb = make_uint2(px_cvt(p[0], p[1]), px_cvt(p[2], p[3]));
-    const bool edge = (own && it.n_row > g) || p0 < ks.lo || p0 + 16 > ks.hi;  // masked keys: wave-uniform
-    bool bad = false;
-    if (edge) {
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) va[dt] = make_uint2(finite2(va[dt].x, &bad), finite2(va[dt].y, &bad));
-    }
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) acc[dt] = mma16(va[dt], pb, acc[dt]);
-    if (edge && __builtin_amdgcn_ballot_w64(bad)) {
-#pragma unroll 1
-      for (int q = max(p0, ks.lo); q < min(p0 + 16, ks.hi); ++q) {
-        const int kk = q - p0, sw = 2 * (kk % (NC / 2));
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const uint2 y = *reinterpret_cast<const uint2*>(
-              &K[16 * D + (kk * NC + ((2 * dt + (lq >> 1)) ^ sw)) * 8 + (lq & 1) * 4]);
-          const float v[4] = {lo_bf16(y.x), hi_bf16(y.x), lo_bf16(y.y), hi_bf16(y.y)};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[dt][e] += !own || q <= rpos ? not_finite(v[e]) : 0.f;
+        for (int e = 0; e < 4; ++e) {
+          x[e] = e >= a && e <= b ? sc[e] * qscale : -INFINITY;
+          lmax = fmaxf(lmax, x[e]);
         }
+        if (__builtin_amdgcn_ballot_w64(lmax > mref[rt] + 8.f)) {
+          const float mn = max_rows4(fmaxf(mref[rt], lmax));
+          const float f = mref[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mref[rt] - mn);
+          lsum[rt] *= f;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) acc[rt][dt] *= f;
+          mref[rt] = mn;
+        }
+        const float mr = mref[rt] == -INFINITY ? 0.f : mref[rt];
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(x[e] - mr);
+          lsum[rt] += p[e];
+        }
+        const uint2 pb = make_uint2(px_cvt(p[0], p[1]), px_cvt(p[2], p[3]));
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) acc[rt][dt] = mma16(va[dt], pb, acc[rt][dt]);
+      }
+      if (bad) {
+        const int seq = own ? kb.seq : ka.seq;
+        const bf16_t* rows = value_rows<bf16_t, D, PAGED>(cv, pc.layer, seq, hk, p0, entry_of<PAGED>(cv, seq, p0));
+#pragma unroll 1
+        for (int p = max(p0, lo); p < min(p0 + 16, hi); ++p)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const uint2 y = *reinterpret_cast<const uint2*>(rows + (p - p0) * D + dt * 16 + lq * 4);
+            const float v[4] = {lo_bf16(y.x), hi_bf16(y.x), lo_bf16(y.y), hi_bf16(y.y)};
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[rt][dt][e] += !own || p <= rpos[rt] ? not_finite(v[e]) : 0.f;
+          }
       }
     }
-  }
-  // the four waves meet in LDS, each wave's outputs in its own ring
-  lsum = sum_rows4(lsum);
-  wait_lds();
-  static_assert(16 * D * 4 <= 2 * TILE, "a wave's outputs fit its ring");
-  {
+    // the waves meet in LDS, each wave's outputs in its own ring
+    wait_lds();
     float* o = reinterpret_cast<float*>(ring);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-      *reinterpret_cast<float4*>(&o[lr * D + dt * 16 + 4 * lq]) =
-          make_float4(acc[dt][0], acc[dt][1], acc[dt][2], acc[dt][3]);
-    if (lq == 0) {
-      s_wm[w][lr] = mref;
-      s_wl[w][lr] = lsum;
+    for (int rt = 0; rt < RT; ++rt) {
+      const float l = sum_rows4(lsum[rt]);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        *reinterpret_cast<float4*>(&o[(16 * rt + lr) * D + dt * 16 + 4 * lq]) =
+            make_float4(acc[rt][dt][0], acc[rt][dt][1], acc[rt][dt][2], acc[rt][dt][3]);
+      if (lq == 0) {
+        s_wm[w][16 * rt + lr] = mref[rt];
+        s_wl[w][16 * rt + lr] = l;
+      }
     }
-  }
+  };
+  if (it.n_row > 16) narrow(std::integral_constant<int, 2>{});
+  else narrow(std::integral_constant<int, 1>{});
   __syncthreads();
-  for (int idx = t; idx < it.n_row * D / 4; idx += 256) {
-    const int r = idx / (D / 4), d = 4 * (idx % (D / 4));
+  constexpr int LPR = D / 4;  // lanes of a row
+  for (int idx = t; idx < it.n_row * LPR; idx += NT) {
+    const int r = idx / LPR, d = 4 * (idx % LPR);
     float M = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) M = fmaxf(M, s_wm[k][r]);
+    for (int k = 0; k < WAVES; ++k) M = fmaxf(M, s_wm[k][r]);
     float L = 0.f;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < WAVES; ++k) {
       const float m = s_wm[k][r];
       const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
       const float4 o = *reinterpret_cast<const float4*>(reinterpret_cast<char*>(s_kv) + k * 2 * TILE + (r * D + d) * 4);
@@ -481,7 +667,9 @@ __global__ void __launch_bounds__(256, 2) prefix_attend_kernel(PrefixCall pc, Ca
       a.w = fmaf(o.w, f, a.w);
     }
     const int row = it.row0 + r;
-    emit8(r, pc.ranks[row / g].tok, hk * g + row % g, d, a.x, a.y, a.z, a.w, M, L);
+    const float top = fmaxf(fmaxf(finite_abs(a.x), finite_abs(a.y)), fmaxf(finite_abs(a.z), finite_abs(a.w)));
+    const Emit<bf16_t, D> em(pc, it, hk, Hkv, r, plan.rank(row / g).tok, hk * g + row % g, M, L, max_lanes<LPR>(top));
+    em.put(d, a.x, a.y, a.z, a.w);
   }
 }
 
@@ -492,8 +680,8 @@ __global__ void __launch_bounds__(256, 2) prefix_attend_kernel(PrefixCall pc, Ca
 // keys; narrow items: the same 16 rows in every wave, 16 of the keys each, merged
 // at the end.  The four k indices of a matrix step are dims 16 c + 4 lq + e of
 // keys and queries alike, so both are read 16 bytes at a time.
-template <int D, bool PAGED>
-__global__ void __launch_bounds__(256) prefix_attend_f32_kernel(PrefixCall pc, CacheView cv) {
+template <int D, bool PAGED, bool VALUE>
+__global__ void __launch_bounds__(256) prefix_attend_f32_kernel(PrefixCall pc, Plan<VALUE> plan, CacheView cv) {
   constexpr int DT = D / 16;
   constexpr int NC = D / 4;         // 16-byte chunks of a row
   constexpr int RI = 64 / NC;       // rows of one DMA instruction
@@ -502,8 +690,8 @@ __global__ void __launch_bounds__(256) prefix_attend_f32_kernel(PrefixCall pc, C
   __shared__ __align__(16) float s_kv[2 * HALF_T];
   __shared__ float s_wm[4][16], s_wl[4][16];
 
-  const PrefixItem it = pc.items[blockIdx.x];
-  const int hk = blockIdx.y;
+  const PrefixItem it = plan.item(blockIdx.y);
+  const int hk = blockIdx.x;
   const int t = threadIdx.x, lane = t & 63, lr = lane & 15, lq = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int Hkv = cv.n_kv_heads;
@@ -511,16 +699,13 @@ __global__ void __launch_bounds__(256) prefix_attend_f32_kernel(PrefixCall pc, C
   const float qscale = 1.4426950408889634f / sqrtf((float)D);
   const bool narrow = it.n_row <= 16;
   const Keys ka{pc.prefix_seq, it.a0, it.a1}, kb{it.seq, it.b0, it.b1};
-  auto tiles_of = [&](const Keys& ks) {
-    return ks.hi > ks.lo ? (ks.hi - 1) / kPfxTile - ks.lo / kPfxTile + 1 : 0;
-  };
-  const int na = tiles_of(ka), nt = na + tiles_of(kb);
+  const int na = tiles_of(ka, kPfxTile), nt = na + tiles_of(kb, kPfxTile);
   float* K = s_kv;
   float* V = s_kv + HALF_T;
 
   const int r = (narrow ? 0 : 16 * w) + lr;
   const int row = it.row0 + (r < it.n_row ? r : 0);
-  const PrefixRank m = pc.ranks[row / g];
+  const PrefixRank m = plan.rank(row / g);
   const int rhead = hk * g + row % g;
   px_f32x4 qf[DT];
   {
@@ -541,9 +726,10 @@ __global__ void __launch_bounds__(256) prefix_attend_f32_kernel(PrefixCall pc, C
     const int p0 = (ks.lo / kPfxTile + (own ? ti - na : ti)) * kPfxTile;
     {
       const int q0 = min(max(p0 + 16 * w, ks.lo & ~15), (ks.hi - 1) & ~15);
-      const Rows16<float, D, PAGED> b = rows16<float, D, PAGED>(cv, pc.layer, ks.seq, hk, q0);
+      const Entry e = entry_of<PAGED>(cv, ks.seq, q0);
       const int rlo = max(ks.lo - q0, 0), rhi = min(ks.hi - 1 - q0, 15);
-      const void *bk = uniform_ptr(b.k), *bv = uniform_ptr(b.v);
+      const void* bk = key_rows<float, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, e);
+      const void* bv = value_rows<float, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, e);
 #pragma unroll
       for (int j = 0; j < KI; ++j) {
         const int rr = j * RI + lane / NC;
@@ -619,26 +805,11 @@ __global__ void __launch_bounds__(256) prefix_attend_f32_kernel(PrefixCall pc, C
     __syncthreads();  // the tile's reads are done before the next one lands
   }
   lsum = sum_rows4(lsum);
-  auto emit = [&](int rr, int rtok, int head, int dim, float4 a, float M, float L) __attribute__((always_inline)) {
-    if (pc.direct) {
-      const float inv = L == 0.f ? 0.f : 1.f / L;
-      const float4 y = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
-      __builtin_memcpy(const_cast<char*>(row_ptr(pc.out, 4, rtok, head)) + dim * 4, &y, 16);
-      if (dim == 0 && pc.lse) pc.lse[(int64_t)rtok * (Hkv * g) + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
-    } else {
-      const int64_t pr = ((int64_t)it.slot * Hkv + hk) * pc.rows + it.row0 + rr;
-      *reinterpret_cast<float4*>(reinterpret_cast<float*>(pc.part_o) + pr * D + dim) = a;
-      if (dim == 0) {
-        pc.part_ml[pr * 2 + 0] = M;
-        pc.part_ml[pr * 2 + 1] = L;
-      }
-    }
-  };
   if (!narrow) {
     if (r >= it.n_row) return;
+    const Emit<float, D> em(pc, it, hk, Hkv, r, m.tok, rhead, mref, lsum, 0.f);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-      emit(r, m.tok, rhead, dt * 16 + 4 * lq, make_float4(acc[dt][0], acc[dt][1], acc[dt][2], acc[dt][3]), mref, lsum);
+    for (int dt = 0; dt < DT; ++dt) em.put(dt * 16 + 4 * lq, acc[dt][0], acc[dt][1], acc[dt][2], acc[dt][3]);
     return;
   }
   static_assert(4 * 16 * D <= 2 * HALF_T, "the waves' outputs fit the tile");
@@ -669,24 +840,30 @@ __global__ void __launch_bounds__(256) prefix_attend_f32_kernel(PrefixCall pc, C
       a.w = fmaf(o.w, f, a.w);
     }
     const int row2 = it.row0 + rr;
-    emit(rr, pc.ranks[row2 / g].tok, hk * g + row2 % g, d, a, M, L);
+    const Emit<float, D> em(pc, it, hk, Hkv, rr, plan.rank(row2 / g).tok, hk * g + row2 % g, M, L, 0.f);
+    em.put(d, a.x, a.y, a.z, a.w);
   }
 }
 
 // ------------------------------------------------------------------ merge
 
 // out = sum_s O_s 2^(M_s - M) / sum_s L_s 2^(M_s - M), M = max_s M_s, over the slots
-// of a row; 16 bytes of output per lane.  Grid (rank, kv heads' rows / rows a block).
-template <typename T, int D>
-__global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixCall pc, CacheView cv) {
-  constexpr int VEC = Store<T>::VEC;
-  constexpr int LPR = D / VEC;  // lanes of a row
-  const int Hkv = cv.n_kv_heads, g = pc.g, Hq = Hkv * g;
-  const PrefixRank m = pc.ranks[blockIdx.x];
-  const int head = blockIdx.y * (256 / LPR) + threadIdx.x / LPR, c = threadIdx.x % LPR;
-  if (head >= Hq) return;
-  const int hk = head / g;
-  const int64_t row = (int64_t)hk * pc.rows + (int64_t)blockIdx.x * g + head % g;
+// of a row (O_s kept times 2^up_s).  A row is shared by LPR lanes of 16 bytes each in
+// SG groups, group k folding slots k, k + SG, ..., so that the slots arrive in few
+// round trips however few rows there are; the groups meet in LDS.
+template <typename T, int D, bool VALUE>
+__global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixCall pc, Plan<VALUE> plan, int Hq) {
+  constexpr int VEC = 16 / (int)sizeof(T);  // elements of a lane: bf16 caches keep fp16 partials
+  constexpr int LPR = D / VEC;
+  constexpr int SG = 4, RPB = 256 / (LPR * SG);
+  __shared__ float s_o[SG][RPB][D];
+  __shared__ float s_m[SG][RPB], s_l[SG][RPB];
+  const int g = pc.g, Hkv = Hq / g;
+  const PrefixRank m = plan.rank(blockIdx.x);
+  const int c = threadIdx.x % LPR, k = threadIdx.x / LPR % SG, rb = threadIdx.x / (LPR * SG);
+  const int head = blockIdx.y * RPB + rb;
+  const int hk = min(head, Hq - 1) / g;
+  const int64_t row = (int64_t)hk * pc.rows + (int64_t)blockIdx.x * g + min(head, Hq - 1) % g;
   const int64_t step = (int64_t)Hkv * pc.rows;  // rows from a slot to the next
   const T* po = reinterpret_cast<const T*>(pc.part_o);
   float M = -INFINITY, L = 0.f, acc[VEC];
@@ -694,67 +871,133 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixCall pc, CacheV
   for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
   constexpr int PF = 4;
   const int n = m.na + m.nb;
-  for (int i0 = 0; i0 < n; i0 += PF) {
+  for (int i0 = k; i0 < n; i0 += SG * PF) {
     uint4 x[PF];
-    float2 ml[PF];
+    float4 ml[PF];
 #pragma unroll
     for (int p = 0; p < PF; ++p) {
-      const int i = min(i0 + p, n - 1);
+      const int i = min(i0 + p * SG, n - 1);
       const int64_t pr = (int64_t)(i < m.na ? i : m.b0 + i - m.na) * step + row;
       x[p] = ld16(po + pr * D + c * VEC);
-      ml[p] = *reinterpret_cast<const float2*>(pc.part_ml + pr * 2);
-      if (i0 + p >= n) ml[p] = make_float2(-INFINITY, 0.f);
+      ml[p] = *reinterpret_cast<const float4*>(pc.part_ml + pr * 4);
+      if (i0 + p * SG >= n) ml[p] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
     }
     float mn = M;
 #pragma unroll
     for (int p = 0; p < PF; ++p) mn = fmaxf(mn, ml[p].x);
     const float mr = mn == -INFINITY ? 0.f : mn;
-    const float f = __builtin_amdgcn_exp2f(M - mr);
+    const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mr);
     L *= f;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) acc[e] *= f;
 #pragma unroll
     for (int p = 0; p < PF; ++p) {
-      const float wgt = ml[p].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[p].x - mr);
+      // a slot without a visible key: no weight (its sum is 0, or NaN where its scores were)
+      const bool none = ml[p].x == -INFINITY;
+      L = fmaf(ml[p].y, none ? 0.f : __builtin_amdgcn_exp2f(ml[p].x - mr), L);
+      const float wgt = none ? 0.f : __builtin_amdgcn_exp2f(ml[p].x - mr - ml[p].z);
       float y[VEC];
-      Store<T>::unpack(x[p], y);
-      L = fmaf(ml[p].y, wgt, L);
-      if (wgt != 0.f) {
+      if constexpr (sizeof(T) == 2) {
+        const px_f16x8 h = __builtin_bit_cast(px_f16x8, x[p]);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) y[e] = (float)h[e];
+      } else {
+        Store<float>::unpack(x[p], y);
+      }
+      if (!none) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) acc[e] = fmaf(y[e], wgt, acc[e]);
       }
     }
     M = mn;
   }
-  const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) acc[e] *= inv;
-  st16_any(const_cast<char*>(row_ptr(pc.out, sizeof(T), m.tok, head)) + c * 16, Store<T>::pack(acc));
-  if (c == 0 && pc.lse) pc.lse[(int64_t)m.tok * Hq + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+  for (int e = 0; e < VEC; e += 4)
+    *reinterpret_cast<float4*>(&s_o[k][rb][c * VEC + e]) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+  if (c == 0) {
+    s_m[k][rb] = M;
+    s_l[k][rb] = L;
+  }
+  __syncthreads();
+  // 256 lanes over RPB rows of D: D RPB / 256 elements each
+  constexpr int EPL = D * RPB / 256;
+  const int r2 = threadIdx.x / (D / EPL), d = threadIdx.x % (D / EPL) * EPL;
+  const int head2 = blockIdx.y * RPB + r2;
+  if (head2 >= Hq) return;
+  float M2 = -INFINITY, L2 = 0.f, y[EPL];
+#pragma unroll
+  for (int q = 0; q < SG; ++q) M2 = fmaxf(M2, s_m[q][r2]);
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) y[e] = 0.f;
+#pragma unroll
+  for (int q = 0; q < SG; ++q) {
+    const float f = s_m[q][r2] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[q][r2] - M2);
+    L2 = fmaf(s_l[q][r2], f, L2);
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) y[e] = fmaf(s_o[q][r2][d + e], f, y[e]);
+  }
+  const float inv = L2 == 0.f ? 0.f : 1.f / L2;
+  T* dst = reinterpret_cast<T*>(const_cast<char*>(row_ptr(pc.out, sizeof(T), m.tok, head2))) + d;
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) y[e] *= inv;
+  if constexpr (sizeof(T) == 2) {
+    uint32_t o[EPL / 2];
+#pragma unroll
+    for (int e = 0; e < EPL / 2; ++e) o[e] = px_cvt(y[2 * e], y[2 * e + 1]);
+    __builtin_memcpy(dst, o, EPL * 2);
+  } else {
+    __builtin_memcpy(dst, y, EPL * 4);
+  }
+  if (d == 0 && pc.lse) pc.lse[(int64_t)m.tok * Hq + head2] = L2 == 0.f ? -INFINITY : (M2 + log2f(L2)) * kLn2;
 }
 
 static int check(hipError_t e) { return e == hipSuccess ? 0 : (int)e; }
 
-int launch_prefix_attend(int dtype, const PrefixCall& call, const CacheView& cv, hipStream_t s) {
-  if (call.n_items == 0) return 0;
-  const dim3 grid(call.n_items, cv.n_kv_heads);
-#define PA(KERNEL, DD, PG) hipLaunchKernelGGL((KERNEL<DD, PG>), grid, dim3(256), 0, s, call, cv)
-#define PAD(KERNEL, PG) { if (cv.head_dim == 64) PA(KERNEL, 64, PG); else PA(KERNEL, 128, PG); }
-#define PAP(KERNEL) { if (cv.page_size) PAD(KERNEL, true) else PAD(KERNEL, false) }
-  if (dtype == 0) PAP(prefix_attend_f32_kernel) else PAP(prefix_attend_kernel)
-#undef PAP
-#undef PAD
+int launch_prefix_attend(int dtype, const PrefixCall& call, const PrefixArgs* args, const PrefixItem* items,
+                         const PrefixRank* ranks, int n_items, int waves, const CacheView& cv, hipStream_t s) {
+  if (n_items == 0) return 0;
+  if (n_items > 65535) return (int)hipErrorInvalidValue;
+  const dim3 grid(cv.n_kv_heads, n_items);
+  const Plan<false> lst{items, ranks};
+#define PA(...) hipLaunchKernelGGL((__VA_ARGS__)
+#define PB(DD, PG)                                                                                                  \
+  {                                                                                                                 \
+    if (waves == 8) PA(prefix_attend_kernel<DD, PG, 8, false>), grid, dim3(512), 0, s, call, lst, cv);              \
+    else if (args) PA(prefix_attend_kernel<DD, PG, 4, true>), grid, dim3(256), 0, s, call, Plan<true>{*args}, cv);  \
+    else PA(prefix_attend_kernel<DD, PG, 4, false>), grid, dim3(256), 0, s, call, lst, cv);                         \
+  }
+#define PF(DD, PG)                                                                                                  \
+  {                                                                                                                 \
+    if (args) PA(prefix_attend_f32_kernel<DD, PG, true>), grid, dim3(256), 0, s, call, Plan<true>{*args}, cv);      \
+    else PA(prefix_attend_f32_kernel<DD, PG, false>), grid, dim3(256), 0, s, call, lst, cv);                        \
+  }
+  const bool paged = cv.page_size != 0, small = cv.head_dim == 64;
+  if (dtype == 0) {
+    if (paged) { if (small) PF(64, true) else PF(128, true) }
+    else { if (small) PF(64, false) else PF(128, false) }
+  } else {
+    if (paged) { if (small) PB(64, true) else PB(128, true) }
+    else { if (small) PB(64, false) else PB(128, false) }
+  }
+#undef PF
+#undef PB
 #undef PA
   return check(hipGetLastError());
 }
 
-int launch_prefix_merge(int dtype, const PrefixCall& call, const CacheView& cv, hipStream_t s) {
-  if (call.n_rank == 0) return 0;
-  const int lanes = cv.head_dim * (dtype == 0 ? 4 : 2) / 16, per = 256 / lanes;
-  const dim3 grid(call.n_rank, (cv.n_kv_heads * call.g + per - 1) / per);
-#define PM(T, DD) hipLaunchKernelGGL((prefix_merge_kernel<T, DD>), grid, dim3(256), 0, s, call, cv)
-  if (dtype == 0) { if (cv.head_dim == 64) PM(float, 64); else PM(float, 128); }
-  else { if (cv.head_dim == 64) PM(bf16_t, 64); else PM(bf16_t, 128); }
+int launch_prefix_merge(int dtype, const PrefixCall& call, const PrefixArgs* args, const PrefixRank* ranks, int n_rank,
+                        int Hq, int D, hipStream_t s) {
+  if (n_rank == 0) return 0;
+  const int rpb = 256 / (D * (dtype == 0 ? 4 : 2) / 16 * 4);
+  const dim3 grid(n_rank, (Hq + rpb - 1) / rpb);
+  const Plan<false> lst{nullptr, ranks};
+#define PM(T, DD)                                                                                             \
+  {                                                                                                           \
+    if (args) hipLaunchKernelGGL((prefix_merge_kernel<T, DD, true>), grid, dim3(256), 0, s, call, Plan<true>{*args}, Hq); \
+    else hipLaunchKernelGGL((prefix_merge_kernel<T, DD, false>), grid, dim3(256), 0, s, call, lst, Hq);       \
+  }
+  if (dtype == 0) { if (D == 64) PM(float, 64) else PM(float, 128) }
+  else { if (D == 64) PM(bf16_t, 64) else PM(bf16_t, 128) }
 #undef PM
   return check(hipGetLastError());
 }

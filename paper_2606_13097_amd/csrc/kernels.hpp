@@ -353,19 +353,38 @@ struct PrefixRank {
 struct PrefixCall {
   RowView q, out;
   float* lse;
-  const PrefixItem* items;
-  const PrefixRank* ranks;
-  void* part_o;     // [slot][Hkv][rows][D], bf16 for bf16 caches
-  float* part_ml;   // [slot][Hkv][rows][2] (max, sum), base 2
-  int32_t n_items, n_rank, rows, g;
+  void* part_o;     // [slot][Hkv][rows][D], fp16 for bf16 caches (see the kernel), else fp32
+  float* part_ml;   // [slot][Hkv][rows][4]: max (base 2), sum, exponent the outputs are kept times, -
+  int32_t rows, g;  // query rows of a kv head, query heads of a group
   int32_t prefix_seq, layer;
   int32_t direct;   // 1: every row has one slot, items write the output
 };
-constexpr int kPfxRows = 128;     // query rows of an item, bf16
+constexpr int kPfxRows = 128;     // query rows of an item, bf16, blocks of 4 waves; of 8 waves twice as many
 constexpr int kPfxRowsF32 = 64;   // fp32
 constexpr int kPfxTile = 64;      // keys of a tile
-int launch_prefix_attend(int dtype, const PrefixCall& call, const CacheView& cv, hipStream_t s);
-int launch_prefix_merge(int dtype, const PrefixCall& call, const CacheView& cv, hipStream_t s);
+// The plan by value, for calls of up to kPfxRanks tokens in kPfxGroups sequences:
+// n_pre prefix items (row block, then slot) of `per` keys, then the groups' own items.
+constexpr int kPfxGroups = 64, kPfxRanks = 128;
+struct PrefixGroup {
+  int32_t seq, end;  // own positions [prefix_len, end)
+  int32_t rows;      // first row | rows << 16
+  int32_t item0;     // first own item of the group
+};
+struct PrefixSmall {
+  int32_t pos;
+  uint16_t tok, nb;  // token, own slots
+};
+struct PrefixArgs {
+  int32_t n_pre, pre_slots, pre_rows, block, per, prefix_len, n_group, pad;
+  PrefixGroup group[kPfxGroups];
+  PrefixSmall rank[kPfxRanks];
+};
+// args null: the plan in device memory (items, ranks); else by value.  waves: 4, or 8
+// (bf16, plans in memory).
+int launch_prefix_attend(int dtype, const PrefixCall& call, const PrefixArgs* args, const PrefixItem* items,
+                         const PrefixRank* ranks, int n_items, int waves, const CacheView& cv, hipStream_t s);
+int launch_prefix_merge(int dtype, const PrefixCall& call, const PrefixArgs* args, const PrefixRank* ranks, int n_rank,
+                        int Hq, int D, hipStream_t s);
 
 // Merge split partials into out: part_o and out fp32 rows, or (mfma_part) both
 // bf16, part_o in the accumulator order of the MFMA prefill kernel.

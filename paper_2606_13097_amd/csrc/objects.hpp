@@ -211,6 +211,8 @@ struct fcg_cache {
   size_t part_bytes = 0;
   void* xpart = nullptr;      // partials of fcg_prefix_attend
   size_t xpart_bytes = 0;
+  bool xpart_captured = false;  // a captured graph uses xpart
+  std::vector<void*> xkept;     // former xparts that captured graphs use
   float* dpart = nullptr;     // decode split partials
   size_t dpart_bytes = 0;
   const fcg_lib* alias_lib = nullptr;  // FCG_ALIAS_V: the library value pages map onto (bound by the first graft)

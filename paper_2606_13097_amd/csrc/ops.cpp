@@ -348,112 +348,208 @@ namespace {
 struct PrefixPlan {
   std::vector<PrefixItem> items;
   std::vector<PrefixRank> ranks;
-  int slots = 0;
-  bool direct = false;
+  PrefixArgs args;
+  int n_items = 0, slots = 0, waves = 4;
+  bool direct = false, by_value = false;
 };
 
-// Cut the call into items.  Tokens of one sequence whose rows fill a block by
-// themselves go over prefix and own keys in one item (no merge between the
-// two); the others share prefix items and have own items per sequence.
-PrefixPlan plan_prefix(const fcg_model_desc& d, int32_t prefix_len, int32_t n, const int32_t* seq, const int32_t* pos) {
-  PrefixPlan p;
+int64_t tiles_of(int64_t lo, int64_t hi) { return hi > lo ? (hi - 1) / kPfxTile - lo / kPfxTile + 1 : 0; }
+
+// Consecutive tokens (in order of position) of one sequence.  Fused: they fill a
+// row block by themselves, which goes over prefix and own keys in one item, so
+// that nothing is merged between the two.  The others share the prefix items and
+// have own items per sequence.
+struct PrefixTokens {
+  int32_t first, n, seq, end;  // of the sorted tokens; end: one past the last attended position
+  bool fused;
+};
+
+// Cut the call into items of row blocks of `block` rows and return the estimated
+// time (us).  The estimate chooses the block shape and the split length; its
+// constants are what the kernel was measured at on a full chip: a tile 2.1 us in a
+// block of 256 rows (one per compute unit) and 3.0 us in each of two blocks of 128
+// rows, 4 us to begin and end an item, and the partials of a slot written and read
+// at 4 TB/s.
+double cut_prefix(const fcg_model_desc& d, int32_t P, const std::vector<PrefixTokens>& toks, int n_tok, int block,
+                  int per_cu, double tile_us, int64_t* per_out) {
   const int g = d.n_q_heads / d.n_kv_heads;
-  const int block = d.dtype == FCG_F32 ? kPfxRowsF32 : kPfxRows;
-  const int P = prefix_len;
+  const int64_t ta = tiles_of(0, P);
+  std::vector<int64_t> len;  // tiles of each row block
+  int64_t small_rows = 0, own_tiles = 0, longest = 1;
+  for (const PrefixTokens& x : toks) {
+    const int64_t own = tiles_of(P, x.end);
+    if (x.fused) {
+      len.push_back(ta + own);
+    } else {
+      small_rows += (int64_t)x.n * g;
+      own_tiles += own;
+      longest = std::max(longest, own);
+    }
+  }
+  for (int64_t r = 0; r < small_rows && ta; r += block) len.push_back(ta);
+  for (int64_t t : len) longest = std::max(longest, t);
+  const int64_t at_once = 256 * per_cu;
+  const double slot_us = (double)n_tok * d.n_q_heads * d.head_dim * 2.0 * 2.0 / 4e6;
+  double best = 1e30;
+  for (int64_t ns = 1; ns <= std::min<int64_t>(64, longest); ++ns) {
+    // at most 256 splits each (slots are counted in 16 bits, the merge reads them all)
+    const int64_t per = (longest + ns - 1) / ns;
+    int64_t blocks = 0, slots = 1;
+    for (int64_t t : len) {
+      blocks += (t + per - 1) / per;
+      slots = std::max(slots, (t + per - 1) / per);
+    }
+    const double rounds = std::ceil((double)blocks * d.n_kv_heads / at_once);
+    // own items of the small groups read each key once, a quarter of a tile's time
+    const double us = rounds * (per * tile_us + 4.0) + 0.25 * own_tiles * d.n_kv_heads / at_once * tile_us +
+                      (small_rows && ta ? (slots + 1) * slot_us + 4.0 : slots > 1 ? slots * slot_us + 4.0 : 0.0);
+    if (us < best) {
+      best = us;
+      *per_out = per;
+    }
+  }
+  return best;
+}
+
+std::vector<PrefixTokens> group_tokens(int g, int32_t n, const std::vector<int32_t>& order, const int32_t* seq,
+                                       const int32_t* pos, int block) {
+  std::vector<PrefixTokens> out, fused;
+  const int32_t per = block / g;  // tokens of a full row block
+  for (int32_t i = 0; i < n;) {
+    int32_t j = i;
+    while (j < n && seq[order[j]] == seq[order[i]]) ++j;
+    while (i < j) {
+      const bool full = j - i >= per || (int64_t)(j - i) * g * 4 >= 3 * block;
+      const int32_t m = full ? std::min(per, j - i) : j - i;
+      (full ? fused : out).push_back(PrefixTokens{i, m, seq[order[i]], pos[order[i + m - 1]] + 1, full});
+      i += m;
+    }
+  }
+  out.insert(out.end(), fused.begin(), fused.end());  // ranks of the shared row blocks come first
+  return out;
+}
+
+void plan_prefix(const fcg_model_desc& d, int32_t P, int32_t n, const int32_t* seq, const int32_t* pos, PrefixPlan* p) {
+  const int g = d.n_q_heads / d.n_kv_heads;
   std::vector<int32_t> order(n);
   for (int32_t t = 0; t < n; ++t) order[t] = t;
   auto less = [&](int32_t a, int32_t b) { return seq[a] != seq[b] ? seq[a] < seq[b] : pos[a] < pos[b]; };
   if (!std::is_sorted(order.begin(), order.end(), less)) std::stable_sort(order.begin(), order.end(), less);
-  struct Group {
-    int32_t first, n, seq, end;  // of `order`; end: one past the last attended position
-    bool big;
-  };
-  std::vector<Group> groups;
-  for (int32_t i = 0; i < n;) {
-    int32_t j = i;
-    while (j < n && seq[order[j]] == seq[order[i]]) ++j;
-    groups.push_back(Group{i, j - i, seq[order[i]], pos[order[j - 1]] + 1, (int64_t)(j - i) * g >= block});
-    i = j;
-  }
-  std::stable_partition(groups.begin(), groups.end(), [](const Group& x) { return !x.big; });
-  // ranks: small groups first
-  p.ranks.reserve(n);
-  std::vector<int32_t> rank0;
-  int32_t n_small = 0;
-  for (const Group& x : groups) {
-    rank0.push_back((int32_t)p.ranks.size());
-    for (int32_t i = 0; i < x.n; ++i) p.ranks.push_back(PrefixRank{order[x.first + i], pos[order[x.first + i]], 0, 0, 0, 0});
-    if (!x.big) n_small += x.n;
-  }
-  auto tiles = [](int64_t lo, int64_t hi) { return hi > lo ? (hi - 1) / kPfxTile - lo / kPfxTile + 1 : 0; };
-  // split length in tiles: the grid about two blocks per compute unit
-  const int64_t ta = tiles(0, P);
-  const int64_t small_rb = ((int64_t)n_small * g + block - 1) / block;
-  int64_t total = small_rb * ta, longest = 0;
-  for (const Group& x : groups) {
-    const int64_t own = tiles(P, x.end);
-    const int64_t rb = x.big ? ((int64_t)x.n * g + block - 1) / block : 1;
-    total += rb * (own + (x.big ? ta : 0));
-    longest = std::max(longest, own + ta);
-  }
-  const int64_t target = 512;
-  int64_t per = std::max<int64_t>({1, (total * d.n_kv_heads + target - 1) / target, (longest + 255) / 256});
-  // prefix items of the small groups
-  int pre_slots = 0;
-  if (n_small && P) {
-    pre_slots = (int)((ta + per - 1) / per);
-    for (int32_t r0 = 0; r0 < n_small * g; r0 += block)
-      for (int s = 0; s < pre_slots; ++s)
-        p.items.push_back(PrefixItem{r0, std::min(block, n_small * g - r0), 0, (int32_t)(s * per * kPfxTile),
-                                     (int32_t)std::min<int64_t>(P, (s + 1) * per * kPfxTile), 0, 0, s});
-    p.slots = pre_slots;
-  }
-  for (size_t gi = 0; gi < groups.size(); ++gi) {
-    const Group& x = groups[gi];
-    const int32_t row0 = rank0[gi] * g, rows = x.n * g;
-    if (!x.big) {
-      // own positions [P, end), cut at multiples of the split length
-      const int64_t t0 = P / kPfxTile, nt = tiles(P, x.end);
-      const int ns = (int)((nt + per - 1) / per);
-      for (int s = 0; s < ns; ++s) {
-        const int64_t lo = std::max<int64_t>(P, (t0 + s * per) * kPfxTile);
-        const int64_t hi = std::min<int64_t>(x.end, (t0 + (s + 1) * per) * kPfxTile);
-        p.items.push_back(PrefixItem{row0, rows, x.seq, 0, 0, (int32_t)lo, (int32_t)hi, pre_slots + s});
-      }
-      for (int32_t i = 0; i < x.n; ++i) {
-        PrefixRank& r = p.ranks[rank0[gi] + i];
-        r.na = (uint16_t)pre_slots;
-        r.b0 = (uint16_t)pre_slots;
-        r.nb = (uint16_t)ns;
-      }
-      p.slots = std::max(p.slots, pre_slots + ns);
-      continue;
+  int block = d.dtype == FCG_F32 ? kPfxRowsF32 : kPfxRows;
+  std::vector<PrefixTokens> toks = group_tokens(g, n, order, seq, pos, block);
+  int64_t per = 1;
+  const double us = cut_prefix(d, P, toks, n, block, 2, 3.0, &per);
+  if (d.dtype == FCG_BF16) {
+    std::vector<PrefixTokens> toks8 = group_tokens(g, n, order, seq, pos, 2 * kPfxRows);
+    int64_t per8 = 1;
+    if (cut_prefix(d, P, toks8, n, 2 * kPfxRows, 1, 2.1, &per8) < us) {
+      p->waves = 8;
+      block = 2 * kPfxRows;
+      toks = std::move(toks8);
+      per = per8;
     }
-    // prefix tiles, then own tiles, one run of tiles cut every `per`
-    const int64_t tb = tiles(P, x.end), t0 = P / kPfxTile;
-    const int ns = (int)((ta + tb + per - 1) / per);
-    for (int32_t r0 = 0; r0 < rows; r0 += block)
+  }
+  const int64_t ta = tiles_of(0, P), t0 = P / kPfxTile;
+  p->ranks.reserve(n);
+  int32_t small_rows = 0, n_small = 0, n_own = 0;
+  std::vector<int32_t> rank0;
+  for (const PrefixTokens& x : toks) {
+    rank0.push_back((int32_t)p->ranks.size());
+    for (int32_t i = 0; i < x.n; ++i)
+      p->ranks.push_back(PrefixRank{order[x.first + i], pos[order[x.first + i]], 0, 0, 0, 0});
+    if (!x.fused) {
+      small_rows += x.n * g;
+      ++n_small;
+    }
+  }
+  const int pre_slots = small_rows && P ? (int)((ta + per - 1) / per) : 0;
+  const int n_pre = (small_rows + block - 1) / block * pre_slots;
+  p->slots = pre_slots;
+  auto own_splits = [&](const PrefixTokens& x) { return (int)((tiles_of(P, x.end) + per - 1) / per); };
+  p->by_value = p->waves == 4 && n_small == (int)toks.size() && n_small <= kPfxGroups && n <= kPfxRanks;
+  if (p->by_value) {
+    PrefixArgs& a = p->args;
+    a.n_pre = n_pre;
+    a.pre_slots = pre_slots;
+    a.pre_rows = small_rows;
+    a.block = block;
+    a.per = (int32_t)(per * kPfxTile);
+    a.prefix_len = P;
+    a.n_group = n_small;
+  }
+  for (size_t gi = 0; gi < toks.size(); ++gi) {
+    const PrefixTokens& x = toks[gi];
+    if (x.fused) break;
+    const int ns = own_splits(x);
+    for (int32_t i = 0; i < x.n; ++i) {
+      PrefixRank& r = p->ranks[rank0[gi] + i];
+      r.na = (uint16_t)pre_slots;
+      r.b0 = (uint16_t)pre_slots;
+      r.nb = (uint16_t)ns;
+      if (p->by_value) p->args.rank[rank0[gi] + i] = PrefixSmall{r.pos, (uint16_t)r.tok, (uint16_t)ns};
+    }
+    if (p->by_value) p->args.group[gi] = PrefixGroup{x.seq, x.end, rank0[gi] * g | x.n * g << 16, n_own};
+    n_own += ns;
+    p->slots = std::max(p->slots, pre_slots + ns);
+  }
+  p->n_items = n_pre + n_own;
+  if (!p->by_value) {
+    for (int32_t r0 = 0; r0 < small_rows && pre_slots; r0 += block)
+      for (int s = 0; s < pre_slots; ++s)
+        p->items.push_back(PrefixItem{r0, std::min(block, small_rows - r0), 0, (int32_t)(s * per * kPfxTile),
+                                      (int32_t)std::min<int64_t>(P, (s + 1) * per * kPfxTile), 0, 0, s});
+    for (size_t gi = 0; gi < toks.size(); ++gi) {
+      const PrefixTokens& x = toks[gi];
+      const int32_t row0 = rank0[gi] * g, rows = x.n * g;
+      if (!x.fused) {
+        const int ns = own_splits(x);
+        for (int s = 0; s < ns; ++s) {  // own positions, cut at multiples of a tile
+          const int64_t cut = (t0 + s * per) * kPfxTile;
+          p->items.push_back(PrefixItem{row0, rows, x.seq, 0, 0, (int32_t)std::max<int64_t>(P, cut),
+                                        (int32_t)std::min<int64_t>(x.end, cut + per * kPfxTile), pre_slots + s});
+        }
+        continue;
+      }
+      // prefix tiles, then own tiles: one run of tiles, cut every `per`
+      const int64_t tb = tiles_of(P, x.end);
+      const int ns = (int)((ta + tb + per - 1) / per);
       for (int s = 0; s < ns; ++s) {
         const int64_t a = s * per, b = std::min(ta + tb, (s + 1) * per);
-        PrefixItem it{row0 + r0, std::min(block, rows - r0), x.seq, 0, 0, 0, 0, s};
+        PrefixItem it{row0, rows, x.seq, 0, 0, 0, 0, s};
         if (a < ta) {
           it.a0 = (int32_t)(a * kPfxTile);
           it.a1 = (int32_t)std::min<int64_t>(P, std::min(b, ta) * kPfxTile);
         }
         if (b > ta) {
-          // up to the item's last row: positions past it are masked for all of its rows
-          const int32_t last = p.ranks[(row0 + r0 + it.n_row - 1) / g].pos + 1;
           it.b0 = (int32_t)std::max<int64_t>(P, (t0 + std::max<int64_t>(a - ta, 0)) * kPfxTile);
-          it.b1 = std::max(it.b0, (int32_t)std::min<int64_t>(last, (t0 + b - ta) * kPfxTile));
+          it.b1 = (int32_t)std::min<int64_t>(x.end, (t0 + b - ta) * kPfxTile);
         }
-        p.items.push_back(it);
+        p->items.push_back(it);
       }
-    for (int32_t i = 0; i < x.n; ++i) p.ranks[rank0[gi] + i].na = (uint16_t)ns;
-    p.slots = std::max(p.slots, ns);
+      for (int32_t i = 0; i < x.n; ++i) p->ranks[rank0[gi] + i].na = (uint16_t)ns;
+      p->slots = std::max(p->slots, ns);
+    }
+    p->n_items = (int)p->items.size();
   }
-  p.direct = n > 0;
-  for (const PrefixRank& r : p.ranks) p.direct = p.direct && r.na + r.nb == 1;
-  return p;
+  p->direct = n > 0;
+  for (const PrefixRank& r : p->ranks) p->direct = p->direct && r.na + r.nb == 1;
+}
+
+// The workspace of prefix partials.  One that a captured graph uses is kept until
+// the cache is destroyed when a larger one takes its place.
+fcg_status prefix_workspace(fcg_cache* c, size_t bytes, bool cap) {
+  if (bytes > c->xpart_bytes) {
+    if (cap) return fail(FCG_ESTATE, "fcg_prefix_attend needs a larger workspace: run a call of this size before the capture");
+    if (c->xpart_captured) {
+      c->xkept.push_back(c->xpart);
+      c->xpart = nullptr;
+      c->xpart_bytes = 0;
+      c->xpart_captured = false;
+    }
+    if (fcg_status st = grow(&c->xpart, &c->xpart_bytes, bytes, "prefix partials")) return st;
+  }
+  if (cap) c->xpart_captured = true;
+  return FCG_OK;
 }
 
 }  // namespace
@@ -482,38 +578,50 @@ fcg_status fcg_prefix_attend(fcg_cache* c, int32_t layer, int32_t prefix_seq, in
     OnDevice dev(c->device);
     HIP_TRY(dev.err, "hipSetDevice");
     hipStream_t s = (hipStream_t)stream;
-    const PrefixPlan p = plan_prefix(d, prefix_len, n_tok, seq, pos);
+    PrefixPlan p;
+    plan_prefix(d, prefix_len, n_tok, seq, pos, &p);
     const int g = d.n_q_heads / d.n_kv_heads;
     const size_t prow = (size_t)p.slots * d.n_kv_heads * n_tok * g;
     const size_t o_bytes = (prow * d.head_dim * esize(d.dtype) + 255) & ~size_t(255);
-    const bool cap = capturing(s);
-    if (cap) return fail(FCG_ESTATE, "fcg_prefix_attend needs an upload here and cannot be captured into a graph");
-    if (!p.direct && p.slots)
-      if (fcg_status st = grow(&c->xpart, &c->xpart_bytes, o_bytes + prow * 8, "prefix partials")) return st;
-    Blob blob;
-    const size_t o_items = blob.add(p.items.data(), p.items.size() * sizeof(PrefixItem));
-    const size_t o_ranks = blob.add(p.ranks.data(), p.ranks.size() * sizeof(PrefixRank));
-    char* dplan = nullptr;
-    size_t off = 0;
-    if (fcg_status st = upload(c, blob, {}, s, &dplan, &off)) return st;
+    const bool merge = !p.direct, work = merge && p.slots;
+    const bool cap = (work || !p.by_value) && capturing(s);
+    // what needs an upload cannot be captured: its staging memory is used again
+    if (cap && !p.by_value) return fail(FCG_ESTATE, "this prefix attention has too many tokens to be captured into a graph");
+    if (work)
+      if (fcg_status st = prefix_workspace(c, o_bytes + prow * 16, cap)) return st;
     PrefixCall pc{};
     pc.q = view_of(q);
     pc.out = view_of(out);
     pc.lse = lse;
-    pc.items = (const PrefixItem*)(dplan + o_items);
-    pc.ranks = (const PrefixRank*)(dplan + o_ranks);
     pc.part_o = c->xpart;
     pc.part_ml = (float*)((char*)c->xpart + o_bytes);
-    pc.n_items = (int32_t)p.items.size();
-    pc.n_rank = n_tok;
     pc.rows = n_tok * g;
     pc.g = g;
     pc.prefix_seq = prefix_seq;
     pc.layer = layer;
     pc.direct = p.direct;
-    if (int rc = launch_prefix_attend(d.dtype, pc, c->view(), s)) return hip_fail((hipError_t)rc, "prefix attention launch");
-    if (!p.direct)
-      if (int rc = launch_prefix_merge(d.dtype, pc, c->view(), s)) return hip_fail((hipError_t)rc, "prefix merge launch");
-    return c->ring.retire(off, blob.bytes.size(), s);
+    const PrefixItem* items = nullptr;
+    const PrefixRank* ranks = nullptr;
+    size_t off = 0, n_blob = 0;
+    if (!p.by_value) {
+      Blob blob;
+      const size_t o_items = blob.add(p.items.data(), p.items.size() * sizeof(PrefixItem));
+      const size_t o_ranks = blob.add(p.ranks.data(), p.ranks.size() * sizeof(PrefixRank));
+      char* dplan = nullptr;
+      if (fcg_status st = upload(c, blob, {}, s, &dplan, &off)) return st;
+      items = (const PrefixItem*)(dplan + o_items);
+      ranks = (const PrefixRank*)(dplan + o_ranks);
+      n_blob = blob.bytes.size();
+    }
+    const PrefixArgs* args = p.by_value ? &p.args : nullptr;
+    constexpr int kGridY = 65535;
+    for (int i0 = 0; i0 < p.n_items; i0 += kGridY)  // more only from plans in memory
+      if (int rc = launch_prefix_attend(d.dtype, pc, args, items + (args ? 0 : i0), ranks, std::min(kGridY, p.n_items - i0),
+                                        p.waves, c->view(), s))
+        return hip_fail((hipError_t)rc, "prefix attention launch");
+    if (merge)
+      if (int rc = launch_prefix_merge(d.dtype, pc, args, ranks, n_tok, d.n_q_heads, d.head_dim, s))
+        return hip_fail((hipError_t)rc, "prefix merge launch");
+    return p.by_value ? FCG_OK : c->ring.retire(off, n_blob, s);
   });
 }
