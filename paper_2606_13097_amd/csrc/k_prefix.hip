@@ -42,6 +42,11 @@ __device__ __forceinline__ px_f32x4 mma32(const uint4& a, const uint4& b, const 
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(px_bf16x8, a), __builtin_bit_cast(px_bf16x8, b), c,
                                                  0, 0, 0);
 }
+typedef float px_f32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ px_f32x16 mma_wide(const uint4& a, const uint4& b, const px_f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(px_bf16x8, a), __builtin_bit_cast(px_bf16x8, b), c,
+                                                 0, 0, 0);
+}
 __device__ __forceinline__ px_f32x4 mma16(const uint2& a, const uint2& b, const px_f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(px_i16x4, a), __builtin_bit_cast(px_i16x4, b), c,
                                                    0, 0, 0);
@@ -76,22 +81,51 @@ __device__ __forceinline__ Entry entry_of(const CacheView& cv, int seq, int pos)
   }
   return e;
 }
-template <int D, bool PAGED>
-__device__ __forceinline__ int64_t rows_off(const CacheView& cv, int layer, int seq, int hk, int q0, const Entry& e) {
-  if (PAGED) return (int64_t)layer * cv.layer_stride + ((int64_t)e.page * cv.n_kv_heads + hk) * 16 * D;
-  return kv_offset<false>(cv, layer, seq, hk, q0);
-}
+// Page entries of a wave's tiles, 64 tiles at a time in the lanes of two registers: one
+// round trip for all of them (an entry read beside the tiles was a miss in its way:
+// each sequence's pages are their own, and scalar loads are waited for with the LDS
+// reads).  at(i, lane_seq, lane_pos): sequence and position of tile i.
+template <bool PAGED>
+struct Entries {
+  int32_t page, alias;
+  int batch = -1;
+  template <typename F>
+  __device__ __forceinline__ Entry get(const CacheView& cv, int i, int n, int lane, F&& at) {
+    if (!PAGED) return Entry{0, -1};
+    if (i >> 6 != batch) {  // wave-uniform
+      batch = i >> 6;
+      int seq, pos;
+      at(min(batch * 64 + lane, n - 1), &seq, &pos);
+      const int32_t* row = cv.page_table + (int64_t)seq * 2 * cv.n_lp + (pos >> 4);
+      page = row[0];
+      alias = cv.v_alias ? row[cv.n_lp] : -1;
+    }
+    return Entry{__builtin_amdgcn_readlane(page, i & 63), __builtin_amdgcn_readlane(alias, i & 63)};
+  }
+};
+
+// Rows of one kv head of the layer: of position q0 (paged: a multiple of 16, its page
+// given), wave-uniform.
 template <typename T, int D, bool PAGED>
-__device__ __forceinline__ const T* key_rows(const CacheView& cv, int layer, int seq, int hk, int q0, const Entry& e) {
-  return (const T*)uniform_ptr(reinterpret_cast<const T*>(cv.k) + rows_off<D, PAGED>(cv, layer, seq, hk, q0, e));
-}
-template <typename T, int D, bool PAGED>
-__device__ __forceinline__ const T* value_rows(const CacheView& cv, int layer, int seq, int hk, int q0, const Entry& e) {
-  const T* p = reinterpret_cast<const T*>(cv.v) + rows_off<D, PAGED>(cv, layer, seq, hk, q0, e);
-  if (PAGED && e.alias >= 0)
-    p = reinterpret_cast<const T*>(cv.lib_v) + (((int64_t)layer * cv.n_kv_heads + hk) * cv.lib_cap + e.alias) * D;
-  return (const T*)uniform_ptr(p);
-}
+struct HeadRows {
+  const T *k, *v, *lib;  // the layer's and head's first row
+  int64_t step;          // paged: elements from a page to the next; else from a sequence to the next
+  __device__ __forceinline__ HeadRows(const CacheView& cv, int layer, int hk) {
+    const int64_t at = (int64_t)layer * cv.layer_stride + (int64_t)hk * (PAGED ? 16 : cv.max_tokens) * D;
+    step = (int64_t)cv.n_kv_heads * (PAGED ? 16 : cv.max_tokens) * D;
+    k = reinterpret_cast<const T*>(cv.k) + at;
+    v = reinterpret_cast<const T*>(cv.v) + at;
+    lib = reinterpret_cast<const T*>(cv.lib_v) + ((int64_t)layer * cv.n_kv_heads + hk) * cv.lib_cap * D;
+  }
+  __device__ __forceinline__ const T* keys(int seq, int q0, const Entry& e) const {
+    return (const T*)uniform_ptr(k + (PAGED ? e.page * step : seq * step + (int64_t)q0 * D));
+  }
+  __device__ __forceinline__ const T* values(int seq, int q0, const Entry& e) const {
+    const T* p = v + (PAGED ? e.page * step : seq * step + (int64_t)q0 * D);
+    if (PAGED && e.alias >= 0) p = lib + (int64_t)e.alias * D;
+    return (const T*)uniform_ptr(p);
+  }
+};
 
 __device__ __forceinline__ const char* row_ptr(const RowView& v, int64_t esize, int tok, int head) {
   return reinterpret_cast<const char*>(v.p) + ((int64_t)tok * v.token + (int64_t)head * v.head) * esize;
@@ -111,6 +145,16 @@ __device__ __forceinline__ uint32_t finite2(uint32_t x, bool* bad) {
 }
 __device__ __forceinline__ float not_finite(float x) { return fabsf(x) < INFINITY ? 0.f : x; }
 __device__ __forceinline__ float finite_abs(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
+
+// over lanes l and l ^ 32
+__device__ __forceinline__ float max_halves(float v) {
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_halves(float v) {
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
 
 // max over each group of N lanes (16 or 32)
 template <int N>
@@ -155,21 +199,29 @@ struct Emit {
       a2 = (float)up;
     }
   }
+  __device__ __forceinline__ void put_aux() const {
+    if (!direct) *reinterpret_cast<float4*>(aux) = make_float4(a0, a1, a2, 0.f);
+    else if (aux) *aux = a0;
+  }
+  // four outputs as they are stored (two-byte kinds)
+  __device__ __forceinline__ uint2 pack(float x0, float x1, float x2, float x3) const {
+    if (direct) return make_uint2(px_cvt(x0 * scale, x1 * scale), px_cvt(x2 * scale, x3 * scale));
+    const px_f16x2 a = __builtin_convertvector((px_f32x2){x0 * scale, x1 * scale}, px_f16x2);
+    const px_f16x2 b = __builtin_convertvector((px_f32x2){x2 * scale, x3 * scale}, px_f16x2);
+    return make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+  }
+  __device__ __forceinline__ void put8(int dim, const uint4& y) const {
+    if (dim == 0) put_aux();
+    st16_any(dst + dim * 2, y);
+  }
   __device__ __forceinline__ void put(int dim, float x0, float x1, float x2, float x3) const {
-    if (dim == 0) {
-      if (!direct) *reinterpret_cast<float4*>(aux) = make_float4(a0, a1, a2, 0.f);
-      else if (aux) *aux = a0;
-    }
+    if (dim == 0) put_aux();
     if (sizeof(T) == 4) {
       const float4 y = make_float4(x0 * scale, x1 * scale, x2 * scale, x3 * scale);
       __builtin_memcpy(dst + dim * 4, &y, 16);
-    } else if (direct) {
-      const uint2 y = make_uint2(px_cvt(x0 * scale, x1 * scale), px_cvt(x2 * scale, x3 * scale));
-      __builtin_memcpy(dst + dim * 2, &y, 8);
     } else {
-      const px_f16x2 a = __builtin_convertvector((px_f32x2){x0 * scale, x1 * scale}, px_f16x2);
-      const px_f16x2 b = __builtin_convertvector((px_f32x2){x2 * scale, x3 * scale}, px_f16x2);
-      st8_nt(dst + dim * 2, __builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+      const uint2 y = pack(x0, x1, x2, x3);
+      __builtin_memcpy(dst + dim * 2, &y, 8);
     }
   }
 };
@@ -240,7 +292,7 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
   constexpr int HALF_T = kPfxTile * D;    // elements of a tile's keys (values)
   __shared__ __align__(16) bf16_t s_kv[NB][2 * HALF_T];
   __shared__ float s_wm[WAVES][32], s_wl[WAVES][32];
-  __shared__ __align__(16) int s_bad[2][4];
+  __shared__ __align__(16) int s_bad[NB][4];  // a tile's value groups that held non-finite elements
 
   const PrefixItem it = plan.item(blockIdx.y);
   const int hk = blockIdx.x;  // fastest: workgroups go to the eight XCDs in turn, so a head's blocks share an L2
@@ -251,25 +303,34 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
   const float qscale = 1.4426950408889634f / sqrtf((float)D);
   const Keys ka{pc.prefix_seq, it.a0, it.a1}, kb{it.seq, it.b0, it.b1};
 
-  // byte offset of this lane's chunk in row r (of 16) for instruction j, and the
-  // chunk's swizzle: keys row % NC, values 2 (row % (NC / 2))
-  auto k_off = [&](int j, int r) __attribute__((always_inline)) -> uint32_t {
-    return (uint32_t)(r * D + ((lane % NC) ^ ((j * RI + lane / NC) % NC)) * 8) * 2;
-  };
-  auto v_off = [&](int j, int r) __attribute__((always_inline)) -> uint32_t {
-    return (uint32_t)(r * D + ((lane % NC) ^ (2 * ((j * RI + lane / NC) % (NC / 2)))) * 8) * 2;
-  };
-  // 16 rows from position q0 of range ks into LDS; rows outside the range re-read one inside it
-  auto issue_k = [&](const Keys& ks, int q0, const void* base, uint32_t lds) __attribute__((always_inline)) {
-    const int rlo = max(ks.lo - q0, 0), rhi = min(ks.hi - 1 - q0, 15);
+  // DMA instruction j of 16 rows fills rows RI j .. RI j + RI - 1: lane l the chunk
+  // position l % NC of row RI j + l / NC.  The chunk that belongs there is the position
+  // XOR the row's swizzle (keys: row % NC; values: 2 (row % (NC / 2))), so the lane's byte
+  // offset in the 16 rows is the same for every group of 16.
+  uint32_t koff[KI], voff[KI];
 #pragma unroll
-    for (int j = 0; j < KI; ++j) dma16s(base, k_off(j, min(max(j * RI + lane / NC, rlo), rhi)), lds + j * 1024);
+  for (int j = 0; j < KI; ++j) {
+    const int r = j * RI + lane / NC;
+    koff[j] = (uint32_t)(r * D + ((lane % NC) ^ (r % NC)) * 8) * 2;
+    voff[j] = (uint32_t)(r * D + ((lane % NC) ^ (2 * (r % (NC / 2)))) * 8) * 2;
+  }
+  // 16 rows from position q0 of range ks into LDS, instruction j of KI; rows outside the
+  // range re-read one inside it
+  auto issue_one = [&](const Keys& ks, int q0, const void* base, uint32_t lds, const uint32_t* off, int j)
+                       __attribute__((always_inline)) {
+    if (q0 >= ks.lo && q0 + 16 <= ks.hi) {  // wave-uniform
+      dma16s(base, off[j], lds + j * 1024);
+    } else {
+      const int rlo = max(ks.lo - q0, 0), rhi = min(ks.hi - 1 - q0, 15), r = j * RI + lane / NC;
+      dma16s(base, off[j] + (uint32_t)((min(max(r, rlo), rhi) - r) * (D * 2)), lds + j * 1024);
+    }
   };
-  auto issue_v = [&](const Keys& ks, int q0, const void* base, uint32_t lds) __attribute__((always_inline)) {
-    const int rlo = max(ks.lo - q0, 0), rhi = min(ks.hi - 1 - q0, 15);
+  auto issue16 = [&](const Keys& ks, int q0, const void* base, uint32_t lds, const uint32_t* off)
+                     __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < KI; ++j) dma16s(base, v_off(j, min(max(j * RI + lane / NC, rlo), rhi)), lds + j * 1024);
+    for (int j = 0; j < KI; ++j) issue_one(ks, q0, base, lds, off, j);
   };
+  const HeadRows<bf16_t, D, PAGED> head(cv, pc.layer, hk);
   // a group of 16 positions with none inside the range stands for the nearest one that has
   auto group_of = [&](const Keys& ks, int p0) __attribute__((always_inline)) {
     return min(max(p0, ks.lo & ~15), (ks.hi - 1) & ~15);
@@ -291,7 +352,9 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
 
   if (it.n_row > 32) {
     // ---------------------------------------------------------------- wide
-    constexpr int RT = 2;
+    constexpr int KS = D / 16;           // 16-deep steps over the head dimension
+    constexpr int DT = D / 32;           // 32-wide output tiles
+    const int lc = lane & 31, lh = lane >> 5;
     constexpr int DPT = 8 * KI / WAVES;  // DMA instructions of this wave for a tile
     const int ta0 = ka.lo / kPfxTile, tb0 = kb.lo / kPfxTile;
     const int na = tiles_of(ka, kPfxTile), nt = na + tiles_of(kb, kPfxTile);
@@ -299,207 +362,344 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
     auto first_of = [&](int ti) __attribute__((always_inline)) {
       return (ti >= na ? tb0 + ti - na : ta0 + ti) * kPfxTile;
     };
-    Entry ent;
-    auto fetch = [&](int ti) __attribute__((always_inline)) {  // the page of this wave's rows of tile ti
-      if (ti >= nt) return;
-      const Keys& ks = ti >= na ? kb : ka;
-      ent = entry_of<PAGED>(cv, ks.seq, group_of(ks, first_of(ti) + 16 * grp));
+    // this lane's query row, column lc of the 32-row matrix operands (rows past the item's
+    // repeat its first one and are not written)
+    const int r = 32 * w + lc;
+    const int row = it.row0 + (r < it.n_row ? r : 0);
+    const PrefixRank m = plan.rank(row / g);
+    const int pmin = plan.rank(it.row0 / g).pos;
+    Entries<PAGED> entries;
+    auto entry = [&](int ti) __attribute__((always_inline)) -> Entry {  // the page of this wave's rows of tile ti
+      return entries.get(cv, ti, nt, lane, [&](int i, int* seq, int* pos) __attribute__((always_inline)) {
+        const bool own = i >= na;
+        *seq = own ? kb.seq : ka.seq;
+        const int lo = own ? kb.lo : ka.lo, hi = own ? kb.hi : ka.hi;
+        *pos = min(max(first_of(i) + 16 * grp, lo & ~15), (hi - 1) & ~15);
+      });
     };
     auto issue = [&](int ti) __attribute__((always_inline)) {
       const Keys ks = ti >= na ? kb : ka;
       const int q0 = group_of(ks, first_of(ti) + 16 * grp);
       bf16_t* buf = s_kv[ti & (NB - 1)];
-      if (WAVES == 4 || w < 4)
-        issue_k(ks, q0, key_rows<bf16_t, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, ent), lds_addr(buf) + grp * (16 * D * 2));
-      if (WAVES == 4 || w >= 4)
-        issue_v(ks, q0, value_rows<bf16_t, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, ent),
-                lds_addr(buf + HALF_T) + grp * (16 * D * 2));
+      const uint32_t lds = lds_addr(buf) + grp * (16 * D * 2);
+      const Entry ent = entry(ti);
+      if (WAVES == 4 || w < 4) issue16(ks, q0, head.keys(ks.seq, q0, ent), lds, koff);
+      if (WAVES == 4 || w >= 4) issue16(ks, q0, head.values(ks.seq, q0, ent), lds + HALF_T * 2, voff);
     };
-    fetch(0);
     if (nt) issue(0);
-    uint4 qf[RT][KS];
-    int rpos[RT], rtok[RT], rhead[RT];
+    const int rpos = m.pos, rhead = hk * g + row % g;
+    uint4 qf[KS];
+    {
+      const char* src = row_ptr(pc.q, 2, m.tok, rhead);
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int r = 16 * (RT * w + rt) + lr;
-      const int row = it.row0 + (r < it.n_row ? r : 0);
-      const PrefixRank m = plan.rank(row / g);
-      rpos[rt] = m.pos;
-      rtok[rt] = m.tok;
-      rhead[rt] = hk * g + row % g;
-      const char* src = row_ptr(pc.q, 2, m.tok, rhead[rt]);
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) qf[rt][ks] = ld16_any(src + (ks * 32 + lq * 8) * 2);
+      for (int ks = 0; ks < KS; ++ks) qf[ks] = ld16_any(src + (ks * 16 + lh * 8) * 2);
     }
     // the compiler cannot see the tile loads: its wait for these must not fall into the loop
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
+    for (int s = 0; s < KS; ++s) asm volatile("" ::"v"(__builtin_bit_cast(u32x4_t, qf[s])));
+    asm volatile("" ::"v"(rpos), "v"(m.tok));
+    float mrow = -INFINITY, lsum = 0.f;
+    px_f32x16 acc[DT];
 #pragma unroll
-      for (int s = 0; s < KS; ++s) asm volatile("" ::"v"(__builtin_bit_cast(u32x4_t, qf[rt][s])));
-      asm volatile("" ::"v"(rpos[rt]), "v"(rtok[rt]));
-    }
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int i = 1; i < NB - 1; ++i) {
-      fetch(i);
-      if (i < nt) issue(i);
-    }
-    fetch(NB - 1);
-    float mrow[RT], lsum[RT];
-    px_f32x4 acc[RT][DT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      mrow[rt] = -INFINITY;
-      lsum[rt] = 0.f;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) acc[rt][dt] = px_f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    const bool busy = 16 * RT * w < it.n_row;  // some row of this wave
+      for (int e = 0; e < 16; ++e) acc[dt][e] = 0.f;
+    const bool busy = 32 * w < it.n_row;  // some row of this wave
 
-    auto step = [&](int ti, auto buf) __attribute__((always_inline)) {
-      bf16_t* K = s_kv[buf];
-      bf16_t* V = K + HALF_T;
-      const bool own = ti >= na;
-      const int lo = own ? kb.lo : ka.lo, hi = own ? kb.hi : ka.hi;
+    px_f32x16 st[2];  // scores of the tile at hand: element 4 q + e of st[kt] is key 32 kt + 8 q + 4 lh + e
+    uint4 pb[4];      // its probabilities, bf16: of keys 16 s + 4 lh .. + 3 and 16 s + 8 + 4 lh .. + 3
+    // A tile with keys that some row of the block does not see (block-uniform).  Own keys
+    // belong to items of one sequence, whose first row has the smallest position.
+    auto is_edge = [&](int ti) __attribute__((always_inline)) -> bool {
       const int p0 = first_of(ti);
-      const bool edge = own || p0 < lo || p0 + kPfxTile > hi;  // masked keys: block-uniform
-      // this wave's loads of the tile have landed (up to NB - 2 later tiles may be in flight) ...
-      const int ahead = min(NB - 2, nt - 1 - ti);
-      if (ahead >= 2) wait_vm<2 * DPT>();
-      else if (ahead == 1) wait_vm<DPT>();
-      else wait_vm<0>();
-      if (edge && (WAVES == 4 || w >= 4))
-      {
-        const bool bad = clean16(V + grp * 16 * D);
-        if (lane == 0) s_bad[buf & 1][grp] = bad;
-      }
-      lds_barrier();  // ... and every wave's; every wave is done with the tile before
-      if (ti + NB - 1 < nt) issue(ti + NB - 1);
-      fetch(ti + NB);
-      if (!busy) return;
-      px_f32x4 st[RT][4];
+      return ti >= na ? p0 < kb.lo || p0 + kPfxTile > min(kb.hi, pmin + 1) : p0 < ka.lo || p0 + kPfxTile > ka.hi;
+    };
+    // key fragment i: keys 32 (i % 2) + lc, dims 16 (i / 2) + 8 lh ..
+    auto kfrag = [&](const bf16_t* K, int i) __attribute__((always_inline)) -> uint4 {
+      return ld16(&K[((i % 2 * 32 + lc) * NC + ((i / 2 * 2 + lh) ^ (lc % NC))) * 8]);
+    };
+    // value fragment i, dt = i % DT, s = i / DT: lane (lc, lh) needs V[key][32 dt + lc] of the
+    // eight keys of pb[s]; in the transpose read lane lr of a 16-lane group addresses the
+    // group's row lr / 4, dims 4 (lr % 4) .. + 3 of its 16
+    const int vr = 4 * lh + (lr >> 2), vsw = 2 * (vr % (NC / 2));
+    auto vfrag = [&](const bf16_t* V, int i) __attribute__((always_inline)) -> uint4 {
+      const int vc = (4 * (i % DT) + 2 * ((lane >> 4) & 1) + ((lr & 3) >> 1)) ^ vsw;
+      const bf16_t* row = &V[((16 * (i / DT) + vr) * NC + vc) * 8 + (lr & 1) * 4];
+      const uint2 lo2 = ld_tr8(row), hi2 = ld_tr8(row + 8 * D);
+      return make_uint4(lo2.x, lo2.y, hi2.x, hi2.y);
+    };
+    // S^T = K Q^T of one tile and O^T += V^T P^T of another (or one of the two), their
+    // fragments read ahead in turn; both take 2 KS = 4 DT fragments
+    // Fragments are read AH steps ahead of their products (a step's products take 64 matrix
+    // cycles, an LDS read returns after more than that); loaded: the first AH already are.
+    constexpr int AH = 3;
+    uint4 kf[AH], vf[AH];
+    auto products = [&](const bf16_t* K, const bf16_t* V, auto with_k, auto with_v, auto loaded, auto&& beside)
+                        __attribute__((always_inline)) {
+      constexpr bool KK = decltype(with_k)::value, VV = decltype(with_v)::value;
+      static_assert(2 * KS == 4 * DT, "as many fragments of both");
+      constexpr int N = 2 * KS;
+      if constexpr (!decltype(loaded)::value) {
 #pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        uint4 kf[KS];
-#pragma unroll
-        for (int s = 0; s < KS; ++s) kf[s] = ld16(&K[((kt * 16 + lr) * NC + ((s * 4 + lq) ^ (lr % NC))) * 8]);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          px_f32x4 c = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int s = 0; s < KS; ++s) c = mma32(kf[s], qf[rt][s], c);
-          st[rt][kt] = c;
+        for (int i = 0; i < AH; ++i) {
+          if (KK) kf[i] = kfrag(K, i);
+          if (VV) vf[i] = vfrag(V, i);
         }
       }
-      if (edge) {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          // key p0 + 16 kt + 4 lq + e is visible iff a <= 16 kt + e <= b
-          const int a = lo - p0 - 4 * lq;
-          const int b = (own ? min(rpos[rt], hi - 1) : hi - 1) - p0 - 4 * lq;
-#pragma unroll
-          for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              st[rt][kt][e] = 16 * kt + e >= a && 16 * kt + e <= b ? st[rt][kt][e] : -INFINITY;
+      for (int i = 0; i < N; ++i) {
+        const uint4 kc = kf[i % AH], vc = vf[i % AH];
+        if constexpr (KK) st[i % 2] = mma_wide(kc, qf[i / 2], i < 2 ? px_f32x16{} : st[i % 2]);
+        if constexpr (VV) acc[i % DT] = mma_wide(vc, pb[i / DT], acc[i % DT]);
+        if (i + AH < N) {
+          if (KK) kf[i % AH] = kfrag(K, i + AH);
+          if (VV) vf[i % AH] = vfrag(V, i + AH);
         }
-      }
-      uint4 pb[RT][2];
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float tmax = -INFINITY;
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) tmax = fmaxf(tmax, st[rt][kt][e]);
-        tmax = max_rows4(tmax) * qscale;
-        // the reference moves only when a row's max grows by more than 2^8: the
-        // probabilities stay below 2^8, harmless in fp32 and bf16
-        if (__builtin_amdgcn_ballot_w64(tmax > mrow[rt] + 8.f)) {
-          const float mnew = fmaxf(mrow[rt], tmax);
-          const float alpha = mrow[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mrow[rt] - mnew);
-          mrow[rt] = mnew;
-          lsum[rt] *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) acc[rt][dt] *= alpha;
-        }
-        const float mref = mrow[rt] == -INFINITY ? 0.f : mrow[rt];
-        float pv[4][4], ps = 0.f;
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            pv[kt][e] = __builtin_amdgcn_exp2f(fmaf(st[rt][kt][e], qscale, -mref));
-            ps += pv[kt][e];
-          }
-        lsum[rt] += ps;
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-          pb[rt][s] = make_uint4(px_cvt(pv[2 * s][0], pv[2 * s][1]), px_cvt(pv[2 * s][2], pv[2 * s][3]),
-                                 px_cvt(pv[2 * s + 1][0], pv[2 * s + 1][1]), px_cvt(pv[2 * s + 1][2], pv[2 * s + 1][3]));
-      }
-      // fragment i = 2 dt + s: lane (lr, lq) needs V[32 s + 4 lq + e][16 dt + lr] and the
-      // same 16 keys later; in the transpose read lane lr addresses row 4 lq + lr / 4
-      const int vr = 4 * lq + (lr >> 2), vsw = 2 * (vr % (NC / 2));
-      auto vfrag = [&](int i) __attribute__((always_inline)) -> uint4 {
-        const int vc = (2 * (i >> 1) + ((lr & 3) >> 1)) ^ vsw;
-        const bf16_t* row = &V[((32 * (i & 1) + vr) * NC + vc) * 8 + (lr & 1) * 4];
-        const uint2 lo2 = ld_tr8(row), hi2 = ld_tr8(row + 16 * D);
-        return make_uint4(lo2.x, lo2.y, hi2.x, hi2.y);
-      };
-      uint4 va = vfrag(0);
-#pragma unroll
-      for (int i = 0; i < 2 * DT; ++i) {
-        const uint4 vn = i + 1 < 2 * DT ? vfrag(i + 1) : va;
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) acc[rt][i >> 1] = mma32(va, pb[rt][i & 1], acc[rt][i >> 1]);
-        va = vn;
-      }
-      const int* sb = s_bad[buf & 1];
-      if (edge && (sb[0] | sb[1] | sb[2] | sb[3])) {
-        const int seq = own ? kb.seq : ka.seq;
-#pragma unroll 1
-        for (int p = max(p0, lo); p < min(p0 + kPfxTile, hi); ++p) {
-          const bf16_t* row = value_rows<bf16_t, D, PAGED>(cv, pc.layer, seq, hk, p & ~15, entry_of<PAGED>(cv, seq, p)) +
-                              (p & 15) * D + lq * 4;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            const uint2 x = *reinterpret_cast<const uint2*>(row + dt * 16);
-            const float v[4] = {lo_bf16(x.x), hi_bf16(x.x), lo_bf16(x.y), hi_bf16(x.y)};
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[rt][dt][e] += !own || p <= rpos[rt] ? not_finite(v[e]) : 0.f;
-          }
-        }
+        beside(i);
+        // no further ahead: the scheduler hoisted all reads and ran out of registers
+        if constexpr (KK && VV) __builtin_amdgcn_sched_barrier(0);
       }
     };
-    // unrolled by the ring, so that every LDS address is a constant past a lane's base
-    for (int ti = 0; ti < nt; ti += NB) {
-      step(ti, std::integral_constant<int, 0>{});
-      if (ti + 1 >= nt) break;
-      step(ti + 1, std::integral_constant<int, 1>{});
-      if constexpr (NB == 4) {
-        if (ti + 2 >= nt) break;
-        step(ti + 2, std::integral_constant<int, 2>{});
-        if (ti + 3 >= nt) break;
-        step(ti + 3, std::integral_constant<int, 3>{});
+    // mask and softmax of tile ti: scores -> probabilities, running max and sum, outputs rescaled
+    auto softmax = [&](int ti, auto masked) __attribute__((always_inline)) {
+      if (decltype(masked)::value && is_edge(ti)) {
+        const bool own = ti >= na;
+        const int lo = own ? kb.lo : ka.lo, hi = own ? kb.hi : ka.hi, p0 = first_of(ti);
+        // key p0 + 32 kt + 8 q + 4 lh + e is visible iff a <= 32 kt + 8 q + e <= b
+        const int b = (own ? min(rpos, hi - 1) : hi - 1) - p0 - 4 * lh;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) st[kt][i] = 32 * kt + 8 * (i / 4) + i % 4 <= b ? st[kt][i] : -INFINITY;
+        if (p0 < lo) {
+          const int a = lo - p0 - 4 * lh;
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st[kt][i] = 32 * kt + 8 * (i / 4) + i % 4 >= a ? st[kt][i] : -INFINITY;
+        }
       }
+      float top[4];  // a wave's dependent instructions are what this costs: four chains
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        top[c] = st[c / 2][c % 2 * 8];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) top[c] = fmaxf(top[c], st[c / 2][c % 2 * 8 + i]);
+      }
+      const float tmax = max_halves(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]))) * qscale;
+      // the reference moves only when a row's max grows by more than 2^8: the
+      // probabilities stay below 2^8, harmless in fp32 and bf16
+      if (__builtin_amdgcn_ballot_w64(tmax > mrow + 8.f)) {
+        const float mnew = fmaxf(mrow, tmax);
+        const float alpha = mrow == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mrow - mnew);
+        mrow = mnew;
+        lsum *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) acc[dt] *= alpha;
+      }
+      const float mref = mrow == -INFINITY ? 0.f : mrow;
+      float pv[2][16];
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) pv[kt][i] = __builtin_amdgcn_exp2f(fmaf(st[kt][i], qscale, -mref));
+      float ps[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        ps[c] = (pv[c / 4][c % 4 * 4] + pv[c / 4][c % 4 * 4 + 1]) + (pv[c / 4][c % 4 * 4 + 2] + pv[c / 4][c % 4 * 4 + 3]);
+      lsum += ((ps[0] + ps[1]) + (ps[2] + ps[3])) + ((ps[4] + ps[5]) + (ps[6] + ps[7]));
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const float* p = &pv[s / 2][s % 2 * 8];
+        pb[s] = make_uint4(px_cvt(p[0], p[1]), px_cvt(p[2], p[3]), px_cvt(p[4], p[5]), px_cvt(p[6], p[7]));
+      }
+      // computed here, not where the products want them (past the barrier that ends the half)
+      if constexpr (WAVES == 8)
+        asm volatile("" ::"v"(__builtin_bit_cast(u32x4_t, pb[0])), "v"(__builtin_bit_cast(u32x4_t, pb[1])),
+                     "v"(__builtin_bit_cast(u32x4_t, pb[2])), "v"(__builtin_bit_cast(u32x4_t, pb[3])), "v"(lsum));
+    };
+    // values of tile ti that were cleaned out of its buffer, to the rows that see them
+    auto restore = [&](int ti) __attribute__((always_inline)) {
+      if (!is_edge(ti)) return;
+      const int* sb = s_bad[ti & (NB - 1)];
+      if (!(sb[0] | sb[1] | sb[2] | sb[3])) return;
+      const bool own = ti >= na;
+      const int lo = own ? kb.lo : ka.lo, hi = own ? kb.hi : ka.hi, p0 = first_of(ti), seq = own ? kb.seq : ka.seq;
+#pragma unroll 1
+      for (int p = max(p0, lo); p < min(p0 + kPfxTile, hi); ++p) {
+        const bf16_t* row = head.values(seq, p & ~15, entry_of<PAGED>(cv, seq, p)) + (p & 15) * D + lh * 4;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint2 x = *reinterpret_cast<const uint2*>(row + dt * 32 + q * 8);
+            const float v[4] = {lo_bf16(x.x), hi_bf16(x.x), lo_bf16(x.y), hi_bf16(x.y)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[dt][4 * q + e] += !own || p <= rpos ? not_finite(v[e]) : 0.f;
+          }
+      }
+    };
+    // this wave's value rows of an edge tile, landed: non-finite elements out
+    auto clean = [&](int ti) __attribute__((always_inline)) {
+      const bool bad = clean16(s_kv[ti & (NB - 1)] + HALF_T + grp * 16 * D);
+      if (lane == 0) s_bad[ti & (NB - 1)][grp] = bad;
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    auto nothing = [](int) {};
+
+    if constexpr (WAVES == 4) {
+      // Two blocks per compute unit: one block's softmax beside the other's products.
+      auto step = [&](int ti, auto buf) __attribute__((always_inline)) {
+        const bf16_t* K = s_kv[buf];
+        wait_vm<0>();  // this wave's loads of the tile have landed ...
+        if (is_edge(ti)) clean(ti);
+        lds_barrier();  // ... and every wave's; every wave is done with the tile before
+        if (ti + 1 < nt) issue(ti + 1);
+        if (!busy) return;
+        products(K, K, Yes{}, No{}, No{}, nothing);
+        softmax(ti, Yes{});
+        products(K, K + HALF_T, No{}, Yes{}, No{}, nothing);
+        restore(ti);
+      };
+      // unrolled by the ring, so that every LDS address is a constant past a lane's base
+      for (int ti = 0; ti < nt; ti += 2) {
+        step(ti, std::integral_constant<int, 0>{});
+        if (ti + 1 < nt) step(ti + 1, std::integral_constant<int, 1>{});
+      }
+    } else if (nt) {
+      // One block per compute unit, two waves per SIMD, half a tile apart: while waves
+      // 0-3 feed the matrix cores (scores of tile t, outputs of tile t - 1), waves 4-7
+      // do the softmax of tile t - 1, and the other way round; a barrier after each
+      // half.  (In step, both waves of a SIMD wanted the matrix cores at once and then
+      // both the vector unit: 37% of the matrix rate.)  Waves 0-3 bring in keys, 4-7
+      // values.  Counting halves so that waves 0-3 multiply tile t in half 2 t and waves
+      // 4-7 in 2 t + 1: tile u is requested in halves 2 u - 4 (keys) and 2 u - 3 (values),
+      // after the last reads of tile u - 4 in its buffer (keys half 2 u - 7, values half
+      // 2 u - 5), and has landed by the end of half 2 u - 1, before its first reads in
+      // half 2 u.
+      const bool late = w >= 4;
+      uint32_t off[KI];
+#pragma unroll
+      for (int j = 0; j < KI; ++j) off[j] = late ? voff[j] : koff[j];
+      auto landed = [&](int ti) __attribute__((always_inline)) {  // tile ti; tile ti + 1 may be in flight
+        if (ti >= nt) return;
+        if (ti + 1 < nt) wait_vm<DPT>();
+        else wait_vm<0>();
+        if (late && is_edge(ti)) clean(ti);
+      };
+      if (1 < nt) issue(1);
+      landed(0);
+      lds_barrier();
+      if (late) lds_barrier();
+      // (waves without rows go along on a repeated one: branches around the products
+      // cost every wave registers)
+      auto half_m = [&](int ti, auto first) __attribute__((always_inline)) {
+        // tile ti + 2, an instruction at a time between the products: requested in one go
+        // they held the wave for 650 cycles
+        const bool more = ti + 2 < nt;
+        const Keys ks = ti + 2 >= na ? kb : ka;
+        const int q0 = more ? group_of(ks, first_of(ti + 2) + 16 * grp) : 0;
+        const Entry ent = entry(min(ti + 2, nt - 1));
+        const void* base = late ? head.values(ks.seq, q0, ent) : head.keys(ks.seq, q0, ent);
+        const uint32_t lds = lds_addr(s_kv[(ti + 2) & (NB - 1)]) + grp * (16 * D * 2) + (late ? HALF_T * 2 : 0);
+        auto beside = [&](int i) __attribute__((always_inline)) {
+          constexpr int EVERY = 2 * KS / KI;
+          if (i % EVERY == EVERY - 1 && more) issue_one(ks, q0, base, lds, off, i / EVERY);
+        };
+        const bf16_t* K = s_kv[ti & (NB - 1)];
+        if constexpr (decltype(first)::value) {
+          products(K, K, Yes{}, No{}, No{}, beside);
+        } else {
+          products(K, s_kv[(ti - 1) & (NB - 1)] + HALF_T, Yes{}, Yes{}, No{}, beside);
+          restore(ti - 1);
+        }
+        if (late) landed(ti + 1);
+        lds_barrier();
+      };
+      auto half_s = [&](int ti) __attribute__((always_inline)) {
+        softmax(ti, Yes{});
+        if (!late) landed(ti + 1);
+        lds_barrier();
+      };
+      half_m(0, Yes{});
+      half_s(0);
+      int ti = 1;
+      // Whole tiles of the prefix, up to the last few: the loop that long prefixes spend
+      // their time in, with no mask and next to no scalar work beside the products (a
+      // wave's scalar and branch instructions do not overlap its own products: with the
+      // general halves they took 700 cycles of 2400). 
+      const int whole = ka.lo % kPfxTile ? 0 : ka.hi / kPfxTile - ta0;
+      if (ti + 3 < whole) {
+        const uint32_t lds0 = lds_addr(s_kv[0]) + grp * (16 * D * 2) + (late ? HALF_T * 2 : 0);
+        const bf16_t* pool = late ? head.v : head.k;
+        const bf16_t* lib = late ? head.lib : head.k;
+        const bf16_t* row = PAGED ? nullptr : pool + ka.seq * head.step + (int64_t)(ta0 * kPfxTile + 16 * grp) * D;
+        const void* base;  // this wave's rows of the tile to request
+        auto next_rows = [&](int t) __attribute__((always_inline)) {
+          const Entry ent = entry(t);
+          base = uniform_ptr(!PAGED ? row + (int64_t)t * (kPfxTile * D)
+                             : late && ent.alias >= 0 ? lib + (int64_t)ent.alias * D : pool + ent.page * head.step);
+        };
+        // the first fragments of tile t's products: its keys have landed a half ago
+        auto preload = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+          for (int i = 0; i < AH; ++i) {
+            kf[i] = kfrag(s_kv[t & (NB - 1)], i);
+            vf[i] = vfrag(s_kv[(t - 1) & (NB - 1)] + HALF_T, i);
+          }
+        };
+        next_rows(ti + 2);
+        preload(ti);
+#pragma unroll 1
+        for (; ti + 3 < whole; ++ti) {
+          const uint32_t lds = lds0 + ((ti + 2) & (NB - 1)) * (2 * HALF_T * 2);
+          auto beside = [&](int i) __attribute__((always_inline)) {
+            constexpr int EVERY = 2 * KS / KI;
+            if (i % EVERY == EVERY - 1) dma16s(base, off[i / EVERY], lds + i / EVERY * 1024);
+          };
+          __builtin_amdgcn_s_setprio(1);  // the other wave's softmax fills the gaps between products, not the reverse
+          products(s_kv[ti & (NB - 1)], s_kv[(ti - 1) & (NB - 1)] + HALF_T, Yes{}, Yes{}, Yes{}, beside);
+          __builtin_amdgcn_s_setprio(0);
+          wait_vm<DPT>();  // this wave's loads of tile ti + 1
+          lds_barrier();
+          __builtin_amdgcn_sched_barrier(0);  // the softmax stays in its half
+          softmax(ti, No{});
+          next_rows(ti + 3);
+          preload(ti + 1);
+          __builtin_amdgcn_sched_barrier(0);
+          lds_barrier();
+        }
+      }
+#pragma unroll 1
+      for (; ti < nt; ++ti) {
+        half_m(ti, No{});
+        half_s(ti);
+      }
+      if (!late) lds_barrier();
+      const bf16_t* K = s_kv[(nt - 1) & (NB - 1)];
+      products(K, K + HALF_T, No{}, Yes{}, No{}, nothing);
+      restore(nt - 1);
     }
+    const float l = sum_halves(lsum);
+    float top = 0.f;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const float l = sum_rows4(lsum[rt]);
-      const int r = 16 * (RT * w + rt) + lr;
-      float top = 0.f;
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, finite_abs(acc[dt][e]));
+    const Emit<bf16_t, D> em(pc, it, hk, Hkv, r, m.tok, rhead, mrow, l, max_halves(top));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, finite_abs(acc[rt][dt][e]));
-      const Emit<bf16_t, D> em(pc, it, hk, Hkv, r, rtok[rt], rhead[rt], mrow[rt], l, max_rows4(top));
-      if (r >= it.n_row) continue;
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-        em.put(dt * 16 + lq * 4, acc[rt][dt][0], acc[rt][dt][1], acc[rt][dt][2], acc[rt][dt][3]);
-    }
+      for (int q = 0; q < 4; q += 2) {
+        // lanes l and l + 32 hold dims 8 q + 0 .. 3 and + 4 .. 7 of q and q + 1: exchanged, the
+        // first has all of q's eight and the other all of q + 1's
+        const uint2 x = em.pack(acc[dt][4 * q], acc[dt][4 * q + 1], acc[dt][4 * q + 2], acc[dt][4 * q + 3]);
+        const uint2 y = em.pack(acc[dt][4 * q + 4], acc[dt][4 * q + 5], acc[dt][4 * q + 6], acc[dt][4 * q + 7]);
+        const auto s0 = __builtin_amdgcn_permlane32_swap(x.x, y.x, false, false);
+        const auto s1 = __builtin_amdgcn_permlane32_swap(x.y, y.y, false, false);
+        if (r < it.n_row) em.put8(dt * 32 + (q + lh) * 8, make_uint4(s0[0], s1[0], s0[1], s1[1]));
+      }
     return;
   }
 
@@ -519,20 +719,21 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
       return (ti >= na ? (kb.lo >> 4) + ti - na : (ka.lo >> 4) + ti) * 16;
     };
     auto own_of = [&](int i) __attribute__((always_inline)) { return w + WAVES * i >= na; };
-    Entry ent;
-    auto fetch = [&](int i) __attribute__((always_inline)) {
-      if (i < n) ent = entry_of<PAGED>(cv, own_of(i) ? kb.seq : ka.seq, first_of(i));
+    Entries<PAGED> entries;
+    auto entry = [&](int i) __attribute__((always_inline)) -> Entry {
+      return entries.get(cv, i, n, lane, [&](int j, int* seq, int* pos) __attribute__((always_inline)) {
+        *seq = own_of(j) ? kb.seq : ka.seq;
+        *pos = first_of(j);
+      });
     };
     auto issue = [&](int i) __attribute__((always_inline)) {
       const Keys ks = own_of(i) ? kb : ka;
       const int q0 = first_of(i);
-      issue_k(ks, q0, key_rows<bf16_t, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, ent), ring_lds + (i & 1) * TILE);
-      issue_v(ks, q0, value_rows<bf16_t, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, ent),
-              ring_lds + (i & 1) * TILE + 16 * D * 2);
+      const Entry ent = entry(i);
+      issue16(ks, q0, head.keys(ks.seq, q0, ent), ring_lds + (i & 1) * TILE, koff);
+      issue16(ks, q0, head.values(ks.seq, q0, ent), ring_lds + (i & 1) * TILE + 16 * D * 2, voff);
     };
-    fetch(0);
     if (n > 0) issue(0);
-    fetch(1);
     uint4 qf[RT][KS];
     int rpos[RT];
 #pragma unroll
@@ -562,7 +763,6 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
       if (i + 1 < n) {
         wait_lds();  // the reads of the buffer's tile before have returned
         issue(i + 1);
-        fetch(i + 2);
         wait_vm<DPT>();
       } else {
         wait_vm<0>();
@@ -614,7 +814,7 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
       }
       if (bad) {
         const int seq = own ? kb.seq : ka.seq;
-        const bf16_t* rows = value_rows<bf16_t, D, PAGED>(cv, pc.layer, seq, hk, p0, entry_of<PAGED>(cv, seq, p0));
+        const bf16_t* rows = head.values(seq, p0, entry_of<PAGED>(cv, seq, p0));
 #pragma unroll 1
         for (int p = max(p0, lo); p < min(p0 + 16, hi); ++p)
 #pragma unroll
@@ -700,6 +900,7 @@ __global__ void __launch_bounds__(256) prefix_attend_f32_kernel(PrefixCall pc, P
   const bool narrow = it.n_row <= 16;
   const Keys ka{pc.prefix_seq, it.a0, it.a1}, kb{it.seq, it.b0, it.b1};
   const int na = tiles_of(ka, kPfxTile), nt = na + tiles_of(kb, kPfxTile);
+  const HeadRows<float, D, PAGED> head(cv, pc.layer, hk);
   float* K = s_kv;
   float* V = s_kv + HALF_T;
 
@@ -728,8 +929,7 @@ __global__ void __launch_bounds__(256) prefix_attend_f32_kernel(PrefixCall pc, P
       const int q0 = min(max(p0 + 16 * w, ks.lo & ~15), (ks.hi - 1) & ~15);
       const Entry e = entry_of<PAGED>(cv, ks.seq, q0);
       const int rlo = max(ks.lo - q0, 0), rhi = min(ks.hi - 1 - q0, 15);
-      const void* bk = key_rows<float, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, e);
-      const void* bv = value_rows<float, D, PAGED>(cv, pc.layer, ks.seq, hk, q0, e);
+      const void *bk = head.keys(ks.seq, q0, e), *bv = head.values(ks.seq, q0, e);
 #pragma unroll
       for (int j = 0; j < KI; ++j) {
         const int rr = j * RI + lane / NC;
