@@ -518,11 +518,12 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
         asm volatile("" ::"v"(__builtin_bit_cast(u32x4_t, pb[0])), "v"(__builtin_bit_cast(u32x4_t, pb[1])),
                      "v"(__builtin_bit_cast(u32x4_t, pb[2])), "v"(__builtin_bit_cast(u32x4_t, pb[3])), "v"(lsum));
     };
+    auto cleaned = [&](int ti) __attribute__((always_inline)) -> bool {
+      const int* sb = s_bad[ti & (NB - 1)];
+      return __builtin_amdgcn_readfirstlane(sb[0] | sb[1] | sb[2] | sb[3]) != 0;
+    };
     // values of tile ti that were cleaned out of its buffer, to the rows that see them
     auto restore = [&](int ti) __attribute__((always_inline)) {
-      if (!is_edge(ti)) return;
-      const int* sb = s_bad[ti & (NB - 1)];
-      if (!(sb[0] | sb[1] | sb[2] | sb[3])) return;
       const bool own = ti >= na;
       const int lo = own ? kb.lo : ka.lo, hi = own ? kb.hi : ka.hi, p0 = first_of(ti), seq = own ? kb.seq : ka.seq;
 #pragma unroll 1
@@ -560,7 +561,7 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
         products(K, K, Yes{}, No{}, No{}, nothing);
         softmax(ti, Yes{});
         products(K, K + HALF_T, No{}, Yes{}, No{}, nothing);
-        restore(ti);
+        if (is_edge(ti) && cleaned(ti)) restore(ti);
       };
       // unrolled by the ring, so that every LDS address is a constant past a lane's base
       for (int ti = 0; ti < nt; ti += 2) {
@@ -582,94 +583,105 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
       uint32_t off[KI];
 #pragma unroll
       for (int j = 0; j < KI; ++j) off[j] = late ? voff[j] : koff[j];
-      auto landed = [&](int ti) __attribute__((always_inline)) {  // tile ti; tile ti + 1 may be in flight
-        if (ti >= nt) return;
-        if (ti + 1 < nt) wait_vm<DPT>();
-        else wait_vm<0>();
-        if (late && is_edge(ti)) clean(ti);
-      };
-      if (1 < nt) issue(1);
-      landed(0);
+      if (1 < nt) {
+        issue(1);
+        wait_vm<DPT>();
+      } else {
+        wait_vm<0>();
+      }
+      if (late && is_edge(0)) clean(0);
       lds_barrier();
       if (late) lds_barrier();
       // (waves without rows go along on a repeated one: branches around the products
       // cost every wave registers)
-      auto half_m = [&](int ti, auto first) __attribute__((always_inline)) {
-        // tile ti + 2, an instruction at a time between the products: requested in one go
-        // they held the wave for 650 cycles
-        const bool more = ti + 2 < nt;
-        const Keys ks = ti + 2 >= na ? kb : ka;
-        const int q0 = more ? group_of(ks, first_of(ti + 2) + 16 * grp) : 0;
-        const Entry ent = entry(min(ti + 2, nt - 1));
-        const void* base = late ? head.values(ks.seq, q0, ent) : head.keys(ks.seq, q0, ent);
-        const uint32_t lds = lds_addr(s_kv[(ti + 2) & (NB - 1)]) + grp * (16 * D * 2) + (late ? HALF_T * 2 : 0);
-        auto beside = [&](int i) __attribute__((always_inline)) {
+      // What a half needs besides its products and its softmax is done in the softmax
+      // half before it: a wave's scalar and branch instructions do not overlap its own
+      // products.
+      const uint32_t lds0 = lds_addr(s_kv[0]) + grp * (16 * D * 2) + (late ? HALF_T * 2 : 0);
+      const void* base;    // this wave's rows of the tile to request next
+      uint32_t offx[KI];   // and the lane's offsets in them
+      bool bad = false;    // values of the tile before were cleaned
+      auto request = [&](int ti, const uint32_t* o) {  // tile ti + 2, an instruction at a time between the products
+        return [=](int i) __attribute__((always_inline)) {
           constexpr int EVERY = 2 * KS / KI;
-          if (i % EVERY == EVERY - 1 && more) issue_one(ks, q0, base, lds, off, i / EVERY);
+          if (i % EVERY == EVERY - 1)
+            dma16s(base, o[i / EVERY], lds0 + ((ti + 2) & (NB - 1)) * (2 * HALF_T * 2) + i / EVERY * 1024);
         };
-        const bf16_t* K = s_kv[ti & (NB - 1)];
-        if constexpr (decltype(first)::value) {
-          products(K, K, Yes{}, No{}, No{}, beside);
-        } else {
-          products(K, s_kv[(ti - 1) & (NB - 1)] + HALF_T, Yes{}, Yes{}, No{}, beside);
-          restore(ti - 1);
+      };
+      // the rows of tile t; past the last tile its rows again, into a buffer that nothing reads
+      auto prepare = [&](int t0) __attribute__((always_inline)) {
+        const int t = min(t0, nt - 1);
+        const Keys ks = t >= na ? kb : ka;
+        const int q0 = group_of(ks, first_of(t) + 16 * grp);
+        const Entry ent = entry(t);
+        base = late ? head.values(ks.seq, q0, ent) : head.keys(ks.seq, q0, ent);
+        const int rlo = max(ks.lo - q0, 0), rhi = min(ks.hi - 1 - q0, 15);
+#pragma unroll
+        for (int j = 0; j < KI; ++j) {
+          const int rr = j * RI + lane / NC;
+          offx[j] = off[j] + (uint32_t)((min(max(rr, rlo), rhi) - rr) * (D * 2));
         }
-        if (late) landed(ti + 1);
+      };
+      // the first fragments of tile t's products: its keys have landed a half ago
+      auto preload = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < AH; ++i) {
+          kf[i] = kfrag(s_kv[t & (NB - 1)], i);
+          vf[i] = vfrag(s_kv[(t - 1) & (NB - 1)] + HALF_T, i);
+        }
+      };
+      auto half_m = [&](int ti, auto first) __attribute__((always_inline)) {
+        const bf16_t* K = s_kv[ti & (NB - 1)];
+        __builtin_amdgcn_s_setprio(1);  // the other wave's softmax fills the gaps between products, not the reverse
+        if constexpr (decltype(first)::value)
+          products(K, K, Yes{}, No{}, No{}, request(ti, offx));
+        else
+          products(K, s_kv[(ti - 1) & (NB - 1)] + HALF_T, Yes{}, Yes{}, Yes{}, request(ti, offx));
+        __builtin_amdgcn_s_setprio(0);
+        if (bad) restore(ti - 1);
+        wait_vm<DPT>();  // this wave's loads of tile ti + 1
+        if (late && ti + 1 < nt && is_edge(ti + 1)) clean(ti + 1);
         lds_barrier();
+        __builtin_amdgcn_sched_barrier(0);  // the softmax stays in its half
       };
       auto half_s = [&](int ti) __attribute__((always_inline)) {
         softmax(ti, Yes{});
-        if (!late) landed(ti + 1);
+        prepare(ti + 3);
+        preload(ti + 1);
+        bad = is_edge(ti) && cleaned(ti);
+        __builtin_amdgcn_sched_barrier(0);
         lds_barrier();
       };
+      prepare(2);
       half_m(0, Yes{});
       half_s(0);
       int ti = 1;
       // Whole tiles of the prefix, up to the last few: the loop that long prefixes spend
-      // their time in, with no mask and next to no scalar work beside the products (a
-      // wave's scalar and branch instructions do not overlap its own products: with the
-      // general halves they took 700 cycles of 2400). 
+      // their time in, with no mask and the least scalar work.
       const int whole = ka.lo % kPfxTile ? 0 : ka.hi / kPfxTile - ta0;
       if (ti + 3 < whole) {
-        const uint32_t lds0 = lds_addr(s_kv[0]) + grp * (16 * D * 2) + (late ? HALF_T * 2 : 0);
+        if (bad) restore(0);
+        bad = false;
         const bf16_t* pool = late ? head.v : head.k;
         const bf16_t* lib = late ? head.lib : head.k;
         const bf16_t* row = PAGED ? nullptr : pool + ka.seq * head.step + (int64_t)(ta0 * kPfxTile + 16 * grp) * D;
-        const void* base;  // this wave's rows of the tile to request
-        auto next_rows = [&](int t) __attribute__((always_inline)) {
-          const Entry ent = entry(t);
-          base = uniform_ptr(!PAGED ? row + (int64_t)t * (kPfxTile * D)
-                             : late && ent.alias >= 0 ? lib + (int64_t)ent.alias * D : pool + ent.page * head.step);
-        };
-        // the first fragments of tile t's products: its keys have landed a half ago
-        auto preload = [&](int t) __attribute__((always_inline)) {
-#pragma unroll
-          for (int i = 0; i < AH; ++i) {
-            kf[i] = kfrag(s_kv[t & (NB - 1)], i);
-            vf[i] = vfrag(s_kv[(t - 1) & (NB - 1)] + HALF_T, i);
-          }
-        };
-        next_rows(ti + 2);
-        preload(ti);
 #pragma unroll 1
         for (; ti + 3 < whole; ++ti) {
-          const uint32_t lds = lds0 + ((ti + 2) & (NB - 1)) * (2 * HALF_T * 2);
-          auto beside = [&](int i) __attribute__((always_inline)) {
-            constexpr int EVERY = 2 * KS / KI;
-            if (i % EVERY == EVERY - 1) dma16s(base, off[i / EVERY], lds + i / EVERY * 1024);
-          };
-          __builtin_amdgcn_s_setprio(1);  // the other wave's softmax fills the gaps between products, not the reverse
-          products(s_kv[ti & (NB - 1)], s_kv[(ti - 1) & (NB - 1)] + HALF_T, Yes{}, Yes{}, Yes{}, beside);
+          __builtin_amdgcn_s_setprio(1);
+          products(s_kv[ti & (NB - 1)], s_kv[(ti - 1) & (NB - 1)] + HALF_T, Yes{}, Yes{}, Yes{}, request(ti, off));
           __builtin_amdgcn_s_setprio(0);
-          wait_vm<DPT>();  // this wave's loads of tile ti + 1
+          wait_vm<DPT>();
           lds_barrier();
-          __builtin_amdgcn_sched_barrier(0);  // the softmax stays in its half
+          __builtin_amdgcn_sched_barrier(0);
           softmax(ti, No{});
-          next_rows(ti + 3);
+          const Entry ent = entry(ti + 3);
+          base = uniform_ptr(!PAGED ? row + (int64_t)(ti + 3) * (kPfxTile * D)
+                             : late && ent.alias >= 0 ? lib + (int64_t)ent.alias * D : pool + ent.page * head.step);
           preload(ti + 1);
           __builtin_amdgcn_sched_barrier(0);
           lds_barrier();
         }
+        prepare(ti + 2);  // (the same rows; offsets for the halves that clamp)
       }
 #pragma unroll 1
       for (; ti < nt; ++ti) {
@@ -679,7 +691,8 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
       if (!late) lds_barrier();
       const bf16_t* K = s_kv[(nt - 1) & (NB - 1)];
       products(K, K + HALF_T, No{}, Yes{}, No{}, nothing);
-      restore(nt - 1);
+      if (bad) restore(nt - 1);
+      wait_vm<0>();  // no load may land in LDS after the block
     }
     const float l = sum_halves(lsum);
     float top = 0.f;
