@@ -364,44 +364,56 @@ struct PrefixTokens {
   bool fused;
 };
 
-// Cut the call into items of row blocks of `block` rows and return the estimated
-// time (us).  The estimate chooses the block shape and the split length; its
-// constants are what the kernel was measured at on a full chip: a tile 2.1 us in a
-// block of 256 rows (one per compute unit) and 3.0 us in each of two blocks of 128
-// rows, 4 us to begin and end an item, and the partials of a slot written and read
-// at 4 TB/s.
-double cut_prefix(const fcg_model_desc& d, int32_t P, const std::vector<PrefixTokens>& toks, int n_tok, int block,
-                  int per_cu, double tile_us, int64_t* per_out) {
+// A block shape of the kernel: rows, blocks at once on the chip, and what an item was
+// measured to take: us per tile with a compute unit to itself and beside a second
+// block, and us to begin and end.
+struct PrefixShape {
+  int rows, at_once;
+  double tile_us, tile2_us, item_us;
+};
+constexpr PrefixShape kShape4{kPfxRows, 512, 1.5, 2.65, 6.0}, kShape8{2 * kPfxRows, 256, 2.0, 2.0, 12.0};
+constexpr PrefixShape kShapeF32{kPfxRowsF32, 512, 4.0, 7.0, 6.0};
+
+// Choose the split length (in tiles) of a call cut into row blocks of a shape, and
+// return the estimated time (us) that the choice of shape goes by: rounds of items,
+// the own items of small groups (5 us and 0.3 us per tile), and the merge, which moves
+// a slot's partials at 4 TB/s.  Against times of 64 tokens over 4.3K shared keys (two
+// row blocks of 128; per 5, 6, 8, 12, 17: 29, 28, 28, 32, 39 us; estimated 27, 28, 30,
+// 36, 42; 256-row blocks: 38 us at best) and of 128 tokens of 8 query heads a kv head
+// over 22K (128-row blocks 140 us, 256-row ones 135; estimated 137 and 115).
+double cut_prefix(const fcg_model_desc& d, int32_t P, const std::vector<PrefixTokens>& toks, int n_tok,
+                  const PrefixShape& shape, int64_t* per_out) {
   const int g = d.n_q_heads / d.n_kv_heads;
   const int64_t ta = tiles_of(0, P);
   std::vector<int64_t> len;  // tiles of each row block
-  int64_t small_rows = 0, own_tiles = 0, longest = 1;
+  int64_t small_rows = 0, longest = 1;
+  double own_us = 0.0;
   for (const PrefixTokens& x : toks) {
     const int64_t own = tiles_of(P, x.end);
     if (x.fused) {
       len.push_back(ta + own);
     } else {
       small_rows += (int64_t)x.n * g;
-      own_tiles += own;
+      own_us += own ? 5.0 + 0.3 * own : 0.0;
       longest = std::max(longest, own);
     }
   }
-  for (int64_t r = 0; r < small_rows && ta; r += block) len.push_back(ta);
+  own_us *= (double)d.n_kv_heads / shape.at_once;
+  for (int64_t r = 0; r < small_rows && ta; r += shape.rows) len.push_back(ta);
   for (int64_t t : len) longest = std::max(longest, t);
-  const int64_t at_once = 256 * per_cu;
   const double slot_us = (double)n_tok * d.n_q_heads * d.head_dim * 2.0 * 2.0 / 4e6;
   double best = 1e30;
+  // at most 64 splits of a row block, and 256 of a sequence's own keys (the merge reads them all)
   for (int64_t ns = 1; ns <= std::min<int64_t>(64, longest); ++ns) {
-    // at most 256 splits each (slots are counted in 16 bits, the merge reads them all)
     const int64_t per = (longest + ns - 1) / ns;
     int64_t blocks = 0, slots = 1;
     for (int64_t t : len) {
       blocks += (t + per - 1) / per;
       slots = std::max(slots, (t + per - 1) / per);
     }
-    const double rounds = std::ceil((double)blocks * d.n_kv_heads / at_once);
-    // own items of the small groups read each key once, a quarter of a tile's time
-    const double us = rounds * (per * tile_us + 4.0) + 0.25 * own_tiles * d.n_kv_heads / at_once * tile_us +
+    blocks *= d.n_kv_heads;
+    const double rounds = std::ceil((double)blocks / shape.at_once);
+    const double us = rounds * (per * (blocks <= 256 ? shape.tile_us : shape.tile2_us) + shape.item_us) + own_us +
                       (small_rows && ta ? (slots + 1) * slot_us + 4.0 : slots > 1 ? slots * slot_us + 4.0 : 0.0);
     if (us < best) {
       best = us;
@@ -435,16 +447,17 @@ void plan_prefix(const fcg_model_desc& d, int32_t P, int32_t n, const int32_t* s
   for (int32_t t = 0; t < n; ++t) order[t] = t;
   auto less = [&](int32_t a, int32_t b) { return seq[a] != seq[b] ? seq[a] < seq[b] : pos[a] < pos[b]; };
   if (!std::is_sorted(order.begin(), order.end(), less)) std::stable_sort(order.begin(), order.end(), less);
-  int block = d.dtype == FCG_F32 ? kPfxRowsF32 : kPfxRows;
+  const PrefixShape& small_shape = d.dtype == FCG_F32 ? kShapeF32 : kShape4;
+  int block = small_shape.rows;
   std::vector<PrefixTokens> toks = group_tokens(g, n, order, seq, pos, block);
   int64_t per = 1;
-  const double us = cut_prefix(d, P, toks, n, block, 2, 3.0, &per);
-  if (d.dtype == FCG_BF16) {
-    std::vector<PrefixTokens> toks8 = group_tokens(g, n, order, seq, pos, 2 * kPfxRows);
+  const double us = cut_prefix(d, P, toks, n, small_shape, &per);
+  if (d.dtype == FCG_BF16 && (int64_t)n * g > kPfxRows) {
+    std::vector<PrefixTokens> toks8 = group_tokens(g, n, order, seq, pos, kShape8.rows);
     int64_t per8 = 1;
-    if (cut_prefix(d, P, toks8, n, 2 * kPfxRows, 1, 2.1, &per8) < us) {
+    if (cut_prefix(d, P, toks8, n, kShape8, &per8) < us) {
       p->waves = 8;
-      block = 2 * kPfxRows;
+      block = kShape8.rows;
       toks = std::move(toks8);
       per = per8;
     }
