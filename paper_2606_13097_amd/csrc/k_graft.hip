@@ -73,7 +73,8 @@ struct RunsInMemory {
 
 // The turn of a block's keys.  The cache's own form: rotate-half over the whole
 // head.  A form by value (RopeArgs): a lane's two vectors of a key row hold both
-// ends of VEC pairs in every form (k_rope.hip), or dimensions that pass unturned.
+// ends of VEC pairs (halves), or whole pairs each (neighbours: vectors c and c + D /
+// 2 / VEC), or dimensions that pass unturned, as in k_rope.hip.
 struct OwnForm {
   const double* inv_freq;
   static constexpr bool kPairs = false;
@@ -146,9 +147,10 @@ __global__ void __launch_bounds__(256) graft_kernel(Runs runs, const T* __restri
   uint4 klo[KP], khi[KP], vv[VP];
   const int kc = t % KT, kr = t / KT;
   const int nturn = form.turned(HALF);          // turned pairs
-  const bool turn = kc * VEC < nturn;
-  const int lo = Form::kPairs || !turn ? 2 * kc * VEC : kc * VEC;
-  const int hi = Form::kPairs || !turn ? lo + VEC : nturn + kc * VEC;
+  const bool turn = kc * VEC < (Form::kPairs ? 2 * nturn : nturn);  // the lane's first vector, for halves both
+  const bool turn_hi = Form::kPairs ? HALF + kc * VEC < 2 * nturn : turn;
+  const int lo = Form::kPairs || turn ? kc * VEC : nturn + kc * VEC;
+  const int hi = Form::kPairs || !turn ? HALF + kc * VEC : nturn + kc * VEC;
 #pragma unroll
   for (int p = 0; p < KP; ++p) {
     const int j = min(p * KR + kr, ch.n - 1);
@@ -172,11 +174,12 @@ __global__ void __launch_bounds__(256) graft_kernel(Runs runs, const T* __restri
   if (t < nturn) form.cs(ch.delta, t, &s_cos[t], &s_sin[t]);
   __syncthreads();  // cos/sin ready
 
-  float c[VEC], s[VEC];
+  float c[VEC], s[VEC];  // neighbours: the first half for the first vector's pairs, the second for the other's
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
-    c[e] = s_cos[kc * VEC + e];  // not used by a lane past the turned pairs
-    s[e] = s_sin[kc * VEC + e];
+    const int i = !Form::kPairs ? kc * VEC + e : (e < VEC / 2 ? kc * VEC / 2 : (HALF + kc * VEC) / 2 - VEC / 2) + e;
+    c[e] = s_cos[i];  // not used by a lane past the turned pairs
+    s[e] = s_sin[i];
   }
 #pragma unroll
   for (int p = 0; p < KP; ++p) {
@@ -187,7 +190,7 @@ __global__ void __launch_bounds__(256) graft_kernel(Runs runs, const T* __restri
       Store<T>::unpack(khi[p], x2);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        if (Form::kPairs) {  // pair kc VEC + e: elements 2e, 2e + 1 of the two vectors end to end
+        if (Form::kPairs) {  // elements 2e, 2e + 1 of the two vectors end to end
           const int i = (2 * e) % VEC;
           const float* x = e < VEC / 2 ? x1 : x2;
           float* y = e < VEC / 2 ? y1 : y2;
@@ -200,7 +203,7 @@ __global__ void __launch_bounds__(256) graft_kernel(Runs runs, const T* __restri
       }
       const int64_t off = dst_off(ch.dst + j);
       st_cache<PAGED>(ck + off + lo, turn ? Store<T>::pack(y1) : klo[p]);
-      st_cache<PAGED>(ck + off + hi, turn ? Store<T>::pack(y2) : khi[p]);
+      st_cache<PAGED>(ck + off + hi, turn_hi ? Store<T>::pack(y2) : khi[p]);
     }
   }
   if (run_aliased) return;

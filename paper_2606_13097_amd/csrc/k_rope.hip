@@ -9,10 +9,13 @@
 // consecutive positions of one sequence) of one layer.  The (cos, sin) of its
 // tokens' pairs are computed once into LDS while the first rows' loads are in
 // flight, and shared by all heads.  A lane moves two 16-byte vectors of a row,
-// chosen so that they hold both ends of 16 / sizeof(T) pairs: vectors c and
-// c + R / 32 (bf16) for halves, 2c and 2c + 1 for neighbours and for the
-// dimensions past R; so every form turns registers only.  Caller rows start at
-// any element (unaligned 16-byte accesses); cache rows are aligned.
+// chosen so that every form turns registers only and that neighbouring lanes
+// move neighbouring vectors: for halves, vectors c and c + R / 2 / VEC hold both
+// ends of VEC pairs; for neighbours each vector holds whole pairs, and a lane
+// takes vectors c and c + D / 2 / VEC; what passes unturned is cut in halves
+// likewise.  (With 2c and 2c + 1 each access covered every other 16 bytes.)
+// Caller rows start at any element (unaligned 16-byte accesses); cache rows are
+// aligned.
 //
 // What bounds it: many tokens, HBM; few, the chain of argument fetch, position,
 // rows and stores.
@@ -113,18 +116,19 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(Where<MODE> where, RopeR
     Item x;
     x.c = i % NCH;
     const int r = r0 + i / NCH;
-    x.tl = r / H;
+    x.tl = H == 1 ? r : (int)__umulhi((unsigned)r, rows.h_magic);  // r / H
     const int h = r - x.tl * H;
     x.kind = h < rows.Hq ? 0 : h < rows.Hq + rows.Hk ? 1 : 2;
     x.head = h - (x.kind == 0 ? 0 : x.kind == 1 ? rows.Hq : rows.Hq + rows.Hk);
     return x;
   };
   // element offsets of the lane's two vectors in the row
+  const bool halves = !PAIRS;
   auto lo_of = [&](const Item& x) __attribute__((always_inline)) {
-    return (PAIRS || x.c >= rchunks || x.kind == 2 ? 2 * x.c : x.c) * VEC;
+    return (halves && x.kind != 2 && x.c >= rchunks ? rchunks + x.c : x.c) * VEC;
   };
   auto hi_of = [&](const Item& x) __attribute__((always_inline)) {
-    return (PAIRS || x.c >= rchunks || x.kind == 2 ? 2 * x.c + 1 : x.c + rchunks) * VEC;
+    return (halves && x.kind != 2 && x.c < rchunks ? rchunks + x.c : NCH + x.c) * VEC;
   };
   auto row_of = [&](const RowView& v, const Item& x) __attribute__((always_inline)) {
     return reinterpret_cast<const T*>(v.p) + (int64_t)layer * v.layer + (int64_t)(g.tok0 + x.tl) * v.token +
@@ -169,26 +173,38 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(Where<MODE> where, RopeR
       if (i >= total) continue;
       const Item x = item_of(i);
       uint4 ya = a[u], yb = b[u];
-      if (x.kind != 2 && x.c < rchunks) {
+      if (PAIRS ? x.kind != 2 && x.c < 2 * rchunks : x.kind != 2 && x.c < rchunks) {
         float xa[VEC], xb[VEC], za[VEC], zb[VEC];
         Store<T>::unpack(ya, xa);
         Store<T>::unpack(yb, xb);
-        const float2* cs = s_cs + x.tl * half + x.c * VEC;
+        if constexpr (PAIRS) {
+          constexpr int P = VEC / 2;  // pairs of a vector
+          const float2* cs = s_cs + x.tl * half + x.c * P;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const float c = cs[e].x, s = cs[e].y;
-          if (PAIRS) {  // pair c VEC + e: elements 2e, 2e + 1 of the two vectors end to end
-            const float p = e < VEC / 2 ? xa[(2 * e) % VEC] : xb[(2 * e) % VEC];
-            const float q = e < VEC / 2 ? xa[(2 * e + 1) % VEC] : xb[(2 * e + 1) % VEC];
-            (e < VEC / 2 ? za : zb)[(2 * e) % VEC] = fmaf(p, c, -q * s);
-            (e < VEC / 2 ? za : zb)[(2 * e + 1) % VEC] = fmaf(q, c, p * s);
-          } else {
-            za[e] = fmaf(xa[e], c, -xb[e] * s);
-            zb[e] = fmaf(xb[e], c, xa[e] * s);
+          for (int e = 0; e < P; ++e) {
+            za[2 * e] = fmaf(xa[2 * e], cs[e].x, -xa[2 * e + 1] * cs[e].y);
+            za[2 * e + 1] = fmaf(xa[2 * e + 1], cs[e].x, xa[2 * e] * cs[e].y);
           }
+          ya = Store<T>::pack(za);
+          if (NCH + x.c < 2 * rchunks) {
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+              const float2 c2 = cs[NCH * P + e];
+              zb[2 * e] = fmaf(xb[2 * e], c2.x, -xb[2 * e + 1] * c2.y);
+              zb[2 * e + 1] = fmaf(xb[2 * e + 1], c2.x, xb[2 * e] * c2.y);
+            }
+            yb = Store<T>::pack(zb);
+          }
+        } else {
+          const float2* cs = s_cs + x.tl * half + x.c * VEC;
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            za[e] = fmaf(xa[e], cs[e].x, -xb[e] * cs[e].y);
+            zb[e] = fmaf(xb[e], cs[e].x, xa[e] * cs[e].y);
+          }
+          ya = Store<T>::pack(za);
+          yb = Store<T>::pack(zb);
         }
-        ya = Store<T>::pack(za);
-        yb = Store<T>::pack(zb);
       }
       if (MODE == kApply || x.kind == 0) {
         T* dst = const_cast<T*>(row_of(x.kind == 0 ? rows.q_out : rows.k_out, x));

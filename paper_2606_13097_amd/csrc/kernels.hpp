@@ -316,6 +316,7 @@ struct RopeRows {
   int32_t n_tok, tb;              // tokens, tokens of a block
   int32_t slice_rows;             // rows of a block (grid y cuts the rows of its tokens)
   int32_t n_layers;
+  uint32_t h_magic;               // ceil(2^32 / rows of a token): r / rows = r * h_magic >> 32 for the rows of a block
   float sign;                     // of the angles
 };
 

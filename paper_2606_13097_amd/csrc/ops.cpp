@@ -142,12 +142,26 @@ fcg_status fcg_rope_destroy(fcg_rope* rope) {
 
 namespace {
 
-// How the tokens' rows are cut into blocks: tokens of a block and, where there
-// are few tokens, rows of a block.
+// How the tokens' rows are cut into blocks.  A pass of a block moves 1024 pairs of
+// vectors, nch of each row: as many tokens as fill whole passes best while there are
+// blocks for two rounds of the chip's compute units; where there are few tokens, a block
+// takes part of one token's rows.
 void cut_rows(RopeRows* rows, int64_t n_tok, int64_t n_layers, int H, int nch) {
-  rows->tb = (int)std::max<int64_t>(1, std::min<int64_t>(kAppMaxTb, n_tok * n_layers / 2048));
+  rows->tb = 1;
+  double best = 0.0;
+  for (int tb = 1; tb <= kAppMaxTb; ++tb) {
+    const int64_t items = (int64_t)tb * H * nch, passes = (items + 1023) / 1024;
+    const int64_t blocks = (n_tok + tb - 1) / tb * n_layers;
+    if (tb > 1 && blocks < 512) break;
+    const double used = (double)items / (double)(passes * 1024);
+    if (used > best + 0.02) {
+      best = used;
+      rows->tb = tb;
+    }
+  }
+  rows->h_magic = H > 1 ? (uint32_t)((((uint64_t)1 << 32) + H - 1) / H) : 0;
   rows->slice_rows = rows->tb * H;
-  const int pass = 256 / nch;  // rows that one pass of a block moves
+  const int pass = 256 / nch;  // rows that 256 lanes move at a time
   if (n_tok * n_layers < 256) rows->slice_rows = std::min(rows->slice_rows, pass);
 }
 
