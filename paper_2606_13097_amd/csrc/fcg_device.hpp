@@ -232,7 +232,10 @@ __device__ __forceinline__ void rope_cs_turns(double pos, double turns, float* c
   sincospif(2.f * (float)(t - rint(t)), s, c);
 }
 
-// 16 and 8 bytes to any address
+// 16 bytes to any address; 16 bytes with the nontemporal hint
 __device__ __forceinline__ void st16_any(void* p, const uint4& v) { __builtin_memcpy(p, &v, 16); }
+__device__ __forceinline__ void st16_nt(void* p, const uint4& v) {
+  __builtin_nontemporal_store(u32x4_t{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4_t*>(p));
+}
 
 }  // namespace fcg

@@ -306,6 +306,8 @@ struct AppendRun {
   int32_t page0;  // its first entry of page[]; bit 31: enter the pages into the device page table
 };
 constexpr int kAppRuns = 64, kAppPages = 384, kAppMaxTb = 16;
+// Pairs of vectors a block moves in a pass (two per lane; with four, 2-5% slower).
+constexpr int kRopePass = 512;
 struct AppendArgs {
   AppendRun run[kAppRuns];
   int32_t page[kAppPages];

@@ -142,27 +142,26 @@ fcg_status fcg_rope_destroy(fcg_rope* rope) {
 
 namespace {
 
-// How the tokens' rows are cut into blocks.  A pass of a block moves 1024 pairs of
-// vectors, nch of each row: as many tokens as fill whole passes best while there are
-// blocks for two rounds of the chip's compute units; where there are few tokens, a block
-// takes part of one token's rows.
+// How the tokens' rows are cut into blocks.  A block moves slice_rows rows of a group of
+// tb tokens in one pass, kRopePass pairs of vectors (nch of each row), or half as many
+// where there are few tokens.  Groups as large as fill their slices best, while there are
+// a few blocks for each compute unit: the (cos, sin) of a token are computed by each block
+// that has rows of it.
 void cut_rows(RopeRows* rows, int64_t n_tok, int64_t n_layers, int H, int nch) {
+  const int slice = (n_tok * n_layers < 256 ? 256 : kRopePass) / nch;
   rows->tb = 1;
   double best = 0.0;
   for (int tb = 1; tb <= kAppMaxTb; ++tb) {
-    const int64_t items = (int64_t)tb * H * nch, passes = (items + 1023) / 1024;
-    const int64_t blocks = (n_tok + tb - 1) / tb * n_layers;
-    if (tb > 1 && blocks < 512) break;
-    const double used = (double)items / (double)(passes * 1024);
+    const int64_t slices = ((int64_t)tb * H + slice - 1) / slice;
+    if (tb > 1 && (n_tok + tb - 1) / tb * slices * n_layers < 2048) break;
+    const double used = (double)tb * H / (double)(slices * slice);
     if (used > best + 0.02) {
       best = used;
       rows->tb = tb;
     }
   }
+  rows->slice_rows = std::min(slice, rows->tb * H);
   rows->h_magic = H > 1 ? (uint32_t)((((uint64_t)1 << 32) + H - 1) / H) : 0;
-  rows->slice_rows = rows->tb * H;
-  const int pass = 256 / nch;  // rows that 256 lanes move at a time
-  if (n_tok * n_layers < 256) rows->slice_rows = std::min(rows->slice_rows, pass);
 }
 
 }  // namespace
@@ -244,14 +243,15 @@ fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_t
   return guarded([&]() -> fcg_status {
     std::vector<std::pair<int32_t, int32_t>> new_pages;
     std::vector<int32_t> order;
+    std::vector<Span> runs_of;  // runs of consecutive positions
     std::string msg;
     if (fcg_status st = c->plan.check_place(layer, n_layers, n_tok, seq, pos, (flags & FCG_REPLACE) != 0, &order,
-                                            &new_pages, &msg))
+                                            &runs_of, &new_pages, &msg))
       return fail(st, msg);
     if (n_tok == 0 || n_layers == 0) return FCG_OK;
     auto commit = [&]() {
-      for (int32_t l = layer; l < layer + n_layers; ++l)
-        for (int32_t t = 0; t < n_tok; ++t) c->plan.mark(seq[t], l, pos[t]);
+      for (const Span& x : runs_of)
+        for (int32_t l = layer; l < layer + n_layers; ++l) c->plan.mark_range(x.seq, l, x.dst, x.len);
     };
     if (c->layout_only()) {
       c->plan.map_pages(new_pages);

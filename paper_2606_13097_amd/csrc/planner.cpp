@@ -151,7 +151,7 @@ fcg_status Planner::check_append(int32_t layer, int32_t n, const int32_t* seq, c
 }
 
 fcg_status Planner::check_place(int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq, const int32_t* pos,
-                                bool replace, std::vector<int32_t>* order,
+                                bool replace, std::vector<int32_t>* order, std::vector<Span>* runs,
                                 std::vector<std::pair<int32_t, int32_t>>* new_pages, std::string* msg) const {
   if (layer < 0 || (int64_t)layer + n_layers > L_) {
     *msg = fmt("layers %lld .. %lld out of range", layer, (int64_t)layer + n_layers - 1);
@@ -182,19 +182,23 @@ fcg_status Planner::check_place(int32_t layer, int32_t n_layers, int32_t n, cons
       return FCG_EOVERLAP;
     }
   }
+  runs->clear();
+  for (int32_t t : *order) {
+    if (!runs->empty() && runs->back().seq == seq[t] && runs->back().dst + runs->back().len == pos[t]) ++runs->back().len;
+    else runs->push_back(Span{seq[t], 0, pos[t], 1, 0});
+  }
   if (!replace)
     for (int32_t l = layer; l < layer + n_layers; ++l)
-      for (int32_t t = 0; t < n; ++t)
-        if (written(seq[t], l, pos[t])) {
-          *msg = fmt("position %lld of sequence %lld already written in layer %lld", pos[t], seq[t], l);
+      for (const Span& x : *runs)
+        if (any_in_range(x.seq, l, x.dst, x.dst + x.len)) {
+          *msg = fmt("span at %lld of sequence %lld meets written positions (layer %lld)", x.dst, x.seq, l);
           return FCG_EOVERLAP;
         }
   std::vector<std::pair<int32_t, int32_t>> touched;
   if (P_ && n_layers)
-    for (int32_t t : *order) {
-      const std::pair<int32_t, int32_t> sl{seq[t], pos[t] / P_};
-      if (touched.empty() || touched.back() != sl) touched.push_back(sl);
-    }
+    for (const Span& x : *runs)
+      for (int32_t lp = x.dst / P_; lp <= (x.dst + x.len - 1) / P_; ++lp)
+        if (touched.empty() || touched.back() != std::pair<int32_t, int32_t>(x.seq, lp)) touched.push_back({x.seq, lp});
   return collect_pages(touched, new_pages, msg);
 }
 
@@ -271,21 +275,23 @@ void Planner::mark(int32_t seq, int32_t layer, int32_t pos) {
   }
 }
 
-void Planner::mark_all_layers(int32_t seq, int32_t dst, int32_t len) {
+void Planner::mark_range(int32_t seq, int32_t layer, int32_t dst, int32_t len) {
   if (len <= 0) return;
-  for (int32_t l = 0; l < L_; ++l) {
-    uint64_t* w = bits(seq, l);
-    int32_t added = 0;
-    for (int32_t p = dst; p < dst + len;) {  // a word at a time
-      const int32_t lo = p & 63, hi = std::min(64, lo + (dst + len - p));
-      const uint64_t mask = (hi == 64 ? ~0ull : ((1ull << hi) - 1)) & ~((1ull << lo) - 1);
-      added += __builtin_popcountll(mask & ~w[p >> 6]);
-      w[p >> 6] |= mask;
-      p += hi - lo;
-    }
-    cnt_[idx(seq, l)] += added;
-    len_[idx(seq, l)] = std::max(len_[idx(seq, l)], dst + len);
+  uint64_t* w = bits(seq, layer);
+  int32_t added = 0;
+  for (int32_t p = dst; p < dst + len;) {  // a word at a time
+    const int32_t lo = p & 63, hi = std::min(64, lo + (dst + len - p));
+    const uint64_t mask = (hi == 64 ? ~0ull : ((1ull << hi) - 1)) & ~((1ull << lo) - 1);
+    added += __builtin_popcountll(mask & ~w[p >> 6]);
+    w[p >> 6] |= mask;
+    p += hi - lo;
   }
+  cnt_[idx(seq, layer)] += added;
+  len_[idx(seq, layer)] = std::max(len_[idx(seq, layer)], dst + len);
+}
+
+void Planner::mark_all_layers(int32_t seq, int32_t dst, int32_t len) {
+  for (int32_t l = 0; l < L_; ++l) mark_range(seq, l, dst, len);
 }
 
 bool Planner::alias_pages(int32_t seq, int32_t dst, int32_t len, int64_t lib_tok0) {

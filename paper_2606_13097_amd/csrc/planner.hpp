@@ -56,10 +56,11 @@ class Planner {
 
   // Tokens placed without attending, in layers [layer, layer + n_layers): holes
   // are allowed; with `replace`, written positions are too.  *order receives the
-  // tokens sorted by (sequence, position).
+  // tokens sorted by (sequence, position), *runs their runs of consecutive
+  // positions (seq, dst, len).
   fcg_status check_place(int32_t layer, int32_t n_layers, int32_t n, const int32_t* seq, const int32_t* pos, bool replace,
-                         std::vector<int32_t>* order, std::vector<std::pair<int32_t, int32_t>>* new_pages,
-                         std::string* msg) const;
+                         std::vector<int32_t>* order, std::vector<Span>* runs,
+                         std::vector<std::pair<int32_t, int32_t>>* new_pages, std::string* msg) const;
   // Tokens that attend to positions [0, prefix_len) of prefix_seq and to
   // [prefix_len, pos] of their own sequence.
   fcg_status check_attend(int32_t layer, int32_t prefix_seq, int32_t prefix_len, int32_t n, const int32_t* seq,
@@ -68,6 +69,7 @@ class Planner {
   // Commits (after a successful check).
   void map_pages(const std::vector<std::pair<int32_t, int32_t>>& new_pages);
   void mark_all_layers(int32_t seq, int32_t dst, int32_t len);
+  void mark_range(int32_t seq, int32_t layer, int32_t dst, int32_t len);
   // graft of len tokens at dst whose first token is library token lib_tok0:
   // with alias_v, the logical pages inside [dst, dst + len) map their values
   // onto the library.  Called before map_pages; true if one of them is mapped

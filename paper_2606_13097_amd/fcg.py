@@ -147,6 +147,8 @@ def _check(status: int) -> None:
 
 
 def _i32(a) -> np.ndarray:
+    if type(a) is np.ndarray and a.dtype == np.int32 and a.flags.c_contiguous:
+        return a
     return np.ascontiguousarray(np.asarray(a, dtype=np.int32))
 
 
@@ -476,23 +478,31 @@ def fcg_rope_destroy(rope: Rope) -> None:
 _TORCH_DT = {torch.float32: FCG_F32, torch.bfloat16: FCG_BF16}
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _view(t, n_layers: int, n_tok: int, n_heads: int, head_dim: int, dtype: int, device, what: str):
-    """fcg_tensor of a [n_layers][n_tok][n_heads][head_dim] tensor (three dimensions: one layer)."""
+    """fcg_tensor of a [n_layers][n_tok][n_heads][head_dim] tensor (three dimensions: one layer).  One call makes up
+    to four of these, a visible part of a small step, so the checks are few and plain."""
     if t is None:
         return None
     if not t.is_cuda or _TORCH_DT.get(t.dtype) != dtype:
         raise ValueError(f"{what}: not a GPU tensor of the expected type")
-    if device is not None and t.device.index != device:
-        raise ValueError(f"{what}: on device {t.device.index}, expected {device}")
-    shape, st = tuple(t.shape), t.stride()
-    if t.dim() == 3:
-        shape, st = (1,) + shape, (0,) + st
-    if shape != (n_layers, n_tok, n_heads, head_dim):
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected "
-                         f"{(n_layers, n_tok, n_heads, head_dim)[0 if t.dim() == 4 else 1:]}")
-    if st[3] != 1 and t.numel():
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{what}: on device {t.get_device()}, expected {device}")
+    st = t.stride()
+    if len(st) == 3 and n_layers == 1:
+        ok = t.shape == (n_tok, n_heads, head_dim)
+        v = TensorView(t.data_ptr(), 0, st[0], st[1])
+    else:
+        ok = t.shape == (n_layers, n_tok, n_heads, head_dim)
+        v = TensorView(t.data_ptr(), *st[:3])
+    if not ok:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(n_layers, n_tok, n_heads, head_dim)} (one layer: "
+                         "or without the first dimension)")
+    if st[-1] != 1 and t.numel():
         raise ValueError(f"{what}: the elements of a row must be adjacent")
-    return TensorView(t.data_ptr(), st[0], st[1], st[2])
+    return v
 
 
 def _ref(v: Optional[TensorView]):
@@ -501,10 +511,11 @@ def _ref(v: Optional[TensorView]):
 
 def _stream_of(stream, device) -> Optional[int]:
     """The given stream, or torch's current stream of ``device``."""
-    if stream is not None or device is None:
-        return _stream(stream) if stream is not None else None
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+    if stream is not None:
+        return _stream(stream)
+    if device is None:
+        return None
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 def fcg_rope_apply(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, flags: int = 0, stream=None) -> None:
@@ -518,15 +529,18 @@ def fcg_rope_apply(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, flag
         raise ValueError("a float32 or bfloat16 tensor of three or four dimensions")
     if (q is None) != (q_out is None) or (k is None) != (k_out is None):
         raise ValueError("an input without its output, or an output without its input")
-    dt, dev, n, d = _TORCH_DT[like.dtype], pos.device.index, pos.numel(), like.shape[-1]
+    dt, dev, n, d = _TORCH_DT[like.dtype], pos.get_device(), pos.numel(), like.shape[-1]
     layers = like.shape[0] if like.dim() == 4 else 1
     hq, hk = 0 if q is None else q.shape[-2], 0 if k is None else k.shape[-2]
-    views = [_view(t, layers, n, h, d, dt, dev, w) for t, h, w in
-             ((q, hq, "q"), (q_out, hq, "q_out"), (k, hk, "k"), (k_out, hk, "k_out"))]
-    vq, vqo, vk, vko = map(_ref, views)
-    with torch.cuda.device(dev):
-        _check(_L.fcg_rope_apply(rope.h, dt, d, layers, n, pos.data_ptr(), hq, vq, vqo, hk, vk, vko, int(flags),
-                                 _stream_of(stream, dev)))
+    vq, vqo = _view(q, layers, n, hq, d, dt, dev, "q"), _view(q_out, layers, n, hq, d, dt, dev, "q_out")
+    vk, vko = _view(k, layers, n, hk, d, dt, dev, "k"), _view(k_out, layers, n, hk, d, dt, dev, "k_out")
+    args = (rope.h, dt, d, layers, n, pos.data_ptr(), hq, _ref(vq), _ref(vqo), hk, _ref(vk), _ref(vko), int(flags),
+            _stream_of(stream, dev))
+    if dev == torch.cuda.current_device():
+        _check(_L.fcg_rope_apply(*args))
+    else:
+        with torch.cuda.device(dev):
+            _check(_L.fcg_rope_apply(*args))
 
 
 def fcg_graft_rope(cache: Cache, lib: Library, rope: Rope, seq: Sequence[int], seg: Sequence[int], dst: Sequence[int],
@@ -549,11 +563,11 @@ def fcg_append(cache: Cache, layer: int, seq, pos, k=None, v=None, rope: Optiona
     if k is not None:
         n_layers = k.shape[0] if k.dim() == 4 else 1
     d, n = cache.desc, int(s.size)
-    views = [_view(t, n_layers, n, h, d.head_dim, d.dtype, cache.device, w) for t, h, w in
-             ((q, d.n_q_heads, "q"), (q_out, d.n_q_heads, "q_out"), (k, d.n_kv_heads, "k"), (v, d.n_kv_heads, "v"))]
-    vq, vqo, vk, vv = map(_ref, views)
-    _check(_L.fcg_append(cache.h, int(layer), int(n_layers), n, _p(s), _p(p), None if rope is None else rope.h, vq, vqo,
-                         vk, vv, int(flags), _stream_of(stream, cache.device)))
+    hq, hkv, hd, dt, dev = d.n_q_heads, d.n_kv_heads, d.head_dim, d.dtype, cache.device
+    vq, vqo = _view(q, n_layers, n, hq, hd, dt, dev, "q"), _view(q_out, n_layers, n, hq, hd, dt, dev, "q_out")
+    vk, vv = _view(k, n_layers, n, hkv, hd, dt, dev, "k"), _view(v, n_layers, n, hkv, hd, dt, dev, "v")
+    _check(_L.fcg_append(cache.h, int(layer), int(n_layers), n, _p(s), _p(p), None if rope is None else rope.h,
+                         _ref(vq), _ref(vqo), _ref(vk), _ref(vv), int(flags), _stream_of(stream, dev)))
 
 
 def fcg_prefix_attend(cache: Cache, layer: int, prefix_seq: int, prefix_len: int, seq, pos, q, out, lse=None,
@@ -564,9 +578,10 @@ def fcg_prefix_attend(cache: Cache, layer: int, prefix_seq: int, prefix_len: int
     if s.ndim != 1 or s.shape != p.shape:
         raise ValueError("seq and pos differ in length")
     d, n = cache.desc, int(s.size)
-    vq, vo = (_view(t, 1, n, d.n_q_heads, d.head_dim, d.dtype, cache.device, w) for t, w in ((q, "q"), (out, "out")))
+    hq, hd, dt, dev = d.n_q_heads, d.head_dim, d.dtype, cache.device
+    vq, vo = _view(q, 1, n, hq, hd, dt, dev, "q"), _view(out, 1, n, hq, hd, dt, dev, "out")
     if lse is not None and (not lse.is_cuda or lse.dtype != torch.float32 or not lse.is_contiguous() or
-                            tuple(lse.shape) != (n, d.n_q_heads) or lse.device.index != cache.device):
+                            lse.shape != (n, d.n_q_heads) or lse.get_device() != cache.device):
         raise ValueError("lse: a contiguous float32 GPU tensor [n_tok][Hq]")
     _check(_L.fcg_prefix_attend(cache.h, int(layer), int(prefix_seq), int(prefix_len), n, _p(s), _p(p), _ref(vq),
                                 _ref(vo), _dptr(lse), _stream_of(stream, cache.device)))
