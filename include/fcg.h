@@ -402,10 +402,11 @@ fcg_status fcg_append(fcg_cache* cache, int32_t layer, int32_t n_layers, int32_t
  * [n_tok][Hq], contiguous, may be null.  out may be q (the same data and
  * strides).
  * The split partials sit in a workspace of the cache, enlarged when a call
- * needs more.  A call can be captured into a graph if a call as large ran
- * before and it has at most 64 tokens of at most 16 / (Hq / Hkv) per sequence (and
- * bf16 caches); a workspace that a capture used is kept until the cache is
- * destroyed.
+ * needs more.  A call can be captured into a graph if a call at least as large
+ * ran before and it has at most 128 tokens, of at most 64 sequences, none with
+ * 96 (fp32: 48) query rows a kv head or more; a workspace that a capture used is
+ * kept until the cache is destroyed, and the calls and graphs of one cache share
+ * it, so they must not overlap.
  * Errors: EINVAL (null arrays or tensors, negative counts or strides,
  * overlapping rows of out), ERANGE (layer, sequences, prefix_len outside [0,
  * max_tokens], pos[t] outside [prefix_len - 1, max_tokens)), EHOLE (an attended

@@ -595,3 +595,155 @@ def test_candidates_over_one_stitched_context(dtype, page):
         at[s] += 1
     step([4, 1, 2], 103)
     c.close(), lib.close()
+
+
+# ------------------------------------------------------------------ graphs, streams, far offsets, block shapes
+
+def test_append_and_attend_replay_in_graphs():
+    """A decode step captured twice (two graphs that share the cache's workspace), replayed with new inputs between
+    eager calls, one of which enlarges the workspace."""
+    P, own = 900, [40 + 7 * i for i in range(8)]
+    sh = Shared("bf16", 8, 2, 128, 16, P, own, 21)
+    c, w = sh.cache, freqs64(64, 1e4)
+    rope, _ = make_rope(64)
+    seq, pos = np.arange(8), np.array([P + n - 1 for n in own])
+    q, k, v = randn(gen(1), 8, 8, 128), randn(gen(2), 8, 2, 128), randn(gen(3), 8, 2, 128)
+    qe, out, lse = torch.empty_like(q), torch.empty_like(q), torch.empty((8, 8), device="cuda")
+
+    def step(stream=None):
+        fcg.fcg_append(c, 1, seq, pos, k, v, rope=rope, q=q, q_out=qe, flags=fcg.FCG_REPLACE, stream=stream)
+        fcg.fcg_prefix_attend(c, 1, sh.pseq, P, seq, pos, qe, out, lse, stream=stream)
+
+    step()
+    graphs = []
+    for _ in range(2):
+        s = torch.cuda.Stream()
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g, stream=s):
+            step()
+        graphs.append(g)
+    many = np.repeat(np.arange(8), 30)
+    mpos = np.concatenate([P + np.arange(n - 30, n) for n in own])
+    mq = randn(gen(9), len(many), 8, 128)
+    for r in range(5):
+        for x, sd in ((q, 100), (k, 200), (v, 300)):
+            x.copy_(randn(gen(sd + r), *x.shape))
+        graphs[r % 2].replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone(), qe.clone()
+        for s in range(8):
+            kk, vv = sh.kv[s]
+            kk[own[s] - 1] = turn64(k[s:s + 1], pos[s:s + 1], w, False)[0].to(torch.bfloat16)
+            vv[own[s] - 1] = v[s]
+        sh.check(seq, pos, got[2], got[0], got[1], f"replay {r}")
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(bits(out), bits(got[0])) and torch.equal(lse, got[1])
+        if r == 1:      # a larger call takes a new workspace; the graphs keep theirs
+            mo = torch.empty_like(mq)
+            fcg.fcg_prefix_attend(c, 1, sh.pseq, P, many, mpos, mq, mo)
+            torch.cuda.synchronize()
+    sh.cache.close()
+
+
+def test_captures_that_need_an_upload_are_refused():
+    sh = Shared("bf16", 8, 2, 64, 16, 100, [40] * 70, 5)
+    c = sh.cache
+    n = 70
+    q, k, v = randn(gen(1), n, 8, 64), randn(gen(2), n, 2, 64), randn(gen(3), n, 2, 64)
+    out = torch.empty_like(q)
+    before = [fcg.fcg_cache_export_layout(c, s, 1) for s in (0, 70)]
+    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=s):
+        for call in (lambda: fcg.fcg_append(c, 1, [0], [0], k[:1], v[:1]),                               # maps a page
+                     lambda: fcg.fcg_append(c, 1, np.arange(n), np.full(n, 139), k, v, flags=fcg.FCG_REPLACE),   # 70 runs
+                     lambda: fcg.fcg_prefix_attend(c, 1, 70, 100, np.arange(n), np.full(n, 139), q, out),      # 70 sequences
+                     lambda: fcg.fcg_prefix_attend(c, 1, 70, 100, [0, 1], [139, 139], q[:2], out[:2])):         # no workspace yet
+            with pytest.raises(fcg.FcgError) as e:
+                call()
+            assert e.value.status == fcg.FCG_ESTATE
+        out.zero_()
+    for b, sq in zip(before, (0, 70)):
+        now = fcg.fcg_cache_export_layout(c, sq, 1)
+        assert b[1] == now[1] and np.array_equal(b[0], now[0]) and np.array_equal(b[2], now[2])
+    g.replay()
+    fcg.fcg_prefix_attend(c, 1, 70, 100, np.arange(n), np.full(n, 139), q, out)
+    torch.cuda.synchronize()
+    sh.check(np.arange(n), np.full(n, 139), q, out, None, "after", np.arange(0, n, 11))
+    c.close()
+
+
+def test_calls_on_another_stream_and_a_strided_result():
+    sh = Shared("bf16", 4, 2, 64, 0, 130, [9, 70], 6)
+    s = torch.cuda.Stream()
+    big = torch.full((5, 9, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    q = randn(gen(1), 2, 4, 64)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        fcg.fcg_prefix_attend(sh.cache, 1, sh.pseq, 130, [0, 1], [138, 199], q, big[1:3, 2:6])
+    s.synchronize()
+    sh.check([0, 1], [138, 199], q, big[1:3, 2:6], None, "stream")
+    rest = torch.ones((5, 9), dtype=torch.bool)
+    rest[1:3, 2:6] = False
+    assert bool((big[rest.cuda()] == 3.0).all())
+    sh.cache.close()
+
+
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("hq,hkv,d", [(32, 2, 128), (16, 4, 64)])
+def test_prefix_attend_blocks_of_many_rows(page, hq, hkv, d):
+    """Calls whose rows fill blocks of 256 by themselves, with a rest that shares one, over whole prefix tiles and own
+    keys that start inside a tile."""
+    P = 2101
+    own = [300, 128, 129, 200, 40]
+    sh = Shared("bf16", hq, hkv, d, page, P, own, 31, shuffle=False)
+    n = [128, 128, 77, 140, 3]
+    seq = np.repeat(np.arange(5), n)
+    pos = np.concatenate([P + own[s] - n[s] + np.arange(n[s]) for s in range(5)])
+    q, out, lse = run_shared(sh, seq, pos, 7)
+    some = np.unique(np.r_[np.arange(0, len(seq), 23), np.flatnonzero(seq == 4), np.cumsum(n) - 1])
+    sh.check(seq, pos, q, out, lse, "blocks", some)
+    sh.cache.close()
+
+
+def test_offsets_past_32_bits():
+    """Pages, sequences and rows whose element offsets pass 2^31."""
+    desc = fcg.model_desc(1, 8, 8, 128, 1e4, "bf16")
+    n0 = 2 ** 31 // (8 * 128) + 64                     # positions before the ones looked at
+    for page in (0, 16):
+        if page:
+            c = fcg.Cache(desc, 3, n0, 16, n0 // 16 + 40)
+            fcg.fcg_append(c, 0, np.zeros(n0, np.int32), np.arange(n0, dtype=np.int32))      # reserved
+        else:
+            c = fcg.Cache(desc, 36, 65536)
+        a, b = (1, 2) if page else (34, 35)
+        P = 150
+        pk, pv = randn(gen(1), P, 8, 128), randn(gen(2), P, 8, 128)
+        ok, ov = randn(gen(3), 3, 8, 128), randn(gen(4), 3, 8, 128)
+        fcg.fcg_append(c, 0, np.full(P, a), np.arange(P), pk, pv)
+        fcg.fcg_append(c, 0, np.full(3, b), P + np.arange(3), ok, ov)
+        q, out = randn(gen(5), 3, 8, 128), torch.empty((3, 8, 128), dtype=torch.bfloat16, device="cuda")
+        fcg.fcg_prefix_attend(c, 0, a, P, np.full(3, b), P + np.arange(3), q, out)
+        torch.cuda.synchronize()
+        w = freqs64(128, 1e4)
+        K = torch.cat([turn64(pk, np.arange(P), w, False), turn64(ok, P + np.arange(3), w, False)]).to(torch.bfloat16)
+        V = torch.cat([pv, ov])
+        ref = attend64(q, K, V, P + np.arange(3), P)
+        # the stored keys may be one rounding from K: each score by another half step of sum |q k|
+        err = (out.double() - ref[0]).abs()
+        tol = 2.0 ** -8 * ref[0].abs() + (2.02 * 2.0 ** -8 + 2.0 ** -13) * ref[2]
+        assert bool((err <= tol).all()), float((err - tol).max())
+        c.close()
+    n, h = 265000, 64
+    x = torch.empty((n, h, 128), dtype=torch.bfloat16, device="cuda")
+    x[-5:] = randn(gen(6), 5, h, 128)
+    x[:5] = randn(gen(7), 5, h, 128)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    rope, w = make_rope(128, True)
+    y = torch.empty_like(x)
+    fcg.fcg_rope_apply(rope, pos, x, y)
+    torch.cuda.synchronize()
+    for sl, p in ((slice(0, 5), np.arange(5)), (slice(n - 5, n), np.arange(n - 5, n))):
+        check_turned(y[sl], turn64(x[sl], p, w, True), x[sl], w, True, 1.0, "bf16", "far rows")
