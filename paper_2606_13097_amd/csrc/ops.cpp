@@ -378,57 +378,80 @@ struct PrefixTokens {
   bool fused;
 };
 
-// A block shape of the kernel: rows, blocks at once on the chip, and what an item was
-// measured to take: us per tile with a compute unit to itself and beside a second
-// block, and us to begin and end.
+// A block shape of the kernel: rows, blocks at once on the chip, the most rows of a
+// narrow item, and what items were measured to take: us per tile with a compute unit to
+// itself and beside a second block, and to begin and end; per tile of a narrow item.
 struct PrefixShape {
-  int rows, at_once;
-  double tile_us, tile2_us, item_us;
+  int rows, at_once, narrow;
+  double tile_us, tile2_us, item_us, ntile_us;
 };
-constexpr PrefixShape kShape4{kPfxRows, 512, 1.5, 2.65, 6.0}, kShape8{2 * kPfxRows, 256, 2.0, 2.0, 12.0};
-constexpr PrefixShape kShapeF32{kPfxRowsF32, 512, 4.0, 7.0, 6.0};
+constexpr PrefixShape kShape4{kPfxRows, 512, 32, 1.5, 2.65, 6.0, 0.45}, kShape8{2 * kPfxRows, 256, 32, 2.0, 2.0, 12.0, 0.3};
+constexpr PrefixShape kShapeF32{kPfxRowsF32, 512, 16, 4.0, 7.0, 6.0, 1.0};
 
 // Choose the split length (in tiles) of a call cut into row blocks of a shape, and
-// return the estimated time (us) that the choice of shape goes by: rounds of items,
-// the own items of small groups (5 us and 0.3 us per tile), and the merge, which moves
-// a slot's partials at 4 TB/s.  Against times of 64 tokens over 4.3K shared keys (two
-// row blocks of 128; per 5, 6, 8, 12, 17: 29, 28, 28, 32, 39 us; estimated 27, 28, 30,
-// 36, 42; 256-row blocks: 38 us at best) and of 128 tokens of 8 query heads a kv head
-// over 22K (128-row blocks 140 us, 256-row ones 135; estimated 137 and 115).
+// return the estimated time (us) that the choice of shape goes by: rounds of wide items,
+// the narrow ones (5 us and their tiles, no faster than 5.3 TB/s), and the merge (a round
+// trip per four slots, and the partials at 4 TB/s).  Against measured times (us):
+//   64 tokens over 4.3K shared keys, two row blocks of 128, per 5, 6, 8, 12, 17 tiles: 29,
+//   28, 28, 32, 39 (blocks of 256 rows: 38 at best);
+//   128 tokens, 8 query heads a kv head, over 22K: 140 (128-row blocks), 135 (256-row);
+//   one token over 8K, per 1, 2, 4, 8, 16: 24, 17, 16, 18, 22;
+//   four tokens over 8K, per 1, 2, 4, 6, 8, 16: 30, 23, 19, 17, 18, 23;
+//   8 tokens over own keys of up to 4K, per 1, 3, 6, 12, 24: 35, 25, 22, 21, 27.
 double cut_prefix(const fcg_model_desc& d, int32_t P, const std::vector<PrefixTokens>& toks, int n_tok,
                   const PrefixShape& shape, int64_t* per_out) {
   const int g = d.n_q_heads / d.n_kv_heads;
   const int64_t ta = tiles_of(0, P);
-  std::vector<int64_t> len;  // tiles of each row block
-  int64_t small_rows = 0, longest = 1;
-  double own_us = 0.0;
+  // row blocks: those with keys of their own by their tiles, the shared ones and the narrow
+  // items by their number (a decode step plans in a few us: no loop over its sequences per
+  // candidate)
+  std::vector<int32_t> wide;
+  int32_t small_rows = 0, longest = 1, own_longest = 0, n_narrow = 0;
+  int64_t narrow_tiles = 0;
+  auto add = [&](int32_t rows, int32_t t) {
+    longest = std::max(longest, t);
+    if (rows > shape.narrow) {
+      wide.push_back(t);
+    } else if (t) {
+      ++n_narrow;
+      narrow_tiles += t;
+    }
+  };
   for (const PrefixTokens& x : toks) {
-    const int64_t own = tiles_of(P, x.end);
-    if (x.fused) {
-      len.push_back(ta + own);
-    } else {
-      small_rows += (int64_t)x.n * g;
-      own_us += own ? 5.0 + 0.3 * own : 0.0;
-      longest = std::max(longest, own);
+    const int32_t own = (int32_t)tiles_of(P, x.end);
+    if (!x.fused) {
+      small_rows += x.n * g;
+      own_longest = std::max(own_longest, own);
     }
+    add(x.n * g, own + (x.fused ? (int32_t)ta : 0));
   }
-  own_us *= (double)d.n_kv_heads / shape.at_once;
-  for (int64_t r = 0; r < small_rows && ta; r += shape.rows) len.push_back(ta);
-  for (int64_t t : len) longest = std::max(longest, t);
-  const double slot_us = (double)n_tok * d.n_q_heads * d.head_dim * 2.0 * 2.0 / 4e6;
+  int32_t n_shared = 0;
+  if (small_rows > shape.narrow && ta) {
+    n_shared = (small_rows + shape.rows - 1) / shape.rows;
+    longest = std::max(longest, (int32_t)ta);
+  } else if (small_rows) {
+    add(small_rows, (int32_t)ta);
+  }
+  const double es = d.dtype == FCG_F32 ? 4.0 : 2.0;
+  const double slot_us = (double)n_tok * d.n_q_heads * d.head_dim * es * 2.0 / 4e6;
+  const double read_us = (double)narrow_tiles * kPfxTile * d.n_kv_heads * d.head_dim * es * 2.0 / 5.3e6;
   double best = 1e30;
-  // at most 64 splits of a row block, and 256 of a sequence's own keys (the merge reads them all)
-  for (int64_t ns = 1; ns <= std::min<int64_t>(64, longest); ++ns) {
-    const int64_t per = (longest + ns - 1) / ns;
-    int64_t blocks = 0, slots = 1;
-    for (int64_t t : len) {
-      blocks += (t + per - 1) / per;
-      slots = std::max(slots, (t + per - 1) / per);
-    }
+  // at most 64 splits: slots are counted in 16 bits, and the merge reads them all
+  for (int32_t ns : {1, 2, 3, 4, 5, 6, 8, 10, 12, 14, 16, 20, 24, 32, 40, 48, 64}) {
+    if (ns > longest) break;
+    const int32_t per = (longest + ns - 1) / ns;
+    int64_t blocks = (int64_t)n_shared * ((ta + per - 1) / per);
+    for (int32_t t : wide) blocks += (t + per - 1) / per;
     blocks *= d.n_kv_heads;
-    const double rounds = std::ceil((double)blocks / shape.at_once);
-    const double us = rounds * (per * (blocks <= 256 ? shape.tile_us : shape.tile2_us) + shape.item_us) + own_us +
-                      (small_rows && ta ? (slots + 1) * slot_us + 4.0 : slots > 1 ? slots * slot_us + 4.0 : 0.0);
+    const double nblocks = d.n_kv_heads * std::max((double)n_narrow, (double)narrow_tiles / per + 0.5 * n_narrow);
+    double us = std::ceil((double)blocks / shape.at_once) *
+                (per * (blocks <= 256 ? shape.tile_us : shape.tile2_us) + shape.item_us);
+    if (n_narrow) {
+      const double rounds = blocks ? nblocks / shape.at_once : std::ceil(nblocks / shape.at_once);
+      us += std::max(rounds * (5.0 + shape.ntile_us * std::min<double>(per, (double)narrow_tiles / n_narrow)), read_us);
+    }
+    const int64_t slots = small_rows ? (ta + per - 1) / per + (own_longest + per - 1) / per : (longest + per - 1) / per;
+    if (slots > 1) us += 3.0 + slots * (0.1 + slot_us);
     if (us < best) {
       best = us;
       *per_out = per;
@@ -451,6 +474,8 @@ std::vector<PrefixTokens> group_tokens(int g, int32_t n, const std::vector<int32
       i += m;
     }
   }
+  // own items that start last should be the short ones: longest first
+  std::stable_sort(out.begin(), out.end(), [](const PrefixTokens& a, const PrefixTokens& b) { return a.end > b.end; });
   out.insert(out.end(), fused.begin(), fused.end());  // ranks of the shared row blocks come first
   return out;
 }
