@@ -343,8 +343,9 @@ fcg_status fcg_rope_destroy(fcg_rope* rope);
  * an input may (stride 0).  Nothing is allocated or uploaded: the call can be
  * captured into a graph, whose replays read pos, q and k anew.
  * Errors: EINVAL (null rope, pos or tensor, dtype, head_dim not 64 or 128 or
- * below rotary_dim, negative counts, flags or strides, overlapping output
- * rows), EHIP. */
+ * below rotary_dim, negative counts, flags or strides, more than 2^30 tokens,
+ * 4096 heads or 65535 layers, overlapping output rows), EHIP.  Runs on the
+ * current device, as the pointers do. */
 #define FCG_ROPE_BACKWARD 1u
 fcg_status fcg_rope_apply(const fcg_rope* rope, int32_t dtype, int32_t head_dim, int32_t n_layers, int32_t n_tok,
                           const int32_t* pos, int32_t n_q_heads, const fcg_tensor* q, const fcg_tensor* q_out,
@@ -402,8 +403,8 @@ fcg_status fcg_append(fcg_cache* cache, int32_t layer, int32_t n_layers, int32_t
  * [n_tok][Hq], contiguous, may be null.  out may be q (the same data and
  * strides).
  * The split partials sit in a workspace of the cache, enlarged when a call
- * needs more.  A call can be captured into a graph if a call at least as large
- * ran before and it has at most 128 tokens, of at most 64 sequences, none with
+ * needs more.  A call can be captured into a graph if it, or one whose partials
+ * take as much, ran before, and it has at most 128 tokens, of at most 64 sequences, none with
  * 96 (fp32: 48) query rows a kv head or more; a workspace that a capture used is
  * kept until the cache is destroyed, and the calls and graphs of one cache share
  * it, so they must not overlap.
@@ -454,13 +455,14 @@ fcg_status fcg_locality_destroy(fcg_locality* loc);
 
 /* Kernel timing (measurement, not part of the method).  While enabled, every
  * call on this cache records HIP events on its stream around its kernels:
- *   FCG_TIME_GRAFT        the graft kernel of fcg_graft
+ *   FCG_TIME_GRAFT        the graft kernel of fcg_graft and fcg_graft_rope
  *   FCG_TIME_PREFILL_ATTN the attention kernel of fcg_patch_prefill
  *   FCG_TIME_PREFILL      all kernels of fcg_patch_prefill (append, attention, merge)
  *   FCG_TIME_DECODE       all kernels of fcg_decode (one per group of 64 sequences)
  *   FCG_TIME_DECODE_ATTN  the attention kernels of fcg_decode (the same kernels: the
  *                         split merge runs inside them)
- * Plan uploads and host work are outside the intervals.  fcg_cache_timing_read
+ * Plan uploads, host work, fcg_append and fcg_prefix_attend are outside the
+ * intervals.  fcg_cache_timing_read
  * waits for the recorded events, returns the number of intervals and their
  * summed duration in milliseconds for one kind (ERANGE for another value),
  * and forgets them.  enable = 0 stops recording (recorded intervals stay

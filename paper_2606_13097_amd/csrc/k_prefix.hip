@@ -2,27 +2,45 @@
 // of several sequences meet each key tile of the prefix together, so the prefix
 // is read once for all of them, and each sequence's rows then meet its own keys.
 //
-// An item (one block per kv head) attends up to 128 query rows (fp32: 64) over
-// prefix positions [a0, a1) and positions [b0, b1) of one sequence, the latter up
-// to each row's own position; what several items leave for a row is merged by
+// An item (one block per kv head) attends up to 128 or 256 query rows (fp32: 64)
+// over prefix positions [a0, a1) and positions [b0, b1) of one sequence, the latter
+// up to each row's own position; what several items leave for a row is merged by
 // prefix_merge_kernel (log-sum-exp).  Rows are sorted by (sequence, position),
 // row = rank * g + query head of the group, whatever their sequences: the
 // prefix part needs no more.
 //
-// Blocks have four waves.  Wide items: wave w owns rows 32 w .. 32 w + 31, and
-// the waves share 64-key tiles (two in LDS, the next one in flight).  Narrow
-// items (at most 16 rows: a decode step's own keys): the waves take 16-key tiles
-// in turn, each through an LDS ring of its own, without barriers, and merge at
-// the end.  In both, S^T = K Q^T and O^T += V^T P^T: lane l holds scores and
-// output of query row l % 16, the probabilities pass from accumulator to operand
-// without leaving their lane, and the online softmax (base 2) exchanges only
-// maxima between the four lanes of a row.  Rows of keys arrive by LDS DMA, whole
-// rows, chunks XOR-swizzled against bank conflicts.
+//   o = sum_j 2^(s_j - m) v_j / sum_j 2^(s_j - m),  s_j = q k_j log2(e) / sqrt(D),
+//
+// in one pass over the keys, m and both sums fp32 (the probabilities enter the
+// product rounded to bf16).  S^T = K Q^T and O^T += V^T P^T: a lane holds scores and
+// outputs of one query row, the probabilities pass from accumulator to operand
+// without leaving their lane, and only maxima and final sums cross lanes.  Rows of
+// keys arrive by LDS DMA, whole rows, chunks XOR-swizzled against bank conflicts.
+//
+// Wide items (more than 32 rows): wave w owns rows 32 w .. 32 w + 31 on 32x32x16
+// products, two lanes a row, and the waves share 64-key tiles.  Blocks of four waves
+// hold two tiles and run two to a compute unit; blocks of eight hold four tiles, and
+// their halves run half a tile apart, one multiplying while the other takes the
+// softmax.  On 32x32 products, because a wave's vector instructions beside another
+// wave's products took 7.1 cycles each there and 9.1 beside 16x16 ones.
+// Narrow items (a decode step's own keys): the waves take 16-key tiles in turn
+// (16x16 products, four lanes a row), each through an LDS ring of its own, without
+// barriers, and merge at the end.
+//
+// What bounds it (bf16, D 128, 8 key heads; times per call, one after the other):
+//   32 sequences of 64 tokens, 4 query heads a key head, over 6007 shared keys and up
+//   to 300 own ones: 204 us for 207 GFLOP, 1.01 PFLOP/s, where an 8192^3 library
+//   product reaches 1.18.  A tile takes 3170 cycles of its compute unit, 2048 of them
+//   matrix cycles; the rest is the softmax that finds no gap between the products.
+//   32 sequences of 4 tokens, 8 query heads, over 22011: 119 us for 94 GFLOP.  Four
+//   row blocks of a head cut in 8 splits each are one round of 256 items; their first
+//   tiles, the partials and the merge (7 us) are what is added to the product rate.
+//   64 sequences of one token, 4 query heads, over 4321: 23.6 us for 57 MB.  Round
+//   trips: page entries, first tiles, partials, merge (4 us).
 //
 // Tiles start on multiples of their length in position, so the 16 keys that one
-// wave brings in lie on one page, whose entry is one scalar load.  Keys of a tile
-// outside the range re-read a key inside it and are masked; a position that is not
-// attended is never read.
+// wave brings in lie on one page.  Keys of a tile outside the range re-read a key
+// inside it and are masked; a position that is not attended is never read.
 #include <type_traits>
 
 #include "fcg_device.hpp"
@@ -659,9 +677,7 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
       // Whole tiles of the prefix, up to the last few: the loop that long prefixes spend
       // their time in, with no mask and the least scalar work.
       const int whole = ka.lo % kPfxTile ? 0 : ka.hi / kPfxTile - ta0;
-      if (ti + 3 < whole) {
-        if (bad) restore(0);
-        bad = false;
+      if (ti + 3 < whole) {  // (tile 0 is whole too: nothing of it was cleaned)
         const bf16_t* pool = late ? head.v : head.k;
         const bf16_t* lib = late ? head.lib : head.k;
         const bf16_t* row = PAGED ? nullptr : pool + ka.seq * head.step + (int64_t)(ta0 * kPfxTile + 16 * grp) * D;
@@ -1175,7 +1191,9 @@ int launch_prefix_attend(int dtype, const PrefixCall& call, const PrefixArgs* ar
 #define PA(...) hipLaunchKernelGGL((__VA_ARGS__)
 #define PB(DD, PG)                                                                                                  \
   {                                                                                                                 \
-    if (waves == 8) PA(prefix_attend_kernel<DD, PG, 8, false>), grid, dim3(512), 0, s, call, lst, cv);              \
+    if (waves == 8 && args)                                                                                         \
+      PA(prefix_attend_kernel<DD, PG, 8, true>), grid, dim3(512), 0, s, call, Plan<true>{*args}, cv);               \
+    else if (waves == 8) PA(prefix_attend_kernel<DD, PG, 8, false>), grid, dim3(512), 0, s, call, lst, cv);         \
     else if (args) PA(prefix_attend_kernel<DD, PG, 4, true>), grid, dim3(256), 0, s, call, Plan<true>{*args}, cv);  \
     else PA(prefix_attend_kernel<DD, PG, 4, false>), grid, dim3(256), 0, s, call, lst, cv);                         \
   }

@@ -383,7 +383,7 @@ struct PrefixArgs {
   PrefixSmall rank[kPfxRanks];
 };
 // args null: the plan in device memory (items, ranks); else by value.  waves: 4, or 8
-// (bf16, plans in memory).
+// (bf16).
 int launch_prefix_attend(int dtype, const PrefixCall& call, const PrefixArgs* args, const PrefixItem* items,
                          const PrefixRank* ranks, int n_items, int waves, const CacheView& cv, hipStream_t s);
 int launch_prefix_merge(int dtype, const PrefixCall& call, const PrefixArgs* args, const PrefixRank* ranks, int n_rank,

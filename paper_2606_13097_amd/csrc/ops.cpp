@@ -176,6 +176,7 @@ fcg_status fcg_rope_apply(const fcg_rope* rope, int32_t dtype, int32_t head_dim,
   if (rope->rot > head_dim) return fail(FCG_EINVAL, "rotary_dim exceeds head_dim");
   if (n_layers < 0 || n_layers > 65535 || n_tok < 0 || n_q_heads < 0 || n_k_heads < 0)
     return fail(FCG_EINVAL, "a count is negative, or more than 65535 layers");
+  if (n_tok > 1 << 30) return fail(FCG_EINVAL, "more than 2^30 tokens");
   if (n_q_heads > 4096 || n_k_heads > 4096) return fail(FCG_EINVAL, "more than 4096 heads");
   if (flags & ~FCG_ROPE_BACKWARD) return fail(FCG_EINVAL, "unknown flags");
   const bool has_q = q && n_q_heads, has_k = k && n_k_heads;
@@ -518,7 +519,7 @@ void plan_prefix(const fcg_model_desc& d, int32_t P, int32_t n, const int32_t* s
   const int n_pre = (small_rows + block - 1) / block * pre_slots;
   p->slots = pre_slots;
   auto own_splits = [&](const PrefixTokens& x) { return (int)((tiles_of(P, x.end) + per - 1) / per); };
-  p->by_value = p->waves == 4 && n_small == (int)toks.size() && n_small <= kPfxGroups && n <= kPfxRanks;
+  p->by_value = n_small == (int)toks.size() && n_small <= kPfxGroups && n <= kPfxRanks;
   if (p->by_value) {
     PrefixArgs& a = p->args;
     a.n_pre = n_pre;

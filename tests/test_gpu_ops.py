@@ -381,14 +381,14 @@ ATTN = [("bf16", 4, 1, 128), ("bf16", 8, 8, 64), ("bf16", 16, 1, 64), ("bf16", 1
         ("f32", 4, 2, 64), ("f32", 8, 1, 128), ("f32", 16, 1, 64), ("f32", 2, 2, 128)]
 
 
-def run_shared(sh, seq, pos, seed, strided=False):
+def run_shared(sh, seq, pos, seed, strided=False, scale=1.0):
     d, n = sh.cache.desc, len(seq)
     if strided:
         buf = randn(gen(seed), n, d.n_q_heads + 3, d.head_dim, dtype=sh.dtype)
         q = buf[:, 1:1 + d.n_q_heads]
         out = torch.full((n, 2 * d.n_q_heads, d.head_dim), float("nan"), dtype=DT[sh.dtype], device="cuda")[:, ::2]
     else:
-        q = randn(gen(seed), n, d.n_q_heads, d.head_dim, dtype=sh.dtype)
+        q = randn(gen(seed), n, d.n_q_heads, d.head_dim, dtype=sh.dtype) * scale
         out = torch.full_like(q, float("nan"))
     lse = torch.full((n, d.n_q_heads), float("nan"), device="cuda")
     fcg.fcg_prefix_attend(sh.cache, 1, sh.pseq if sh.P else -1, sh.P, seq, pos, q, out, lse)
@@ -647,6 +647,36 @@ def test_append_and_attend_replay_in_graphs():
     sh.cache.close()
 
 
+def test_prefix_attend_of_128_tokens_replays_in_a_graph():
+    """The largest call that can be captured, over a prefix long enough for blocks of 256 rows."""
+    P, own = 7001, [4 + 2 * i for i in range(32)]
+    sh = Shared("bf16", 64, 8, 128, 16, P, own, 17, shuffle=False)
+    seq = np.repeat(np.arange(32), 4)
+    pos = np.concatenate([P + n - 4 + np.arange(4) for n in own])
+    q = randn(gen(1), 128, 64, 128)
+    out, lse = torch.empty_like(q), torch.empty((128, 64), device="cuda")
+
+    def call():
+        fcg.fcg_prefix_attend(sh.cache, 1, sh.pseq, P, seq, pos, q, out, lse)
+
+    call()
+    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=s):
+        call()
+    for r in range(3):
+        q.copy_(randn(gen(50 + r), 128, 64, 128))
+        out.fill_(float("nan")), lse.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(bits(out), bits(got[0])) and torch.equal(lse, got[1])
+    sh.check(seq, pos, q, got[0], got[1], "replay", [0, 3, 65, 127])
+    sh.cache.close()
+
+
 def test_captures_that_need_an_upload_are_refused():
     sh = Shared("bf16", 8, 2, 64, 16, 100, [40] * 70, 5)
     c = sh.cache
@@ -706,6 +736,93 @@ def test_prefix_attend_blocks_of_many_rows(page, hq, hkv, d):
     some = np.unique(np.r_[np.arange(0, len(seq), 23), np.flatnonzero(seq == 4), np.cumsum(n) - 1])
     sh.check(seq, pos, q, out, lse, "blocks", some)
     sh.cache.close()
+
+
+MANY = [128, 128, 77, 130, 128, 3]          # tokens of a sequence: blocks of 256 rows full and shared
+
+
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (32, 8, 64), (16, 8, 64)])
+def test_prefix_attend_blocks_of_256_rows(page, hq, hkv, d):
+    """Calls large enough for blocks of 256 rows: fused and shared ones, tiles that hold the end of the prefix and the
+    first own keys; also with scores so far apart that a few keys, in any tile, make the result."""
+    P, own = 5003, [300, 128, 129, 200, 140, 90]
+    sh = Shared("bf16", hq, hkv, d, page, P, own, 41, shuffle=False)
+    seq = np.repeat(np.arange(6), MANY)
+    pos = np.concatenate([P + own[s] - MANY[s] + np.arange(MANY[s]) for s in range(6)])
+    some = np.unique(np.r_[np.arange(0, len(seq), 19), np.flatnonzero(seq == 5), np.cumsum(MANY) - 1])
+    for scale in (1.0, 8.0):
+        q, out, lse = run_shared(sh, seq, pos, 7, scale=scale)
+        sh.check(seq, pos, q, out, lse, f"blocks, queries times {scale}", some)
+    # values and keys of one sequence that are not finite reach exactly the rows that see them
+    k, v = sh.kv[1]
+    v[60, 0, 5], v[60, 1, 7], k[100, 2, 3] = float("inf"), float("nan"), float("nan")
+    sh.put(1, np.arange(P, P + own[1]), k, v)
+    q, out, lse = run_shared(sh, seq, pos, 8)
+    v[60, 0, 5] = v[60, 1, 7] = k[100, 2, 3] = 0.0
+    g, o = hq // hkv, out.view(len(seq), hkv, hq // hkv, d)
+    at = np.flatnonzero(seq == 1)
+    sees = torch.as_tensor(at[pos[at] >= P + 60], device="cuda")
+    keys = torch.as_tensor(at[pos[at] >= P + 100], device="cuda")
+    assert torch.isposinf(o[sees, 0, :, 5]).all() and torch.isnan(o[sees, 1, :, 7]).all() and torch.isnan(o[keys, 2]).all()
+    assert torch.isnan(lse.view(len(seq), hkv, g)[keys, 2]).all()
+    rest = torch.ones_like(o, dtype=torch.bool)
+    rest[sees, 0, :, 5] = rest[sees, 1, :, 7] = rest[keys, 2] = False
+    assert torch.isfinite(o[rest]).all()
+    look = np.unique(np.r_[some[seq[some] != 1], at[::9][pos[at[::9]] < P + 100]])
+    out2 = torch.zeros_like(o)
+    out2[rest] = o[rest]
+    for s in np.unique(seq[look]):
+        t = look[seq[look] == s]
+        K, V = sh.joined(int(s))
+        ref = list(attend64(q[t], K, V, pos[t], P))
+        ref[0] = ref[0] * rest[t].view(len(t), hq, d)
+        check_attend(out2[t].view(len(t), hq, d), lse[t], ref, "bf16", len(K), d, f"around them, sequence {s}")
+    sh.cache.close()
+
+
+def test_prefix_attend_one_item_a_row():
+    """As many row blocks as fill the chip: no split, results written without a merge, in the queries' place too."""
+    P, n = 4099, 32
+    sh = Shared("bf16", 32, 8, 128, 16, P, [64 + i for i in range(n)], 43, shuffle=False)
+    seq = np.repeat(np.arange(n), 64)
+    pos = np.concatenate([P + i + np.arange(64) for i in range(n)])
+    some = np.unique(np.r_[np.arange(0, len(seq), 97), len(seq) - 1])
+    for scale in (1.0, 8.0):
+        q, out, lse = run_shared(sh, seq, pos, 3, scale=scale)
+        sh.check(seq, pos, q, out, lse, f"direct, queries times {scale}", some)
+        fcg.fcg_prefix_attend(sh.cache, 1, sh.pseq, P, seq, pos, q, q)
+        torch.cuda.synchronize()
+        assert torch.equal(bits(q), bits(out))
+    sh.cache.close()
+
+
+def test_prefix_attend_blocks_of_256_rows_read_values_in_the_library():
+    """The same over a prefix of two grafted segments whose values stay in the library, but for the page they share."""
+    lens, hq, hkv, d = [2503, 2500], 32, 8, 128
+    P = sum(lens)
+    desc = fcg.model_desc(1, hq, hkv, d, 1e4, "bf16")
+    lib = fcg.Library(desc, P, 2)
+    k, v = randn(gen(0), P, hkv, d), randn(gen(1), P, hkv, d)
+    for p0, n in ((0, lens[0]), (lens[0], lens[1])):        # at their own positions: keys as they are
+        fcg.fcg_lib_add_segment(lib, n, p0, k[None, p0:p0 + n].contiguous(), v[None, p0:p0 + n].contiguous())
+    c = fcg.Cache(desc, 7, P + 140, 16, 7 * (P + 140) // 16, flags=fcg.FCG_ALIAS_V)
+    fcg.fcg_graft(c, lib, [6, 6], [1, 0], [lens[0], 0])
+    alias = fcg.fcg_cache_export_v_alias(c, 6)[:P // 16]
+    assert (alias >= 0).sum() == P // 16 - 1
+    seq = np.repeat(np.arange(6), MANY)
+    pos = np.concatenate([P + np.arange(n) for n in MANY])
+    ok, ov = torch.zeros((len(seq), hkv, d), dtype=torch.bfloat16, device="cuda"), randn(gen(3), len(seq), hkv, d)
+    fcg.fcg_append(c, 0, seq, pos, ok, ov)
+    q = randn(gen(4), len(seq), hq, d) * 8.0
+    out = torch.full_like(q, float("nan"))
+    fcg.fcg_prefix_attend(c, 0, 6, P, seq, pos, q, out)
+    torch.cuda.synchronize()
+    for t in range(0, len(seq), 17):
+        own = torch.as_tensor(np.flatnonzero(seq == seq[t]), device="cuda")
+        K, V = torch.cat([k, ok[own]]), torch.cat([v, ov[own]])
+        check_attend(out[t:t + 1], None, attend64(q[t:t + 1], K, V, pos[t:t + 1], P), "bf16", len(K), d, f"token {t}")
+    c.close(), lib.close()
 
 
 def test_offsets_past_32_bits():
