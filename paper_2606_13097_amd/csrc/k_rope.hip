@@ -5,20 +5,25 @@
 // for the pairs (i, i + R/2) or (2i, 2i + 1) of the first R dimensions of a
 // head; the others are copied.  The backward pass negates the angle.
 //
-// A block owns up to 16 tokens at consecutive indices (and, appending, at
-// consecutive positions of one sequence) of one layer.  The (cos, sin) of its
-// tokens' pairs are computed once into LDS while the first rows' loads are in
-// flight, and shared by all heads.  A lane moves two 16-byte vectors of a row,
-// chosen so that every form turns registers only and that neighbouring lanes
-// move neighbouring vectors: for halves, vectors c and c + R / 2 / VEC hold both
-// ends of VEC pairs; for neighbours each vector holds whole pairs, and a lane
-// takes vectors c and c + D / 2 / VEC; what passes unturned is cut in halves
-// likewise.  (With 2c and 2c + 1 each access covered every other 16 bytes.)
-// Caller rows start at any element (unaligned 16-byte accesses); cache rows are
-// aligned.
+// A block moves one pass of rows (kRopePass pairs of vectors, a pair for each
+// lane) of up to 16 tokens at consecutive indices (and, appending, at consecutive
+// positions of one sequence), of one layer or of every gridDim.z-th.  The (cos,
+// sin) of its tokens' pairs are computed once into LDS while the first rows' loads
+// are in flight, and shared by heads and layers; with several layers, the next
+// one's rows are requested before the last one's are turned and stored.  A lane
+// moves two 16-byte vectors of a row, chosen so that every form turns registers
+// only and that neighbouring lanes move neighbouring vectors: for halves, vectors
+// c and c + R / 2 / VEC hold both ends of VEC pairs; for neighbours each vector
+// holds whole pairs, and a lane takes vectors c and c + D / 2 / VEC; what passes
+// unturned is cut in halves likewise.  (With 2c and 2c + 1 each access covered
+// every other 16 bytes.)  Caller rows start at any element (unaligned 16-byte
+// accesses); cache rows are aligned.
 //
-// What bounds it: many tokens, HBM; few, the chain of argument fetch, position,
-// rows and stores.
+// What bounds it: many tokens, the memory (bf16, D 128: keys of 32 layers of 713
+// tokens of 8 heads, 93 MB read and written, 15.4 us, a copy of as many bytes 13.6;
+// keys, values and queries of 8 layers of 11K tokens into pages, 2.2 GB, 416 us, 5.3
+// TB/s, a copy 5.2); few, the chain of argument fetch, position, rows and stores (3 us
+// for one token).
 #include "fcg_device.hpp"
 #include "kernels.hpp"
 
@@ -76,11 +81,9 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(Where<MODE> where, RopeR
                                                         RopeArgs ra, const float2* __restrict__ tab) {
   constexpr int VEC = Store<T>::VEC;
   constexpr int NCH = D / (2 * VEC);  // vector pairs of a row
-  constexpr int U = kRopePass / 256;  // vector pairs of a lane in flight
   __shared__ __align__(16) float2 s_cs[kAppMaxTb * kRopePairs];
 
   const int t = threadIdx.x;
-  const int layer = blockIdx.z;
   AppendGroup g;
   if constexpr (MODE == kApply) {
     g.tok0 = blockIdx.x * rows.tb;
@@ -94,6 +97,7 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(Where<MODE> where, RopeR
   const int H = rows.Hq + rows.Hk + rows.Hv;
   const int r0 = blockIdx.y * rows.slice_rows;
   const int nrow = min(rows.slice_rows, g.n * H - r0);  // rows of this block, token-major
+  if (nrow <= 0) return;  // (block-uniform) a slice past a short group's rows
   const int total = nrow * NCH;
   auto tl_of = [&](int r) __attribute__((always_inline)) {  // r / H
     return H == 1 ? r : (int)__umulhi((unsigned)r, rows.h_magic);
@@ -102,7 +106,7 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(Where<MODE> where, RopeR
   const int rchunks = half / VEC;  // vector pairs that turn
 
   if constexpr (MODE != kApply && PAGED) {
-    if (g.enter && blockIdx.y == 0 && layer == 0 && t == 0) {
+    if (g.enter && blockIdx.y == 0 && blockIdx.z == 0 && t == 0) {
       int32_t* row = const_cast<int32_t*>(cv.page_table) + (int64_t)g.seq * 2 * cv.n_lp + (g.pos0 >> 4);
       row[0] = g.page_a;
       row[cv.n_lp] = -1;
@@ -113,123 +117,114 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(Where<MODE> where, RopeR
     }
   }
 
-  struct Item {
-    int tl, kind, head, c;  // token of the group, 0 q / 1 k / 2 v, head, vector pair
+  // This lane's vectors: vector pair c of a row (token tl of the group, q, k or v,
+  // head); lanes past the rows repeat the last one and store nothing.
+  const bool mine = t < total;
+  const int i = min(t, total - 1), c = i % NCH, r = r0 + i / NCH;
+  const int tl = tl_of(r), hh = r - tl * H;
+  const int kind = hh < rows.Hq ? 0 : hh < rows.Hq + rows.Hk ? 1 : 2;
+  const int head = hh - (kind == 0 ? 0 : kind == 1 ? rows.Hq : rows.Hq + rows.Hk);
+  const bool turn = kind != 2 && c < (PAIRS ? 2 * rchunks : rchunks);  // the first vector, for halves both
+  // element offsets of the two vectors in the row
+  const int lo = (!PAIRS && kind != 2 && c >= rchunks ? rchunks + c : c) * VEC;
+  const int hi = (!PAIRS && kind != 2 && c < rchunks ? rchunks + c : NCH + c) * VEC;
+  auto row_of = [&](const RowView& v) __attribute__((always_inline)) {  // of layer 0
+    return reinterpret_cast<const T*>(v.p) + (int64_t)(g.tok0 + tl) * v.token + (int64_t)head * v.head;
   };
-  auto item_of = [&](int i) __attribute__((always_inline)) -> Item {
-    Item x;
-    x.c = i % NCH;
-    const int r = r0 + i / NCH;
-    x.tl = tl_of(r);
-    const int h = r - x.tl * H;
-    x.kind = h < rows.Hq ? 0 : h < rows.Hq + rows.Hk ? 1 : 2;
-    x.head = h - (x.kind == 0 ? 0 : x.kind == 1 ? rows.Hq : rows.Hq + rows.Hk);
-    return x;
+  const T* src = row_of(kind == 0 ? rows.q : kind == 1 ? rows.k : rows.v);
+  const int64_t src_layer = kind == 0 ? rows.q.layer : kind == 1 ? rows.k.layer : rows.v.layer;
+  const bool to_cache = MODE != kApply && kind != 0;
+  T* dst;
+  int64_t dst_layer;
+  if (!to_cache) {
+    dst = const_cast<T*>(row_of(kind == 0 ? rows.q_out : rows.k_out));
+    dst_layer = kind == 0 ? rows.q_out.layer : rows.k_out.layer;
+  } else {
+    const int pos = g.pos0 + tl;
+    int64_t off = (int64_t)layer0 * cv.layer_stride;
+    if (PAGED) {
+      const int page = (pos >> 4) == (g.pos0 >> 4) ? g.page_a : g.page_b;
+      off += (((int64_t)page * cv.n_kv_heads + head) * 16 + (pos & 15)) * D;
+    } else {
+      off += (((int64_t)g.seq * cv.n_kv_heads + head) * cv.max_tokens + pos) * D;
+    }
+    dst = reinterpret_cast<T*>(kind == 1 ? cv.k : cv.v) + off;
+    dst_layer = cv.layer_stride;
+  }
+  uint4 a, b;
+  auto load = [&](int layer) __attribute__((always_inline)) {
+    const T* p = src + layer * src_layer;
+    a = ld16_any(p + lo);
+    b = ld16_any(p + hi);
   };
-  // element offsets of the lane's two vectors in the row
-  const bool halves = !PAIRS;
-  auto lo_of = [&](const Item& x) __attribute__((always_inline)) {
-    return (halves && x.kind != 2 && x.c >= rchunks ? rchunks + x.c : x.c) * VEC;
-  };
-  auto hi_of = [&](const Item& x) __attribute__((always_inline)) {
-    return (halves && x.kind != 2 && x.c < rchunks ? rchunks + x.c : NCH + x.c) * VEC;
-  };
-  auto row_of = [&](const RowView& v, const Item& x) __attribute__((always_inline)) {
-    return reinterpret_cast<const T*>(v.p) + (int64_t)layer * v.layer + (int64_t)(g.tok0 + x.tl) * v.token +
-           (int64_t)x.head * v.head;
-  };
+  load(blockIdx.z);
 
-  for (int i0 = t; i0 - t < total; i0 += 256 * U) {
-    uint4 a[U], b[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + 256 * u;
-      if (i < total) {
-        const Item x = item_of(i);
-        const T* src = row_of(x.kind == 0 ? rows.q : x.kind == 1 ? rows.k : rows.v, x);
-        a[u] = ld16_any(src + lo_of(x));
-        b[u] = ld16_any(src + hi_of(x));
-      }
+  // the (cos, sin) of the rows' tokens
+  const int n_cs = (tl_of(r0 + nrow - 1) - tl0 + 1) * half;
+  for (int j = t; j < n_cs; j += 256) {
+    const int tj = tl0 + j / half, pr = j % half;
+    float cs, sn;
+    if (MODE != kApply && tab) {
+      const float2 e = tab[(int64_t)(g.pos0 + tj) * half + pr];
+      cs = e.x;
+      sn = e.y;
+    } else {
+      int pos;
+      if constexpr (MODE == kApply) pos = where.pos[g.tok0 + tj];
+      else pos = g.pos0 + tj;
+      rope_cs_turns((double)pos, ra.turns[pr], &cs, &sn);
+      cs *= ra.m;
+      sn *= ra.m * rows.sign;
     }
-    if (i0 == t) {  // (block-uniform) the (cos, sin) of the rows' tokens, behind the first loads
-      const int n_cs = (tl_of(r0 + nrow - 1) - tl0 + 1) * half;
-      for (int i = t; i < n_cs; i += 256) {
-        const int tl = tl0 + i / half, pr = i % half;
-        float c, s;
-        if (MODE != kApply && tab) {
-          const float2 cs = tab[(int64_t)(g.pos0 + tl) * half + pr];
-          c = cs.x;
-          s = cs.y;
-        } else {
-          int pos;
-          if constexpr (MODE == kApply) pos = where.pos[g.tok0 + tl];
-          else pos = g.pos0 + tl;
-          rope_cs_turns((double)pos, ra.turns[pr], &c, &s);
-          c *= ra.m;
-          s *= ra.m * rows.sign;
+    s_cs[j] = make_float2(cs, sn);
+  }
+  __syncthreads();
+
+  const float2* cs = s_cs + (tl - tl0) * half + c * (PAIRS ? VEC / 2 : VEC);  // of the lane's first pair
+  for (int layer = blockIdx.z; layer < rows.n_layers; layer += gridDim.z) {
+    uint4 ya = a, yb = b;
+    if (layer + (int)gridDim.z < rows.n_layers) load(layer + gridDim.z);
+    if (turn) {
+      float xa[VEC], xb[VEC], za[VEC], zb[VEC];
+      Store<T>::unpack(ya, xa);
+      Store<T>::unpack(yb, xb);
+      if constexpr (PAIRS) {
+        constexpr int P = VEC / 2;  // pairs of a vector
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+          za[2 * e] = fmaf(xa[2 * e], cs[e].x, -xa[2 * e + 1] * cs[e].y);
+          za[2 * e + 1] = fmaf(xa[2 * e + 1], cs[e].x, xa[2 * e] * cs[e].y);
         }
-        s_cs[i] = make_float2(c, s);
-      }
-      __syncthreads();
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + 256 * u;
-      if (i >= total) continue;
-      const Item x = item_of(i);
-      uint4 ya = a[u], yb = b[u];
-      if (PAIRS ? x.kind != 2 && x.c < 2 * rchunks : x.kind != 2 && x.c < rchunks) {
-        float xa[VEC], xb[VEC], za[VEC], zb[VEC];
-        Store<T>::unpack(ya, xa);
-        Store<T>::unpack(yb, xb);
-        if constexpr (PAIRS) {
-          constexpr int P = VEC / 2;  // pairs of a vector
-          const float2* cs = s_cs + (x.tl - tl0) * half + x.c * P;
+        ya = Store<T>::pack(za);
+        if (NCH + c < 2 * rchunks) {
 #pragma unroll
           for (int e = 0; e < P; ++e) {
-            za[2 * e] = fmaf(xa[2 * e], cs[e].x, -xa[2 * e + 1] * cs[e].y);
-            za[2 * e + 1] = fmaf(xa[2 * e + 1], cs[e].x, xa[2 * e] * cs[e].y);
+            const float2 c2 = cs[NCH * P + e];
+            zb[2 * e] = fmaf(xb[2 * e], c2.x, -xb[2 * e + 1] * c2.y);
+            zb[2 * e + 1] = fmaf(xb[2 * e + 1], c2.x, xb[2 * e] * c2.y);
           }
-          ya = Store<T>::pack(za);
-          if (NCH + x.c < 2 * rchunks) {
-#pragma unroll
-            for (int e = 0; e < P; ++e) {
-              const float2 c2 = cs[NCH * P + e];
-              zb[2 * e] = fmaf(xb[2 * e], c2.x, -xb[2 * e + 1] * c2.y);
-              zb[2 * e + 1] = fmaf(xb[2 * e + 1], c2.x, xb[2 * e] * c2.y);
-            }
-            yb = Store<T>::pack(zb);
-          }
-        } else {
-          const float2* cs = s_cs + (x.tl - tl0) * half + x.c * VEC;
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            za[e] = fmaf(xa[e], cs[e].x, -xb[e] * cs[e].y);
-            zb[e] = fmaf(xb[e], cs[e].x, xa[e] * cs[e].y);
-          }
-          ya = Store<T>::pack(za);
           yb = Store<T>::pack(zb);
         }
-      }
-      if (MODE == kApply || x.kind == 0) {
-        T* dst = const_cast<T*>(row_of(x.kind == 0 ? rows.q_out : rows.k_out, x));
-        st16_any(dst + lo_of(x), ya);
-        st16_any(dst + hi_of(x), yb);
       } else {
-        const int pos = g.pos0 + x.tl;
-        int64_t off = (int64_t)(layer0 + layer) * cv.layer_stride;
-        if (PAGED) {
-          const int page = (pos >> 4) == (g.pos0 >> 4) ? g.page_a : g.page_b;
-          off += (((int64_t)page * cv.n_kv_heads + x.head) * 16 + (pos & 15)) * D;
-        } else {
-          off += (((int64_t)g.seq * cv.n_kv_heads + x.head) * cv.max_tokens + pos) * D;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          za[e] = fmaf(xa[e], cs[e].x, -xb[e] * cs[e].y);
+          zb[e] = fmaf(xb[e], cs[e].x, xa[e] * cs[e].y);
         }
-        T* dst = reinterpret_cast<T*>(x.kind == 1 ? cv.k : cv.v) + off;
-        // past this L2: whoever reads the rows next runs on any XCD (8 layers of 11K tokens
-        // into pages 447 -> 432 us, 32 layers of 129 into a contiguous cache 21.0 -> 20.3)
-        st16_nt(dst + lo_of(x), ya);
-        st16_nt(dst + hi_of(x), yb);
+        ya = Store<T>::pack(za);
+        yb = Store<T>::pack(zb);
       }
+    }
+    if (!mine) continue;
+    T* p = dst + layer * dst_layer;
+    if (!to_cache) {
+      st16_any(p + lo, ya);
+      st16_any(p + hi, yb);
+    } else {
+      // past this L2: whoever reads the rows next runs on any XCD (8 layers of 11K tokens
+      // into pages 447 -> 432 us, 32 layers of 129 into a contiguous cache 21.0 -> 20.3)
+      st16_nt(p + lo, ya);
+      st16_nt(p + hi, yb);
     }
   }
 }
@@ -257,7 +252,7 @@ int launch_rope_apply(int dtype, int D, bool pairs, const RopeRows& rows, const 
                       hipStream_t s) {
   const int H = rows.Hq + rows.Hk;
   const dim3 grid((rows.n_tok + rows.tb - 1) / rows.tb, (rows.tb * H + rows.slice_rows - 1) / rows.slice_rows,
-                  rows.n_layers);
+                  rows.grid_layers);
   launch_rows<kApply, false>(dtype, D, pairs, grid, Where<kApply>{pos}, rows, CacheView{}, 0, ra, nullptr, s);
   return check(hipGetLastError());
 }
@@ -266,7 +261,7 @@ int launch_append(int dtype, bool pairs, const RopeRows& rows, const AppendArgs&
                   const AppendGroup* groups, int n_groups, const CacheView& cv, int layer0, const RopeArgs& ra,
                   const float2* tab, hipStream_t s) {
   const int H = rows.Hq + rows.Hk + rows.Hv;
-  const dim3 grid(n_groups, (rows.tb * H + rows.slice_rows - 1) / rows.slice_rows, rows.n_layers);
+  const dim3 grid(n_groups, (rows.tb * H + rows.slice_rows - 1) / rows.slice_rows, rows.grid_layers);
 #define AP(PG)                                                                                                     \
   {                                                                                                                \
     if (groups)                                                                                                    \

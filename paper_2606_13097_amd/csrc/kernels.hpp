@@ -306,8 +306,8 @@ struct AppendRun {
   int32_t page0;  // its first entry of page[]; bit 31: enter the pages into the device page table
 };
 constexpr int kAppRuns = 64, kAppPages = 384, kAppMaxTb = 16;
-// Pairs of vectors a block moves in a pass (two per lane; with four, 2-5% slower).
-constexpr int kRopePass = 512;
+// Pairs of vectors a block moves, of each of its layers: one per lane (two: 2 to 12% slower).
+constexpr int kRopePass = 256;
 struct AppendArgs {
   AppendRun run[kAppRuns];
   int32_t page[kAppPages];
@@ -317,7 +317,7 @@ struct RopeRows {
   int32_t Hq, Hk, Hv;             // rows per token of each kind
   int32_t n_tok, tb;              // tokens, tokens of a block
   int32_t slice_rows;             // rows of a block (grid y cuts the rows of its tokens)
-  int32_t n_layers;
+  int32_t n_layers, grid_layers;  // layers, layers at once (a block takes every grid_layers-th)
   uint32_t h_magic;               // ceil(2^32 / rows of a token): r / rows = r * h_magic >> 32 for the rows of a block
   float sign;                     // of the angles
 };

@@ -58,6 +58,45 @@ def test_rope_apply_all_forms(dtype, pairs, d, rot):
                     check_turned(y, turn64(x, pos, w, pairs, m, sign), x, w, pairs, m, dtype, f"{name} {kind} {sign}")
 
 
+@pytest.mark.parametrize("dtype,layers", [("bf16", 11), ("f32", 11), ("bf16", 23)])
+def test_rope_apply_of_many_layers_in_place(dtype, layers):
+    """Blocks that take several layers, not all as many; every layer from other rows, input and output the same."""
+    n, hq, hk, d = 700, 8, 4, 128
+    rope, w = make_rope(96, True, m=1.5)
+    pos = np.random.default_rng(layers).integers(0, 30000, n)
+    x = randn(gen(layers), layers, n, hq + hk + 1, d, dtype=dtype)
+    was = x.clone()
+    fcg.fcg_rope_apply(rope, torch.as_tensor(pos, dtype=torch.int32, device="cuda"), x[:, :, :hq], x[:, :, :hq],
+                       x[:, :, hq:hq + hk], x[:, :, hq:hq + hk])
+    torch.cuda.synchronize()
+    ref = turn64(was[:, :, :hq + hk], pos, w, True, 1.5)
+    check_turned(x[:, :, :hq + hk], ref, was[:, :, :hq + hk], w, True, 1.5, dtype, "in place")
+    assert torch.equal(bits(x[:, :, hq + hk:].contiguous()), bits(was[:, :, hq + hk:].contiguous()))
+
+
+@pytest.mark.parametrize("page", [0, 16])
+def test_append_of_many_layers(page):
+    """The same appending: pages, caches and q_out of every layer."""
+    L, n, hq, hkv, d = 13, 300, 16, 4, 128
+    rope, w = make_rope(64)
+    c = fcg.Cache(fcg.model_desc(L + 2, hq, hkv, d, 1e4, "bf16"), 2, 400, page, 60 if page else 0)
+    mem = fill_memory(c, "bf16", 7.0)
+    seq, pos = np.r_[np.zeros(200, int), np.ones(100, int)], np.r_[np.arange(3, 203), np.arange(50, 150)]
+    q, k, v = randn(gen(1), L, n, hq, d), randn(gen(2), L, n, hkv, d), randn(gen(3), L, n, hkv, d)
+    qo = torch.empty_like(q)
+    fcg.fcg_append(c, 1, seq, pos, k, v, rope=rope, q=q, q_out=qo, n_layers=L)
+    torch.cuda.synchronize()
+    check_turned(qo, turn64(q, pos, w, False), q, w, False, 1.0, "bf16", "q")
+    for s in (0, 1):
+        i = torch.as_tensor(np.flatnonzero(seq == s), device="cuda")
+        K, V = (torch.stack([rows_of(c, m, l, s, pos[seq == s]) for l in range(1, L + 1)]) for m in mem)
+        check_turned(K, turn64(k[:, i], pos[seq == s], w, False), k[:, i], w, False, 1.0, "bf16", f"keys of {s}")
+        assert torch.equal(bits(V.contiguous()), bits(v[:, i].contiguous()))
+    for m in mem:
+        assert bool((m[0] == 7.0).all()) and bool((m[L + 1] == 7.0).all())
+    c.close()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("offset", [0, 1, 3])
 def test_rope_apply_takes_slices_any_start_and_in_place(dtype, offset):
