@@ -59,6 +59,17 @@ bool Planner::any_in_range(int32_t seq, int32_t layer, int32_t a, int32_t b) con
   return false;
 }
 
+bool Planner::all_in_range(int32_t seq, int32_t layer, int32_t a, int32_t b) const {
+  const uint64_t* w = bits(seq, layer);
+  for (int32_t p = a; p < b;) {
+    const int32_t lo = p & 63, hi = std::min(64, lo + (b - p));
+    const uint64_t mask = (hi == 64 ? ~0ull : ((1ull << hi) - 1)) & ~((1ull << lo) - 1);
+    if ((w[p >> 6] & mask) != mask) return false;
+    p += hi - lo;
+  }
+  return true;
+}
+
 int32_t Planner::count_below(int32_t seq, int32_t layer, int32_t b) const {
   const uint64_t* w = bits(seq, layer);
   int32_t c = 0, full = b >> 6;
@@ -214,7 +225,7 @@ fcg_status Planner::check_attend(int32_t layer, int32_t prefix_seq, int32_t pref
     if (seq[t] < 0 || seq[t] >= S_) { *msg = fmt("sequence %lld out of range", seq[t]); return FCG_ERANGE; }
     if (pos[t] < prefix_len - 1 || pos[t] >= T_) { *msg = fmt("position %lld out of range", pos[t]); return FCG_ERANGE; }
   }
-  if (n && prefix_len && count_below(prefix_seq, layer, prefix_len) != prefix_len) {
+  if (n && prefix_len && !all_in_range(prefix_seq, layer, 0, prefix_len)) {
     *msg = fmt("sequence %lld has unwritten positions below %lld (layer %lld)", prefix_seq, prefix_len, layer);
     return FCG_EHOLE;
   }
@@ -222,7 +233,7 @@ fcg_status Planner::check_attend(int32_t layer, int32_t prefix_seq, int32_t pref
   for (int32_t t = 0; t < n;) {
     int32_t u = t, top = pos[t];
     for (; u < n && seq[u] == seq[t]; ++u) top = std::max(top, pos[u]);
-    if (count_below(seq[t], layer, top + 1) - count_below(seq[t], layer, prefix_len) != top + 1 - prefix_len) {
+    if (!all_in_range(seq[t], layer, prefix_len, top + 1)) {
       *msg = fmt("sequence %lld has unwritten positions in %lld .. %lld", seq[t], prefix_len, top);
       return FCG_EHOLE;
     }

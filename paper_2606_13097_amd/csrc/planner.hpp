@@ -96,6 +96,7 @@ class Planner {
   const uint64_t* bits(int32_t seq, int32_t layer) const { return bits_.data() + idx(seq, layer) * W_; }
   uint64_t* bits(int32_t seq, int32_t layer) { return bits_.data() + idx(seq, layer) * W_; }
   bool any_in_range(int32_t seq, int32_t layer, int32_t a, int32_t b) const;  // [a, b)
+  bool all_in_range(int32_t seq, int32_t layer, int32_t a, int32_t b) const;  // every position of [a, b) written
   int32_t count_below(int32_t seq, int32_t layer, int32_t b) const;           // written in [0, b)
   fcg_status collect_pages(const std::vector<std::pair<int32_t, int32_t>>& seq_lpage,
                            std::vector<std::pair<int32_t, int32_t>>* new_pages, std::string* msg) const;

@@ -152,8 +152,15 @@ def _i32(a) -> np.ndarray:
     return np.ascontiguousarray(np.asarray(a, dtype=np.int32))
 
 
+_first_byte = C.c_char.from_buffer
+
+
 def _p(a: np.ndarray):
-    return a.ctypes.data if a.size else None
+    """Address of an array's data (``.ctypes.data`` costs about two microseconds, this a third of one, but it takes
+    writable arrays only)."""
+    if not a.size:
+        return None
+    return C.addressof(_first_byte(a)) if a.flags.writeable else a.ctypes.data
 
 
 _SMALL = 64  # int32 arrays up to this length go as ctypes arrays
