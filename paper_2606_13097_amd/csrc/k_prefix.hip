@@ -905,12 +905,14 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
 // ------------------------------------------------------------------ fp32
 
 // The same items on fp32 caches with v_mfma_f32_16x16x4_f32 (exact products,
-// fp32 sums).  One 64-key tile in LDS; wide items: 16 rows per wave and all 64
-// keys; narrow items: the same 16 rows in every wave, 16 of the keys each, merged
-// at the end.  The four k indices of a matrix step are dims 16 c + 4 lq + e of
-// keys and queries alike, so both are read 16 bytes at a time.
+// fp32 sums).  One 64-key tile in LDS, two blocks per compute unit; wide items: 16
+// rows per wave and all 64 keys; narrow items: the same 16 rows in every wave, 16 of
+// the keys each, merged at the end.  The four k indices of a matrix step are dims
+// 16 c + 4 lq + e of keys and queries alike, so both are read 16 bytes at a time.
+// The next tile's keys are requested when every wave is done with this one's, and
+// arrive beside the products with its values; values likewise.
 template <int D, bool PAGED, bool VALUE>
-__global__ void __launch_bounds__(256) prefix_attend_f32_kernel(PrefixCall pc, Plan<VALUE> plan, CacheView cv) {
+__global__ void __launch_bounds__(256, 2) prefix_attend_f32_kernel(PrefixCall pc, Plan<VALUE> plan, CacheView cv) {
   constexpr int DT = D / 16;
   constexpr int NC = D / 4;         // 16-byte chunks of a row
   constexpr int RI = 64 / NC;       // rows of one DMA instruction
@@ -943,95 +945,154 @@ __global__ void __launch_bounds__(256) prefix_attend_f32_kernel(PrefixCall pc, P
 #pragma unroll
     for (int c = 0; c < DT; ++c) qf[c] = __builtin_bit_cast(px_f32x4, ld16_any(src + (16 * c + 4 * lq) * 4));
   }
+  // the compiler cannot see the tile loads: its wait for these must not fall into the loop
+#pragma unroll
+  for (int c = 0; c < DT; ++c) asm volatile("" ::"v"(qf[c]));
+  asm volatile("" ::"v"(m.pos), "v"(m.tok));
   float mref = -INFINITY, lsum = 0.f;
   px_f32x4 acc[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) acc[dt] = px_f32x4{0.f, 0.f, 0.f, 0.f};
   const bool busy = narrow || 16 * w < it.n_row;
-  const int kt0 = narrow ? w : 0, kt1 = narrow ? w + 1 : 4;
-#pragma unroll 1
-  for (int ti = 0; ti < nt; ++ti) {
-    const bool own = ti >= na;
-    const Keys ks = own ? kb : ka;
-    const int p0 = (ks.lo / kPfxTile + (own ? ti - na : ti)) * kPfxTile;
-    {
-      const int q0 = min(max(p0 + 16 * w, ks.lo & ~15), (ks.hi - 1) & ~15);
-      const Entry e = entry_of<PAGED>(cv, ks.seq, q0);
-      const int rlo = max(ks.lo - q0, 0), rhi = min(ks.hi - 1 - q0, 15);
-      const void *bk = head.keys(ks.seq, q0, e), *bv = head.values(ks.seq, q0, e);
+  const int pmin = __builtin_amdgcn_readfirstlane(plan.rank(it.row0 / g).pos);
+  auto first_of = [&](int ti) __attribute__((always_inline)) {
+    return ((ti >= na ? kb.lo : ka.lo) / kPfxTile + (ti >= na ? ti - na : ti)) * kPfxTile;
+  };
+  // keys or values of tile ti, 16 rows by each wave
+  auto issue = [&](int ti, auto values) __attribute__((always_inline)) {
+    const Keys ks = ti >= na ? kb : ka;
+    const int q0 = min(max(first_of(ti) + 16 * w, ks.lo & ~15), (ks.hi - 1) & ~15);
+    const Entry e = entry_of<PAGED>(cv, ks.seq, q0);
+    const int rlo = max(ks.lo - q0, 0), rhi = min(ks.hi - 1 - q0, 15);
+    constexpr bool VV = decltype(values)::value;
+    const void* base = VV ? head.values(ks.seq, q0, e) : head.keys(ks.seq, q0, e);
 #pragma unroll
-      for (int j = 0; j < KI; ++j) {
-        const int rr = j * RI + lane / NC;
-        const uint32_t off = (uint32_t)(min(max(rr, rlo), rhi) * D + ((lane % NC) ^ rr) * 4) * 4;
-        dma16s(bk, off, lds_addr(K) + (w * 16 * D) * 4 + j * 1024);
-        dma16s(bv, off, lds_addr(V) + (w * 16 * D) * 4 + j * 1024);
-      }
+    for (int j = 0; j < KI; ++j) {
+      const int rr = j * RI + lane / NC;
+      dma16s(base, (uint32_t)(min(max(rr, rlo), rhi) * D + ((lane % NC) ^ rr) * 4) * 4,
+             lds_addr(VV ? V : K) + (w * 16 * D) * 4 + j * 1024);
     }
-    wait_vm<0>();
-    __syncthreads();
+  };
+  // LDS offsets (floats).  Chunk x of row r lies at x ^ (r % 16), so chunk 4 c + lq of key lr at
+  // 4 (c ^ lr / 4) + (lq ^ lr % 4), and element 16 dt + lr of key 4 lq + e at chunk
+  // 4 (dt ^ lq) + (lr / 4 ^ e): four offsets each for the low two bits of c, dt and e
+  int kat[4], vat[4][4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    kat[c] = lr * D + 16 * (c ^ (lr >> 2)) + 4 * (lq ^ (lr & 3));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) vat[c][e] = (4 * lq + e) * D + 16 * (c ^ lq) + 4 * ((lr >> 2) ^ e) + (lr & 3);
+  }
+  // tile ti of the products: NK groups of 16 keys, from group k0 on
+  auto tile = [&](int ti, int k0, auto groups) __attribute__((always_inline)) {
+    constexpr int NK = decltype(groups)::value;
+    const bool own = ti >= na;
+    const int lo = own ? kb.lo : ka.lo, hi = own ? kb.hi : ka.hi, p0 = first_of(ti) + 16 * k0;
+    const bool last = ti + 1 == nt;
+    px_f32x4 st[NK];
+    wait_vm<KI>();  // this wave's keys of the tile have landed ...
+    lds_barrier();  // ... and every wave's
     if (busy) {
-      for (int kt = kt0; kt < kt1; ++kt) {
-        px_f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+      const float* Kt = K + k0 * 16 * D;
 #pragma unroll
-        for (int c = 0; c < DT; ++c) {
-          const px_f32x4 kf =
-              *reinterpret_cast<const px_f32x4*>(&K[((kt * 16 + lr) * NC + ((4 * c + lq) ^ lr)) * 4]);
+      for (int kt = 0; kt < NK; ++kt) st[kt] = px_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[c][e], sc, 0, 0, 0);
+      for (int c = 0; c < DT; ++c)
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt) {
+          const px_f32x4 kf = *reinterpret_cast<const px_f32x4*>(&Kt[kat[c & 3] + (c >> 2) * 64 + kt * 16 * D]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) st[kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[c][e], st[kt], 0, 0, 0);
         }
-        const int base = p0 + 16 * kt;
-        const int lo = ks.lo - base - 4 * lq, hi = (own ? min(m.pos, ks.hi - 1) : ks.hi - 1) - base - 4 * lq;
-        float x[4], lmax = -INFINITY;
+    }
+    lds_barrier();
+    if (!last) issue(ti + 1, std::false_type{});
+    float p[NK][4];
+    // some row of the item does not see some key (wave-uniform); own keys belong to items of
+    // one sequence, whose first row has the smallest position
+    const bool edge = p0 < lo || p0 + 16 * NK > (own ? min(hi, pmin + 1) : hi);
+    if (busy) {
+      if (edge) {
+        const int a = lo - p0 - 4 * lq, b = (own ? min(m.pos, hi - 1) : hi - 1) - p0 - 4 * lq;
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) st[kt][e] = 16 * kt + e >= a && 16 * kt + e <= b ? st[kt][e] : -INFINITY;
+      }
+      float lmax = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lmax = fmaxf(lmax, st[kt][e]);
+      lmax *= qscale;
+      // as above: the reference moves when a row's max grows by more than 2^8
+      if (__builtin_amdgcn_ballot_w64(lmax > mref + 8.f)) {
+        const float mn = max_rows4(fmaxf(mref, lmax));
+        const float f = mref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mref - mn);
+        lsum *= f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) acc[dt] *= f;
+        mref = mn;
+      }
+      const float mr = mref == -INFINITY ? 0.f : mref;
+#pragma unroll
+      for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          x[e] = e >= lo && e <= hi ? sc[e] * qscale : -INFINITY;
-          lmax = fmaxf(lmax, x[e]);
+          p[kt][e] = __builtin_amdgcn_exp2f(fmaf(st[kt][e], qscale, -mr));
+          lsum += p[kt][e];
         }
-        if (__builtin_amdgcn_ballot_w64(lmax > mref)) {
-          const float mn = max_rows4(fmaxf(mref, lmax));
-          const float f = mref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mref - mn);
-          lsum *= f;
+    }
+    if (!last) wait_vm<KI>();  // the tile's values
+    else wait_vm<0>();
+    lds_barrier();
+    if (busy) {
+      const float* Vt = V + k0 * 16 * D;
+      bool bad = false;
+      auto output = [&](auto clean) __attribute__((always_inline)) {
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) acc[dt] *= f;
-          mref = mn;
-        }
-        const float mr = mref == -INFINITY ? 0.f : mref;
-        float p[4];
+        for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(x[e] - mr);
-          lsum += p[e];
-        }
-        const bool edge = own || base < ks.lo || base + 16 > ks.hi;  // masked keys: wave-uniform
-        bool bad = false;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int key = 4 * lq + e;
-            float v = V[((kt * 16 + key) * NC + ((4 * dt + (lr >> 2)) ^ key)) * 4 + (lr & 3)];
-            if (edge) {
-              bad = bad || !(fabsf(v) < INFINITY);
-              v = fabsf(v) < INFINITY ? v : 0.f;
-            }
-            acc[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[e], acc[dt], 0, 0, 0);
-          }
-        if (edge && __builtin_amdgcn_ballot_w64(bad)) {
-#pragma unroll 1
-          for (int q = max(base, ks.lo); q < min(base + 16, ks.hi); ++q) {
-            const int key = q - base;
+          for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
-              const px_f32x4 v =
-                  *reinterpret_cast<const px_f32x4*>(&V[((kt * 16 + key) * NC + ((4 * dt + lq) ^ key)) * 4]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[dt][e] += !own || q <= m.pos ? not_finite(v[e]) : 0.f;
+              float v = Vt[vat[dt & 3][e] + (dt >> 2) * 64 + kt * 16 * D];
+              if constexpr (decltype(clean)::value) {
+                bad = bad || !(fabsf(v) < INFINITY);
+                v = fabsf(v) < INFINITY ? v : 0.f;
+              }
+              acc[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[kt][e], acc[dt], 0, 0, 0);
             }
+      };
+      if (edge) output(std::true_type{});
+      else output(std::false_type{});
+      if (edge && __builtin_amdgcn_ballot_w64(bad)) {
+#pragma unroll 1
+        for (int q = max(p0, lo); q < min(p0 + 16 * NK, hi); ++q) {
+          const int key = q - p0;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const px_f32x4 v =
+                *reinterpret_cast<const px_f32x4*>(&Vt[(key * NC + ((4 * dt + lq) ^ (key & 15))) * 4]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[dt][e] += !own || q <= m.pos ? not_finite(v[e]) : 0.f;
           }
         }
       }
     }
-    __syncthreads();  // the tile's reads are done before the next one lands
+    lds_barrier();
+    if (!last) issue(ti + 1, std::true_type{});
+  };
+  if (nt) {
+    issue(0, std::false_type{});
+    issue(0, std::true_type{});
+  }
+  if (narrow) {
+#pragma unroll 1
+    for (int ti = 0; ti < nt; ++ti) tile(ti, w, std::integral_constant<int, 1>{});
+  } else {
+#pragma unroll 1
+    for (int ti = 0; ti < nt; ++ti) tile(ti, 0, std::integral_constant<int, 4>{});
   }
   lsum = sum_rows4(lsum);
   if (!narrow) {

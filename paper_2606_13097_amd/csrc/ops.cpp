@@ -394,7 +394,7 @@ struct PrefixShape {
   double tile_us, tile2_us, item_us, ntile_us;
 };
 constexpr PrefixShape kShape4{kPfxRows, 512, 32, 1.5, 2.65, 6.0, 0.45}, kShape8{2 * kPfxRows, 256, 32, 2.0, 2.0, 12.0, 0.3};
-constexpr PrefixShape kShapeF32{kPfxRowsF32, 512, 16, 4.0, 7.0, 6.0, 1.0};
+constexpr PrefixShape kShapeF32{kPfxRowsF32, 512, 16, 5.0, 9.5, 6.0, 1.0};
 
 // Choose the split length (in tiles) of a call cut into row blocks of a shape, and
 // return the estimated time (us) that the choice of shape goes by: rounds of wide items,
