@@ -75,7 +75,7 @@ struct RunsInMemory {
 // head.  A form by value (RopeArgs): a lane's two vectors of a key row hold both
 // ends of VEC pairs (halves), or whole pairs each (neighbours: vectors c and c + D /
 // 2 / VEC), or dimensions that pass unturned, as in k_rope.hip.  Either way the
-// memory bounds the kernel: neighbouring pairs, 32 layers of 4.0K tokens (bf16, D 128,
+// memory bounds the kernel: neighbouring pairs, 32 layers of 4.1K tokens (bf16, D 128,
 // 8 heads, 1.06 GB read and written) take 200 us, a copy of as many bytes 197 to 211;
 // half a head turned into pages, 2.2 GB 461 us (4.8 TB/s), a copy 427.
 struct OwnForm {

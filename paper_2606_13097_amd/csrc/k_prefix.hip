@@ -29,10 +29,10 @@
 //
 // What bounds it (bf16, D 128, 8 key heads; times per call, one after the other):
 //   32 sequences of 64 tokens, 4 query heads a key head, over 6007 shared keys and up
-//   to 300 own ones: 204 us for 207 GFLOP, 1.01 PFLOP/s, where an 8192^3 library
+//   to 300 own ones: 198 us for 207 GFLOP, 1.04 PFLOP/s, where an 8192^3 library
 //   product reaches 1.18.  A tile takes 3170 cycles of its compute unit, 2048 of them
 //   matrix cycles; the rest is the softmax that finds no gap between the products.
-//   32 sequences of 4 tokens, 8 query heads, over 22011: 119 us for 94 GFLOP.  Four
+//   32 sequences of 4 tokens, 8 query heads, over 22011: 116 us for 94 GFLOP.  Four
 //   row blocks of a head cut in 8 splits each are one round of 256 items; their first
 //   tiles, the partials and the merge (7 us) are what is added to the product rate.
 //   64 sequences of one token, 4 query heads, over 4321: 23.6 us for 57 MB.  Round
