@@ -750,14 +750,14 @@ fcg_status graft(fcg_cache* c, const fcg_lib* lib, const fcg_rope* rope, int32_t
 
 fcg_status fcg_graft(fcg_cache* c, const fcg_lib* lib, int32_t n_items, const int32_t* seq, const int32_t* seg,
                      const int32_t* dst, void* stream) {
-  return graft(c, lib, nullptr, n_items, seq, seg, dst, stream);
+  return guarded([&] { return graft(c, lib, nullptr, n_items, seq, seg, dst, stream); });
 }
 
 fcg_status fcg_graft_rope(fcg_cache* c, const fcg_lib* lib, const fcg_rope* rope, int32_t n_items, const int32_t* seq,
                           const int32_t* seg, const int32_t* dst, void* stream) {
   if (!rope) return fail(FCG_EINVAL, "null rope");
   if (c && rope->rot > c->desc.head_dim) return fail(FCG_EINVAL, "rotary_dim exceeds head_dim");
-  return graft(c, lib, rope, n_items, seq, seg, dst, stream);
+  return guarded([&] { return graft(c, lib, rope, n_items, seq, seg, dst, stream); });
 }
 
 namespace {

@@ -8,7 +8,9 @@
 #include <algorithm>
 #include <cstring>
 #include <deque>
+#include <exception>
 #include <map>
+#include <new>
 #include <string>
 #include <tuple>
 #include <unordered_map>
@@ -29,6 +31,18 @@ fcg_status hip_fail(hipError_t e, const char* what);
     hipError_t e_ = (expr);                               \
     if (e_ != hipSuccess) return fcg::hip_fail(e_, what); \
   } while (0)
+
+// Body of an entry point: host allocations that fail become a status.
+template <typename F>
+fcg_status guarded(F&& f) {
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    return report(FCG_ENOMEM, "host allocation");
+  } catch (const std::exception& e) {
+    return report(FCG_ENOMEM, e.what());
+  }
+}
 
 inline size_t esize(int32_t dtype) { return dtype == FCG_F32 ? 4 : 2; }
 

@@ -2,7 +2,6 @@
 // (include/fcg.h): rotary handles, rope apply, append, prefix attention.
 #include <algorithm>
 #include <cmath>
-#include <new>
 
 #include "objects.hpp"
 
@@ -11,18 +10,6 @@ using namespace fcg;
 namespace {
 
 fcg_status fail(fcg_status s, const std::string& msg) { return report(s, msg); }
-
-// Body of an entry point: host allocations that fail become a status.
-template <typename F>
-fcg_status guarded(F&& f) {
-  try {
-    return f();
-  } catch (const std::bad_alloc&) {
-    return fail(FCG_ENOMEM, "host allocation");
-  } catch (const std::exception& e) {
-    return fail(FCG_ENOMEM, e.what());
-  }
-}
 
 // The handle's device for the call, the caller's again afterwards.
 struct OnDevice {

@@ -483,33 +483,25 @@ def fcg_rope_destroy(rope: Rope) -> None:
 
 
 _TORCH_DT = {torch.float32: FCG_F32, torch.bfloat16: FCG_BF16}
+_DT_TORCH = {v: k for k, v in _TORCH_DT.items()}
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _view(t, n_layers: int, n_tok: int, n_heads: int, head_dim: int, dtype: int, device, what: str):
-    """fcg_tensor of a [n_layers][n_tok][n_heads][head_dim] tensor (three dimensions: one layer).  One call makes up
-    to four of these, a visible part of a small step, so the checks are few and plain."""
+def _view(t, shape: tuple, dtype, device, what: str):
+    """fcg_tensor of a tensor of shape [n_layers][n_tok][n_heads][head_dim], or without the first dimension (one layer).
+    One call makes up to four of these, a visible part of a small step, so the checks are few and plain."""
     if t is None:
         return None
-    if not t.is_cuda or _TORCH_DT.get(t.dtype) != dtype:
-        raise ValueError(f"{what}: not a GPU tensor of the expected type")
-    if device is not None and t.get_device() != device:
-        raise ValueError(f"{what}: on device {t.get_device()}, expected {device}")
-    st = t.stride()
-    if len(st) == 3 and n_layers == 1:
-        ok = t.shape == (n_tok, n_heads, head_dim)
-        v = TensorView(t.data_ptr(), 0, st[0], st[1])
-    else:
-        ok = t.shape == (n_layers, n_tok, n_heads, head_dim)
-        v = TensorView(t.data_ptr(), *st[:3])
-    if not ok:
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(n_layers, n_tok, n_heads, head_dim)} (one layer: "
-                         "or without the first dimension)")
+    if t.dtype is not dtype or (t.get_device() != device if device is not None else not t.is_cuda):
+        raise ValueError(f"{what}: a {t.dtype} tensor on {t.device}, expected {dtype} on GPU {device}")
+    st, sh = t.stride(), t.shape
+    if sh != shape and (sh != shape[1:] or shape[0] != 1):
+        raise ValueError(f"{what}: shape {tuple(sh)}, expected {shape} (one layer: or without the first dimension)")
     if st[-1] != 1 and t.numel():
         raise ValueError(f"{what}: the elements of a row must be adjacent")
-    return v
+    return TensorView(t.data_ptr(), *st[:3]) if len(st) == 4 else TensorView(t.data_ptr(), 0, st[0], st[1])
 
 
 def _ref(v: Optional[TensorView]):
@@ -536,13 +528,14 @@ def fcg_rope_apply(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, flag
         raise ValueError("a float32 or bfloat16 tensor of three or four dimensions")
     if (q is None) != (q_out is None) or (k is None) != (k_out is None):
         raise ValueError("an input without its output, or an output without its input")
-    dt, dev, n, d = _TORCH_DT[like.dtype], pos.get_device(), pos.numel(), like.shape[-1]
+    td, dev, n, d = like.dtype, pos.get_device(), pos.numel(), like.shape[-1]
     layers = like.shape[0] if like.dim() == 4 else 1
     hq, hk = 0 if q is None else q.shape[-2], 0 if k is None else k.shape[-2]
-    vq, vqo = _view(q, layers, n, hq, d, dt, dev, "q"), _view(q_out, layers, n, hq, d, dt, dev, "q_out")
-    vk, vko = _view(k, layers, n, hk, d, dt, dev, "k"), _view(k_out, layers, n, hk, d, dt, dev, "k_out")
-    args = (rope.h, dt, d, layers, n, pos.data_ptr(), hq, _ref(vq), _ref(vqo), hk, _ref(vk), _ref(vko), int(flags),
-            _stream_of(stream, dev))
+    sq, sk = (layers, n, hq, d), (layers, n, hk, d)
+    vq, vqo = _view(q, sq, td, dev, "q"), _view(q_out, sq, td, dev, "q_out")
+    vk, vko = _view(k, sk, td, dev, "k"), _view(k_out, sk, td, dev, "k_out")
+    args = (rope.h, _TORCH_DT[td], d, layers, n, pos.data_ptr(), hq, _ref(vq), _ref(vqo), hk, _ref(vk), _ref(vko),
+            int(flags), _stream_of(stream, dev))
     if dev == torch.cuda.current_device():
         _check(_L.fcg_rope_apply(*args))
     else:
@@ -570,9 +563,10 @@ def fcg_append(cache: Cache, layer: int, seq, pos, k=None, v=None, rope: Optiona
     if k is not None:
         n_layers = k.shape[0] if k.dim() == 4 else 1
     d, n = cache.desc, int(s.size)
-    hq, hkv, hd, dt, dev = d.n_q_heads, d.n_kv_heads, d.head_dim, d.dtype, cache.device
-    vq, vqo = _view(q, n_layers, n, hq, hd, dt, dev, "q"), _view(q_out, n_layers, n, hq, hd, dt, dev, "q_out")
-    vk, vv = _view(k, n_layers, n, hkv, hd, dt, dev, "k"), _view(v, n_layers, n, hkv, hd, dt, dev, "v")
+    sq, skv = (n_layers, n, d.n_q_heads, d.head_dim), (n_layers, n, d.n_kv_heads, d.head_dim)
+    td, dev = _DT_TORCH[d.dtype], cache.device
+    vq, vqo = _view(q, sq, td, dev, "q"), _view(q_out, sq, td, dev, "q_out")
+    vk, vv = _view(k, skv, td, dev, "k"), _view(v, skv, td, dev, "v")
     _check(_L.fcg_append(cache.h, int(layer), int(n_layers), n, _p(s), _p(p), None if rope is None else rope.h,
                          _ref(vq), _ref(vqo), _ref(vk), _ref(vv), int(flags), _stream_of(stream, dev)))
 
@@ -585,8 +579,8 @@ def fcg_prefix_attend(cache: Cache, layer: int, prefix_seq: int, prefix_len: int
     if s.ndim != 1 or s.shape != p.shape:
         raise ValueError("seq and pos differ in length")
     d, n = cache.desc, int(s.size)
-    hq, hd, dt, dev = d.n_q_heads, d.head_dim, d.dtype, cache.device
-    vq, vo = _view(q, 1, n, hq, hd, dt, dev, "q"), _view(out, 1, n, hq, hd, dt, dev, "out")
+    sq, td, dev = (1, n, d.n_q_heads, d.head_dim), _DT_TORCH[d.dtype], cache.device
+    vq, vo = _view(q, sq, td, dev, "q"), _view(out, sq, td, dev, "out")
     if lse is not None and (not lse.is_cuda or lse.dtype != torch.float32 or not lse.is_contiguous() or
                             lse.shape != (n, d.n_q_heads) or lse.get_device() != cache.device):
         raise ValueError("lse: a contiguous float32 GPU tensor [n_tok][Hq]")
