@@ -251,13 +251,17 @@ template <>
 struct Plan<false> {
   const PrefixItem* items;
   const PrefixRank* ranks;
-  __device__ __forceinline__ PrefixItem item(int b) const { return items[b]; }
+  __device__ __forceinline__ bool paired(int) const { return false; }
+  __device__ __forceinline__ PrefixItem item(int b, int) const { return items[b]; }
   __device__ __forceinline__ PrefixRank rank(int r) const { return ranks[r]; }
 };
 template <>
 struct Plan<true> {
   PrefixArgs a;
-  __device__ __forceinline__ PrefixItem item(int b) const {
+  // block b holds two own items, one of them for each half of its waves
+  __device__ __forceinline__ bool paired(int b) const { return a.paired && b >= a.n_pre; }
+  // half: of the block's waves, if paired (an item without rows where there is none left)
+  __device__ __forceinline__ PrefixItem item(int b, int half) const {
     PrefixItem it{};
     if (b < a.n_pre) {
       const int rb = b / a.pre_slots, s = b - rb * a.pre_slots;
@@ -270,7 +274,8 @@ struct Plan<true> {
     }
     // the group is the last one whose first item is at most b: one group per lane
     static_assert(kPfxGroups == 64, "one group per lane");
-    const int lane = threadIdx.x & 63, x = b - a.n_pre;
+    const int lane = threadIdx.x & 63, x = a.paired ? 2 * (b - a.n_pre) + half : b - a.n_pre;
+    if (half && x >= a.paired) return it;
     const PrefixGroup mine = a.group[min(lane, a.n_group - 1)];
     const uint64_t below = __builtin_amdgcn_ballot_w64(lane < a.n_group && mine.item0 <= x);
     const int r = 63 - __builtin_clzll(below);
@@ -312,14 +317,15 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
   __shared__ float s_wm[WAVES][32], s_wl[WAVES][32];
   __shared__ __align__(16) int s_bad[NB][4];  // a tile's value groups that held non-finite elements
 
-  const PrefixItem it = plan.item(blockIdx.y);
+  PrefixItem it = plan.item(blockIdx.y, 0);
   const int hk = blockIdx.x;  // fastest: workgroups go to the eight XCDs in turn, so a head's blocks share an L2
   const int t = threadIdx.x, lane = t & 63, lr = lane & 15, lq = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int Hkv = cv.n_kv_heads;
   const int g = pc.g;
   const float qscale = 1.4426950408889634f / sqrtf((float)D);
-  const Keys ka{pc.prefix_seq, it.a0, it.a1}, kb{it.seq, it.b0, it.b1};
+  const Keys ka{pc.prefix_seq, it.a0, it.a1};
+  Keys kb{it.seq, it.b0, it.b1};
 
   // DMA instruction j of 16 rows fills rows RI j .. RI j + RI - 1: lane l the chunk
   // position l % NC of row RI j + l / NC.  The chunk that belongs there is the position
@@ -738,16 +744,22 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
   static_assert(WAVES * 2 * TILE == sizeof(s_kv) || WAVES == 8, "a ring of two per wave");
   static_assert(WAVES * 2 * TILE <= sizeof(s_kv) && 32 * D * 4 <= 2 * TILE, "rings and results fit");
   char* ring = reinterpret_cast<char*>(s_kv) + w * 2 * TILE;
+  // this item's waves: w0 .. w0 + nw - 1
+  const int nw = plan.paired(blockIdx.y) ? WAVES / 2 : WAVES, w0 = w & ~(nw - 1), wi = w - w0;
+  if (w0) {
+    it = plan.item(blockIdx.y, 1);
+    kb = Keys{it.seq, it.b0, it.b1};
+  }
   auto narrow = [&](auto row_tiles) __attribute__((always_inline)) {
     constexpr int RT = decltype(row_tiles)::value;
     const uint32_t ring_lds = lds_addr(ring);
     const int na = tiles_of(ka, 16), nb = tiles_of(kb, 16);
-    const int n = (na + nb - w + WAVES - 1) / WAVES;  // this wave's tiles: w, w + WAVES, ...
+    const int n = (na + nb - wi + nw - 1) / nw;  // this wave's tiles: wi, wi + nw, ...
     auto first_of = [&](int i) __attribute__((always_inline)) {
-      const int ti = w + WAVES * i;
+      const int ti = wi + nw * i;
       return (ti >= na ? (kb.lo >> 4) + ti - na : (ka.lo >> 4) + ti) * 16;
     };
-    auto own_of = [&](int i) __attribute__((always_inline)) { return w + WAVES * i >= na; };
+    auto own_of = [&](int i) __attribute__((always_inline)) { return wi + nw * i >= na; };
     Entries<PAGED> entries;
     auto entry = [&](int i) __attribute__((always_inline)) -> Entry {
       return entries.get(cv, i, n, lane, [&](int j, int* seq, int* pos) __attribute__((always_inline)) {
@@ -877,19 +889,22 @@ __global__ void __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) prefix_attend_
   else narrow(std::integral_constant<int, 1>{});
   __syncthreads();
   constexpr int LPR = D / 4;  // lanes of a row
-  for (int idx = t; idx < it.n_row * LPR; idx += NT) {
+  for (int idx = t - w0 * 64; idx < it.n_row * LPR; idx += nw * 64) {
     const int r = idx / LPR, d = 4 * (idx % LPR);
     float M = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < WAVES; ++k) M = fmaxf(M, s_wm[k][r]);
+    for (int k = 0; k < WAVES; ++k)
+      if (k < nw) M = fmaxf(M, s_wm[w0 + k][r]);
     float L = 0.f;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < WAVES; ++k) {
-      const float m = s_wm[k][r];
+      if (k >= nw) break;
+      const float m = s_wm[w0 + k][r];
       const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
-      const float4 o = *reinterpret_cast<const float4*>(reinterpret_cast<char*>(s_kv) + k * 2 * TILE + (r * D + d) * 4);
-      L = fmaf(s_wl[k][r], f, L);
+      const float4 o =
+          *reinterpret_cast<const float4*>(reinterpret_cast<char*>(s_kv) + (w0 + k) * 2 * TILE + (r * D + d) * 4);
+      L = fmaf(s_wl[w0 + k][r], f, L);
       a.x = fmaf(o.x, f, a.x);
       a.y = fmaf(o.y, f, a.y);
       a.z = fmaf(o.z, f, a.z);
@@ -921,7 +936,7 @@ __global__ void __launch_bounds__(256, 2) prefix_attend_f32_kernel(PrefixCall pc
   __shared__ __align__(16) float s_kv[2 * HALF_T];
   __shared__ float s_wm[4][16], s_wl[4][16];
 
-  const PrefixItem it = plan.item(blockIdx.y);
+  const PrefixItem it = plan.item(blockIdx.y, 0);
   const int hk = blockIdx.x;
   const int t = threadIdx.x, lane = t & 63, lr = lane & 15, lq = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);

@@ -366,7 +366,8 @@ constexpr int kPfxRows = 128;     // query rows of an item, bf16, blocks of 4 wa
 constexpr int kPfxRowsF32 = 64;   // fp32
 constexpr int kPfxTile = 64;      // keys of a tile
 // The plan by value, for calls of up to kPfxRanks tokens in kPfxGroups sequences:
-// n_pre prefix items (row block, then slot) of `per` keys, then the groups' own items.
+// n_pre prefix items (row block, then slot) of `per` keys, then the groups' own items;
+// paired, if not 0: their number, and two of them share a block, half of its waves each.
 constexpr int kPfxGroups = 64, kPfxRanks = 128;
 struct PrefixGroup {
   int32_t seq, end;  // own positions [prefix_len, end)
@@ -378,7 +379,7 @@ struct PrefixSmall {
   uint16_t tok, nb;  // token, own slots
 };
 struct PrefixArgs {
-  int32_t n_pre, pre_slots, pre_rows, block, per, prefix_len, n_group, pad;
+  int32_t n_pre, pre_slots, pre_rows, block, per, prefix_len, n_group, paired;
   PrefixGroup group[kPfxGroups];
   PrefixSmall rank[kPfxRanks];
 };

@@ -820,6 +820,38 @@ def test_prefix_attend_blocks_of_256_rows(page, hq, hkv, d):
     sh.cache.close()
 
 
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("hq,hkv,d,n_seq,P", [(64, 8, 128, 47, 2000), (64, 32, 64, 37, 0), (32, 16, 128, 64, 65),
+                                              (128, 16, 64, 63, 300)])
+def test_prefix_attend_more_own_items_than_run_at_once(page, hq, hkv, d, n_seq, P):
+    """Small own parts that share blocks two by two: an odd number of them, of one to three tokens or none past the
+    prefix, rows in one or two matrix tiles, lengths down to one key, values that are not finite behind a row's end."""
+    rng = np.random.default_rng(n_seq)
+    g = hq // hkv
+    n = rng.integers(1, 4 if 3 * g <= 32 else 2, n_seq)
+    n[rng.permutation(n_seq)[:max(0, int(n.sum()) - 128)]] = 1
+    n = np.minimum(n, 128 // n_seq)
+    own = [int(rng.integers(m, m + 1 if i % 5 == 0 else 150)) for i, m in enumerate(n)]
+    sh = Shared("bf16", hq, hkv, d, page, P, own, 51, shuffle=False)
+    seq = np.repeat(np.arange(n_seq), n)
+    pos = np.concatenate([P + own[s] - n[s] + np.arange(n[s]) for s in range(n_seq)])
+    if P:
+        pos[np.flatnonzero(seq == 7)[0]] = P - 1        # the prefix only
+    cut = 11                                            # its last key is not attended, and not finite
+    own_cut = np.flatnonzero(seq == cut)
+    if own[cut] > n[cut]:
+        pos[own_cut] -= 1
+        k, v = sh.kv[cut]
+        k[-1], v[-1] = float("nan"), float("inf")
+        sh.put(cut, np.arange(P, P + own[cut]), k, v)
+    mix = rng.permutation(len(seq))
+    seq, pos = seq[mix], pos[mix]
+    for scale in (1.0, 8.0):
+        q, out, lse = run_shared(sh, seq, pos, 5, scale=scale)
+        sh.check(seq, pos, q, out, lse, f"queries times {scale}", np.arange(0, len(seq), 3))
+    sh.cache.close()
+
+
 def test_prefix_attend_one_item_a_row():
     """As many row blocks as fill the chip: no split, results written without a merge, in the queries' place too."""
     P, n = 4099, 32
