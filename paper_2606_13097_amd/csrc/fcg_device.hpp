@@ -238,4 +238,14 @@ __device__ __forceinline__ void st16_nt(void* p, const uint4& v) {
   __builtin_nontemporal_store(u32x4_t{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4_t*>(p));
 }
 
+// the same to and from any address
+typedef u32x4_t u32x4_any_t __attribute__((aligned(2)));
+__device__ __forceinline__ void st16_nt_any(void* p, const uint4& v) {
+  __builtin_nontemporal_store(u32x4_t{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4_any_t*>(p));
+}
+__device__ __forceinline__ uint4 ld16_nt_any(const void* p) {
+  const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any_t*>(p));
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+
 }  // namespace fcg

@@ -154,8 +154,13 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(Where<MODE> where, RopeR
   uint4 a, b;
   auto load = [&](int layer) __attribute__((always_inline)) {
     const T* p = src + layer * src_layer;
-    a = ld16_any(p + lo);
-    b = ld16_any(p + hi);
+    if (rows.stream) {  // (uniform) more than the last-level cache holds
+      a = ld16_nt_any(p + lo);
+      b = ld16_nt_any(p + hi);
+    } else {
+      a = ld16_any(p + lo);
+      b = ld16_any(p + hi);
+    }
   };
   load(blockIdx.z);
 
@@ -217,12 +222,13 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(Where<MODE> where, RopeR
     }
     if (!mine) continue;
     T* p = dst + layer * dst_layer;
+    // past this L2: whoever reads the rows next runs on any XCD, and inputs that lie in the
+    // last-level cache stay there (new inputs each pass, keys of 32 layers of 713 tokens
+    // 18.1 -> 15.4 us, fp32 gradients of 4.7K tokens 20.8 -> 17.2)
     if (!to_cache) {
-      st16_any(p + lo, ya);
-      st16_any(p + hi, yb);
+      st16_nt_any(p + lo, ya);
+      st16_nt_any(p + hi, yb);
     } else {
-      // past this L2: whoever reads the rows next runs on any XCD (8 layers of 11K tokens
-      // into pages 447 -> 432 us, 32 layers of 129 into a contiguous cache 21.0 -> 20.3)
       st16_nt(p + lo, ya);
       st16_nt(p + hi, yb);
     }

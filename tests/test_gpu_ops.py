@@ -760,6 +760,32 @@ def test_calls_on_another_stream_and_a_strided_result():
     sh.cache.close()
 
 
+def test_calls_larger_than_the_caches_equal_their_layers():
+    """More than 256 MB of rows in one call (read and written past the caches): the bits of a call per layer."""
+    L, n, hq, hkv, d = 9, 5001, 16, 8, 128
+    rope, _ = make_rope(128, True, "ntk")
+    c = fcg.Cache(fcg.model_desc(L, hq, hkv, d, 1e4, "bf16"), 2, n + 40, 16, 2 * (n + 40) // 16 + 2)
+    mem = fill_memory(c, "bf16", 7.0)
+    q, k, v = randn(gen(1), L, n, hq, d), randn(gen(2), L, n, hkv, d), randn(gen(3), L, n, hkv, d)
+    assert q.numel() * 2 + k.numel() * 4 > 2 ** 28
+    qo = torch.empty_like(q)
+    pos = np.arange(17, 17 + n)
+    dpos = torch.as_tensor(pos, dtype=torch.int32, device="cuda")
+    fcg.fcg_append(c, 0, np.ones(n, int), pos, k, v, rope=rope, q=q, q_out=qo, n_layers=L)
+    qq = torch.cat([q, q], 2)                       # 369 MB
+    fcg.fcg_rope_apply(rope, dpos, qq, qq)
+    torch.cuda.synchronize()
+    assert torch.equal(bits(qq[:, :, :hq].contiguous()), bits(qo))
+    for l in range(L):
+        q1, k1 = torch.empty_like(q[l]), torch.empty_like(k[l])
+        fcg.fcg_rope_apply(rope, dpos, q[l], q1, k[l], k1)
+        torch.cuda.synchronize()
+        assert torch.equal(bits(q1), bits(qo[l])) and torch.equal(bits(qq[l, :, hq:].contiguous()), bits(q1))
+        assert torch.equal(bits(rows_of(c, mem[0], l, 1, pos)), bits(k1))
+        assert torch.equal(bits(rows_of(c, mem[1], l, 1, pos)), bits(v[l]))
+    c.close()
+
+
 @pytest.mark.parametrize("page", [0, 16])
 @pytest.mark.parametrize("hq,hkv,d", [(32, 2, 128), (16, 4, 64)])
 def test_prefix_attend_blocks_of_many_rows(page, hq, hkv, d):
