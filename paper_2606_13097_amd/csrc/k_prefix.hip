@@ -25,17 +25,18 @@
 // wave's products took 7.1 cycles each there and 9.1 beside 16x16 ones.
 // Narrow items (a decode step's own keys): the waves take 16-key tiles in turn
 // (16x16 products, four lanes a row), each through an LDS ring of its own, without
-// barriers, and merge at the end.
+// barriers, and merge at the end; two such items may share a block, half of its waves
+// each.
 //
 // What bounds it (bf16, D 128, 8 key heads; times per call, one after the other):
 //   32 sequences of 64 tokens, 4 query heads a key head, over 6007 shared keys and up
-//   to 300 own ones: 198 us for 207 GFLOP, 1.04 PFLOP/s, where an 8192^3 library
+//   to 300 own ones: 198 to 214 us for 207 GFLOP, 1.0 PFLOP/s, where an 8192^3 library
 //   product reaches 1.18.  A tile takes 3170 cycles of its compute unit, 2048 of them
 //   matrix cycles; the rest is the softmax that finds no gap between the products.
-//   32 sequences of 4 tokens, 8 query heads, over 22011: 116 us for 94 GFLOP.  Four
+//   32 sequences of 4 tokens, 8 query heads, over 22011: 116 to 123 us for 94 GFLOP.  Four
 //   row blocks of a head cut in 8 splits each are one round of 256 items; their first
 //   tiles, the partials and the merge (7 us) are what is added to the product rate.
-//   64 sequences of one token, 4 query heads, over 4321: 23.6 us for 57 MB.  Round
+//   64 sequences of one token, 4 query heads, over 4321: 21.8 us for 57 MB.  Round
 //   trips: page entries, first tiles, partials, merge (4 us).
 //
 // Tiles start on multiples of their length in position, so the 16 keys that one

@@ -20,10 +20,10 @@
 // accesses); cache rows are aligned.
 //
 // What bounds it: many tokens, the memory (bf16, D 128: keys of 32 layers of 713
-// tokens of 8 heads, 93 MB read and written, 15.4 us, a copy of as many bytes 13.6;
-// keys, values and queries of 8 layers of 11K tokens into pages, 2.2 GB, 416 us, 5.3
-// TB/s, a copy 5.2); few, the chain of argument fetch, position, rows and stores (3 us
-// for one token).
+// tokens of 8 heads, 93 MB read and written, 15.5 us on the same buffers again and
+// 17.6 on new ones, a copy of as many bytes 13.6 and 19.3; keys, values and queries of
+// 8 layers of 11K tokens into pages, 2.2 GB, 390 us, 5.6 TB/s, a copy 5.2); few, the
+// chain of argument fetch, position, rows and stores (3 us for one token).
 #include "fcg_device.hpp"
 #include "kernels.hpp"
 
@@ -222,15 +222,21 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(Where<MODE> where, RopeR
     }
     if (!mine) continue;
     T* p = dst + layer * dst_layer;
-    // past this L2: whoever reads the rows next runs on any XCD, and inputs that lie in the
-    // last-level cache stay there (new inputs each pass, keys of 32 layers of 713 tokens
-    // 18.1 -> 15.4 us, fp32 gradients of 4.7K tokens 20.8 -> 17.2)
-    if (!to_cache) {
+    // Caller tensors are read next: plain stores leave them in the last-level cache (keys
+    // of 32 layers of 713 tokens, new inputs each pass: 20 us and 30 with a kernel that reads
+    // them, past the caches 16 and 33; fp32 gradients of 4.7K tokens 23 and 41, 17 and 51).
+    // Cache rows, and results larger than that cache, go past the L2: whoever reads them next
+    // runs on any XCD (8 layers of 11K tokens into pages 447 -> 432 us, 32 layers of 129 into
+    // a contiguous cache 21.0 -> 20.3).
+    if (to_cache) {
+      st16_nt(p + lo, ya);
+      st16_nt(p + hi, yb);
+    } else if (rows.stream) {
       st16_nt_any(p + lo, ya);
       st16_nt_any(p + hi, yb);
     } else {
-      st16_nt(p + lo, ya);
-      st16_nt(p + hi, yb);
+      st16_any(p + lo, ya);
+      st16_any(p + hi, yb);
     }
   }
 }

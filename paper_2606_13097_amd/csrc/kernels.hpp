@@ -320,7 +320,7 @@ struct RopeRows {
   int32_t n_layers, grid_layers;  // layers, layers at once (a block takes every grid_layers-th)
   uint32_t h_magic;               // ceil(2^32 / rows of a token): r / rows = r * h_magic >> 32 for the rows of a block
   float sign;                     // of the angles
-  int32_t stream;                 // 1: read past the caches
+  int32_t stream;                 // 1: read and write past the caches
 };
 
 // Turn rows into caller tensors: q -> q_out, k -> k_out, token t at device pos[t].

@@ -156,8 +156,9 @@ void cut_rows(RopeRows* rows, int64_t n_tok, int64_t n_layers, int H, int nch) {
   const int64_t blocks = (n_tok + rows->tb - 1) / rows->tb * (((int64_t)rows->tb * H + slice - 1) / slice) * n_layers;
   const int64_t each = (blocks + kResident - 1) / kResident;
   rows->grid_layers = (int32_t)(each <= 4 ? (n_layers + each - 1) / each : n_layers);
-  // More than the last-level cache (256 MB): reading past the caches spares it for what is
-  // written (2.2 GB in all: 401 -> 387 us).  Less may lie there: 96 MB in all 17.2, so 21.4.
+  // More than the last-level cache holds (256 MB): nothing of it will be there when it is read
+  // (2.2 GB in all, plain 414 us, written past the caches 401, read so too 385).  Less may lie
+  // there (96 MB in all 17.2 us, read past the caches 21.4).
   rows->stream = n_tok * n_layers * H * nch * 32 > (int64_t)256 << 20;
 }
 
