@@ -154,7 +154,6 @@ fcg_status fcg::grow(void** p, size_t* have, size_t need, const char* what) {
 
 void fcg::stage_pages(fcg_cache* c, const std::vector<std::pair<int32_t, int32_t>>& new_pages, Blob* blob,
                       std::vector<std::pair<int32_t, size_t>>* rows, std::vector<int32_t> seqs) {
-  c->plan.map_pages(new_pages);
   for (auto& sl : new_pages)  // in (sequence, logical page) order
     if (seqs.empty() || seqs.back() != sl.first) seqs.push_back(sl.first);
   if (!std::is_sorted(seqs.begin(), seqs.end())) std::sort(seqs.begin(), seqs.end());
@@ -163,11 +162,12 @@ void fcg::stage_pages(fcg_cache* c, const std::vector<std::pair<int32_t, int32_t
 }
 
 fcg_status fcg::upload(fcg_cache* c, const Blob& blob, const std::vector<std::pair<int32_t, size_t>>& rows,
-                       hipStream_t s, char** dev, size_t* off_out) {
+                       hipStream_t s, char** dev, Staged* staged) {
   const size_t n = std::max<size_t>((blob.bytes.size() + 255) & ~size_t(255), 256);
   size_t off;
   fcg_status st = c->ring.acquire(n, &off);
   if (st) return st;
+  if (staged) staged->sent();
   std::memcpy(c->ring.host + off, blob.bytes.data(), blob.bytes.size());
   const size_t row_bytes = 2 * (size_t)c->plan.n_logical_pages() * sizeof(int32_t);
   const size_t stride = (row_bytes + 255) & ~size_t(255);
@@ -187,7 +187,6 @@ fcg_status fcg::upload(fcg_cache* c, const Blob& blob, const std::vector<std::pa
     a.bytes = 0;
   }
   *dev = c->ring.dev + off;
-  *off_out = off;
   return FCG_OK;
 }
 
@@ -554,12 +553,11 @@ fcg_status fcg_cache_truncate(fcg_cache* c, int32_t seq, int32_t pos, void* stre
   for (const Unalias& u : un) items.push_back(UnaliasItem{u.lib_tok, u.page, u.rows});
   const size_t o_items = blob.add(items.data(), items.size() * sizeof(UnaliasItem));
   char* dev;
-  size_t off;
-  if (fcg_status st = upload(c, blob, rows, s, &dev, &off)) return st;
+  if (fcg_status st = upload(c, blob, rows, s, &dev, nullptr)) return st;
   int rc = launch_unalias(c->desc.dtype, (const UnaliasItem*)(dev + o_items), (int)items.size(), c->alias_lib->v,
                           c->alias_lib->cap, c->view(), c->desc.n_layers, s);
   if (rc) return hip_fail((hipError_t)rc, "unalias launch");
-  return c->ring.retire(off, blob.bytes.size(), s);
+  return c->ring.retire(s);
 }
 
 fcg_status fcg_cache_export_v_alias(const fcg_cache* c, int32_t seq, int32_t* v_alias) {
@@ -678,21 +676,29 @@ fcg_status graft(fcg_cache* c, const fcg_lib* lib, const fcg_rope* rope, int32_t
     return fail(FCG_EINVAL, "a cache with FCG_ALIAS_V grafts from one library only");
   for (auto& sp : spans)
     if (lib->segs[sp.seg].tok_off < 0) return fail(FCG_ESTATE, "segment is not in device memory (fcg_lib_reload)");
+  Staged staged(c, new_pages);
   std::vector<int32_t> realiased;  // sequences of which a page mapped before now reads its values from the library
   if (c->plan.alias_v()) {
-    c->alias_lib = lib;
+    realiased.reserve(n_items);
     if (c->alias_segs.empty()) c->alias_segs.resize(c->n_seqs);
+    for (auto& sp : spans) {  // room for the segments that commit() notes
+      auto& a = c->alias_segs[sp.seq];
+      if (a.capacity() - a.size() < (size_t)n_items) a.reserve(std::max(2 * a.capacity(), a.size() + n_items));
+    }
+    staged.alias(lib, spans, &realiased);
+  }
+  auto commit = [&]() {
+    staged.keep();
     for (auto& sp : spans) {
-      if (c->plan.alias_pages(sp.seq, sp.dst, sp.len, lib->segs[sp.seg].tok_off)) realiased.push_back(sp.seq);
+      c->plan.mark_all_layers(sp.seq, sp.dst, sp.len);
+      if (!c->plan.alias_v()) continue;
       ++lib->segs[sp.seg].pins;  // its values may now be read in place: no offload until the sequence is reset
       c->alias_segs[sp.seq].push_back(sp.seg);
     }
-  }
-  if (c->layout_only()) {
-    c->plan.map_pages(new_pages);
-    for (auto& s : spans) c->plan.mark_all_layers(s.seq, s.dst, s.len);
     return FCG_OK;
-  }
+  };
+  staged.map();
+  if (c->layout_only()) return commit();
   HIP_TRY(hipSetDevice(c->device), "hipSetDevice");
   hipStream_t s = (hipStream_t)stream;
   Blob blob;
@@ -725,9 +731,8 @@ fcg_status graft(fcg_cache* c, const fcg_lib* lib, const fcg_rope* rope, int32_t
   const size_t o_chunks = by_value ? 0 : blob.add(chunks.data(), chunks.size() * sizeof(GraftChunk));
   const bool upload_plan = !by_value || !rows.empty();
   char* dev = nullptr;
-  size_t off = 0;
   if (upload_plan)
-    if (fcg_status st = upload(c, blob, rows, s, &dev, &off)) return st;
+    if (fcg_status st = upload(c, blob, rows, s, &dev, &staged)) return st;
   if (!(lib->flags & FCG_LAYOUT_ONLY))  // segments reloaded on another stream are in place first
     HIP_TRY(hipStreamWaitEvent(s, lib->reload_done, 0), "hipStreamWaitEvent");
   const KTime tg{timing_event(c), timing_event(c)};
@@ -741,9 +746,8 @@ fcg_status graft(fcg_cache* c, const fcg_lib* lib, const fcg_rope* rope, int32_t
   if (rc) return hip_fail((hipError_t)rc, "graft launch");
   if (!(lib->flags & FCG_LAYOUT_ONLY)) HIP_TRY(hipEventRecord(lib->graft_done, s), "hipEventRecord");
   if (upload_plan)
-    if (fcg_status st = c->ring.retire(off, blob.bytes.size(), s)) return st;
-  for (auto& sp : spans) c->plan.mark_all_layers(sp.seq, sp.dst, sp.len);
-  return FCG_OK;
+    if (fcg_status st = c->ring.retire(s)) return st;
+  return commit();
 }
 
 }  // namespace
@@ -916,6 +920,8 @@ fcg_status run_attention(fcg_cache* c, int32_t layer, const std::vector<TokenMet
     if (fcg_status st = grow((void**)&c->part, &c->part_bytes, (po + pml) * sizeof(float), "split partials")) return st;
   Blob blob;
   std::vector<std::pair<int32_t, size_t>> rows;
+  Staged staged(c, new_pages);
+  staged.map();
   stage_pages(c, new_pages, &blob, &rows);
   // fused calls take their whole plan by value: an upload (one more launch
   // before the kernel) only when the call maps new pages
@@ -923,9 +929,8 @@ fcg_status run_attention(fcg_cache* c, int32_t layer, const std::vector<TokenMet
   const size_t o_meta = fused ? 0 : blob.add(meta.data(), meta.size() * sizeof(TokenMeta));
   const size_t o_items = mfma ? 0 : blob.add(items.data(), items.size() * sizeof(AttnItem));
   char* dev = nullptr;
-  size_t off = 0;
   if (upload_plan)
-    if (fcg_status st = upload(c, blob, rows, s, &dev, &off)) return st;
+    if (fcg_status st = upload(c, blob, rows, s, &dev, &staged)) return st;
   const TokenMeta* dmeta = fused ? nullptr : (const TokenMeta*)(dev + o_meta);
   const CacheView cv = c->view();
   // timing: the append kernel opens the call's interval, the attention
@@ -972,7 +977,10 @@ fcg_status run_attention(fcg_cache* c, int32_t layer, const std::vector<TokenMet
   }
   time_open(c, FCG_TIME_PREFILL, e_call0);
   time_close(c, FCG_TIME_PREFILL, e_call1);
-  return upload_plan ? c->ring.retire(off, blob.bytes.size(), s) : FCG_OK;
+  if (upload_plan)
+    if (fcg_status st = c->ring.retire(s)) return st;
+  staged.keep();
+  return FCG_OK;
 }
 
 // One decode launch per group of up to kMaxDecodeSeqs sequences; the launch
@@ -1043,10 +1051,14 @@ fcg_status run_decode(fcg_cache* c, int32_t layer, int32_t n, const int32_t* seq
   if (fcg_status st = grow((void**)&c->dpart, &c->dpart_bytes, (plan.part_o + plan.part_ml) * sizeof(float),
                            "decode partials"))
     return st;
-  c->plan.map_pages(new_pages);
+  Staged staged(c, new_pages);
+  staged.map();
   const std::vector<int32_t> np = decode_new_pages(c, n, seqs, pos, new_pages);
-  return launch_decode_groups(c, layer, n, seqs, pos, np, plan, q, k, v, out, c->dpart, c->dpart + plan.part_o,
-                              c->d_count, c->timing, s);
+  if (fcg_status st = launch_decode_groups(c, layer, n, seqs, pos, np, plan, q, k, v, out, c->dpart,
+                                           c->dpart + plan.part_o, c->d_count, c->timing, s))
+    return st;
+  staged.keep();
+  return FCG_OK;
 }
 
 }  // namespace
@@ -1125,12 +1137,14 @@ fcg_status fcg_decode_noalloc(fcg_cache* c, int32_t layer, int32_t n_seqs, const
     hipStream_t s = (hipStream_t)stream;
     void* base = nullptr;
     if (int rc = noalloc_scratch(s, &base)) return hip_fail((hipError_t)rc, "static scratch");
-    c->plan.map_pages(new_pages);
+    Staged staged(c, new_pages);
+    staged.map();
     const std::vector<int32_t> np = decode_new_pages(c, n_seqs, seqs, pos, new_pages);
     float* po = reinterpret_cast<float*>(static_cast<char*>(base) + kNoAllocCountBytes);
     if (fcg_status st = launch_decode_groups(c, layer, n_seqs, seqs, pos, np, plan, q, k, v, out, po,
                                              po + plan.part_o, static_cast<int32_t*>(base), false, s))
       return st;
+    staged.keep();
   } else {
     c->plan.map_pages(new_pages);
   }

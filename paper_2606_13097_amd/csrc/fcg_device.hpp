@@ -2,6 +2,7 @@
 // conversion, 16-byte vector access, rotary angles.
 #pragma once
 
+#include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

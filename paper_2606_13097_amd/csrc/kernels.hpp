@@ -2,7 +2,6 @@
 // kernels.  Plain structs and pointers only.
 #pragma once
 
-#include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -49,11 +49,13 @@ inline size_t esize(int32_t dtype) { return dtype == FCG_F32 ? 4 : 2; }
 // Staging of per-call plans: a pinned host ring mirrored by a device ring.  A
 // call packs its arrays into one blob, which one kernel on the call's stream
 // takes from the host ring (upload), and records an event after its last kernel;
-// a region is reused only after its event.
+// a region is reused only after its event.  What can fail for want of memory is
+// done when a region is acquired, before the call launches anything.
 struct Ring {
   char* host = nullptr;
   char* dev = nullptr;
   size_t cap = 0, head = 0;
+  bool open = false;  // a region is acquired and not retired
   std::deque<std::tuple<size_t, size_t, hipEvent_t>> inflight;
   std::vector<hipEvent_t> spare;
 
@@ -82,6 +84,10 @@ struct Ring {
   }
   // Region [off, off + n) of both rings, free for writing.
   fcg_status acquire(size_t n, size_t* off) {
+    if (open) {  // by a call that failed before it could retire it: its kernels may still read it
+      HIP_TRY(hipDeviceSynchronize(), "hipDeviceSynchronize(staging)");
+      open = false;
+    }
     fcg_status st = reserve(n);
     if (st) return st;
     if (head + n > cap) head = 0;
@@ -95,20 +101,23 @@ struct Ring {
       spare.push_back(std::get<2>(*it));
       it = inflight.erase(it);
     }
+    if (spare.empty()) {
+      spare.reserve(inflight.size() + 1);  // room for every event to come back
+      hipEvent_t e;
+      HIP_TRY(hipEventCreateWithFlags(&e, hipEventDisableTiming), "hipEventCreate");
+      spare.push_back(e);
+    }
+    inflight.emplace_back(a, b, spare.back());
+    spare.pop_back();
+    open = true;
     head = b;
     *off = a;
     return FCG_OK;
   }
-  fcg_status retire(size_t off, size_t n, hipStream_t s) {
-    hipEvent_t e;
-    if (!spare.empty()) {
-      e = spare.back();
-      spare.pop_back();
-    } else {
-      HIP_TRY(hipEventCreateWithFlags(&e, hipEventDisableTiming), "hipEventCreate");
-    }
-    HIP_TRY(hipEventRecord(e, s), "hipEventRecord");
-    inflight.emplace_back(off, off + n, e);
+  // The last region acquired is free once the stream has come here.
+  fcg_status retire(hipStream_t s) {
+    HIP_TRY(hipEventRecord(std::get<2>(inflight.back()), s), "hipEventRecord");
+    open = false;
     return FCG_OK;
   }
 };
@@ -267,17 +276,57 @@ namespace fcg {
 // Enlarge a workspace (waits for the device when it replaces one).
 fcg_status grow(void** p, size_t* have, size_t need, const char* what);
 
-// After a planner check: map the new pages, and prepare the device copies of
-// the page-table rows that change (appended to the blob): those of the new
-// pages' sequences and of `seqs`.
+// What a call changes in the planner before its last step that can fail: taken
+// back when the call ends without keep().  Otherwise the planner would have pages
+// that the device table has not, which a later call would not enter, and read.
+class Staged {
+ public:
+  Staged(fcg_cache* c, const std::vector<std::pair<int32_t, int32_t>>& new_pages) : c_(c), pages_(new_pages) {}
+  Staged(const Staged&) = delete;
+  Staged& operator=(const Staged&) = delete;
+  ~Staged() {
+    if (!c_) return;
+    if (mapped_) c_->plan.unmap_pages(pages_);
+    if (!spans_) return;
+    for (const Span& x : *spans_) c_->plan.unalias_pages(x.seq, x.dst, x.len, sent_);
+    c_->alias_lib = bound_;
+  }
+  // Values of the pages that the spans cover read from the library.  *again (room for
+  // all spans) receives the sequences of which a page mapped before is among them.
+  void alias(const fcg_lib* lib, const std::vector<Span>& spans, std::vector<int32_t>* again) {
+    bound_ = c_->alias_lib;
+    spans_ = &spans;
+    c_->alias_lib = lib;
+    for (const Span& x : spans)
+      if (c_->plan.alias_pages(x.seq, x.dst, x.len, lib->segs[x.seg].tok_off)) again->push_back(x.seq);
+  }
+  void map() {
+    c_->plan.map_pages(pages_);
+    mapped_ = true;
+  }
+  void sent() { sent_ = true; }  // page rows may be in the device table from here on
+  void keep() { c_ = nullptr; }
+
+ private:
+  fcg_cache* c_;
+  const std::vector<std::pair<int32_t, int32_t>>& pages_;
+  const std::vector<Span>* spans_ = nullptr;
+  const fcg_lib* bound_ = nullptr;
+  bool mapped_ = false, sent_ = false;
+};
+
+// After the call's pages are mapped: prepare the device copies of the page-table
+// rows that change (appended to the blob): those of the new pages' sequences and
+// of `seqs`.
 void stage_pages(fcg_cache* c, const std::vector<std::pair<int32_t, int32_t>>& new_pages, Blob* blob,
                  std::vector<std::pair<int32_t, size_t>>* rows, std::vector<int32_t> seqs = {});
 
 // Upload a plan: the staged page rows (at the front of the blob, in the order
 // staged) into the device page table, the rest of the blob into the device ring,
-// both read by one small kernel from the pinned ring.  *dev and *off_out receive
-// the blob's place in the device ring.
+// both read by one small kernel from the pinned ring.  *dev receives the blob's place
+// in the device ring, which the caller retires after its last kernel.  staged (may be
+// null) learns that page rows are on their way.
 fcg_status upload(fcg_cache* c, const Blob& blob, const std::vector<std::pair<int32_t, size_t>>& rows, hipStream_t s,
-                  char** dev, size_t* off_out);
+                  char** dev, Staged* staged);
 
 }  // namespace fcg

@@ -248,14 +248,16 @@ fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_t
                                             &runs_of, &new_pages, &msg))
       return fail(st, msg);
     if (n_tok == 0 || n_layers == 0) return FCG_OK;
+    Staged staged(c, new_pages);
     auto commit = [&]() {
+      staged.keep();
       for (const Span& x : runs_of)
         for (int32_t l = layer; l < layer + n_layers; ++l) c->plan.mark_range(x.seq, l, x.dst, x.len);
+      return FCG_OK;
     };
     if (c->layout_only()) {
-      c->plan.map_pages(new_pages);
-      commit();
-      return FCG_OK;
+      staged.map();
+      return commit();
     }
     OnDevice dev(c->device);
     HIP_TRY(dev.err, "hipSetDevice");
@@ -306,8 +308,8 @@ fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_t
     }();
     const bool pairs = rope && rope->pairs();
     const float2* tab = rope ? nullptr : c->d_rope;
+    staged.map();
     if (by_value) {
-      c->plan.map_pages(new_pages);
       AppendArgs args;
       size_t np = 0;  // new_pages is sorted by (sequence, logical page)
       for (size_t i = 0; i < runs.size(); ++i) {
@@ -323,8 +325,7 @@ fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_t
       const int rc = launch_append(d.dtype, pairs, rows, args, (int)runs.size(), nullptr, n_groups, c->view(), layer, ra,
                                    tab, s);
       if (rc) return hip_fail((hipError_t)rc, "append launch");
-      commit();
-      return FCG_OK;
+      return commit();
     }
     Blob blob;
     std::vector<std::pair<int32_t, size_t>> page_rows;
@@ -342,15 +343,14 @@ fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_t
         }
     const size_t o_groups = blob.add(groups.data(), groups.size() * sizeof(AppendGroup));
     char* dplan = nullptr;
-    size_t off = 0;
-    if (fcg_status st = upload(c, blob, page_rows, s, &dplan, &off)) return st;
+    if (fcg_status st = upload(c, blob, page_rows, s, &dplan, &staged)) return st;
     if (has_k) {
       const int rc = launch_append(d.dtype, pairs, rows, AppendArgs{}, 0, (const AppendGroup*)(dplan + o_groups),
                                    (int)groups.size(), c->view(), layer, ra, tab, s);
       if (rc) return hip_fail((hipError_t)rc, "append launch");
     }
-    commit();
-    return c->ring.retire(off, blob.bytes.size(), s);
+    if (fcg_status st = c->ring.retire(s)) return st;
+    return commit();
   });
 }
 
@@ -667,16 +667,14 @@ fcg_status fcg_prefix_attend(fcg_cache* c, int32_t layer, int32_t prefix_seq, in
     pc.direct = p.direct;
     const PrefixItem* items = nullptr;
     const PrefixRank* ranks = nullptr;
-    size_t off = 0, n_blob = 0;
     if (!p.by_value) {
       Blob blob;
       const size_t o_items = blob.add(p.items.data(), p.items.size() * sizeof(PrefixItem));
       const size_t o_ranks = blob.add(p.ranks.data(), p.ranks.size() * sizeof(PrefixRank));
       char* dplan = nullptr;
-      if (fcg_status st = upload(c, blob, {}, s, &dplan, &off)) return st;
+      if (fcg_status st = upload(c, blob, {}, s, &dplan, nullptr)) return st;
       items = (const PrefixItem*)(dplan + o_items);
       ranks = (const PrefixRank*)(dplan + o_ranks);
-      n_blob = blob.bytes.size();
     }
     const PrefixArgs* args = p.by_value ? &p.args : nullptr;
     constexpr int kGridY = 65535;
@@ -687,6 +685,6 @@ fcg_status fcg_prefix_attend(fcg_cache* c, int32_t layer, int32_t prefix_seq, in
     if (merge)
       if (int rc = launch_prefix_merge(d.dtype, pc, args, ranks, n_tok, d.n_q_heads, d.head_dim, s))
         return hip_fail((hipError_t)rc, "prefix merge launch");
-    return p.by_value ? FCG_OK : c->ring.retire(off, n_blob, s);
+    return p.by_value ? FCG_OK : c->ring.retire(s);
   });
 }

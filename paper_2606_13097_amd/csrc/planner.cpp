@@ -276,6 +276,14 @@ void Planner::map_pages(const std::vector<std::pair<int32_t, int32_t>>& new_page
   for (auto& sl : new_pages) page_table_[(size_t)sl.first * NLP_ + sl.second] = take_page();
 }
 
+void Planner::unmap_pages(const std::vector<std::pair<int32_t, int32_t>>& new_pages) {
+  for (auto& sl : new_pages) {
+    int32_t& e = page_table_[(size_t)sl.first * NLP_ + sl.second];
+    if (e >= 0) return_page(e);
+    e = -1;
+  }
+}
+
 void Planner::mark(int32_t seq, int32_t layer, int32_t pos) {
   uint64_t& w = bits(seq, layer)[pos >> 6];
   uint64_t b = 1ull << (pos & 63);
@@ -313,6 +321,18 @@ bool Planner::alias_pages(int32_t seq, int32_t dst, int32_t len, int64_t lib_tok
     mapped |= page_table_[(size_t)seq * NLP_ + lp] >= 0;
   }
   return mapped;
+}
+
+void Planner::unalias_pages(int32_t seq, int32_t dst, int32_t len, bool unmap) {
+  if (!AV_) return;
+  for (int32_t lp = (dst + P_ - 1) / P_; (lp + 1) * P_ <= dst + len; ++lp) {
+    valias_[(size_t)seq * NLP_ + lp] = -1;
+    int32_t& e = page_table_[(size_t)seq * NLP_ + lp];
+    if (unmap && e >= 0) {
+      return_page(e);
+      e = -1;
+    }
+  }
 }
 
 void Planner::reset(int32_t seq) {

@@ -66,8 +66,10 @@ class Planner {
   fcg_status check_attend(int32_t layer, int32_t prefix_seq, int32_t prefix_len, int32_t n, const int32_t* seq,
                           const int32_t* pos, std::string* msg) const;
 
-  // Commits (after a successful check).
+  // Commits (after a successful check); nothing here allocates or fails.
   void map_pages(const std::vector<std::pair<int32_t, int32_t>>& new_pages);
+  // the last map_pages taken back: its pages return to the pool
+  void unmap_pages(const std::vector<std::pair<int32_t, int32_t>>& new_pages);
   void mark_all_layers(int32_t seq, int32_t dst, int32_t len);
   void mark_range(int32_t seq, int32_t layer, int32_t dst, int32_t len);
   // graft of len tokens at dst whose first token is library token lib_tok0:
@@ -76,6 +78,10 @@ class Planner {
   // already (a cut left it mapped and empty), so that the sequence's device row
   // changes although the call need not map a page of it
   bool alias_pages(int32_t seq, int32_t dst, int32_t len, int64_t lib_tok0);
+  // alias_pages taken back: these pages have values of their own again.  unmap:
+  // those of them that are mapped, which hold no written position, return to the
+  // pool (their device entries may name the library: mapped anew they are entered anew)
+  void unalias_pages(int32_t seq, int32_t dst, int32_t len, bool unmap);
   void mark(int32_t seq, int32_t layer, int32_t pos);
   void reset(int32_t seq);
   // keep [0, pos) in every layer (the caller checked the range); a split
