@@ -8,6 +8,7 @@
 #include <cstring>
 #include <deque>
 #include <map>
+#include <memory>
 #include <new>
 #include <string>
 #include <tuple>
@@ -245,37 +246,40 @@ fcg_status fcg_lib_create(const fcg_model_desc* desc, int64_t capacity_tokens, i
 
 fcg_status fcg_lib_add_segment(fcg_lib* lib, int32_t len, int32_t src_pos0, const void* k, const void* v,
                                void* stream, int32_t* seg_id) {
-  if (!lib) return fail(FCG_EINVAL, "null library");
-  if (len < 1) return fail(FCG_EINVAL, "segment length must be >= 1");
-  if (src_pos0 < 0) return fail(FCG_ERANGE, "negative source position");
-  if ((k == nullptr) != (v == nullptr)) return fail(FCG_EINVAL, "k and v must both be given or both be null");
-  if (k && (lib->flags & FCG_LAYOUT_ONLY)) return fail(FCG_EINVAL, "a layout-only library takes no data");
-  if ((int32_t)lib->segs.size() >= lib->max_segments) return fail(FCG_ENOMEM, "max_segments reached");
-  const bool reuse = !lib->free_tok.empty();
-  const int64_t off = lib->alloc(len);
-  if (off < 0) return fail(FCG_ENOMEM, "library capacity exhausted");
-  const Segment sg{off, len, src_pos0};
-  if (!(lib->flags & FCG_LAYOUT_ONLY)) {
-    HIP_TRY(hipSetDevice(lib->device), "hipSetDevice");
-    // a range an offload freed is written only after that offload has read it
-    // and after the last graft (which may have read it) has run
-    if (reuse) {
-      HIP_TRY(hipStreamWaitEvent((hipStream_t)stream, lib->freed, 0), "hipStreamWaitEvent");
-      HIP_TRY(hipStreamWaitEvent((hipStream_t)stream, lib->graft_done, 0), "hipStreamWaitEvent");
+  return guarded([&]() -> fcg_status {
+    if (!lib) return fail(FCG_EINVAL, "null library");
+    if (len < 1) return fail(FCG_EINVAL, "segment length must be >= 1");
+    if (src_pos0 < 0) return fail(FCG_ERANGE, "negative source position");
+    if ((k == nullptr) != (v == nullptr)) return fail(FCG_EINVAL, "k and v must both be given or both be null");
+    if (k && (lib->flags & FCG_LAYOUT_ONLY)) return fail(FCG_EINVAL, "a layout-only library takes no data");
+    if ((int32_t)lib->segs.size() >= lib->max_segments) return fail(FCG_ENOMEM, "max_segments reached");
+    if (lib->segs.size() == lib->segs.capacity()) lib->segs.reserve(std::max<size_t>(16, 2 * lib->segs.size()));
+    const bool reuse = !lib->free_tok.empty();
+    const int64_t off = lib->alloc(len);
+    if (off < 0) return fail(FCG_ENOMEM, "library capacity exhausted");
+    const Segment sg{off, len, src_pos0};
+    if (!(lib->flags & FCG_LAYOUT_ONLY)) {
+      HIP_TRY(hipSetDevice(lib->device), "hipSetDevice");
+      // a range an offload freed is written only after that offload has read it
+      // and after the last graft (which may have read it) has run
+      if (reuse) {
+        HIP_TRY(hipStreamWaitEvent((hipStream_t)stream, lib->freed, 0), "hipStreamWaitEvent");
+        HIP_TRY(hipStreamWaitEvent((hipStream_t)stream, lib->graft_done, 0), "hipStreamWaitEvent");
+      }
     }
-  }
-  if (k) {
-    const fcg_model_desc& d = lib->desc;
-    int rc = launch_lib_ingest(d.dtype, k, v, lib->k, lib->v, d.n_layers, len, d.n_kv_heads, d.head_dim, lib->cap,
-                               sg.tok_off, (hipStream_t)stream);
-    if (rc) {
-      lib->release(off, len);
-      return hip_fail((hipError_t)rc, "ingest launch");
+    if (k) {
+      const fcg_model_desc& d = lib->desc;
+      int rc = launch_lib_ingest(d.dtype, k, v, lib->k, lib->v, d.n_layers, len, d.n_kv_heads, d.head_dim, lib->cap,
+                                 sg.tok_off, (hipStream_t)stream);
+      if (rc) {
+        lib->release(off, len);
+        return hip_fail((hipError_t)rc, "ingest launch");
+      }
     }
-  }
-  lib->segs.push_back(sg);
-  if (seg_id) *seg_id = (int32_t)lib->segs.size() - 1;
-  return FCG_OK;
+    lib->segs.push_back(sg);
+    if (seg_id) *seg_id = (int32_t)lib->segs.size() - 1;
+    return FCG_OK;
+  });
 }
 
 fcg_status fcg_lib_host_reserve(fcg_lib* lib, int64_t host_tokens) {
@@ -319,55 +323,59 @@ fcg_status copy_segment(fcg_lib* lib, const Segment& sg, bool to_host, hipStream
 }  // namespace
 
 fcg_status fcg_lib_offload(fcg_lib* lib, int32_t seg_id, void* stream) {
-  if (!lib) return fail(FCG_EINVAL, "null library");
-  if (seg_id < 0 || seg_id >= (int32_t)lib->segs.size()) return fail(FCG_ERANGE, "segment id out of range");
-  Segment& sg = lib->segs[seg_id];
-  if (sg.tok_off < 0) return fail(FCG_ESTATE, "segment is not in device memory");
-  if (sg.pins) return fail(FCG_ESTATE, "a cache reads this segment's values in place (FCG_ALIAS_V)");
-  if (!lib->host_cap) return fail(FCG_ESTATE, "no host tier (fcg_lib_host_reserve)");
-  const bool copy = sg.host_off < 0;
-  if (copy && lib->host_used + sg.len > lib->host_cap) return fail(FCG_ENOMEM, "host tier full");
-  hipStream_t s = (hipStream_t)stream;
-  if (copy) {
-    sg.host_off = lib->host_used;
-    if (!(lib->flags & FCG_LAYOUT_ONLY)) {
-      HIP_TRY(hipSetDevice(lib->device), "hipSetDevice");
-      if (fcg_status st = copy_segment(lib, sg, true, s)) {
-        sg.host_off = -1;
-        return st;
+  return guarded([&]() -> fcg_status {
+    if (!lib) return fail(FCG_EINVAL, "null library");
+    if (seg_id < 0 || seg_id >= (int32_t)lib->segs.size()) return fail(FCG_ERANGE, "segment id out of range");
+    Segment& sg = lib->segs[seg_id];
+    if (sg.tok_off < 0) return fail(FCG_ESTATE, "segment is not in device memory");
+    if (sg.pins) return fail(FCG_ESTATE, "a cache reads this segment's values in place (FCG_ALIAS_V)");
+    if (!lib->host_cap) return fail(FCG_ESTATE, "no host tier (fcg_lib_host_reserve)");
+    const bool copy = sg.host_off < 0;
+    if (copy && lib->host_used + sg.len > lib->host_cap) return fail(FCG_ENOMEM, "host tier full");
+    hipStream_t s = (hipStream_t)stream;
+    if (copy) {
+      sg.host_off = lib->host_used;
+      if (!(lib->flags & FCG_LAYOUT_ONLY)) {
+        HIP_TRY(hipSetDevice(lib->device), "hipSetDevice");
+        if (fcg_status st = copy_segment(lib, sg, true, s)) {
+          sg.host_off = -1;
+          return st;
+        }
       }
+      lib->host_used += sg.len;
     }
-    lib->host_used += sg.len;
-  }
-  if (!(lib->flags & FCG_LAYOUT_ONLY)) HIP_TRY(hipEventRecord(lib->freed, s), "hipEventRecord");
-  lib->release(sg.tok_off, sg.len);
-  sg.tok_off = -1;
-  return FCG_OK;
+    if (!(lib->flags & FCG_LAYOUT_ONLY)) HIP_TRY(hipEventRecord(lib->freed, s), "hipEventRecord");
+    lib->release(sg.tok_off, sg.len);
+    sg.tok_off = -1;
+    return FCG_OK;
+  });
 }
 
 fcg_status fcg_lib_reload(fcg_lib* lib, int32_t seg_id, void* stream) {
-  if (!lib) return fail(FCG_EINVAL, "null library");
-  if (seg_id < 0 || seg_id >= (int32_t)lib->segs.size()) return fail(FCG_ERANGE, "segment id out of range");
-  Segment& sg = lib->segs[seg_id];
-  if (sg.tok_off >= 0) return fail(FCG_ESTATE, "segment is already in device memory");
-  const int64_t off = lib->alloc(sg.len);
-  if (off < 0) return fail(FCG_ENOMEM, "library capacity exhausted");
-  sg.tok_off = off;
-  if (!(lib->flags & FCG_LAYOUT_ONLY)) {
-    HIP_TRY(hipSetDevice(lib->device), "hipSetDevice");
-    hipStream_t s = (hipStream_t)stream;
-    fcg_status st = FCG_OK;
-    if (hipStreamWaitEvent(s, lib->freed, 0) != hipSuccess || hipStreamWaitEvent(s, lib->graft_done, 0) != hipSuccess)
-      st = fail(FCG_EHIP, "hipStreamWaitEvent");
-    if (!st) st = copy_segment(lib, sg, false, s);
-    if (!st && hipEventRecord(lib->reload_done, s) != hipSuccess) st = fail(FCG_EHIP, "hipEventRecord");
-    if (st) {
-      lib->release(off, sg.len);
-      sg.tok_off = -1;
-      return st;
+  return guarded([&]() -> fcg_status {
+    if (!lib) return fail(FCG_EINVAL, "null library");
+    if (seg_id < 0 || seg_id >= (int32_t)lib->segs.size()) return fail(FCG_ERANGE, "segment id out of range");
+    Segment& sg = lib->segs[seg_id];
+    if (sg.tok_off >= 0) return fail(FCG_ESTATE, "segment is already in device memory");
+    const int64_t off = lib->alloc(sg.len);
+    if (off < 0) return fail(FCG_ENOMEM, "library capacity exhausted");
+    sg.tok_off = off;
+    if (!(lib->flags & FCG_LAYOUT_ONLY)) {
+      HIP_TRY(hipSetDevice(lib->device), "hipSetDevice");
+      hipStream_t s = (hipStream_t)stream;
+      fcg_status st = FCG_OK;
+      if (hipStreamWaitEvent(s, lib->freed, 0) != hipSuccess || hipStreamWaitEvent(s, lib->graft_done, 0) != hipSuccess)
+        st = fail(FCG_EHIP, "hipStreamWaitEvent");
+      if (!st) st = copy_segment(lib, sg, false, s);
+      if (!st && hipEventRecord(lib->reload_done, s) != hipSuccess) st = fail(FCG_EHIP, "hipEventRecord");
+      if (st) {
+        lib->release(off, sg.len);
+        sg.tok_off = -1;
+        return st;
+      }
     }
-  }
-  return FCG_OK;
+    return FCG_OK;
+  });
 }
 
 fcg_status fcg_lib_segment_state(const fcg_lib* lib, int32_t seg_id, int32_t* in_device, int32_t* on_host) {
@@ -381,49 +389,51 @@ fcg_status fcg_lib_segment_state(const fcg_lib* lib, int32_t seg_id, int32_t* in
 
 fcg_status fcg_lib_update_residency(fcg_lib* lib, const fcg_locality* loc, int64_t budget_bytes, double ppl_threshold,
                                     void* stream, int32_t* n_offloaded, int32_t* n_reloaded) {
-  if (!lib || !loc) return fail(FCG_EINVAL, "null library or scorer");
-  const int32_t n = (int32_t)lib->segs.size();
-  if (locality_size(loc) != n) return fail(FCG_EINVAL, "the scorer must track one function per library segment");
-  if (!(ppl_threshold >= 0)) return fail(FCG_EINVAL, "the perplexity threshold must be >= 0");
-  const fcg_model_desc& d = lib->desc;
-  const int64_t b_tok = 2LL * d.n_layers * d.n_kv_heads * d.head_dim * (int64_t)esize(d.dtype);  // K+V, all layers
-  if (budget_bytes < 0) {
-    // the hyperparameter table's GPU memory threshold and reserve: 0.85 of the
-    // device memory, less 2 GB, less what the rest of the process holds; never
-    // more than the slabs
-    budget_bytes = lib->cap * b_tok;
-    if (!(lib->flags & FCG_LAYOUT_ONLY)) {
-      HIP_TRY(hipSetDevice(lib->device), "hipSetDevice");
-      size_t free_b = 0, total_b = 0;
-      HIP_TRY(hipMemGetInfo(&free_b, &total_b), "hipMemGetInfo");
-      const int64_t others = (int64_t)(total_b - free_b) - lib->cap * b_tok;
-      const int64_t limit = (int64_t)(0.85 * (double)total_b) - (2LL << 30) - std::max<int64_t>(others, 0);
-      budget_bytes = std::max<int64_t>(0, std::min(budget_bytes, limit));
+  return guarded([&]() -> fcg_status {
+    if (!lib || !loc) return fail(FCG_EINVAL, "null library or scorer");
+    const int32_t n = (int32_t)lib->segs.size();
+    if (locality_size(loc) != n) return fail(FCG_EINVAL, "the scorer must track one function per library segment");
+    if (!(ppl_threshold >= 0)) return fail(FCG_EINVAL, "the perplexity threshold must be >= 0");
+    const fcg_model_desc& d = lib->desc;
+    const int64_t b_tok = 2LL * d.n_layers * d.n_kv_heads * d.head_dim * (int64_t)esize(d.dtype);  // K+V, all layers
+    if (budget_bytes < 0) {
+      // the hyperparameter table's GPU memory threshold and reserve: 0.85 of the
+      // device memory, less 2 GB, less what the rest of the process holds; never
+      // more than the slabs
+      budget_bytes = lib->cap * b_tok;
+      if (!(lib->flags & FCG_LAYOUT_ONLY)) {
+        HIP_TRY(hipSetDevice(lib->device), "hipSetDevice");
+        size_t free_b = 0, total_b = 0;
+        HIP_TRY(hipMemGetInfo(&free_b, &total_b), "hipMemGetInfo");
+        const int64_t others = (int64_t)(total_b - free_b) - lib->cap * b_tok;
+        const int64_t limit = (int64_t)(0.85 * (double)total_b) - (2LL << 30) - std::max<int64_t>(others, 0);
+        budget_bytes = std::max<int64_t>(0, std::min(budget_bytes, limit));
+      }
     }
-  }
-  std::vector<int64_t> cost(n);
-  std::vector<uint8_t> pinned(n), keep(n);
-  for (int32_t f = 0; f < n; ++f) {
-    cost[f] = lib->segs[f].len * b_tok;
-    pinned[f] = lib->segs[f].pins > 0;
-  }
-  if (fcg_status st = locality_residency(loc, budget_bytes, cost.data(), ppl_threshold, pinned.data(), keep.data()))
-    return st;
-  int32_t n_off = 0, n_re = 0;
-  // offloads first: they free the ranges the reloads may take
-  for (int32_t f = 0; f < n; ++f)
-    if (!keep[f] && lib->segs[f].tok_off >= 0) {
-      if (fcg_status st = fcg_lib_offload(lib, f, stream)) return st;
-      ++n_off;
+    std::vector<int64_t> cost(n);
+    std::vector<uint8_t> pinned(n), keep(n);
+    for (int32_t f = 0; f < n; ++f) {
+      cost[f] = lib->segs[f].len * b_tok;
+      pinned[f] = lib->segs[f].pins > 0;
     }
-  for (int32_t f = 0; f < n; ++f)
-    if (keep[f] && lib->segs[f].tok_off < 0) {
-      if (fcg_status st = fcg_lib_reload(lib, f, stream)) return st;
-      ++n_re;
-    }
-  if (n_offloaded) *n_offloaded = n_off;
-  if (n_reloaded) *n_reloaded = n_re;
-  return FCG_OK;
+    if (fcg_status st = locality_residency(loc, budget_bytes, cost.data(), ppl_threshold, pinned.data(), keep.data()))
+      return st;
+    int32_t n_off = 0, n_re = 0;
+    // offloads first: they free the ranges the reloads may take
+    for (int32_t f = 0; f < n; ++f)
+      if (!keep[f] && lib->segs[f].tok_off >= 0) {
+        if (fcg_status st = fcg_lib_offload(lib, f, stream)) return st;
+        ++n_off;
+      }
+    for (int32_t f = 0; f < n; ++f)
+      if (keep[f] && lib->segs[f].tok_off < 0) {
+        if (fcg_status st = fcg_lib_reload(lib, f, stream)) return st;
+        ++n_re;
+      }
+    if (n_offloaded) *n_offloaded = n_off;
+    if (n_reloaded) *n_reloaded = n_re;
+    return FCG_OK;
+  });
 }
 
 fcg_status fcg_lib_segment_info(const fcg_lib* lib, int32_t seg_id, int64_t* tok_off, int32_t* len,
@@ -470,56 +480,47 @@ fcg_status fcg_lib_destroy(fcg_lib* lib) {
 
 fcg_status fcg_cache_create(const fcg_model_desc* desc, int32_t n_seqs, int32_t max_tokens, int32_t page_size,
                             int32_t n_pages, uint32_t flags, fcg_cache** out) {
-  if (!out) return fail(FCG_EINVAL, "null output handle");
-  if (fcg_status st = check_desc(desc)) return st;
-  if (n_seqs < 1 || max_tokens < 1) return fail(FCG_EINVAL, "n_seqs and max_tokens must be >= 1");
-  if ((int64_t)max_tokens * desc->head_dim >= ((int64_t)1 << 31))
-    return fail(FCG_EINVAL, "max_tokens * head_dim must stay below 2^31");
-  if (page_size != 0 && page_size != 16) return fail(FCG_EINVAL, "page_size must be 0 (contiguous) or 16");
-  if (page_size && n_pages < 1) return fail(FCG_EINVAL, "a paged cache needs n_pages >= 1");
-  if (flags & ~(FCG_LAYOUT_ONLY | FCG_ALIAS_V)) return fail(FCG_EINVAL, "unknown flags");
-  if ((flags & FCG_ALIAS_V) && !page_size) return fail(FCG_EINVAL, "FCG_ALIAS_V needs a paged cache");
-  fcg_cache* c = new (std::nothrow) fcg_cache(*desc, n_seqs, max_tokens, page_size, page_size ? n_pages : 0, flags);
-  if (!c) return fail(FCG_ENOMEM, "host allocation");
-  if (!c->layout_only()) {
-    hipGetDevice(&c->device);
-    const int64_t per_layer = page_size ? (int64_t)n_pages * desc->n_kv_heads * page_size * desc->head_dim
-                                        : (int64_t)n_seqs * desc->n_kv_heads * max_tokens * desc->head_dim;
-    c->layer_stride = per_layer;
-    const size_t bytes = (size_t)per_layer * desc->n_layers * esize(desc->dtype);
-    bool ok = hipMalloc(&c->k, bytes) == hipSuccess && hipMalloc(&c->v, bytes) == hipSuccess;
-    if (ok && page_size) {
-      const size_t pt = (size_t)n_seqs * 2 * c->plan.n_logical_pages() * sizeof(int32_t);
-      ok = hipMalloc((void**)&c->d_page_table, pt) == hipSuccess && hipMemset(c->d_page_table, 0xFF, pt) == hipSuccess;
+  return guarded([&]() -> fcg_status {
+    if (!out) return fail(FCG_EINVAL, "null output handle");
+    if (fcg_status st = check_desc(desc)) return st;
+    if (n_seqs < 1 || max_tokens < 1) return fail(FCG_EINVAL, "n_seqs and max_tokens must be >= 1");
+    if ((int64_t)max_tokens * desc->head_dim >= ((int64_t)1 << 31))
+      return fail(FCG_EINVAL, "max_tokens * head_dim must stay below 2^31");
+    if (page_size != 0 && page_size != 16) return fail(FCG_EINVAL, "page_size must be 0 (contiguous) or 16");
+    if (page_size && n_pages < 1) return fail(FCG_EINVAL, "a paged cache needs n_pages >= 1");
+    if (flags & ~(FCG_LAYOUT_ONLY | FCG_ALIAS_V)) return fail(FCG_EINVAL, "unknown flags");
+    if ((flags & FCG_ALIAS_V) && !page_size) return fail(FCG_EINVAL, "FCG_ALIAS_V needs a paged cache");
+    std::unique_ptr<fcg_cache, decltype(&fcg_cache_destroy)> owner(
+        new fcg_cache(*desc, n_seqs, max_tokens, page_size, page_size ? n_pages : 0, flags), fcg_cache_destroy);
+    fcg_cache* c = owner.get();
+    if (!c->layout_only()) {
+      hipGetDevice(&c->device);
+      const int64_t per_layer = page_size ? (int64_t)n_pages * desc->n_kv_heads * page_size * desc->head_dim
+                                          : (int64_t)n_seqs * desc->n_kv_heads * max_tokens * desc->head_dim;
+      c->layer_stride = per_layer;
+      const size_t bytes = (size_t)per_layer * desc->n_layers * esize(desc->dtype);
+      bool ok = hipMalloc(&c->k, bytes) == hipSuccess && hipMalloc(&c->v, bytes) == hipSuccess;
+      if (ok && page_size) {
+        const size_t pt = (size_t)n_seqs * 2 * c->plan.n_logical_pages() * sizeof(int32_t);
+        ok = hipMalloc((void**)&c->d_page_table, pt) == hipSuccess && hipMemset(c->d_page_table, 0xFF, pt) == hipSuccess;
+      }
+      if (ok) {
+        const size_t nc = (size_t)kMaxDecodeSeqs * desc->n_kv_heads * kCountStride * sizeof(int32_t);
+        ok = hipMalloc((void**)&c->d_count, nc) == hipSuccess && hipMemset(c->d_count, 0, nc) == hipSuccess;
+      }
+      if (!ok) return fail(FCG_ENOMEM, "cache does not fit in device memory");
+      if (fcg_status st = upload_inv_freq(*desc, &c->d_inv_freq)) return st;
+      // rotary table of every position the cache can hold, computed once here
+      const int half = desc->head_dim / 2;
+      if (hipMalloc((void**)&c->d_rope, (size_t)max_tokens * half * sizeof(float2)) != hipSuccess)
+        return fail(FCG_ENOMEM, "rotary table does not fit in device memory");
+      int rc = launch_rope_table(c->d_inv_freq, half, max_tokens, c->d_rope, nullptr);
+      if (rc == 0) rc = (int)hipStreamSynchronize(nullptr);
+      if (rc) return hip_fail((hipError_t)rc, "rotary table");
     }
-    if (ok) {
-      const size_t nc = (size_t)kMaxDecodeSeqs * desc->n_kv_heads * kCountStride * sizeof(int32_t);
-      ok = hipMalloc((void**)&c->d_count, nc) == hipSuccess && hipMemset(c->d_count, 0, nc) == hipSuccess;
-    }
-    if (!ok) {
-      fcg_cache_destroy(c);
-      return fail(FCG_ENOMEM, "cache does not fit in device memory");
-    }
-    if (fcg_status st = upload_inv_freq(*desc, &c->d_inv_freq)) {
-      fcg_cache_destroy(c);
-      return st;
-    }
-    // rotary table of every position the cache can hold, computed once here
-    const int half = desc->head_dim / 2;
-    if (hipMalloc((void**)&c->d_rope, (size_t)max_tokens * half * sizeof(float2)) != hipSuccess) {
-      fcg_cache_destroy(c);
-      return fail(FCG_ENOMEM, "rotary table does not fit in device memory");
-    }
-    int rc = launch_rope_table(c->d_inv_freq, half, max_tokens, c->d_rope, nullptr);
-    if (rc == 0) rc = (int)hipStreamSynchronize(nullptr);
-    if (rc) {
-      fcg_cache_destroy(c);
-      return hip_fail((hipError_t)rc, "rotary table");
-    }
-
-  }
-  *out = c;
-  return FCG_OK;
+    *out = owner.release();
+    return FCG_OK;
+  });
 }
 
 fcg_status fcg_cache_reset(fcg_cache* c, int32_t seq) {
@@ -537,27 +538,34 @@ fcg_status fcg_cache_reset(fcg_cache* c, int32_t seq) {
 }
 
 fcg_status fcg_cache_truncate(fcg_cache* c, int32_t seq, int32_t pos, void* stream) {
-  if (!c) return fail(FCG_EINVAL, "null cache");
-  if (seq < 0 || seq >= c->n_seqs) return fail(FCG_ERANGE, "sequence out of range");
-  if (pos < 0 || pos > c->max_tokens) return fail(FCG_ERANGE, "position out of range");
-  std::vector<Unalias> un;
-  c->plan.truncate(seq, pos, &un);  // freed page-table rows: as for fcg_cache_reset
-  if (un.empty() || c->layout_only()) return FCG_OK;
-  // a value page mapped onto the library and split by the cut: copy its kept
-  // rows into the page and upload the sequence's row without the alias
-  HIP_TRY(hipSetDevice(c->device), "hipSetDevice");
-  hipStream_t s = (hipStream_t)stream;
-  Blob blob;
-  std::vector<std::pair<int32_t, size_t>> rows{{seq, stage_row(c, seq, &blob)}};
-  std::vector<UnaliasItem> items;
-  for (const Unalias& u : un) items.push_back(UnaliasItem{u.lib_tok, u.page, u.rows});
-  const size_t o_items = blob.add(items.data(), items.size() * sizeof(UnaliasItem));
-  char* dev;
-  if (fcg_status st = upload(c, blob, rows, s, &dev, nullptr)) return st;
-  int rc = launch_unalias(c->desc.dtype, (const UnaliasItem*)(dev + o_items), (int)items.size(), c->alias_lib->v,
-                          c->alias_lib->cap, c->view(), c->desc.n_layers, s);
-  if (rc) return hip_fail((hipError_t)rc, "unalias launch");
-  return c->ring.retire(s);
+  return guarded([&]() -> fcg_status {
+    if (!c) return fail(FCG_EINVAL, "null cache");
+    if (seq < 0 || seq >= c->n_seqs) return fail(FCG_ERANGE, "sequence out of range");
+    if (pos < 0 || pos > c->max_tokens) return fail(FCG_ERANGE, "position out of range");
+    Unalias cut;
+    if (c->plan.splits_alias(seq, pos, &cut) && !c->layout_only()) {
+      // a value page mapped onto the library and split by the cut: copy its kept
+      // rows into the page and upload the sequence's row without the alias (before the
+      // planner forgets it: a failure here leaves the sequence as it was)
+      HIP_TRY(hipSetDevice(c->device), "hipSetDevice");
+      hipStream_t s = (hipStream_t)stream;
+      Blob blob;
+      std::vector<std::pair<int32_t, size_t>> rows{{seq, stage_row(c, seq, &blob)}};
+      const int32_t own = -1;
+      std::memcpy(blob.bytes.data() + rows[0].second + sizeof(int32_t) * (c->plan.n_logical_pages() + pos / 16), &own,
+                  sizeof own);
+      const UnaliasItem item{cut.lib_tok, cut.page, cut.rows};
+      const size_t o_item = blob.add(&item, sizeof item);
+      char* dev;
+      if (fcg_status st = upload(c, blob, rows, s, &dev, nullptr)) return st;
+      int rc = launch_unalias(c->desc.dtype, (const UnaliasItem*)(dev + o_item), 1, c->alias_lib->v, c->alias_lib->cap,
+                              c->view(), c->desc.n_layers, s);
+      if (rc) return hip_fail((hipError_t)rc, "unalias launch");
+      if (fcg_status st = c->ring.retire(s)) return st;
+    }
+    c->plan.truncate(seq, pos);  // freed page-table rows: as for fcg_cache_reset
+    return FCG_OK;
+  });
 }
 
 fcg_status fcg_cache_export_v_alias(const fcg_cache* c, int32_t seq, int32_t* v_alias) {
@@ -597,25 +605,27 @@ fcg_status fcg_cache_timing(fcg_cache* c, int32_t enable) {
 }
 
 fcg_status fcg_cache_timing_read(fcg_cache* c, int32_t kind, int32_t* count, double* total_ms) {
-  if (!c) return fail(FCG_EINVAL, "null cache");
-  if (kind < 0 || kind > FCG_TIME_DECODE_ATTN) return fail(FCG_ERANGE, "unknown timing kind");
-  double ms = 0.0;
-  int32_t n = 0;
-  for (auto& sp : c->spans[kind]) {
-    if (sp.second) {
-      HIP_TRY(hipEventSynchronize(sp.second), "hipEventSynchronize(timing)");
-      float t = 0.f;
-      HIP_TRY(hipEventElapsedTime(&t, sp.first, sp.second), "hipEventElapsedTime");
-      ms += t;
-      ++n;
-      event_put(c, sp.second);
+  return guarded([&]() -> fcg_status {
+    if (!c) return fail(FCG_EINVAL, "null cache");
+    if (kind < 0 || kind > FCG_TIME_DECODE_ATTN) return fail(FCG_ERANGE, "unknown timing kind");
+    double ms = 0.0;
+    int32_t n = 0;
+    for (auto& sp : c->spans[kind]) {
+      if (sp.second) {
+        HIP_TRY(hipEventSynchronize(sp.second), "hipEventSynchronize(timing)");
+        float t = 0.f;
+        HIP_TRY(hipEventElapsedTime(&t, sp.first, sp.second), "hipEventElapsedTime");
+        ms += t;
+        ++n;
+        event_put(c, sp.second);
+      }
+      event_put(c, sp.first);
     }
-    event_put(c, sp.first);
-  }
-  c->spans[kind].clear();
-  if (count) *count = n;
-  if (total_ms) *total_ms = ms;
-  return FCG_OK;
+    c->spans[kind].clear();
+    if (count) *count = n;
+    if (total_ms) *total_ms = ms;
+    return FCG_OK;
+  });
 }
 
 fcg_status fcg_cache_destroy(fcg_cache* c) {
@@ -1065,94 +1075,100 @@ fcg_status run_decode(fcg_cache* c, int32_t layer, int32_t n, const int32_t* seq
 
 fcg_status fcg_patch_prefill(fcg_cache* c, int32_t layer, int32_t n_tok, const int32_t* seq, const int32_t* pos,
                              const void* q, const void* k, const void* v, void* out, void* stream) {
-  if (!c) return fail(FCG_EINVAL, "null cache");
-  if (n_tok < 0) return fail(FCG_EINVAL, "negative token count");
-  if (n_tok > 0 && (!seq || !pos)) return fail(FCG_EINVAL, "null token array");
-  if (n_tok > 0 && !c->layout_only() && (!q || !k || !v || !out)) return fail(FCG_EINVAL, "null tensor");
-  std::vector<std::pair<int32_t, int32_t>> new_pages;
-  std::string msg;
-  if (fcg_status st = c->plan.check_append(layer, n_tok, seq, pos, &new_pages, &msg)) return fail(st, msg);
-  if (n_tok == 0) return FCG_OK;
-  if (c->layout_only()) {
-    c->plan.map_pages(new_pages);
+  return guarded([&]() -> fcg_status {
+    if (!c) return fail(FCG_EINVAL, "null cache");
+    if (n_tok < 0) return fail(FCG_EINVAL, "negative token count");
+    if (n_tok > 0 && (!seq || !pos)) return fail(FCG_EINVAL, "null token array");
+    if (n_tok > 0 && !c->layout_only() && (!q || !k || !v || !out)) return fail(FCG_EINVAL, "null tensor");
+    std::vector<std::pair<int32_t, int32_t>> new_pages;
+    std::string msg;
+    if (fcg_status st = c->plan.check_append(layer, n_tok, seq, pos, &new_pages, &msg)) return fail(st, msg);
+    if (n_tok == 0) return FCG_OK;
+    if (c->layout_only()) {
+      c->plan.map_pages(new_pages);
+      for (int32_t t = 0; t < n_tok; ++t) c->plan.mark(seq[t], layer, pos[t]);
+      return FCG_OK;
+    }
+    HIP_TRY(hipSetDevice(c->device), "hipSetDevice");
+    std::vector<TokenMeta> meta(n_tok);
+    for (int32_t t = 0; t < n_tok; ++t) meta[t] = TokenMeta{t, seq[t], pos[t], 0};
+    std::sort(meta.begin(), meta.end(), [](const TokenMeta& a, const TokenMeta& b) {
+      return a.seq != b.seq ? a.seq < b.seq : a.pos < b.pos;
+    });
+    if (fcg_status st = run_attention(c, layer, meta, q, k, v, out, new_pages, (hipStream_t)stream)) return st;
     for (int32_t t = 0; t < n_tok; ++t) c->plan.mark(seq[t], layer, pos[t]);
     return FCG_OK;
-  }
-  HIP_TRY(hipSetDevice(c->device), "hipSetDevice");
-  std::vector<TokenMeta> meta(n_tok);
-  for (int32_t t = 0; t < n_tok; ++t) meta[t] = TokenMeta{t, seq[t], pos[t], 0};
-  std::sort(meta.begin(), meta.end(), [](const TokenMeta& a, const TokenMeta& b) {
-    return a.seq != b.seq ? a.seq < b.seq : a.pos < b.pos;
   });
-  if (fcg_status st = run_attention(c, layer, meta, q, k, v, out, new_pages, (hipStream_t)stream)) return st;
-  for (int32_t t = 0; t < n_tok; ++t) c->plan.mark(seq[t], layer, pos[t]);
-  return FCG_OK;
 }
 
 fcg_status fcg_decode(fcg_cache* c, int32_t layer, int32_t n_seqs, const int32_t* seqs, const void* q,
                       const void* k, const void* v, void* out, int32_t* positions_out, void* stream) {
-  if (!c) return fail(FCG_EINVAL, "null cache");
-  if (n_seqs < 0) return fail(FCG_EINVAL, "negative sequence count");
-  if (n_seqs > 0 && !seqs) return fail(FCG_EINVAL, "null sequence array");
-  if (n_seqs > 0 && !c->layout_only() && (!q || !k || !v || !out)) return fail(FCG_EINVAL, "null tensor");
-  std::vector<int32_t> pos;
-  std::vector<std::pair<int32_t, int32_t>> new_pages;
-  std::string msg;
-  if (fcg_status st = c->plan.check_decode(layer, n_seqs, seqs, &pos, &new_pages, &msg)) return fail(st, msg);
-  if (n_seqs == 0) return FCG_OK;
-  if (!c->layout_only()) {
-    HIP_TRY(hipSetDevice(c->device), "hipSetDevice");
-    if (fcg_status st = run_decode(c, layer, n_seqs, seqs, pos, q, k, v, out, new_pages, (hipStream_t)stream))
-      return st;
-  } else {
-    c->plan.map_pages(new_pages);
-  }
-  for (int32_t i = 0; i < n_seqs; ++i) {
-    c->plan.mark(seqs[i], layer, pos[i]);
-    if (positions_out) positions_out[i] = pos[i];
-  }
-  return FCG_OK;
+  return guarded([&]() -> fcg_status {
+    if (!c) return fail(FCG_EINVAL, "null cache");
+    if (n_seqs < 0) return fail(FCG_EINVAL, "negative sequence count");
+    if (n_seqs > 0 && !seqs) return fail(FCG_EINVAL, "null sequence array");
+    if (n_seqs > 0 && !c->layout_only() && (!q || !k || !v || !out)) return fail(FCG_EINVAL, "null tensor");
+    std::vector<int32_t> pos;
+    std::vector<std::pair<int32_t, int32_t>> new_pages;
+    std::string msg;
+    if (fcg_status st = c->plan.check_decode(layer, n_seqs, seqs, &pos, &new_pages, &msg)) return fail(st, msg);
+    if (n_seqs == 0) return FCG_OK;
+    if (!c->layout_only()) {
+      HIP_TRY(hipSetDevice(c->device), "hipSetDevice");
+      if (fcg_status st = run_decode(c, layer, n_seqs, seqs, pos, q, k, v, out, new_pages, (hipStream_t)stream))
+        return st;
+    } else {
+      c->plan.map_pages(new_pages);
+    }
+    for (int32_t i = 0; i < n_seqs; ++i) {
+      c->plan.mark(seqs[i], layer, pos[i]);
+      if (positions_out) positions_out[i] = pos[i];
+    }
+    return FCG_OK;
+  });
 }
 
 fcg_status fcg_decode_noalloc(fcg_cache* c, int32_t layer, int32_t n_seqs, const int32_t* seqs, const void* q,
                               const void* k, const void* v, void* out, int32_t* positions_out, void* stream) {
-  if (!c) return fail(FCG_EINVAL, "null cache");
-  if (n_seqs < 0) return fail(FCG_EINVAL, "negative sequence count");
-  if (n_seqs > 0 && !seqs) return fail(FCG_EINVAL, "null sequence array");
-  if (n_seqs > 0 && !c->layout_only() && (!q || !k || !v || !out)) return fail(FCG_EINVAL, "null tensor");
-  if (c->desc.n_kv_heads > kNoAllocMaxKvHeads)
-    return fail(FCG_EINVAL, "fcg_decode_noalloc supports at most " + std::to_string(kNoAllocMaxKvHeads) + " kv heads");
-  std::vector<int32_t> pos;
-  std::vector<std::pair<int32_t, int32_t>> new_pages;
-  std::string msg;
-  if (fcg_status st = c->plan.check_decode(layer, n_seqs, seqs, &pos, &new_pages, &msg)) return fail(st, msg);
-  if (n_seqs == 0) return FCG_OK;
-  const DecodePlan plan = plan_decode(c->desc, pos, kMaxDecodeSeqs);
-  const size_t need = (plan.part_o + plan.part_ml) * sizeof(float);
-  if (need > kNoAllocPartBytes)
-    return fail(FCG_ENOMEM, "this step needs " + std::to_string(need) + " bytes of split partials; the static scratch of "
-                                "fcg_decode_noalloc holds " + std::to_string(kNoAllocPartBytes) + " (use fcg_decode)");
-  if (!c->layout_only()) {
-    HIP_TRY(hipSetDevice(c->device), "hipSetDevice");
-    hipStream_t s = (hipStream_t)stream;
-    void* base = nullptr;
-    if (int rc = noalloc_scratch(s, &base)) return hip_fail((hipError_t)rc, "static scratch");
-    Staged staged(c, new_pages);
-    staged.map();
-    const std::vector<int32_t> np = decode_new_pages(c, n_seqs, seqs, pos, new_pages);
-    float* po = reinterpret_cast<float*>(static_cast<char*>(base) + kNoAllocCountBytes);
-    if (fcg_status st = launch_decode_groups(c, layer, n_seqs, seqs, pos, np, plan, q, k, v, out, po,
-                                             po + plan.part_o, static_cast<int32_t*>(base), false, s))
-      return st;
-    staged.keep();
-  } else {
-    c->plan.map_pages(new_pages);
-  }
-  for (int32_t i = 0; i < n_seqs; ++i) {
-    c->plan.mark(seqs[i], layer, pos[i]);
-    if (positions_out) positions_out[i] = pos[i];
-  }
-  return FCG_OK;
+  return guarded([&]() -> fcg_status {
+    if (!c) return fail(FCG_EINVAL, "null cache");
+    if (n_seqs < 0) return fail(FCG_EINVAL, "negative sequence count");
+    if (n_seqs > 0 && !seqs) return fail(FCG_EINVAL, "null sequence array");
+    if (n_seqs > 0 && !c->layout_only() && (!q || !k || !v || !out)) return fail(FCG_EINVAL, "null tensor");
+    if (c->desc.n_kv_heads > kNoAllocMaxKvHeads)
+      return fail(FCG_EINVAL, "fcg_decode_noalloc supports at most " + std::to_string(kNoAllocMaxKvHeads) + " kv heads");
+    std::vector<int32_t> pos;
+    std::vector<std::pair<int32_t, int32_t>> new_pages;
+    std::string msg;
+    if (fcg_status st = c->plan.check_decode(layer, n_seqs, seqs, &pos, &new_pages, &msg)) return fail(st, msg);
+    if (n_seqs == 0) return FCG_OK;
+    const DecodePlan plan = plan_decode(c->desc, pos, kMaxDecodeSeqs);
+    const size_t need = (plan.part_o + plan.part_ml) * sizeof(float);
+    if (need > kNoAllocPartBytes)
+      return fail(FCG_ENOMEM, "this step needs " + std::to_string(need) + " bytes of split partials; the static scratch of "
+                                  "fcg_decode_noalloc holds " + std::to_string(kNoAllocPartBytes) + " (use fcg_decode)");
+    if (!c->layout_only()) {
+      HIP_TRY(hipSetDevice(c->device), "hipSetDevice");
+      hipStream_t s = (hipStream_t)stream;
+      void* base = nullptr;
+      if (int rc = noalloc_scratch(s, &base)) return hip_fail((hipError_t)rc, "static scratch");
+      Staged staged(c, new_pages);
+      staged.map();
+      const std::vector<int32_t> np = decode_new_pages(c, n_seqs, seqs, pos, new_pages);
+      float* po = reinterpret_cast<float*>(static_cast<char*>(base) + kNoAllocCountBytes);
+      if (fcg_status st = launch_decode_groups(c, layer, n_seqs, seqs, pos, np, plan, q, k, v, out, po,
+                                               po + plan.part_o, static_cast<int32_t*>(base), false, s))
+        return st;
+      staged.keep();
+    } else {
+      c->plan.map_pages(new_pages);
+    }
+    for (int32_t i = 0; i < n_seqs; ++i) {
+      c->plan.mark(seqs[i], layer, pos[i]);
+      if (positions_out) positions_out[i] = pos[i];
+    }
+    return FCG_OK;
+  });
 }
 
 }  // extern "C"

@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <cmath>
 #include <deque>
+#include <memory>
 #include <new>
 #include <numeric>
 #include <string>
@@ -102,25 +103,30 @@ extern "C" {
 
 fcg_status fcg_locality_create(int32_t n_funcs, int32_t window, double alpha, double beta, double gamma,
                                fcg_locality** out) {
-  if (!out) return fcg::report(FCG_EINVAL, "null output handle");
-  if (n_funcs < 1 || window < 1) return fcg::report(FCG_EINVAL, "n_funcs and window must be >= 1");
-  if (!(alpha >= 0 && beta >= 0 && gamma >= 0) || std::fabs(alpha + beta + gamma - 1.0) > 1e-9)
-    return fcg::report(FCG_EINVAL, "alpha, beta, gamma must be >= 0 and sum to 1");
-  fcg_locality* L = new (std::nothrow) fcg_locality{n_funcs, window, alpha, beta, gamma, {}, {}};
-  if (!L) return fcg::report(FCG_ENOMEM, "host allocation");
-  L->ppl.assign(n_funcs, 0.0);
-  *out = L;
-  return FCG_OK;
+  return fcg::guarded([&]() -> fcg_status {
+    if (!out) return fcg::report(FCG_EINVAL, "null output handle");
+    if (n_funcs < 1 || window < 1) return fcg::report(FCG_EINVAL, "n_funcs and window must be >= 1");
+    if (!(alpha >= 0 && beta >= 0 && gamma >= 0) || std::fabs(alpha + beta + gamma - 1.0) > 1e-9)
+      return fcg::report(FCG_EINVAL, "alpha, beta, gamma must be >= 0 and sum to 1");
+    fcg_locality* L = new (std::nothrow) fcg_locality{n_funcs, window, alpha, beta, gamma, {}, {}};
+    if (!L) return fcg::report(FCG_ENOMEM, "host allocation");
+    std::unique_ptr<fcg_locality> owner(L);
+    L->ppl.assign(n_funcs, 0.0);
+    *out = owner.release();
+    return FCG_OK;
+  });
 }
 
 fcg_status fcg_locality_record(fcg_locality* L, int32_t n, const int32_t* func_ids) {
-  if (!L) return fcg::report(FCG_EINVAL, "null handle");
-  if (n < 0 || (n > 0 && !func_ids)) return fcg::report(FCG_EINVAL, "bad trace");
-  for (int32_t i = 0; i < n; ++i)
-    if (func_ids[i] < 0 || func_ids[i] >= L->n) return fcg::report(FCG_ERANGE, "function id out of range");
-  L->traces.emplace_back(func_ids, func_ids + n);
-  if ((int32_t)L->traces.size() > L->window) L->traces.pop_front();
-  return FCG_OK;
+  return fcg::guarded([&]() -> fcg_status {
+    if (!L) return fcg::report(FCG_EINVAL, "null handle");
+    if (n < 0 || (n > 0 && !func_ids)) return fcg::report(FCG_EINVAL, "bad trace");
+    for (int32_t i = 0; i < n; ++i)
+      if (func_ids[i] < 0 || func_ids[i] >= L->n) return fcg::report(FCG_ERANGE, "function id out of range");
+    L->traces.emplace_back(func_ids, func_ids + n);
+    if ((int32_t)L->traces.size() > L->window) L->traces.pop_front();
+    return FCG_OK;
+  });
 }
 
 fcg_status fcg_locality_set_ppl(fcg_locality* L, int32_t func, double ppl) {
@@ -132,13 +138,17 @@ fcg_status fcg_locality_set_ppl(fcg_locality* L, int32_t func, double ppl) {
 }
 
 fcg_status fcg_locality_scores(const fcg_locality* L, double* scores) {
-  if (!L || !scores) return fcg::report(FCG_EINVAL, "null argument");
-  compute_scores(*L, scores);
-  return FCG_OK;
+  return fcg::guarded([&]() -> fcg_status {
+    if (!L || !scores) return fcg::report(FCG_EINVAL, "null argument");
+    compute_scores(*L, scores);
+    return FCG_OK;
+  });
 }
 
 fcg_status fcg_locality_residency(const fcg_locality* L, int64_t budget, const int64_t* cost, uint8_t* resident) {
-  return fcg::locality_residency(L, budget, cost, 0.0, nullptr, resident);
+  return fcg::guarded([&]() -> fcg_status {
+    return fcg::locality_residency(L, budget, cost, 0.0, nullptr, resident);
+  });
 }
 
 fcg_status fcg_locality_destroy(fcg_locality* L) {

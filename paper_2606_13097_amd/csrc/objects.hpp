@@ -8,7 +8,6 @@
 #include <algorithm>
 #include <cstring>
 #include <deque>
-#include <exception>
 #include <map>
 #include <new>
 #include <string>
@@ -31,18 +30,6 @@ fcg_status hip_fail(hipError_t e, const char* what);
     hipError_t e_ = (expr);                               \
     if (e_ != hipSuccess) return fcg::hip_fail(e_, what); \
   } while (0)
-
-// Body of an entry point: host allocations that fail become a status.
-template <typename F>
-fcg_status guarded(F&& f) {
-  try {
-    return f();
-  } catch (const std::bad_alloc&) {
-    return report(FCG_ENOMEM, "host allocation");
-  } catch (const std::exception& e) {
-    return report(FCG_ENOMEM, e.what());
-  }
-}
 
 inline size_t esize(int32_t dtype) { return dtype == FCG_F32 ? 4 : 2; }
 
@@ -184,8 +171,12 @@ struct fcg_lib {
     for (auto it = free_tok.begin(); it != free_tok.end(); ++it)
       if (it->second >= len) {
         const int64_t off = it->first, rest = it->second - len;
-        free_tok.erase(it);
-        if (rest) free_tok[off + len] = rest;
+        auto node = free_tok.extract(it);  // (a new one could fail after the range is gone)
+        if (rest) {
+          node.key() = off + len;
+          node.mapped() = rest;
+          free_tok.insert(std::move(node));
+        }
         return off;
       }
     if (used + len > cap) return -1;

@@ -348,14 +348,16 @@ void Planner::reset(int32_t seq) {
   }
 }
 
-void Planner::truncate(int32_t seq, int32_t pos, std::vector<Unalias>* unalias) {
-  if (P_ && pos % P_ && pos < T_) {
-    int32_t& a = valias_[(size_t)seq * NLP_ + pos / P_];
-    if (a >= 0) {
-      if (unalias) unalias->push_back(Unalias{seq, page_table_[(size_t)seq * NLP_ + pos / P_], pos % P_, a});
-      a = -1;
-    }
-  }
+bool Planner::splits_alias(int32_t seq, int32_t pos, Unalias* cut) const {
+  if (!P_ || pos % P_ == 0 || pos >= T_) return false;
+  const size_t at = (size_t)seq * NLP_ + pos / P_;
+  if (valias_[at] < 0) return false;
+  *cut = Unalias{seq, page_table_[at], pos % P_, valias_[at]};
+  return true;
+}
+
+void Planner::truncate(int32_t seq, int32_t pos) {
+  if (P_ && pos % P_ && pos < T_) valias_[(size_t)seq * NLP_ + pos / P_] = -1;
   for (int32_t l = 0; l < L_; ++l) {
     int32_t &len = len_[idx(seq, l)], &cnt = cnt_[idx(seq, l)];
     if (len <= pos) continue;  // nothing at or past pos

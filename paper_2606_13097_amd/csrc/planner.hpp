@@ -85,8 +85,10 @@ class Planner {
   void mark(int32_t seq, int32_t layer, int32_t pos);
   void reset(int32_t seq);
   // keep [0, pos) in every layer (the caller checked the range); a split
-  // page mapped onto the library is appended to *unalias and unmapped
-  void truncate(int32_t seq, int32_t pos, std::vector<Unalias>* unalias = nullptr);
+  // page mapped onto the library has its own values afterwards
+  void truncate(int32_t seq, int32_t pos);
+  // whether that cut splits a page mapped onto the library: *cut
+  bool splits_alias(int32_t seq, int32_t pos, Unalias* cut) const;
 
   // Queries.
   bool written(int32_t seq, int32_t layer, int32_t pos) const;

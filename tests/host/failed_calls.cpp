@@ -148,6 +148,70 @@ Call graft(std::vector<int32_t> seq, std::vector<int32_t> seg, std::vector<int32
   };
 }
 
+Call prefill(std::vector<int32_t> seq, std::vector<int32_t> pos) {
+  return [=](World& w) {
+    return fcg_patch_prefill(w.cache, 0, (int)seq.size(), seq.data(), pos.data(), w.data.data(), w.data.data(),
+                             w.data.data(), w.data.data(), nullptr);
+  };
+}
+
+Call decode(std::vector<int32_t> seq, bool noalloc) {
+  return [=](World& w) {
+    float* x = w.data.data();
+    return (noalloc ? fcg_decode_noalloc : fcg_decode)(w.cache, 0, (int)seq.size(), seq.data(), x, x, x, x, nullptr, nullptr);
+  };
+}
+
+// calls without a layout to compare: a failed allocation is a status, not an exception
+void entry_points_return_a_status() {
+  const fcg_model_desc d = desc(FCG_BF16);
+  auto each = [](const char* name, const std::function<fcg_status()>& call) {
+    for (int n = 0; n < 1000; ++n) {
+      host::fail_alloc = n;
+      const fcg_status st = call();
+      const bool reached = host::fail_alloc < 0;
+      host::fail_alloc = -1;
+      // (a sort does without the room it would like)
+      CHECK(st == FCG_OK || (reached && st == FCG_ENOMEM), "%s, allocation %d: status %d", name, n, st);
+      if (!reached) return;
+    }
+    CHECK(false, "%s: never got through", name);
+  };
+  each("cache", [&] {
+    fcg_cache* c = nullptr;
+    const fcg_status st = fcg_cache_create(&d, 3, 100, 16, 40, 0, &c);
+    const long left = host::fail_alloc;
+    fcg_cache_destroy(c);
+    host::fail_alloc = left;
+    return st;
+  });
+  World w(FCG_BF16, 16, 0);
+  int32_t id = 0;
+  if (fcg_lib_host_reserve(w.lib, 400) != FCG_OK) std::abort();
+  each("segment", [&] { return fcg_lib_add_segment(w.lib, 16, 0, nullptr, nullptr, nullptr, &id); });
+  const int64_t used = w.lib->used;
+  for (int i = 0; i < 3; ++i) {
+    each("offload", [&] { return w.lib->segs[i].tok_off < 0 ? FCG_OK : fcg_lib_offload(w.lib, i, nullptr); });
+    each("reload", [&] { return w.lib->segs[i].tok_off >= 0 ? FCG_OK : fcg_lib_reload(w.lib, i, nullptr); });
+  }
+  CHECK(w.lib->used == used, "offload and reload: %lld tokens used", (long long)w.lib->used);
+  fcg_locality* loc = nullptr;
+  each("scorer", [&] {
+    fcg_locality_destroy(loc);
+    loc = nullptr;
+    return fcg_locality_create(4, 3, 0.4, 0.3, 0.3, &loc);
+  });
+  const std::vector<int32_t> trace = {0, 1, 2, 3};
+  std::vector<double> score(4);
+  std::vector<int64_t> cost(4, 1);
+  std::vector<uint8_t> keep(4);
+  each("record", [&] { return fcg_locality_record(loc, 4, trace.data()); });
+  each("scores", [&] { return fcg_locality_scores(loc, score.data()); });
+  each("residency", [&] { return fcg_locality_residency(loc, 2, cost.data(), keep.data()); });
+  each("update", [&] { return fcg_lib_update_residency(w.lib, loc, (int64_t)1 << 30, 0.0, nullptr, nullptr, nullptr); });
+  fcg_locality_destroy(loc);
+}
+
 }  // namespace
 
 int main() {
@@ -194,6 +258,24 @@ int main() {
       CHECK(table_agrees(w), "append after a failed graft, HIP call %d", n);
     }
   }
+  // the calls with attention
+  every_failure("prefill", FCG_BF16, 16, 0, nullptr, prefill(zero40, iota(40)), decode({0}, false));
+  std::vector<int32_t> back = iota(40, 39, -1);
+  every_failure("prefill, tokens backwards", FCG_BF16, 16, 0, nullptr, prefill(zero40, back), decode({0}, true));
+  every_failure("prefill fp32", FCG_F32, 16, 0, nullptr, prefill(zero40, iota(40)), decode({0}, false));
+  const Call sixteen = [](World& w) {
+    std::vector<int32_t> seq, pos;
+    for (int s = 0; s < SEQS; ++s)
+      for (int p = 0; p < 16; ++p) seq.push_back(s), pos.push_back(p);
+    return fcg_append(w.cache, 0, L, (int)seq.size(), seq.data(), pos.data(), nullptr, nullptr, nullptr, nullptr, nullptr,
+                      0, nullptr);
+  };
+  every_failure("decode", FCG_BF16, 16, 0, sixteen, decode(all, false), decode(all, false));
+  every_failure("decode without allocation", FCG_BF16, 16, 0, sixteen, decode(all, true), decode(all, true));
+  // a cut inside a page whose values are read from the library
+  every_failure("cut", FCG_BF16, 16, FCG_ALIAS_V, graft({0}, {0}, {0}),
+                [](World& w) { return fcg_cache_truncate(w.cache, 0, 40, nullptr); }, append({0, 0}, {40, 41}, true));
+  entry_points_return_a_status();
   if (!failures) std::printf("ok\n");
   return failures ? 1 : 0;
 }
