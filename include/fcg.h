@@ -375,7 +375,8 @@ fcg_status fcg_graft_rope(fcg_cache* cache, const fcg_lib* lib, const fcg_rope* 
  * rejected draft) instead of refused.
  * A call can be captured into a graph if it maps no page and the tokens form at
  * most 64 runs (consecutive positions of one sequence at consecutive indices)
- * on at most 384 pages; replays write the same places.
+ * on at most 384 pages; replays write the same places.  A reservation that maps no
+ * page launches nothing.
  * Errors: EINVAL (null arrays or tensors, negative counts or strides, flags,
  * rotary_dim above the head, overlapping rows of q_out), ERANGE (layers,
  * sequence, position), EOVERLAP (a position given twice; one written in one of

@@ -259,6 +259,7 @@ fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_t
       staged.map();
       return commit();
     }
+    if (!has_k && new_pages.empty()) return commit();  // nothing for the device to do
     OnDevice dev(c->device);
     HIP_TRY(dev.err, "hipSetDevice");
     hipStream_t s = (hipStream_t)stream;

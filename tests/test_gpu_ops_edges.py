@@ -1,0 +1,50 @@
+"""Rotary forms, append and prefix attention on the GPU: calls at the edges of what their documentation allows."""
+import numpy as np
+import pytest
+import torch
+
+from opsutil import attend64, cache_memory, check_attend, randn
+from paper_2606_13097_amd import fcg
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _gpu(request):
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU")
+    print(f"[gpu] {request.node.name}", flush=True)
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+@pytest.mark.parametrize("page", [0, 16])
+def test_reservations_while_a_stream_is_captured(page):
+    """Positions of a contiguous cache, or on pages mapped before, are reserved by the host alone: between captured calls,
+    and their rows keep what they hold."""
+    c = fcg.Cache(fcg.model_desc(1, 4, 2, 64, 1e4, "bf16"), 2, 64, page, 8 if page else 0)
+    K, V = cache_memory(c, "bf16")
+    k, v = randn(gen(1), 20, 2, 64), randn(gen(2), 20, 2, 64)
+    fcg.fcg_append(c, 0, np.zeros(20), np.arange(20), k, v)
+    torch.cuda.synchronize()
+    was = K.clone(), V.clone()
+    fcg.fcg_cache_truncate(c, 0, 18)                   # both pages stay mapped
+    q, out = randn(gen(3), 1, 4, 64), torch.empty((1, 4, 64), dtype=torch.bfloat16, device="cuda")
+    fcg.fcg_prefix_attend(c, 0, 0, 18, [0], [17], q, out)
+    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=s):
+        fcg.fcg_append(c, 0, [0, 0], [19, 18])
+        fcg.fcg_prefix_attend(c, 0, 0, 20, [0], [19], q, out)
+    assert fcg.fcg_cache_export_layout(c, 0, 0)[1] == 20
+    for _ in range(2):
+        out.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        keys = K[0, 0].transpose(0, 1)[:20] if not page else torch.cat([K[0, 0].transpose(0, 1), K[0, 1].transpose(0, 1)])[:20]
+        vals = V[0, 0].transpose(0, 1)[:20] if not page else torch.cat([V[0, 0].transpose(0, 1), V[0, 1].transpose(0, 1)])[:20]
+        check_attend(out, None, attend64(q, keys, vals, [19], 20), "bf16", 20, 64, "replay")
+    assert torch.equal(K.view(torch.int16), was[0].view(torch.int16)) and torch.equal(V.view(torch.int16), was[1].view(torch.int16))
+    c.close()
