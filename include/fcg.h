@@ -409,8 +409,8 @@ fcg_status fcg_append(fcg_cache* cache, int32_t layer, int32_t n_layers, int32_t
  * 96 (fp32: 48) query rows a kv head or more; a workspace that a capture used is
  * kept until the cache is destroyed, and the calls and graphs of one cache share
  * it, so they must not overlap.
- * Errors: EINVAL (null arrays or tensors, negative counts or strides,
- * overlapping rows of out), ERANGE (layer, sequences, prefix_len outside [0,
+ * Errors: EINVAL (null arrays or tensors, negative counts or strides, more than
+ * 2^24 - 1 tokens or 2^30 query rows, overlapping rows of out), ERANGE (layer, sequences, prefix_len outside [0,
  * max_tokens], pos[t] outside [prefix_len - 1, max_tokens)), EHOLE (an attended
  * position is not written), ESTATE (a capture that would need an upload or a
  * larger workspace), ENOMEM, EHIP. */

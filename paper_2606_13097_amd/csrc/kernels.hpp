@@ -322,13 +322,17 @@ struct RopeRows {
   int32_t stream;                 // 1: read and write past the caches
 };
 
+// Blocks along x of a launch of 256 threads a block: HIP takes fewer than 2^32 threads.
+constexpr int kGridX = (1 << 24) - 1;
+
 // Turn rows into caller tensors: q -> q_out, k -> k_out, token t at device pos[t].
+// At most kGridX groups of rows.tb tokens.
 int launch_rope_apply(int dtype, int D, bool pairs, const RopeRows& rows, const int32_t* pos, const RopeArgs& ra,
                       hipStream_t s);
 
 // Turn and append: q -> q_out, k and v -> the cache rows of layers layer0 ...  tab
 // non-null: the cache's rotary table (whole head, rotate-half) instead of ra.
-// groups null: the plan by value (n_groups groups of n_runs runs).
+// groups null: the plan by value (n_groups groups of n_runs runs).  n_groups <= kGridX.
 int launch_append(int dtype, bool pairs, const RopeRows& rows, const AppendArgs& args, int n_runs,
                   const AppendGroup* groups, int n_groups, const CacheView& cv, int layer0, const RopeArgs& ra,
                   const float2* tab, hipStream_t s);
@@ -387,6 +391,7 @@ struct PrefixArgs {
 // (bf16).
 int launch_prefix_attend(int dtype, const PrefixCall& call, const PrefixArgs* args, const PrefixItem* items,
                          const PrefixRank* ranks, int n_items, int waves, const CacheView& cv, hipStream_t s);
+// n_rank <= kGridX
 int launch_prefix_merge(int dtype, const PrefixCall& call, const PrefixArgs* args, const PrefixRank* ranks, int n_rank,
                         int Hq, int D, hipStream_t s);
 

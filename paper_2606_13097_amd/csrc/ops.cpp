@@ -212,8 +212,16 @@ fcg_status fcg_rope_apply(const fcg_rope* rope, int32_t dtype, int32_t head_dim,
   rows.n_layers = n_layers;
   rows.sign = flags & FCG_ROPE_BACKWARD ? -1.f : 1.f;
   cut_rows(&rows, n_tok, n_layers, rows.Hq + rows.Hk, head_dim * (int)esize(dtype) / 32);
-  if (int rc = launch_rope_apply(dtype, head_dim, rope->pairs(), rows, pos, rope->args(), (hipStream_t)stream))
-    return hip_fail((hipError_t)rc, "rope launch");
+  const RopeArgs args = rope->args();
+  const int64_t per = (int64_t)kGridX * rows.tb;  // tokens of a launch
+  for (int64_t t0 = 0; t0 < n_tok; t0 += per) {
+    RopeRows part = rows;
+    for (RowView* v : {&part.q, &part.q_out, &part.k, &part.k_out})
+      if (v->p) v->p = (const char*)v->p + t0 * v->token * (int64_t)esize(dtype);
+    part.n_tok = (int32_t)std::min<int64_t>(per, n_tok - t0);
+    if (int rc = launch_rope_apply(dtype, head_dim, rope->pairs(), part, pos + t0, args, (hipStream_t)stream))
+      return hip_fail((hipError_t)rc, "rope launch");
+  }
   return FCG_OK;
 }
 
@@ -298,7 +306,7 @@ fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_t
         n_page += (r.pos0 + r.n - 1) / 16 - r.pos0 / 16 + 1;
       }
     }
-    const bool by_value = (int)runs.size() <= kAppRuns && n_page <= kAppPages && has_k;
+    const bool by_value = (int)runs.size() <= kAppRuns && n_page <= kAppPages && has_k && n_groups <= kGridX;
     // what needs an upload cannot be captured: its staging memory is used again
     if ((!by_value || !new_pages.empty()) && capturing(s))
       return fail(FCG_ESTATE, "this append maps pages or has too many runs to be captured into a graph");
@@ -345,11 +353,10 @@ fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_t
     const size_t o_groups = blob.add(groups.data(), groups.size() * sizeof(AppendGroup));
     char* dplan = nullptr;
     if (fcg_status st = upload(c, blob, page_rows, s, &dplan, &staged)) return st;
-    if (has_k) {
-      const int rc = launch_append(d.dtype, pairs, rows, AppendArgs{}, 0, (const AppendGroup*)(dplan + o_groups),
-                                   (int)groups.size(), c->view(), layer, ra, tab, s);
-      if (rc) return hip_fail((hipError_t)rc, "append launch");
-    }
+    for (size_t i = 0; i < groups.size(); i += kGridX)
+      if (int rc = launch_append(d.dtype, pairs, rows, AppendArgs{}, 0, (const AppendGroup*)(dplan + o_groups) + i,
+                                 (int)std::min<size_t>(kGridX, groups.size() - i), c->view(), layer, ra, tab, s))
+        return hip_fail((hipError_t)rc, "append launch");
     if (fcg_status st = c->ring.retire(s)) return st;
     return commit();
   });
@@ -636,7 +643,8 @@ fcg_status fcg_prefix_attend(fcg_cache* c, int32_t layer, int32_t prefix_seq, in
     a.layer = b.layer = 0;
     if (fcg_status st = check_alias(&a, &b, "out")) return st;
   }
-  if ((int64_t)n_tok * d.n_q_heads > INT32_MAX / 2) return fail(FCG_EINVAL, "too many query rows for one call");
+  if (n_tok > kGridX) return fail(FCG_EINVAL, "more than 2^24 - 1 tokens");
+  if ((int64_t)n_tok * d.n_q_heads > 1 << 30) return fail(FCG_EINVAL, "more than 2^30 query rows");
   return guarded([&]() -> fcg_status {
     std::string msg;
     if (fcg_status st = c->plan.check_attend(layer, prefix_seq, prefix_len, n_tok, seq, pos, &msg)) return fail(st, msg);

@@ -4,6 +4,8 @@
 // to fail, by its number.
 #pragma once
 
+#include <sys/mman.h>
+
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -61,14 +63,21 @@ hipError_t hipSetDevice(int d) {
   host::device = d;
   return hipSuccess;
 }
+// (zeros; pages that nothing touches take no memory, so caches may be larger than the machine's)
 hipError_t hipMalloc(void** p, size_t n) {
   if (host::next_hip_fails()) return hipErrorOutOfMemory;
-  *p = std::calloc(1, n ? n : 1);
-  return *p ? hipSuccess : hipErrorOutOfMemory;
+  char* a = (char*)mmap(nullptr, n + 4096, PROT_READ | PROT_WRITE, MAP_PRIVATE | MAP_ANONYMOUS | MAP_NORESERVE, -1, 0);
+  if (a == (char*)MAP_FAILED) return hipErrorOutOfMemory;
+  *(size_t*)a = n + 4096;
+  *p = a + 4096;
+  return hipSuccess;
 }
 hipError_t hipHostMalloc(void** p, size_t n, unsigned) { return hipMalloc(p, n); }
-hipError_t hipFree(void* p) { std::free(p); return hipSuccess; }
-hipError_t hipHostFree(void* p) { std::free(p); return hipSuccess; }
+hipError_t hipFree(void* p) {
+  if (p) munmap((char*)p - 4096, *(size_t*)((char*)p - 4096));
+  return hipSuccess;
+}
+hipError_t hipHostFree(void* p) { return hipFree(p); }
 hipError_t hipMemset(void* p, int v, size_t n) { std::memset(p, v, n); return host::hip(); }
 hipError_t hipMemcpy(void* d, const void* s, size_t n, hipMemcpyKind) { std::memcpy(d, s, n); return host::hip(); }
 hipError_t hipMemcpy2DAsync(void*, size_t, const void*, size_t, size_t, size_t, hipMemcpyKind, hipStream_t) {

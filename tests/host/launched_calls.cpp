@@ -57,11 +57,86 @@ void reservations() {
   }
 }
 
+bool fits(const fcg::RopeRows& r, int64_t groups) {
+  const int64_t slices = (r.tb * (r.Hq + r.Hk + r.Hv) + r.slice_rows - 1) / r.slice_rows;
+  return groups * 256 < (int64_t)1 << 32 && slices <= 65535 && r.grid_layers <= 65535;
+}
+
+// Up to 2^30 tokens: launches of fewer than 2^32 threads along x that follow each other.
+void long_encodings() {
+  fcg_rope_desc rd{};
+  rd.rotary_dim = 64;
+  rd.theta = 1e4;
+  rd.attn_factor = 1.0;
+  fcg_rope* rope = nullptr;
+  if (fcg_rope_create(&rd, &rope)) std::abort();
+  std::vector<host::Apply> seen;
+  host::applies = &seen;
+  char* const base = (char*)0x100000;  // (nothing is read)
+  const int32_t* const pos = (const int32_t*)0x40000000;
+  struct {
+    int32_t n, hq, hk;
+  } cases[] = {{1 << 30, 1, 0}, {(1 << 28) + 5, 0, 1}, {20000000, 64, 1}, {20000000, 33, 0}, {1000, 8, 8}, {1 << 30, 4096, 4096}};
+  for (const auto& x : cases)
+    for (int32_t dtype : {FCG_BF16, FCG_F32}) {
+      const int64_t es = dtype == FCG_F32 ? 4 : 2;
+      seen.clear();
+      const fcg_tensor q{base, 0, x.hq * 64, 64}, k{base + 64, 0, x.hk * 64, 64};
+      CHECK(fcg_rope_apply(rope, dtype, 64, 1, x.n, pos, x.hq, &q, &q, x.hk, &k, &k, 0, nullptr) == FCG_OK, "%d tokens: %s",
+            x.n, fcg_last_error());
+      int64_t at = 0;
+      for (const host::Apply& a : seen) {
+        CHECK(fits(a.rows, (a.rows.n_tok + (int64_t)a.rows.tb - 1) / a.rows.tb), "%d tokens, %d + %d heads: a launch of %d tokens by %d",
+              x.n, x.hq, x.hk, a.rows.n_tok, a.rows.tb);
+        CHECK(a.pos == pos + at, "positions of token %lld", (long long)at);
+        if (x.hq) CHECK((const char*)a.rows.q.p == base + at * x.hq * 64 * es && a.rows.q_out.p == a.rows.q.p, "q of token %lld", (long long)at);
+        if (x.hk) CHECK((const char*)a.rows.k.p == base + 64 + at * x.hk * 64 * es && a.rows.k_out.p == a.rows.k.p, "k of token %lld", (long long)at);
+        CHECK((a.rows.q.p != nullptr) == (x.hq > 0) && (a.rows.k.p != nullptr) == (x.hk > 0), "rows that are not given");
+        at += a.rows.n_tok;
+      }
+      CHECK(at == x.n, "%d tokens: %lld launched", x.n, (long long)at);
+    }
+  host::applies = nullptr;
+  fcg_rope_destroy(rope);
+}
+
+// More groups of tokens than a launch takes: several launches of the list.
+void long_appends() {
+  const int n = (1 << 24) + 3000;
+  fcg_cache* c = cache_of(FCG_BF16, 32, 32, 64, 1, n, 0, 0, 1);
+  std::vector<int32_t> seq(n), pos(n);
+  std::iota(pos.begin(), pos.end(), 0);
+  std::vector<host::Append> seen;
+  host::appends = &seen;
+  float x;
+  const fcg_tensor kv{&x, 0, 0, 64};
+  CHECK(fcg_append(c, 0, 1, n, seq.data(), pos.data(), nullptr, nullptr, nullptr, &kv, &kv, 0, nullptr) == FCG_OK, "%s",
+        fcg_last_error());
+  int64_t at = 0;
+  for (const host::Append& a : seen) {
+    CHECK(fits(a.rows, a.n_groups), "a launch of %d groups", a.n_groups);
+    if (!a.groups) {
+      CHECK(false, "a plan by value");
+      break;
+    }
+    for (int i = 0; i < a.n_groups && failures < 20; at += a.groups[i++].n)
+      CHECK(a.groups[i].tok0 == at && a.groups[i].pos0 == at, "group %d: token %d, not %lld", i, a.groups[i].tok0, (long long)at);
+  }
+  CHECK(at == n && seen.size() > 1, "%lld tokens in %zu launches", (long long)at, seen.size());
+  // as many tokens that attend: refused, as documented
+  const fcg_tensor q{&x, 0, 0, 0}, out{&x, 0, 32 * 64, 64};
+  CHECK(fcg_prefix_attend(c, 0, 0, 0, 1 << 24, seq.data(), pos.data(), &q, &out, nullptr, nullptr) == FCG_EINVAL, "2^24 tokens");
+  host::appends = nullptr;
+  fcg_cache_destroy(c);
+}
+
 }  // namespace
 
 int main() {
   std::setvbuf(stdout, nullptr, _IOLBF, 0);
   reservations();
+  long_encodings();
+  long_appends();
   if (!failures) std::printf("ok\n");
   return failures ? 1 : 0;
 }

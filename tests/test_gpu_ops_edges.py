@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from opsutil import attend64, cache_memory, check_attend, randn
+from opsutil import attend64, cache_memory, check_attend, check_turned, freqs64, randn, turn64
 from paper_2606_13097_amd import fcg
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +48,23 @@ def test_reservations_while_a_stream_is_captured(page):
         check_attend(out, None, attend64(q, keys, vals, [19], 20), "bf16", 20, 64, "replay")
     assert torch.equal(K.view(torch.int16), was[0].view(torch.int16)) and torch.equal(V.view(torch.int16), was[1].view(torch.int16))
     c.close()
+
+
+def test_rope_apply_of_more_tokens_than_a_launch_takes():
+    """2^28 tokens of one head of 64 (34 GB, in place): groups of 16 tokens, 2^24 of them, are one block too many for a
+    launch of 256 threads a block, so the rest is a second one."""
+    n, first = 2 ** 28 + 5, 16 * (2 ** 24 - 1)          # tokens of the first launch
+    x = torch.zeros((n, 1, 64), dtype=torch.bfloat16, device="cuda")
+    at = torch.as_tensor(np.r_[0:4, 2 ** 27:2 ** 27 + 3, first - 3:first + 4, n - 4:n], device="cuda")
+    was = randn(gen(1), len(at), 1, 64)
+    x[at] = was
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    fcg.fcg_rope_apply(fcg.fcg_rope_create(48, layout=fcg.FCG_ROPE_PAIRS), pos, x, x)
+    torch.cuda.synchronize()
+    got = x[at]
+    w = freqs64(48, 1e4)
+    # angles up to 2^28 radians: the rounding of their product, 2^-53 of it, and of the frequency in turns as much
+    # again, is another 2^28 2^-52 = 2^-24 of sum |a| + |b| (inside the factor 1.5 on the bound of cos and sin)
+    check_turned(got, turn64(was, at.cpu().numpy(), w, True), was, w, True, 1.5, "bf16", "far tokens")
+    x[at] = 0
+    assert not x[:2 ** 20].any() and not x[first - 2 ** 20:].any()
