@@ -316,8 +316,9 @@ typedef struct {
   double orig_tokens;   /* > 0 (PARTS) */
   double low_turns;     /* 0 <= low_turns < high_turns (PARTS) */
   double high_turns;
-  double attn_factor;   /* m > 0: the rotated dimensions of encoded queries and keys are multiplied by it */
-  const double* freqs;  /* host [R / 2], finite, in radians per position (GIVEN), read by the call */
+  double attn_factor;   /* m > 0, a normal fp32 number: the rotated dimensions of encoded queries and keys are
+                           multiplied by it */
+  const double* freqs;  /* host [R / 2], finite (and 2^31 times as much), in radians per position (GIVEN), read by the call */
 } fcg_rope_desc;
 
 /* Create a rotary handle: host memory only, usable on every device and from
@@ -333,8 +334,9 @@ fcg_status fcg_rope_destroy(fcg_rope* rope);
  * (device int32 [n_tok], any value, shared by the layers) and m the attention
  * factor, the pair (a, b) of every head becomes
  *   (m (a cos(p w_i) - b sin(p w_i)), m (b cos(p w_i) + a sin(p w_i))),
- * the angle taken in 64 bits, the turn in 32, rounded once to dtype; dimensions
- * past rotary_dim are copied.  FCG_ROPE_BACKWARD: the gradient of that map (the
+ * the angle taken in 64 bits (within 2^-51 |p w_i| radians: it holds little past
+ * |p w_i| of 2^45), its cos and sin (within 2^-22) and the turn in 32, rounded once
+ * to dtype; dimensions past rotary_dim are copied.  FCG_ROPE_BACKWARD: the gradient of that map (the
  * angle negated, the factor kept), from the gradient of its result to that of
  * its input.  q [n_layers][n_tok][n_q_heads][head_dim] and k alike, each with
  * an output of its own shape; either may be left out (null pointer or zero
@@ -354,8 +356,10 @@ fcg_status fcg_rope_apply(const fcg_rope* rope, int32_t dtype, int32_t head_dim,
 
 /* Cache-stitching as fcg_graft, for segments whose keys carry the rotary form
  * of `rope`: keys turn by the angles of delta = dst[i] - src_pos0 (without the
- * attention factor, which the encoded keys hold already), dimensions past
- * rotary_dim and values are copied bit for bit.  Errors as fcg_graft, and
+ * attention factor, which the encoded keys hold already), cos and sin as in
+ * fcg_rope_apply (fcg_graft's are 64-bit ones rounded to fp32, so a handle of the
+ * cache's own form may leave other last bits), dimensions past rotary_dim and
+ * values are copied bit for bit.  Errors as fcg_graft, and
  * EINVAL (null rope, rotary_dim above the head). */
 fcg_status fcg_graft_rope(fcg_cache* cache, const fcg_lib* lib, const fcg_rope* rope, int32_t n_items,
                           const int32_t* seq, const int32_t* seg, const int32_t* dst, void* stream);

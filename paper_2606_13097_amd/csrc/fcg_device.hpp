@@ -223,9 +223,10 @@ __device__ __forceinline__ void rope_cs(double pos, double w, float* c, float* s
 
 // cos and sin of pos * w for a rotary pair, w given as `turns` = w / (2 pi) turns
 // per position: the product and its distance to the nearest whole turn are
-// float64 (exact after the product's rounding, 2^-53 of up to 2^31 turns), the
-// rest of the angle is at most half a turn and goes through the fp32 sincospi,
-// so each of the two is within about 2^-23 of the definition at any position.
+// float64, the rest of the angle is at most half a turn and goes through the fp32
+// sincospi.  Two errors: the rest rounded to fp32 and sincospi itself, together
+// within 2^-22; and the roundings of `turns` and of the product, an angle of less
+// than 2^-51 |pos w| radians, which is the smaller one up to |pos w| = 2^29.
 // The float64 sincos of rope_cs costs several times as much, most of it the
 // range reduction that one rint does here.
 __device__ __forceinline__ void rope_cs_turns(double pos, double turns, float* c, float* s) {

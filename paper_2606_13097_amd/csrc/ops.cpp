@@ -1,6 +1,7 @@
 // Entry points around the cache that take a rotary handle or a shared prefix
 // (include/fcg.h): rotary handles, rope apply, append, prefix attention.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "objects.hpp"
@@ -78,7 +79,9 @@ fcg_status fcg_rope_create(const fcg_rope_desc* d, fcg_rope** out) {
     return fail(FCG_EINVAL, "rotary_dim must be a multiple of 16 in [16, 128]");
   if (d->layout != FCG_ROPE_HALF && d->layout != FCG_ROPE_PAIRS) return fail(FCG_EINVAL, "unknown rope layout");
   if (d->scaling < FCG_ROPE_PLAIN || d->scaling > FCG_ROPE_GIVEN) return fail(FCG_EINVAL, "unknown rope scaling");
-  if (!(d->attn_factor > 0.0) || !std::isfinite(d->attn_factor)) return fail(FCG_EINVAL, "attn_factor must be > 0");
+  // (the kernels take it in fp32)
+  if (!(d->attn_factor >= (double)FLT_MIN && d->attn_factor <= (double)FLT_MAX))
+    return fail(FCG_EINVAL, "attn_factor must be > 0, in the range of normal fp32 numbers");
   const bool given = d->scaling == FCG_ROPE_GIVEN, scaled = d->scaling != FCG_ROPE_PLAIN && !given;
   if (!given && (!(d->theta > 1.0) || !std::isfinite(d->theta))) return fail(FCG_EINVAL, "theta must be > 1");
   if (scaled && (!(d->factor >= 1.0) || !std::isfinite(d->factor))) return fail(FCG_EINVAL, "factor must be >= 1");
@@ -91,7 +94,8 @@ fcg_status fcg_rope_create(const fcg_rope_desc* d, fcg_rope** out) {
   if (given) {
     if (!d->freqs) return fail(FCG_EINVAL, "null frequencies");
     for (int i = 0; i < n; ++i)
-      if (!std::isfinite(d->freqs[i])) return fail(FCG_EINVAL, "a frequency is not finite");
+      if (!std::isfinite(d->freqs[i] * 2147483648.0))
+        return fail(FCG_EINVAL, "a frequency, or its angle at position 2^31, is not finite");
   }
   return guarded([&]() -> fcg_status {
     std::vector<double> w(n);
