@@ -494,6 +494,9 @@ def _view(t, shape: tuple, dtype, device, what: str):
     One call makes up to four of these, a visible part of a small step, so the checks are few and plain."""
     if t is None:
         return None
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what}: requires a gradient, which these calls do not record (call under torch.no_grad(), "
+                         "or from the forward of an autograd function)")
     if t.dtype is not dtype or (t.get_device() != device if device is not None else not t.is_cuda):
         raise ValueError(f"{what}: a {t.dtype} tensor on {t.device}, expected {dtype} on GPU {device}")
     st, sh = t.stride(), t.shape
@@ -518,7 +521,8 @@ def _stream_of(stream, device) -> Optional[int]:
 
 
 def fcg_rope_apply(rope: Rope, pos, q=None, q_out=None, k=None, k_out=None, flags: int = 0, stream=None) -> None:
-    """Encode q and k ([n][heads][head_dim], or with layers in front) at ``pos`` (int32 GPU tensor [n]) into q_out, k_out."""
+    """Encode q and k ([n][heads][head_dim], or with layers in front) at ``pos`` (int32 GPU tensor [n]) into q_out, k_out.
+    Records no gradient (and refuses tensors that would need it): FCG_ROPE_BACKWARD is that of an autograd function."""
     if not pos.is_cuda or pos.dtype != torch.int32 or pos.dim() != 1 or not pos.is_contiguous():
         raise ValueError("pos: a contiguous int32 GPU tensor [n_tok]")
     like = q if q is not None else k

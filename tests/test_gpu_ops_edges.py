@@ -68,3 +68,45 @@ def test_rope_apply_of_more_tokens_than_a_launch_takes():
     check_turned(got, turn64(was, at.cpu().numpy(), w, True), was, w, True, 1.5, "bf16", "far tokens")
     x[at] = 0
     assert not x[:2 ** 20].any() and not x[first - 2 ** 20:].any()
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+def test_rope_apply_in_an_autograd_function(pairs):
+    """Forward and backward as a program would join them, gradients against the formula's; tensors that need a gradient
+    are refused where none would be recorded."""
+    n, h, d = 33, 3, 64
+    rope = fcg.fcg_rope_create(48, layout=int(pairs), attn_factor=1.25)
+    w = freqs64(48, 1e4)
+    pos = torch.arange(7, 7 + n, dtype=torch.int32, device="cuda")
+
+    class Encode(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            y = torch.empty_like(x)
+            fcg.fcg_rope_apply(rope, pos, x, y)
+            return y
+
+        @staticmethod
+        def backward(ctx, gy):
+            gx = torch.empty_like(gy)
+            fcg.fcg_rope_apply(rope, pos, gy.contiguous(), gx, flags=fcg.FCG_ROPE_BACKWARD)
+            return gx
+
+    x = randn(gen(1), n, h, d, dtype="f32").requires_grad_()
+    gy = randn(gen(2), n, h, d, dtype="f32")
+    Encode.apply(x).backward(gy)
+    torch.cuda.synchronize()
+    p = np.arange(7, 7 + n)
+    check_turned(x.grad, turn64(gy, p, w, pairs, 1.25, -1.0), gy, w, pairs, 1.25, "f32", "gradient")
+    y = torch.empty_like(x)
+    with pytest.raises(ValueError, match="gradient"):
+        fcg.fcg_rope_apply(rope, pos, x, y)
+    c = fcg.Cache(fcg.model_desc(1, h, h, d, 1e4, "f32"), 1, 64)
+    with pytest.raises(ValueError, match="gradient"):
+        fcg.fcg_append(c, 0, np.zeros(n), np.arange(n), x, x)
+    assert fcg.fcg_cache_export_layout(c, 0, 0)[1] == 0
+    with torch.no_grad():
+        fcg.fcg_append(c, 0, np.zeros(n), np.arange(n), x, x)
+    with pytest.raises(ValueError, match="gradient"):
+        fcg.fcg_prefix_attend(c, 0, 0, n, [0] * n, [n - 1] * n, x, y)
+    c.close()

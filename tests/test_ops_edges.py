@@ -43,3 +43,13 @@ def test_angle_error_of_a_pair():
         off = np.abs(off - np.rint(off)) * two_pi
         assert (off <= 2.0 ** -51 * np.abs(exact) + 1e-18).all()
         assert (off > 2.0 ** -54 * np.abs(exact)).any()        # (and not far below it)
+
+
+def test_tensors_that_need_a_gradient_are_refused():
+    """The calls record none: a result without one, silently, would train nothing."""
+    x = torch.zeros((2, 4, 64), requires_grad=True)
+    with pytest.raises(ValueError, match="gradient"):
+        fcg._view(x, (1, 2, 4, 64), torch.float32, None, "q")
+    for t in (x.detach(), x):
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):     # past that check
+            fcg._view(t, (1, 2, 4, 64), torch.float32, None, "q")
