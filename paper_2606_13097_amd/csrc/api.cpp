@@ -709,7 +709,8 @@ fcg_status graft(fcg_cache* c, const fcg_lib* lib, const fcg_rope* rope, int32_t
   };
   staged.map();
   if (c->layout_only()) return commit();
-  HIP_TRY(hipSetDevice(c->device), "hipSetDevice");
+  OnDevice dev_of(c->device);
+  HIP_TRY(dev_of.err, "hipSetDevice");
   hipStream_t s = (hipStream_t)stream;
   Blob blob;
   std::vector<std::pair<int32_t, size_t>> rows;

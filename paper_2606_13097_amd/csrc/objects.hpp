@@ -31,6 +31,20 @@ fcg_status hip_fail(hipError_t e, const char* what);
     if (e_ != hipSuccess) return fcg::hip_fail(e_, what); \
   } while (0)
 
+// The handle's device for the call, the caller's again afterwards.
+struct OnDevice {
+  int before = -1;
+  hipError_t err = hipSuccess;
+  explicit OnDevice(int device) {
+    err = hipGetDevice(&before);
+    if (err == hipSuccess && before != device) err = hipSetDevice(device);
+    else if (err == hipSuccess) before = -1;
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
 inline size_t esize(int32_t dtype) { return dtype == FCG_F32 ? 4 : 2; }
 
 // Staging of per-call plans: a pinned host ring mirrored by a device ring.  A

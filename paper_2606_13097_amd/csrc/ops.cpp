@@ -12,20 +12,6 @@ namespace {
 
 fcg_status fail(fcg_status s, const std::string& msg) { return report(s, msg); }
 
-// The handle's device for the call, the caller's again afterwards.
-struct OnDevice {
-  int before = -1;
-  hipError_t err = hipSuccess;
-  explicit OnDevice(int device) {
-    err = hipGetDevice(&before);
-    if (err == hipSuccess && before != device) err = hipSetDevice(device);
-    else if (err == hipSuccess) before = -1;
-  }
-  ~OnDevice() {
-    if (before >= 0) (void)hipSetDevice(before);
-  }
-};
-
 bool capturing(hipStream_t s) {
   hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(s, &st) == hipSuccess) return st != hipStreamCaptureStatusNone;

@@ -552,7 +552,7 @@ def fcg_graft_rope(cache: Cache, lib: Library, rope: Rope, seq: Sequence[int], s
     s, g, d = _i32(seq), _i32(seg), _i32(dst)
     if not (s.size == g.size == d.size):
         raise ValueError("seq, seg and dst differ in length")
-    _check(_L.fcg_graft_rope(cache.h, lib.h, rope.h, int(s.size), _p(s), _p(g), _p(d), _stream(stream)))
+    _check(_L.fcg_graft_rope(cache.h, lib.h, rope.h, int(s.size), _p(s), _p(g), _p(d), _stream_of(stream, cache.device)))
 
 
 def fcg_append(cache: Cache, layer: int, seq, pos, k=None, v=None, rope: Optional[Rope] = None, q=None, q_out=None,

@@ -21,11 +21,13 @@ inline long fail_alloc = -1, fail_hip = -1;
 inline bool capture = false;            // streams report a capture
 inline int device = 0;                  // the current device
 inline int launches = 0;                // kernels launched
+inline int launch_device = -1;          // the device of the last one
 inline bool next_hip_fails() { return fail_hip >= 0 && fail_hip-- == 0; }
 inline hipError_t hip() { return next_hip_fails() ? hipErrorUnknown : hipSuccess; }
 inline int launch() {
   if (next_hip_fails()) return (int)hipErrorUnknown;
   ++launches;
+  launch_device = device;
   return 0;
 }
 

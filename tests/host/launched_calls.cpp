@@ -130,6 +130,40 @@ void long_appends() {
   fcg_cache_destroy(c);
 }
 
+// The calls of rotary forms, appending and prefix attention run on their cache's device
+// and leave the caller's current one as it was.
+void devices() {
+  const fcg_model_desc m{1, 4, 2, 64, 1e4, FCG_BF16, 0};
+  fcg_rope_desc rd{};
+  rd.rotary_dim = 64;
+  rd.theta = 1e4;
+  rd.attn_factor = 1.0;
+  fcg_rope* rope = nullptr;
+  fcg_lib* lib = nullptr;
+  int32_t id;
+  float x = 0;
+  host::device = 3;
+  fcg_cache* c = cache_of(FCG_BF16, 4, 2, 64, 3, 100, 16, 20, 1);
+  if (fcg_rope_create(&rd, &rope) || fcg_lib_create(&m, 64, 1, 0, &lib) || fcg_lib_add_segment(lib, 40, 0, &x, &x, nullptr, &id))
+    std::abort();
+  host::device = 1;
+  auto check = [&](fcg_status st, const char* what) {
+    CHECK(st == FCG_OK, "%s: %s", what, fcg_last_error());
+    CHECK(host::launch_device == 3, "%s: launched on device %d", what, host::launch_device);
+    CHECK(host::device == 1, "%s: left device %d current", what, host::device);
+    host::launch_device = -1;
+  };
+  const int32_t seq[1] = {0}, seg[1] = {0}, dst[1] = {0}, pos[1] = {40};
+  const fcg_tensor q{&x, 0, 256, 64}, kv{&x, 0, 128, 64};
+  check(fcg_graft_rope(c, lib, rope, 1, seq, seg, dst, nullptr), "graft_rope");
+  check(fcg_append(c, 0, 1, 1, seq, pos, rope, &q, &q, &kv, &kv, 0, nullptr), "append");
+  check(fcg_prefix_attend(c, 0, 0, 40, 1, seq, pos, &q, &q, nullptr, nullptr), "prefix_attend");
+  CHECK(fcg_graft_rope(c, lib, rope, 1, seq, seg, dst, nullptr) == FCG_EOVERLAP && host::device == 1, "a refused graft");
+  fcg_cache_destroy(c);
+  fcg_lib_destroy(lib);
+  fcg_rope_destroy(rope);
+}
+
 }  // namespace
 
 int main() {
@@ -137,6 +171,7 @@ int main() {
   reservations();
   long_encodings();
   long_appends();
+  devices();
   if (!failures) std::printf("ok\n");
   return failures ? 1 : 0;
 }

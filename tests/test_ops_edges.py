@@ -53,3 +53,22 @@ def test_tensors_that_need_a_gradient_are_refused():
     for t in (x.detach(), x):
         with torch.no_grad(), pytest.raises(ValueError, match="GPU"):     # past that check
             fcg._view(t, (1, 2, 4, 64), torch.float32, None, "q")
+
+
+def test_calls_take_the_stream_of_their_caches_device(monkeypatch):
+    """Without a stream: torch's current one of the cache's device, not of the current device."""
+    d = fcg.model_desc(1, 4, 2, 64, 1e4, "bf16")
+    c = fcg.Cache(d, 2, 64, 16, 8, flags=fcg.FCG_LAYOUT_ONLY)
+    lib = fcg.Library(d, 64, 1, flags=fcg.FCG_LAYOUT_ONLY)
+    fcg.fcg_lib_add_segment(lib, 16, 0)
+    rope = fcg.fcg_rope_create(32)
+    seen = {}
+    for name in ("fcg_graft_rope", "fcg_append", "fcg_prefix_attend"):
+        monkeypatch.setattr(fcg._L, name, lambda *a, name=name: seen.setdefault(name, a[-1]) and 0)
+    monkeypatch.setattr(fcg, "_raw_stream", lambda device: 1000 + device)
+    monkeypatch.setattr(fcg, "_current_stream", lambda: 1)
+    c.device = 5
+    fcg.fcg_graft_rope(c, lib, rope, [0], [0], [0])
+    fcg.fcg_append(c, 0, [0], [20])
+    fcg.fcg_prefix_attend(c, 0, 0, 16, [0], [15], None, None)
+    assert seen == dict.fromkeys(seen, 1005) and len(seen) == 3
