@@ -1200,8 +1200,11 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixCall pc, Plan<V
     for (int p = 0; p < PF; ++p) {
       // a slot without a visible key: no weight (its sum is 0, or NaN where its scores were)
       const bool none = ml[p].x == -INFINITY;
-      L = fmaf(ml[p].y, none ? 0.f : __builtin_amdgcn_exp2f(ml[p].x - mr), L);
-      const float wgt = none ? 0.f : __builtin_amdgcn_exp2f(ml[p].x - mr - ml[p].z);
+      const float part = none ? 0.f : __builtin_amdgcn_exp2f(ml[p].x - mr);
+      L = fmaf(ml[p].y, part, L);
+      // the two powers apart: of one sum of exponents, small values' (up 126) came out as 0
+      // and others lost bits of the first to the size of the second
+      const float wgt = part * __builtin_amdgcn_exp2f(-ml[p].z);
       float y[VEC];
       if constexpr (sizeof(T) == 2) {
         const px_f16x8 h = __builtin_bit_cast(px_f16x8, x[p]);

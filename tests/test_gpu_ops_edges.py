@@ -110,3 +110,42 @@ def test_rope_apply_in_an_autograd_function(pairs):
     with pytest.raises(ValueError, match="gradient"):
         fcg.fcg_prefix_attend(c, 0, 0, n, [0] * n, [n - 1] * n, x, y)
     c.close()
+
+
+@pytest.mark.parametrize("hq,hkv,d,n_seq,P", [(8, 1, 128, 1, 3001), (32, 8, 128, 20, 700), (16, 4, 64, 33, 2300)])
+def test_prefix_attend_of_very_small_and_large_values(hq, hkv, d, n_seq, P):
+    """Attention is linear in the values: multiplied by a power of two, the result is the same one times it, bit for bit
+    while nothing leaves the normal numbers, however the splits keep what they hold."""
+    own = [1 + 7 * i % 60 for i in range(n_seq)]
+    c = fcg.Cache(fcg.model_desc(1, hq, hkv, d, 1e4, "bf16"), n_seq + 1, P + 61, 0)
+    K, V = cache_memory(c, "bf16")
+    seq = np.concatenate([np.full(P, n_seq)] + [np.full(n, s) for s, n in enumerate(own)])
+    pos = np.concatenate([np.arange(P)] + [P + np.arange(n) for n in own])
+    fcg.fcg_append(c, 0, seq, pos, randn(gen(1), len(seq), hkv, d), randn(gen(2), len(seq), hkv, d))
+    torch.cuda.synchronize()
+    V0 = torch.nan_to_num(V.float(), 0.0, 0.0, 0.0).bfloat16()
+    q = randn(gen(3), n_seq, hq, d)
+    tseq, tpos = np.arange(n_seq), np.array([P + n - 1 for n in own])
+
+    def call(scale):
+        V.copy_(V0 * scale)
+        out, lse = torch.empty_like(q), torch.empty((n_seq, hq), device="cuda")
+        fcg.fcg_prefix_attend(c, 0, n_seq, P, tseq, tpos, q, out, lse)
+        torch.cuda.synchronize()
+        return out, lse
+
+    ref, lse0 = call(1.0)
+    for e in (-116, -112, -100, -40, 40, 100):
+        out, lse = call(2.0 ** e)
+        want = ref.double() * 2.0 ** e
+        ok = want.abs() >= 2.0 ** -120                 # what is smaller may have left the normal numbers on the way
+        # (results are about sqrt(e / P) of a value: at 2^-116, 4% of them or more are that large)
+        n_ok, off = int(ok.sum()), float(((out.double() - want) / want)[ok].abs().max())
+        assert n_ok > 0.01 * ok.numel() and torch.equal(lse, lse0)
+        # 2^-112 and below: values under 2^-14 become subnormal, off by 2^-134 at most (bf16 steps there are 2^-133).  That
+        # moves a mean of them by no more, 2^-14 of the results looked at and so less than half a step of theirs (2^-8):
+        # one step (2^-7) where it carries one over a border
+        assert off <= (2.0 ** -7 if e < -100 else 0.0), f"values times 2^{e}: off by {off} of the result"
+        rest = float((out.double() - want).abs()[~ok].amax()) if n_ok < ok.numel() else 0.0
+        assert rest <= 2.0 ** -126
+    c.close()
