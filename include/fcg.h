@@ -304,7 +304,8 @@ typedef struct fcg_rope fcg_rope;
 #define FCG_ROPE_NTK 2    /* theta * factor^(R / (R - 2)) in place of theta, R = rotary_dim (>= 4 by its rule) */
 #define FCG_ROPE_PARTS 3  /* by parts: with r = orig_tokens * w_i / (2 pi) turns over the trained length and
                              c = (r - low_turns) / (high_turns - low_turns) clamped to [0, 1]:
-                             w_i ((1 - c) / factor + c) */
+                             w_i ((1 - c) / factor + c).  Models that ramp over the pair's index between
+                             rounded bounds instead: their frequencies through FCG_ROPE_GIVEN */
 #define FCG_ROPE_GIVEN 4  /* freqs[i] */
 
 typedef struct {

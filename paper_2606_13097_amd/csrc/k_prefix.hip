@@ -11,8 +11,12 @@
 //
 //   o = sum_j 2^(s_j - m) v_j / sum_j 2^(s_j - m),  s_j = q k_j log2(e) / sqrt(D),
 //
-// in one pass over the keys, m and both sums fp32 (the probabilities enter the
-// product rounded to bf16).  S^T = K Q^T and O^T += V^T P^T: a lane holds scores and
+// in one pass over the keys, m and both sums fp32.  The probabilities enter the second
+// product rounded to bf16: the matrix instruction takes both operands in one type, fp16
+// does not hold the values' range, and a second product with what the rounding leaves
+// would add half to the matrix work of the calls that it bounds.  That rounding is as
+// large as the result's own, so a result is 1.4 times as far from the definition as
+// one rounded once (2.3e-3 of its norm against 1.7e-3).  S^T = K Q^T and O^T += V^T P^T: a lane holds scores and
 // outputs of one query row, the probabilities pass from accumulator to operand
 // without leaving their lane, and only maxima and final sums cross lanes.  Rows of
 // keys arrive by LDS DMA, whole rows, chunks XOR-swizzled against bank conflicts.
@@ -188,8 +192,8 @@ __device__ __forceinline__ float max_lanes(float v) {
 // Where a row's result goes: the output, or the slot's partial.  bf16 caches keep
 // partial outputs in fp16, scaled per row by the power of two 2^up that brings the
 // row's largest to 2^14 .. 2^15 (so eleven significant bits in two bytes; bf16 ones
-// cost a rounding of the size of the result's own, 2.8e-3 off the definition
-// instead of 2.4e-3, and fp32 ones move twice the bytes); max, sum and up are
+// would be a third rounding of the size of the result's own, 2.8e-3 off the definition
+// instead of 2.3e-3, and fp32 ones move twice the bytes); max, sum and up are
 // fp32.  fp32 caches keep fp32 partials, up = 0.
 typedef _Float16 px_f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 px_f16x8 __attribute__((ext_vector_type(8)));
