@@ -565,7 +565,10 @@ def fcg_append(cache: Cache, layer: int, seq, pos, k=None, v=None, rope: Optiona
     if q is not None and q_out is None:
         raise ValueError("q without q_out")
     if k is not None:
-        n_layers = k.shape[0] if k.dim() == 4 else 1
+        layers = k.shape[0] if k.dim() == 4 else 1
+        if n_layers != 1 and n_layers != layers:
+            raise ValueError(f"n_layers {n_layers}, but k has {layers} layers")
+        n_layers = layers
     d, n = cache.desc, int(s.size)
     sq, skv = (n_layers, n, d.n_q_heads, d.head_dim), (n_layers, n, d.n_kv_heads, d.head_dim)
     td, dev = _DT_TORCH[d.dtype], cache.device

@@ -72,3 +72,16 @@ def test_calls_take_the_stream_of_their_caches_device(monkeypatch):
     fcg.fcg_append(c, 0, [0], [20])
     fcg.fcg_prefix_attend(c, 0, 0, 16, [0], [15], None, None)
     assert seen == dict.fromkeys(seen, 1005) and len(seen) == 3
+
+
+def test_append_refuses_a_layer_count_that_its_keys_contradict():
+    """n_layers is that of reservations; keys bring theirs.  Another one was ignored: the other layers stayed unwritten."""
+    c = fcg.Cache(fcg.model_desc(4, 4, 2, 64, 1e4, "bf16"), 2, 64, flags=fcg.FCG_LAYOUT_ONLY)
+    for shape, n in (((3, 2, 64), 2), ((2, 3, 2, 64), 3), ((2, 3, 2, 64), 4), ((1, 3, 2, 64), 2)):
+        with pytest.raises(ValueError, match="layers"):
+            x = torch.zeros(shape, dtype=torch.bfloat16)
+            fcg.fcg_append(c, 0, [0, 0, 0], [0, 1, 2], x, x, n_layers=n)
+    for shape, n in (((3, 2, 64), 1), ((2, 3, 2, 64), 1), ((2, 3, 2, 64), 2)):      # past that check
+        with pytest.raises(ValueError, match="GPU"):
+            x = torch.zeros(shape, dtype=torch.bfloat16)
+            fcg.fcg_append(c, 0, [0, 0, 0], [0, 1, 2], x, x, n_layers=n)
