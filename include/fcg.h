@@ -423,6 +423,76 @@ fcg_status fcg_prefix_attend(fcg_cache* cache, int32_t layer, int32_t prefix_seq
                              const int32_t* seq, const int32_t* pos, const fcg_tensor* q, const fcg_tensor* out,
                              float* lse, void* stream);
 
+/* ------------------------------------------- norms of queries and keys */
+
+/* Models that normalise queries and keys head by head before they turn them.
+ * A row x of head_dim elements becomes
+ *   n = (offset + weight) x / sqrt(mean(x^2) + eps),
+ * the mean over the head, in fp32.  weight: device, storage dtype, head_dim
+ * adjacent elements that may start anywhere, `head` elements from a head's to
+ * the next head's and `layer` from a layer's to the next (0: shared); null: all
+ * ones, offset ignored.  offset is 1 for models that store the distance from 1. */
+typedef struct {
+  const void* weight;
+  int64_t layer; /* >= 0; layers count from the call's first one */
+  int64_t head;  /* >= 0 */
+  double eps;    /* > 0, a normal fp32 number */
+  double offset; /* finite in fp32 */
+} fcg_norm;
+
+/* fcg_rope_apply of normalised rows in one pass: norm, turn and attention
+ * factor in fp32, rounded once to dtype.  Arguments, in-place outputs and
+ * capture as there; q_norm or k_norm null: those rows are turned only.  A row
+ * of which an element is not finite, or whose squares add up past the fp32
+ * range, gives what that arithmetic gives (NaN; zeros).
+ * Errors: as fcg_rope_apply, and EINVAL (a norm's strides, eps or offset). */
+fcg_status fcg_norm_rope_apply(const fcg_rope* rope, int32_t dtype, int32_t head_dim, int32_t n_layers, int32_t n_tok,
+                               const int32_t* pos, int32_t n_q_heads, const fcg_norm* q_norm, const fcg_tensor* q,
+                               const fcg_tensor* q_out, int32_t n_k_heads, const fcg_norm* k_norm,
+                               const fcg_tensor* k, const fcg_tensor* k_out, void* stream);
+
+/* One side, queries or keys, of fcg_norm_rope_backward. */
+typedef struct {
+  int32_t heads;
+  const fcg_norm* norm; /* null: rows that are turned only */
+  fcg_tensor x;         /* the forward pass's input (not read with norm null) */
+  fcg_tensor grad;      /* the gradient of its result */
+  fcg_tensor dx;        /* receives the gradient of its input; may be x or grad in place */
+  float* dweight;       /* receives the gradient of the weights, device fp32, contiguous: [n_layers][heads][head_dim],
+                           or [n_layers][head_dim] where the norm's head stride is 0 or there is one head (weights shared
+                           by layers: their sum over layers is the caller's); null: not wanted */
+} fcg_norm_side;
+
+/* Device bytes that fcg_norm_rope_backward needs with weight gradients for such
+ * sides (heads of 0: none).  Errors: EINVAL (counts, head_dim, null output). */
+fcg_status fcg_norm_rope_workspace(int32_t head_dim, int32_t n_layers, int32_t n_tok, int32_t n_q_heads,
+                                   int32_t n_k_heads, int64_t* bytes);
+
+/* The gradient of fcg_norm_rope_apply: with dn the gradient turned back (and
+ * times the attention factor), s = 1 / sqrt(mean(x^2) + eps) and w the weights
+ * with their offset,
+ *   dweight = sum over rows of dn x s,  dx = s (dn w - x s mean(dn w x s)),
+ * in fp32; dx rounded once to dtype, dweight fp32, added up in a fixed order
+ * (the same call gives the same bits).  q, k: host; either may be null.
+ * workspace: device, 16-byte aligned, fcg_norm_rope_workspace bytes, of any
+ * content, for this call alone until it is done; null where no dweight is
+ * wanted.  Nothing is allocated or uploaded: the call can be captured.
+ * Errors: as fcg_norm_rope_apply, and EINVAL (a dweight without weights, a
+ * workspace that is too small or not aligned). */
+fcg_status fcg_norm_rope_backward(const fcg_rope* rope, int32_t dtype, int32_t head_dim, int32_t n_layers,
+                                  int32_t n_tok, const int32_t* pos, const fcg_norm_side* q, const fcg_norm_side* k,
+                                  void* workspace, int64_t workspace_bytes, void* stream);
+
+/* fcg_append of normalised queries and keys (values as they are).  q_norm and
+ * k_norm may be null: those rows are turned only.  The same bits for a query or
+ * key as fcg_norm_rope_apply with the same rope gives.
+ * Errors: as fcg_append, and EINVAL (a norm's strides, eps or offset; a norm
+ * without the rows it is for). */
+fcg_status fcg_append_norm(fcg_cache* cache, int32_t layer, int32_t n_layers, int32_t n_tok, const int32_t* seq,
+                           const int32_t* pos, const fcg_rope* rope, const fcg_norm* q_norm, const fcg_norm* k_norm,
+                           const fcg_tensor* q, const fcg_tensor* q_out, const fcg_tensor* k, const fcg_tensor* v,
+                           uint32_t flags, void* stream);
+
 /* ------------------------------------------------- code-cache management */
 
 /* Locality score of the cache entries (Sec. 4.1, Eq. 3; App. B.1, Eq. 8-10;

@@ -342,6 +342,49 @@ int launch_graft_rope(int dtype, bool pairs, const GraftChunk* runs, const Graft
                       const void* lib_k, const void* lib_v, int64_t cap, const CacheView& cv, const RopeArgs& ra, int L,
                       hipStream_t s, KTime tm = {});
 
+// Norm of each row before its turn: weights in the storage dtype, strides in elements
+// between layers and heads (0: shared).
+struct NormView {
+  const void* w;  // null: ones
+  int64_t layer, head;
+  float eps, offset;
+  int32_t on;  // 0: these rows are turned only
+};
+template <bool NORM>
+struct NormArgs {};
+template <>
+struct NormArgs<true> {
+  NormView q, k;
+};
+
+// launch_rope_apply and launch_append with norms.
+int launch_norm_rope(int dtype, int D, bool pairs, const RopeRows& rows, const int32_t* pos, const RopeArgs& ra,
+                     const NormArgs<true>& norm, hipStream_t s);
+int launch_append_norm(int dtype, bool pairs, const RopeRows& rows, const AppendArgs& args, int n_runs,
+                       const AppendGroup* groups, int n_groups, const CacheView& cv, int layer0, const RopeArgs& ra,
+                       const float2* tab, const NormArgs<true>& norm, hipStream_t s);
+
+// The gradient of norm and turn.  A side is the queries or the keys; its blocks take
+// head_blocks ranges of `heads_per` heads, `spread` of them beside each other every
+// `spread`-th chunk of norm_tokens(D) tokens.  Weight gradients: a partial [D] for each
+// (layer, weight head, partial of `parts`), summed by a second launch.
+constexpr int kNormHeads = 8;
+constexpr int norm_tokens(int D) { return D == 64 ? 64 : 32; }
+struct NormSide {
+  RowView x, gy, dx;
+  NormView norm;
+  float* dw;         // [layers][weight heads][D], null: not asked for
+  int64_t part0;     // first partial of the side, in floats
+  int32_t heads, w_heads, heads_per, head_blocks, spread, parts;
+};
+struct NormGradArgs {
+  NormSide side[2];
+  const int32_t* pos;
+  float* part;
+  int32_t n_tok, n_layers, blocks_q;  // blocks of the first side (of one layer)
+};
+int launch_norm_rope_grad(int dtype, int D, bool pairs, const NormGradArgs& args, const RopeArgs& ra, hipStream_t s);
+
 // Attention over a shared prefix.  Query rows are sorted by rank (token) and,
 // per kv head, numbered rank * g + j; an item attends rows [row0, row0 + n_row)
 // over prefix positions [a0, a1) and then positions [b0, b1) of sequence seq,

@@ -5,57 +5,9 @@
 #include <cmath>
 
 #include "objects.hpp"
+#include "ops.hpp"
 
 using namespace fcg;
-
-namespace {
-
-fcg_status fail(fcg_status s, const std::string& msg) { return report(s, msg); }
-
-bool capturing(hipStream_t s) {
-  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(s, &st) == hipSuccess) return st != hipStreamCaptureStatusNone;
-  (void)hipGetLastError();  // not this call's error
-  return false;
-}
-
-RowView view_of(const fcg_tensor* t) {
-  return t ? RowView{t->data, t->layer, t->token, t->head} : RowView{nullptr, 0, 0, 0};
-}
-
-// strides of a tensor [layers][tokens][heads][D]
-fcg_status check_strides(const fcg_tensor* t, const char* what) {
-  if (t && (t->layer < 0 || t->token < 0 || t->head < 0))
-    return fail(FCG_EINVAL, std::string(what) + ": negative stride");
-  return FCG_OK;
-}
-
-// Rows of an output must not meet: sorted by stride, each dimension steps over
-// what the smaller ones cover.
-fcg_status check_output(const fcg_tensor* t, int64_t layers, int64_t tokens, int64_t heads, int64_t D, const char* what) {
-  std::pair<int64_t, int64_t> dim[3] = {{t->layer, layers}, {t->token, tokens}, {t->head, heads}};  // stride, size
-  std::sort(dim, dim + 3);
-  int64_t extent = D;
-  for (auto& d : dim) {
-    if (d.second <= 1) continue;
-    if (d.first < extent) return fail(FCG_EINVAL, std::string(what) + ": rows of an output overlap");
-    extent = d.first * (d.second - 1) + extent;
-  }
-  return FCG_OK;
-}
-
-bool same_view(const fcg_tensor* a, const fcg_tensor* b) {
-  return a->data == b->data && a->layer == b->layer && a->token == b->token && a->head == b->head;
-}
-
-// an output that starts where its input does is that input in place, or an error
-fcg_status check_alias(const fcg_tensor* in, const fcg_tensor* out, const char* what) {
-  if (in->data == out->data && !same_view(in, out))
-    return fail(FCG_EINVAL, std::string(what) + ": an output in its input's place needs its strides");
-  return FCG_OK;
-}
-
-}  // namespace
 
 // ---------------------------------------------------------------- rotary forms
 
@@ -117,8 +69,6 @@ fcg_status fcg_rope_destroy(fcg_rope* rope) {
   return FCG_OK;
 }
 
-namespace {
-
 // How the tokens' rows are cut into blocks.  A block moves slice_rows rows of a group of
 // tb tokens, kRopePass pairs of vectors (nch of each row).  Groups as large as fill their
 // slices best, while there are a few blocks for each compute unit: the (cos, sin) of a token
@@ -127,7 +77,7 @@ namespace {
 // they do (32 layers of 713 tokens of 8 heads, one layer a block 18.2 us, two 17.3, three
 // 16.2, four 16.7); larger calls keep one (8 layers of 11K tokens into pages, one 417 us,
 // two 429, three 436).
-void cut_rows(RopeRows* rows, int64_t n_tok, int64_t n_layers, int H, int nch) {
+void fcg::cut_rows(RopeRows* rows, int64_t n_tok, int64_t n_layers, int H, int nch) {
   constexpr int64_t kResident = 2048;
   const int slice = kRopePass / nch;
   rows->tb = 1;
@@ -151,8 +101,6 @@ void cut_rows(RopeRows* rows, int64_t n_tok, int64_t n_layers, int H, int nch) {
   // there (96 MB in all 17.2 us, read past the caches 21.4).
   rows->stream = n_tok * n_layers * H * nch * 32 > (int64_t)256 << 20;
 }
-
-}  // namespace
 
 fcg_status fcg_rope_apply(const fcg_rope* rope, int32_t dtype, int32_t head_dim, int32_t n_layers, int32_t n_tok,
                           const int32_t* pos, int32_t n_q_heads, const fcg_tensor* q, const fcg_tensor* q_out,
@@ -217,9 +165,10 @@ fcg_status fcg_rope_apply(const fcg_rope* rope, int32_t dtype, int32_t head_dim,
 
 // ---------------------------------------------------------------------- append
 
-fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_tok, const int32_t* seq,
-                      const int32_t* pos, const fcg_rope* rope, const fcg_tensor* q, const fcg_tensor* q_out,
-                      const fcg_tensor* k, const fcg_tensor* v, uint32_t flags, void* stream) {
+fcg_status fcg::append_tokens(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_tok, const int32_t* seq,
+                              const int32_t* pos, const fcg_rope* rope, const fcg_tensor* q, const fcg_tensor* q_out,
+                              const fcg_tensor* k, const fcg_tensor* v, uint32_t flags, void* stream,
+                              const AppendLaunch& launch) {
   if (!c) return fail(FCG_EINVAL, "null cache");
   if (n_layers < 0 || n_tok < 0) return fail(FCG_EINVAL, "negative count");
   if (n_tok > 0 && (!seq || !pos)) return fail(FCG_EINVAL, "null token array");
@@ -321,8 +270,8 @@ fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_t
         }
         args.run[i] = r;
       }
-      const int rc = launch_append(d.dtype, pairs, rows, args, (int)runs.size(), nullptr, n_groups, c->view(), layer, ra,
-                                   tab, s);
+      const int rc = launch.fn(launch.context, d.dtype, pairs, rows, args, (int)runs.size(), nullptr, n_groups, c->view(),
+                               layer, ra, tab, s);
       if (rc) return hip_fail((hipError_t)rc, "append launch");
       return commit();
     }
@@ -344,12 +293,25 @@ fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_t
     char* dplan = nullptr;
     if (fcg_status st = upload(c, blob, page_rows, s, &dplan, &staged)) return st;
     for (size_t i = 0; i < groups.size(); i += kGridX)
-      if (int rc = launch_append(d.dtype, pairs, rows, AppendArgs{}, 0, (const AppendGroup*)(dplan + o_groups) + i,
-                                 (int)std::min<size_t>(kGridX, groups.size() - i), c->view(), layer, ra, tab, s))
+      if (int rc = launch.fn(launch.context, d.dtype, pairs, rows, AppendArgs{}, 0,
+                             (const AppendGroup*)(dplan + o_groups) + i, (int)std::min<size_t>(kGridX, groups.size() - i),
+                             c->view(), layer, ra, tab, s))
         return hip_fail((hipError_t)rc, "append launch");
     if (fcg_status st = c->ring.retire(s)) return st;
     return commit();
   });
+}
+
+fcg_status fcg_append(fcg_cache* c, int32_t layer, int32_t n_layers, int32_t n_tok, const int32_t* seq,
+                      const int32_t* pos, const fcg_rope* rope, const fcg_tensor* q, const fcg_tensor* q_out,
+                      const fcg_tensor* k, const fcg_tensor* v, uint32_t flags, void* stream) {
+  auto launch = [](const void*, int dtype, bool pairs, const RopeRows& rows, const AppendArgs& args, int n_runs,
+                   const AppendGroup* groups, int n_groups, const CacheView& cv, int layer0, const RopeArgs& ra,
+                   const float2* tab, hipStream_t s) {
+    return launch_append(dtype, pairs, rows, args, n_runs, groups, n_groups, cv, layer0, ra, tab, s);
+  };
+  return append_tokens(c, layer, n_layers, n_tok, seq, pos, rope, q, q_out, k, v, flags, stream,
+                       AppendLaunch{launch, nullptr});
 }
 
 // ------------------------------------------------------------ prefix attention
@@ -598,11 +560,14 @@ void plan_prefix(const fcg_model_desc& d, int32_t P, int32_t n, const int32_t* s
   for (const PrefixRank& r : p->ranks) p->direct = p->direct && r.na + r.nb == 1;
 }
 
+}  // namespace
+
 // The workspace of prefix partials.  One that a captured graph uses is kept until
 // the cache is destroyed when a larger one takes its place.
-fcg_status prefix_workspace(fcg_cache* c, size_t bytes, bool cap) {
+fcg_status fcg::prefix_workspace(fcg_cache* c, size_t bytes, bool cap, const char* call) {
   if (bytes > c->xpart_bytes) {
-    if (cap) return fail(FCG_ESTATE, "fcg_prefix_attend needs a larger workspace: run a call of this size before the capture");
+    if (cap)
+      return fail(FCG_ESTATE, std::string(call) + " needs a larger workspace: run a call of this size before the capture");
     if (c->xpart_captured) {
       c->xkept.push_back(c->xpart);
       c->xpart = nullptr;
@@ -614,8 +579,6 @@ fcg_status prefix_workspace(fcg_cache* c, size_t bytes, bool cap) {
   if (cap) c->xpart_captured = true;
   return FCG_OK;
 }
-
-}  // namespace
 
 fcg_status fcg_prefix_attend(fcg_cache* c, int32_t layer, int32_t prefix_seq, int32_t prefix_len, int32_t n_tok,
                              const int32_t* seq, const int32_t* pos, const fcg_tensor* q, const fcg_tensor* out,
@@ -652,7 +615,7 @@ fcg_status fcg_prefix_attend(fcg_cache* c, int32_t layer, int32_t prefix_seq, in
     // what needs an upload cannot be captured: its staging memory is used again
     if (cap && !p.by_value) return fail(FCG_ESTATE, "this prefix attention has too many tokens to be captured into a graph");
     if (work)
-      if (fcg_status st = prefix_workspace(c, o_bytes + prow * 16, cap)) return st;
+      if (fcg_status st = prefix_workspace(c, o_bytes + prow * 16, cap, "fcg_prefix_attend")) return st;
     PrefixCall pc{};
     pc.q = view_of(q);
     pc.out = view_of(out);

@@ -43,6 +43,7 @@ EXPORTS = [
     "fcg_locality_residency", "fcg_locality_destroy",
     "fcg_rope_create", "fcg_rope_frequencies", "fcg_rope_destroy", "fcg_rope_apply", "fcg_graft_rope", "fcg_append",
     "fcg_prefix_attend",
+    "fcg_norm_rope_apply", "fcg_norm_rope_workspace", "fcg_norm_rope_backward", "fcg_append_norm",
 ]
 FCG_ROPE_HALF, FCG_ROPE_PAIRS = 0, 1
 FCG_ROPE_PLAIN, FCG_ROPE_LINEAR, FCG_ROPE_NTK, FCG_ROPE_PARTS, FCG_ROPE_GIVEN = range(5)
@@ -72,6 +73,18 @@ class RopeDesc(C.Structure):
 class TensorView(C.Structure):
     """``fcg_tensor``: address and strides (elements) of layer, token and head."""
     _fields_ = [("data", C.c_void_p), ("layer", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class NormDesc(C.Structure):
+    """``fcg_norm``: weights of a row norm and their strides."""
+    _fields_ = [("weight", C.c_void_p), ("layer", C.c_int64), ("head", C.c_int64), ("eps", C.c_double),
+                ("offset", C.c_double)]
+
+
+class NormSide(C.Structure):
+    """``fcg_norm_side``: queries or keys of a norm's gradient."""
+    _fields_ = [("heads", C.c_int32), ("norm", C.POINTER(NormDesc)), ("x", TensorView), ("grad", TensorView),
+                ("dx", TensorView), ("dweight", C.c_void_p)]
 
 
 def model_desc(n_layers, n_q_heads, n_kv_heads, head_dim, rope_theta, dtype) -> ModelDesc:
@@ -126,6 +139,13 @@ def _load():
         "fcg_graft_rope": [P, P, P, I32, P, P, P, P],
         "fcg_append": [P, I32, I32, I32, P, P, P, PT, PT, PT, PT, U32, P],
         "fcg_prefix_attend": [P, I32, I32, I32, I32, P, P, PT, PT, P, P],
+    })
+    PN, PS = C.POINTER(NormDesc), C.POINTER(NormSide)
+    sig.update({
+        "fcg_norm_rope_apply": [P, I32, I32, I32, I32, P, I32, PN, PT, PT, I32, PN, PT, PT, P],
+        "fcg_norm_rope_workspace": [I32, I32, I32, I32, I32, PI64],
+        "fcg_norm_rope_backward": [P, I32, I32, I32, I32, P, PS, PS, P, I64, P],
+        "fcg_append_norm": [P, I32, I32, I32, P, P, P, PN, PN, PT, PT, PT, PT, U32, P],
     })
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -593,6 +613,158 @@ def fcg_prefix_attend(cache: Cache, layer: int, prefix_seq: int, prefix_len: int
         raise ValueError("lse: a contiguous float32 GPU tensor [n_tok][Hq]")
     _check(_L.fcg_prefix_attend(cache.h, int(layer), int(prefix_seq), int(prefix_len), n, _p(s), _p(p), _ref(vq),
                                 _ref(vo), _dptr(lse), _stream_of(stream, cache.device)))
+
+
+# ------------------------------------------- norms of queries and keys
+
+class Norm:
+    """A norm of rows (``fcg_norm``): (offset + weight) x / sqrt(mean(x^2) + eps) over each head.  weight: [head_dim],
+    [heads][head_dim] or [layers][heads][head_dim] (a dimension of 1 is shared), or None for ones."""
+
+    def __init__(self, weight=None, eps: float = 1e-6, offset: float = 0.0):
+        if weight is not None:
+            if weight.dim() not in (1, 2, 3) or (weight.numel() and weight.stride(-1) != 1):
+                raise ValueError("norm weight: one to three dimensions, the elements of a head adjacent")
+        self.weight = weight
+        step = [0, 0]
+        if weight is not None:
+            for i, (n, st) in enumerate(zip(weight.shape[-2::-1], weight.stride()[-2::-1])):   # heads, then layers
+                step[i] = st if n > 1 else 0
+        self.desc = NormDesc(None if weight is None else weight.data_ptr(), step[1], step[0], float(eps), float(offset))
+
+    def dweight_shape(self, layers: int, heads: int) -> tuple:
+        """Shape of the weights' gradient: [layers][heads or 1][head_dim]."""
+        return (layers, heads if self.desc.head and heads > 1 else 1, self.weight.shape[-1])
+
+
+def _norm_ref(norm: Optional[Norm], layers: int, heads: int, d: int, dtype, device, what: str):
+    if norm is None:
+        return None
+    w = norm.weight
+    if w is not None:
+        if w.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{what}: the weights require a gradient, which these calls do not record")
+        if w.dtype is not dtype or w.get_device() != device:
+            raise ValueError(f"{what}: weights of {w.dtype} on {w.device}, expected {dtype} on GPU {device}")
+        sh = w.shape
+        if sh[-1] != d or (len(sh) > 1 and sh[-2] not in (1, heads)) or (len(sh) > 2 and sh[0] not in (1, layers)):
+            raise ValueError(f"{what}: weights of shape {tuple(sh)} for {layers} layers of {heads} heads of {d}")
+    return C.byref(norm.desc)
+
+
+def _rows_of(pos, q, k):
+    """(dtype, device, layers, tokens, head_dim, query heads, key heads) of the rows at ``pos``."""
+    if not pos.is_cuda or pos.dtype != torch.int32 or pos.dim() != 1 or not pos.is_contiguous():
+        raise ValueError("pos: a contiguous int32 GPU tensor [n_tok]")
+    like = q if q is not None else k
+    if like is None:
+        raise ValueError("neither q nor k")
+    if like.dtype not in _TORCH_DT or like.dim() not in (3, 4):
+        raise ValueError("a float32 or bfloat16 tensor of three or four dimensions")
+    layers = like.shape[0] if like.dim() == 4 else 1
+    return (like.dtype, pos.get_device(), layers, pos.numel(), like.shape[-1], 0 if q is None else q.shape[-2],
+            0 if k is None else k.shape[-2])
+
+
+def _on_device(dev: int, fn, args) -> None:
+    if dev == torch.cuda.current_device():
+        _check(fn(*args))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args))
+
+
+def _workspace(given, nbytes: int, dev: int, stream):
+    """(address, bytes) of a call's workspace; without one, memory of the current stream's pool."""
+    if given is None:
+        if not nbytes:
+            return None, 0, None
+        if stream is not None and _stream(stream) != _stream_of(None, dev):
+            raise ValueError("a call on a stream other than the current one needs a workspace of its own")
+        given = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{dev}")
+    if given.get_device() != dev or not given.is_contiguous():
+        raise ValueError(f"workspace: a contiguous tensor on GPU {dev}")
+    return given.data_ptr(), given.numel() * given.element_size(), given
+
+
+def fcg_norm_rope_apply(rope: Rope, pos, q=None, q_norm: Optional[Norm] = None, q_out=None, k=None,
+                        k_norm: Optional[Norm] = None, k_out=None, stream=None) -> None:
+    """``fcg_rope_apply`` of rows that q_norm and k_norm normalise first; records no gradient either."""
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError("an input without its output, or an output without its input")
+    td, dev, layers, n, d, hq, hk = _rows_of(pos, q, k)
+    sq, sk = (layers, n, hq, d), (layers, n, hk, d)
+    vq, vqo = _view(q, sq, td, dev, "q"), _view(q_out, sq, td, dev, "q_out")
+    vk, vko = _view(k, sk, td, dev, "k"), _view(k_out, sk, td, dev, "k_out")
+    nq = None if q is None else _norm_ref(q_norm, layers, hq, d, td, dev, "q_norm")
+    nk = None if k is None else _norm_ref(k_norm, layers, hk, d, td, dev, "k_norm")
+    _on_device(dev, _L.fcg_norm_rope_apply, (rope.h, _TORCH_DT[td], d, layers, n, pos.data_ptr(), hq, nq, _ref(vq),
+                                             _ref(vqo), hk, nk, _ref(vk), _ref(vko), _stream_of(stream, dev)))
+
+
+def fcg_norm_rope_workspace(n_layers: int, n_tok: int, n_q_heads: int, n_k_heads: int, head_dim: int) -> int:
+    """Bytes that ``fcg_norm_rope_backward`` needs for weight gradients."""
+    n = C.c_int64()
+    _check(_L.fcg_norm_rope_workspace(int(head_dim), int(n_layers), int(n_tok), int(n_q_heads), int(n_k_heads), C.byref(n)))
+    return n.value
+
+
+def _norm_side(x, norm, grad, dx, dw, shape, td, dev, what: str):
+    if grad is None:
+        if x is not None or dx is not None or dw is not None:
+            raise ValueError(f"{what}: without the gradient of its result")
+        return None
+    if dx is None or (x is None and norm is not None):
+        raise ValueError(f"{what}: a gradient without the input or its own output")
+    ref = _norm_ref(norm, shape[0], shape[2], shape[3], td, dev, what + "_norm")
+    if dw is not None:
+        if norm is None or norm.weight is None:
+            raise ValueError(f"{what}: a gradient of weights that are not given")
+        want = norm.dweight_shape(shape[0], shape[2])
+        if (dw.dtype != torch.float32 or dw.get_device() != dev or not dw.is_contiguous() or
+                dw.numel() != want[0] * want[1] * want[2]):
+            raise ValueError(f"{what}: weight gradient, a contiguous float32 GPU tensor {want}")
+    empty = TensorView(None, 0, 0, 0)
+    return NormSide(shape[2], None if ref is None else C.pointer(norm.desc), _view(x, shape, td, dev, what) or empty,
+                    _view(grad, shape, td, dev, what + "_grad"), _view(dx, shape, td, dev, "d" + what), _dptr(dw))
+
+
+def fcg_norm_rope_backward(rope: Rope, pos, q=None, q_norm: Optional[Norm] = None, q_grad=None, dq=None, dq_weight=None,
+                           k=None, k_norm: Optional[Norm] = None, k_grad=None, dk=None, dk_weight=None, workspace=None,
+                           stream=None) -> None:
+    """Gradient of ``fcg_norm_rope_apply``: from that of its results (q_grad, k_grad) to that of its inputs (dq, dk) and
+    of the norms' weights (float32, of ``Norm.dweight_shape``)."""
+    td, dev, layers, n, d, hq, hk = _rows_of(pos, q_grad, k_grad)
+    sides = (_norm_side(q, q_norm, q_grad, dq, dq_weight, (layers, n, hq, d), td, dev, "q"),
+             _norm_side(k, k_norm, k_grad, dk, dk_weight, (layers, n, hk, d), td, dev, "k"))
+    need = 0
+    if workspace is None and (dq_weight is not None or dk_weight is not None):
+        need = fcg_norm_rope_workspace(layers, n, hq, hk, d)
+    ws, nbytes, keep = _workspace(workspace, need, dev, stream)
+    _on_device(dev, _L.fcg_norm_rope_backward, (rope.h, _TORCH_DT[td], d, layers, n, pos.data_ptr(), _ref(sides[0]),
+                                                _ref(sides[1]), ws, nbytes, _stream_of(stream, dev)))
+
+
+def fcg_append_norm(cache: Cache, layer: int, seq, pos, k, v, k_norm: Optional[Norm] = None, rope: Optional[Rope] = None,
+                    q=None, q_norm: Optional[Norm] = None, q_out=None, flags: int = 0, stream=None) -> None:
+    """``fcg_append`` of keys and queries that k_norm and q_norm normalise first."""
+    s, p = _i32(seq), _i32(pos)
+    if s.ndim != 1 or s.shape != p.shape:
+        raise ValueError("seq and pos differ in length")
+    if k is None or v is None:
+        raise ValueError("k and v")
+    if (q is None) != (q_out is None) or (q is None and q_norm is not None):
+        raise ValueError("q, its norm and q_out belong together")
+    layers = k.shape[0] if k.dim() == 4 else 1
+    d, n = cache.desc, int(s.size)
+    td, dev = _DT_TORCH[d.dtype], cache.device
+    sq, skv = (layers, n, d.n_q_heads, d.head_dim), (layers, n, d.n_kv_heads, d.head_dim)
+    vq, vqo = _view(q, sq, td, dev, "q"), _view(q_out, sq, td, dev, "q_out")
+    vk, vv = _view(k, skv, td, dev, "k"), _view(v, skv, td, dev, "v")
+    nq = _norm_ref(q_norm, layers, d.n_q_heads, d.head_dim, td, dev, "q_norm")
+    nk = _norm_ref(k_norm, layers, d.n_kv_heads, d.head_dim, td, dev, "k_norm")
+    _check(_L.fcg_append_norm(cache.h, int(layer), layers, n, _p(s), _p(p), None if rope is None else rope.h, nq, nk,
+                              _ref(vq), _ref(vqo), _ref(vk), _ref(vv), int(flags), _stream_of(stream, dev)))
 
 
 def fcg_status_string(status: int) -> str:
