@@ -493,6 +493,28 @@ fcg_status fcg_append_norm(fcg_cache* cache, int32_t layer, int32_t n_layers, in
                            const fcg_tensor* q, const fcg_tensor* q_out, const fcg_tensor* k, const fcg_tensor* v,
                            uint32_t flags, void* stream);
 
+/* ------------------------------------ what a cache keeps of its positions */
+
+/* The attention weight that the tokens of a call put on each position they
+ * attend to: for the tokens, keys and q of an fcg_prefix_attend at one layer and
+ * the lse it returned (device fp32 [n_tok][Hq], contiguous),
+ *   weights[s][h][j] = sum of exp(q k_j / sqrt(D) - lse[t])
+ * over the tokens t that attend to position j of sequence s and over the query
+ * heads of kv head h, in fp32, added up in a fixed order (the same call gives
+ * the same bits).  weights: device fp32 [n_seqs][Hkv][max_tokens], one layer's,
+ * contiguous: prefix positions in row prefix_seq, own positions in each token's
+ * row; elements of positions that no token of the call attends to stay as they
+ * are.  FCG_ADD: the sums are added to what the elements hold (a decode loop
+ * that keeps score; clear them first).
+ * Split partials sit in the workspace of fcg_prefix_attend, with its rules for
+ * captures and overlapping calls; a call can be captured if it has at most 128
+ * tokens of at most 64 sequences (and attends to less than 8 million positions).
+ * Errors: as fcg_prefix_attend (of q, lse and weights none may be null). */
+#define FCG_ADD 1u
+fcg_status fcg_attend_weights(fcg_cache* cache, int32_t layer, int32_t prefix_seq, int32_t prefix_len, int32_t n_tok,
+                              const int32_t* seq, const int32_t* pos, const fcg_tensor* q, const float* lse,
+                              float* weights, uint32_t flags, void* stream);
+
 /* ------------------------------------------------- code-cache management */
 
 /* Locality score of the cache entries (Sec. 4.1, Eq. 3; App. B.1, Eq. 8-10;

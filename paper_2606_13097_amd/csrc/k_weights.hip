@@ -1,0 +1,277 @@
+// Attention weight that each cached position receives from the queries of a call, for
+// gfx950:
+//
+//   W[j] (+)= sum over rows r that see key j of 2^(q_r k_j c - l_r),
+//   c = log2(e) / sqrt(D), l_r = log2(e) lse_r,
+//
+// the probabilities recomputed from the log-sum-exp that attention returned.  A block
+// holds 128 or 256 keys of one kv head as matrix operands in registers and takes the
+// query rows past them, 64 at a time through LDS, so a key is read once for every
+// split of the rows and the sums stay in registers: S = Q K^T with a key per
+// lane (32x32 products), the 16 rows a lane has of each product added up there, the two
+// lanes of a key joined at the end.  No atomics: the same call gives the same bits.
+//
+// Where a call has few keys and many rows, its rows are cut into splits that leave
+// partials, added in their order by weights_merge_kernel.
+//
+// fp32 caches: the same on 32x32x2 products, four for each 16-byte vector (elements e of
+// the two lanes' vectors together make a product's depth of two; the order of the head's
+// elements in a sum is free).
+#include "fcg_device.hpp"
+#include "kernels.hpp"
+
+namespace fcg {
+
+namespace {
+
+typedef __bf16 wt_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float wt_f32x16 __attribute__((ext_vector_type(16)));
+
+template <typename T>
+__device__ __forceinline__ wt_f32x16 mma(const uint4& a, const uint4& b, wt_f32x16 c);
+template <>
+__device__ __forceinline__ wt_f32x16 mma<bf16_t>(const uint4& a, const uint4& b, wt_f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(wt_bf16x8, a), __builtin_bit_cast(wt_bf16x8, b), c,
+                                                 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ wt_f32x16 mma<float>(const uint4& a, const uint4& b, wt_f32x16 c) {
+  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+}
+
+constexpr int kTileRows = 64;  // query rows of an LDS tile
+
+// The plan of a call: in device memory, or by value.
+template <bool VALUE>
+struct Plan {};
+template <>
+struct Plan<false> {
+  const WeightItem* items;
+  const WeightRank* ranks;
+  __device__ __forceinline__ WeightItem item(int b) const { return items[b]; }
+  __device__ __forceinline__ WeightRank rank(int r) const { return ranks[r]; }
+};
+template <>
+struct Plan<true> {
+  WeightArgs a;
+  __device__ __forceinline__ WeightItem item(int b) const {
+    if (b < a.n_pre) return cut(a.pre, b);
+    // the group is the last one whose first item is at most b
+    static_assert(kWgtGroups == 64, "one group per lane");
+    const int lane = threadIdx.x & 63;
+    const WeightGroup mine = a.group[min(lane, a.n_group - 1)];
+    const uint64_t below = __builtin_amdgcn_ballot_w64(lane < a.n_group && mine.item0 <= b);
+    const int r = 63 - __builtin_clzll(below);
+    WeightGroup x;
+    x.seq = __builtin_amdgcn_readlane(mine.seq, r);
+    x.lo = __builtin_amdgcn_readlane(mine.lo, r);
+    x.hi = __builtin_amdgcn_readlane(mine.hi, r);
+    x.row0 = __builtin_amdgcn_readlane(mine.row0, r);
+    x.rows = __builtin_amdgcn_readlane(mine.rows, r);
+    x.item0 = __builtin_amdgcn_readlane(mine.item0, r);
+    x.kb0 = __builtin_amdgcn_readlane(mine.kb0, r);
+    return cut(x, b);
+  }
+  __device__ __forceinline__ WeightItem cut(const WeightGroup& x, int b) const {
+    const int ns = (x.rows + a.split_rows - 1) / a.split_rows, kb = (b - x.item0) / ns, s = b - x.item0 - kb * ns;
+    WeightItem it;
+    it.seq = x.seq;
+    it.k0 = x.lo + kb * a.block;
+    it.k1 = min(x.hi, it.k0 + a.block);
+    it.row0 = x.row0 + s * a.split_rows;
+    it.n_row = min(a.split_rows, x.rows - s * a.split_rows);
+    it.kb = x.kb0 + kb;
+    it.split = s;
+    it.n_split = ns;
+    return it;
+  }
+  __device__ __forceinline__ WeightRank rank(int r) const { return a.rank[r]; }
+};
+
+}  // namespace
+
+template <typename T, int D, bool PAGED, int KN, bool VALUE>
+__global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightCall wc, Plan<VALUE> plan, CacheView cv) {
+  constexpr int NC = D * (int)sizeof(T) / 16;  // 16-byte chunks of a row
+  constexpr int KS = NC / 2;                   // a pair of lanes takes two chunks a step
+  constexpr int SW = NC < 16 ? NC : 16;        // rows' chunks are XORed with the row modulo this
+  constexpr int PF = kTileRows * NC / 256;     // chunks of a tile that a thread brings in
+  __shared__ __align__(16) uint4 s_q[2][kTileRows * NC];
+  __shared__ __align__(16) float s_l[2][kTileRows];
+  __shared__ __align__(16) int s_pos[2][kTileRows];
+
+  const WeightItem it = plan.item(blockIdx.y);
+  const int hk = blockIdx.x;
+  const int t = threadIdx.x, lane = t & 63, lc = lane & 31, lh = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int g = 1 << wc.g_shift;
+
+  // this wave's keys, 32 for each of KN: lane lc (and lc + 32) the key key0 + 32 i + lc
+  uint4 kf[KN][KS];
+  const int key0 = it.k0 + 32 * KN * w;
+#pragma unroll
+  for (int i = 0; i < KN; ++i) {
+    const int key = min(key0 + 32 * i + lc, it.k1 - 1);
+    const T* row = reinterpret_cast<const T*>(cv.k) + kv_offset<PAGED>(cv, wc.layer, it.seq, hk, key);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) kf[i][s] = ld16(reinterpret_cast<const char*>(row) + (2 * s + lh) * 16);
+  }
+
+  const int n_tile = (it.n_row + kTileRows - 1) / kTileRows;
+  uint4 pf[PF];
+  float pl = 0.f;
+  int pp = 0;
+  // rows past the item's repeat its last one and see no key
+  auto fetch = [&](int ti) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < PF; ++j) {
+      const int c = j * 256 + t, r = min(ti * kTileRows + c / NC, it.n_row - 1), row = it.row0 + r;
+      const int tok = plan.rank(row >> wc.g_shift).tok, head = (hk << wc.g_shift) + (row & (g - 1));
+      const T* src = reinterpret_cast<const T*>(wc.q.p) + (int64_t)tok * wc.q.token + (int64_t)head * wc.q.head;
+      pf[j] = ld16_any(reinterpret_cast<const char*>(src) + c % NC * 16);
+    }
+    if (t < kTileRows) {
+      const int r = ti * kTileRows + t, row = it.row0 + min(r, it.n_row - 1);
+      const WeightRank m = plan.rank(row >> wc.g_shift);
+      pl = wc.lse[(int64_t)m.tok * wc.n_q_heads + (hk << wc.g_shift) + (row & (g - 1))] * 1.4426950408889634f;
+      pp = r < it.n_row ? m.pos : -1;
+    }
+  };
+  auto put = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < PF; ++j) {
+      const int c = j * 256 + t, r = c / NC;
+      s_q[b][r * NC + ((c % NC) ^ (r % SW))] = pf[j];
+    }
+    if (t < kTileRows) {
+      s_l[b][t] = pl;
+      s_pos[b][t] = pp;
+    }
+  };
+  fetch(0);
+  put(0);
+  __syncthreads();
+
+  const float scale = 1.4426950408889634f / sqrtf((float)D);
+  float sum[KN];
+#pragma unroll
+  for (int i = 0; i < KN; ++i) sum[i] = 0.f;
+  for (int ti = 0; ti < n_tile; ++ti) {
+    const int b = ti & 1;
+    if (ti + 1 < n_tile) fetch(ti + 1);
+    const int left = it.n_row - ti * kTileRows;
+#pragma unroll
+    for (int sub = 0; sub < kTileRows / 32; ++sub) {
+      if (sub * 32 >= left) break;
+      const int r0 = sub * 32;
+      wt_f32x16 st[KN];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const uint4 qf = s_q[b][(r0 + lc) * NC + ((2 * s + lh) ^ (lc % SW))];
+#pragma unroll
+        for (int i = 0; i < KN; ++i) st[i] = mma<T>(qf, kf[i][s], s ? st[i] : wt_f32x16{});
+      }
+      // element 4 q + e of st is row r0 + 8 q + 4 lh + e; a row sees keys up to its position,
+      // and rows of a tile are sorted by it (rows past the item's, with -1, come last)
+      float l[16];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float4 x = *reinterpret_cast<const float4*>(&s_l[b][r0 + 8 * q + 4 * lh]);
+        l[4 * q] = x.x;
+        l[4 * q + 1] = x.y;
+        l[4 * q + 2] = x.z;
+        l[4 * q + 3] = x.w;
+      }
+      const bool edge = min(s_pos[b][r0], s_pos[b][r0 + 31]) < key0 + 32 * KN - 1;
+#pragma unroll
+      for (int i = 0; i < KN; ++i) {
+        float p[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(st[i][e], scale, -l[e]));
+        if (__builtin_amdgcn_readfirstlane(edge)) {
+          const int key = key0 + 32 * i + lc;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int4 x = *reinterpret_cast<const int4*>(&s_pos[b][r0 + 8 * q + 4 * lh]);
+            p[4 * q] = key <= x.x ? p[4 * q] : 0.f;
+            p[4 * q + 1] = key <= x.y ? p[4 * q + 1] : 0.f;
+            p[4 * q + 2] = key <= x.z ? p[4 * q + 2] : 0.f;
+            p[4 * q + 3] = key <= x.w ? p[4 * q + 3] : 0.f;
+          }
+        }
+#pragma unroll
+        for (int n = 8; n >= 1; n /= 2)
+#pragma unroll
+          for (int e = 0; e < n; ++e) p[e] += p[e + n];
+        sum[i] += p[0];
+      }
+    }
+    if (ti + 1 < n_tile) put(b ^ 1);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < KN; ++i) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[i]), __float_as_uint(sum[i]), false, false);
+    const float total = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    const int key = key0 + 32 * i + lc;
+    if (lh || key >= it.k1) continue;
+    if (it.n_split > 1) {
+      wc.part[(((int64_t)it.split * wc.n_kb + it.kb) * cv.n_kv_heads + hk) * (128 * KN) + key - it.k0] = total;
+    } else {
+      float* dst = wc.weights + ((int64_t)it.seq * cv.n_kv_heads + hk) * cv.max_tokens + key;
+      *dst = wc.add ? *dst + total : total;
+    }
+  }
+}
+
+// The splits of each block of keys added up: one block of threads a block of keys (its
+// first item, b, tells which) and kv head.
+template <bool VALUE>
+__global__ void __launch_bounds__(256) weights_merge_kernel(WeightCall wc, Plan<VALUE> plan, CacheView cv, int block) {
+  const WeightItem it = plan.item(blockIdx.y);
+  const int key = it.k0 + threadIdx.x;
+  if (it.split || it.n_split == 1 || key >= it.k1) return;
+  const float* p = wc.part + ((int64_t)it.kb * cv.n_kv_heads + blockIdx.x) * block + threadIdx.x;
+  float total = 0.f;
+#pragma unroll 8
+  for (int s = 0; s < it.n_split; ++s) total += p[(int64_t)s * wc.n_kb * cv.n_kv_heads * block];
+  float* dst = wc.weights + ((int64_t)it.seq * cv.n_kv_heads + blockIdx.x) * cv.max_tokens + key;
+  *dst = wc.add ? *dst + total : total;
+}
+
+namespace {
+
+int check(hipError_t e) { return e == hipSuccess ? 0 : (int)e; }
+
+template <bool VALUE>
+int launch(int dtype, const WeightCall& wc, const Plan<VALUE>& plan, int n_items, int block, const CacheView& cv,
+           hipStream_t s) {
+  const dim3 grid(cv.n_kv_heads, n_items);
+#define WK(T, DD, PG, KN) hipLaunchKernelGGL((attend_weights_kernel<T, DD, PG, KN, VALUE>), grid, dim3(256), 0, s, wc, plan, cv)
+#define WKN(T, DD, PG) { if (block == 256) WK(T, DD, PG, 2); else WK(T, DD, PG, 1); }
+#define WKP(T, DD) { if (cv.page_size) WKN(T, DD, true) else WKN(T, DD, false) }
+  if (dtype == 0) { if (cv.head_dim == 64) WKP(float, 64) else WKP(float, 128) }
+  else { if (cv.head_dim == 64) WKP(bf16_t, 64) else WKP(bf16_t, 128) }
+#undef WKP
+#undef WKN
+#undef WK
+  if (int rc = check(hipGetLastError())) return rc;
+  if (wc.part) {
+    hipLaunchKernelGGL((weights_merge_kernel<VALUE>), grid, dim3(block), 0, s, wc, plan, cv, block);
+    return check(hipGetLastError());
+  }
+  return 0;
+}
+
+}  // namespace
+
+int launch_attend_weights(int dtype, const WeightCall& call, const WeightArgs* args, const WeightItem* items,
+                          const WeightRank* ranks, int n_items, int block, const CacheView& cv, hipStream_t s) {
+  if (args) return launch<true>(dtype, call, Plan<true>{*args}, n_items, block, cv, s);
+  return launch<false>(dtype, call, Plan<false>{items, ranks}, n_items, block, cv, s);
+}
+
+}  // namespace fcg

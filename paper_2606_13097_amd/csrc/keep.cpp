@@ -1,0 +1,169 @@
+// Entry points of what a cache keeps of its positions (include/fcg.h): the attention
+// weight they receive.
+#include <algorithm>
+
+#include "objects.hpp"
+#include "ops.hpp"
+
+using namespace fcg;
+
+// ------------------------------------------------- attention weight per position
+
+namespace {
+
+constexpr int kGridY = 65535;
+
+struct WeightPlan {
+  std::vector<WeightItem> items;
+  std::vector<WeightRank> ranks;
+  WeightArgs args;
+  int n_items = 0, n_kb = 0, splits = 1, block = 128;
+  bool by_value = false;
+};
+
+// Blocks of 256 keys (the rows are read half as often from LDS) where that leaves two
+// blocks of threads for each of 256 compute units, else of 128; the rows cut into splits
+// of at least 256 where even those are too few.
+void plan_weights(const fcg_model_desc& d, int32_t prefix_seq, int32_t P, int32_t n, const int32_t* seq,
+                  const int32_t* pos, WeightPlan* p) {
+  constexpr int64_t kBlocks = 512;
+  const int g = d.n_q_heads / d.n_kv_heads;
+  std::vector<int32_t> order(n);
+  for (int32_t t = 0; t < n; ++t) order[t] = t;
+  auto less = [&](int32_t a, int32_t b) { return seq[a] != seq[b] ? seq[a] < seq[b] : pos[a] < pos[b]; };
+  if (!std::is_sorted(order.begin(), order.end(), less)) std::stable_sort(order.begin(), order.end(), less);
+  p->ranks.reserve(n);
+  std::vector<WeightGroup> groups;
+  if (P && n) groups.push_back(WeightGroup{prefix_seq, 0, P, 0, n * g, 0, 0});
+  for (int32_t i = 0; i < n;) {
+    int32_t j = i;
+    for (; j < n && seq[order[j]] == seq[order[i]]; ++j) p->ranks.push_back(WeightRank{order[j], pos[order[j]]});
+    const int32_t end = pos[order[j - 1]] + 1;
+    if (end > P) groups.push_back(WeightGroup{seq[order[i]], P, end, i * g, (j - i) * g, 0, 0});
+    i = j;
+  }
+  auto blocks = [&](int64_t len) {
+    int64_t b = 0;
+    for (const WeightGroup& x : groups) b += (x.hi - x.lo + len - 1) / len;
+    return b * d.n_kv_heads;
+  };
+  p->block = blocks(256) >= kBlocks ? 256 : 128;
+  const int64_t have = std::max<int64_t>(1, blocks(p->block));
+  int32_t rows = 1;
+  for (const WeightGroup& x : groups) rows = std::max(rows, x.rows);
+  const int64_t want = (kBlocks + have - 1) / have;
+  int32_t split_rows = (int32_t)std::max<int64_t>(256, (rows / want + 63) / 64 * 64);
+  const int pre = P && n ? 1 : 0;  // the first group is the prefix
+  int64_t all = 0;
+  for (const WeightGroup& x : groups)
+    all += (int64_t)((x.hi - x.lo + p->block - 1) / p->block) * ((x.rows + split_rows - 1) / split_rows);
+  p->by_value = (int)groups.size() - pre <= kWgtGroups && n <= kWgtRanks && all <= kGridY;
+  WeightArgs& a = p->args;
+  if (p->by_value) {
+    a.n_group = (int)groups.size() - pre;
+    a.block = p->block;
+    a.split_rows = split_rows;
+    a.n_pre = 0;
+    std::copy(p->ranks.begin(), p->ranks.end(), a.rank);
+  }
+  for (size_t i = 0; i < groups.size(); ++i) {
+    WeightGroup& x = groups[i];
+    const int32_t nkb = (x.hi - x.lo + p->block - 1) / p->block;
+    x.kb0 = p->n_kb;
+    x.item0 = p->n_items;
+    p->n_kb += nkb;
+    if (p->by_value) {
+      const int32_t ns = (x.rows + split_rows - 1) / split_rows;
+      p->n_items += nkb * ns;
+      p->splits = std::max(p->splits, ns);
+      if ((int)i < pre) {
+        a.pre = x;
+        a.n_pre = p->n_items;
+      } else {
+        a.group[i - pre] = x;
+      }
+      continue;
+    }
+    int32_t r = x.row0 / g;
+    const int32_t r1 = r + x.rows / g;
+    for (int32_t kb = 0; kb < nkb; ++kb) {
+      WeightItem it{x.seq, x.lo + kb * p->block, 0, 0, 0, x.kb0 + kb, 0, 0};
+      it.k1 = std::min(x.hi, it.k0 + p->block);
+      // own keys: from the first row that sees one of them (rows of several sequences,
+      // before the shared prefix, all see all)
+      if (x.lo >= P)
+        while (r < r1 && p->ranks[r].pos < it.k0) ++r;
+      const int32_t left = (r1 - r) * g;
+      it.n_split = (left + split_rows - 1) / split_rows;
+      p->splits = std::max(p->splits, it.n_split);
+      for (; it.split < it.n_split; ++it.split) {
+        it.row0 = r * g + it.split * split_rows;
+        it.n_row = std::min(split_rows, left - it.split * split_rows);
+        p->items.push_back(it);
+      }
+    }
+  }
+  if (!p->by_value) p->n_items = (int)p->items.size();
+}
+
+}  // namespace
+
+fcg_status fcg_attend_weights(fcg_cache* c, int32_t layer, int32_t prefix_seq, int32_t prefix_len, int32_t n_tok,
+                              const int32_t* seq, const int32_t* pos, const fcg_tensor* q, const float* lse,
+                              float* weights, uint32_t flags, void* stream) {
+  if (!c) return fail(FCG_EINVAL, "null cache");
+  if (n_tok < 0) return fail(FCG_EINVAL, "negative token count");
+  if (n_tok > 0 && (!seq || !pos)) return fail(FCG_EINVAL, "null token array");
+  if (flags & ~FCG_ADD) return fail(FCG_EINVAL, "unknown flags");
+  const fcg_model_desc& d = c->desc;
+  if (n_tok > 0 && !c->layout_only()) {
+    if (!q || !q->data || !lse || !weights) return fail(FCG_EINVAL, "null tensor");
+    if (fcg_status st = check_strides(q, "q")) return st;
+  }
+  if (n_tok > kGridX) return fail(FCG_EINVAL, "more than 2^24 - 1 tokens");
+  if ((int64_t)n_tok * d.n_q_heads > 1 << 30) return fail(FCG_EINVAL, "more than 2^30 query rows");
+  return guarded([&]() -> fcg_status {
+    std::string msg;
+    if (fcg_status st = c->plan.check_attend(layer, prefix_seq, prefix_len, n_tok, seq, pos, &msg)) return fail(st, msg);
+    if (n_tok == 0 || c->layout_only()) return FCG_OK;
+    OnDevice dev(c->device);
+    HIP_TRY(dev.err, "hipSetDevice");
+    hipStream_t s = (hipStream_t)stream;
+    WeightPlan p;
+    plan_weights(d, prefix_seq, prefix_len, n_tok, seq, pos, &p);
+    if (!p.n_items) return FCG_OK;  // no token has a key
+    const bool split = p.splits > 1;
+    const bool cap = (split || !p.by_value) && capturing(s);
+    // what needs an upload cannot be captured: its staging memory is used again
+    if (cap && !p.by_value) return fail(FCG_ESTATE, "this call has too many tokens or sequences to be captured into a graph");
+    if (split)
+      if (fcg_status st = prefix_workspace(c, (size_t)p.splits * p.n_kb * d.n_kv_heads * p.block * 4, cap, "fcg_attend_weights"))
+        return st;
+    WeightCall wc{};
+    wc.q = view_of(q);
+    wc.lse = lse;
+    wc.weights = weights;
+    wc.part = split ? (float*)c->xpart : nullptr;
+    wc.n_q_heads = d.n_q_heads;
+    while ((d.n_kv_heads << wc.g_shift) < d.n_q_heads) ++wc.g_shift;
+    wc.layer = layer;
+    wc.n_kb = p.n_kb;
+    wc.add = (flags & FCG_ADD) != 0;
+    const WeightItem* items = nullptr;
+    const WeightRank* ranks = nullptr;
+    if (!p.by_value) {
+      Blob blob;
+      const size_t o_items = blob.add(p.items.data(), p.items.size() * sizeof(WeightItem));
+      const size_t o_ranks = blob.add(p.ranks.data(), p.ranks.size() * sizeof(WeightRank));
+      char* dplan = nullptr;
+      if (fcg_status st = upload(c, blob, {}, s, &dplan, nullptr)) return st;
+      items = (const WeightItem*)(dplan + o_items);
+      ranks = (const WeightRank*)(dplan + o_ranks);
+    }
+    for (int i0 = 0; i0 < p.n_items; i0 += kGridY)
+      if (int rc = launch_attend_weights(d.dtype, wc, p.by_value ? &p.args : nullptr, items ? items + i0 : nullptr, ranks,
+                                         std::min(kGridY, p.n_items - i0), p.block, c->view(), s))
+        return hip_fail((hipError_t)rc, "attention weights launch");
+    return p.by_value ? FCG_OK : c->ring.retire(s);
+  });
+}

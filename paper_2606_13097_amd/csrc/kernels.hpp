@@ -438,6 +438,40 @@ int launch_prefix_attend(int dtype, const PrefixCall& call, const PrefixArgs* ar
 int launch_prefix_merge(int dtype, const PrefixCall& call, const PrefixArgs* args, const PrefixRank* ranks, int n_rank,
                         int Hq, int D, hipStream_t s);
 
+// Attention weight per cached position.  Query rows are sorted by rank (token) and, per
+// kv head, numbered rank << g_shift | j.  An item takes rows [row0, row0 + n_row) past
+// keys [k0, k1) of a sequence, a row seeing keys up to its rank's position; the keys are
+// block kb of the call, and split `split` of n_split of its rows.
+struct WeightItem {
+  int32_t seq, k0, k1, row0, n_row, kb, split, n_split;
+};
+struct WeightRank {
+  int32_t tok, pos;
+};
+struct WeightCall {
+  RowView q;
+  const float* lse;  // [tokens][n_q_heads]
+  float* weights;    // [n_seqs][Hkv][max_tokens]
+  float* part;       // [split][n_kb][Hkv][block], null: no item is split
+  int32_t n_q_heads, g_shift, layer, n_kb, add;
+};
+// The plan by value, for calls of up to kWgtRanks tokens in kWgtGroups sequences: blocks of
+// `block` keys of [lo, hi), splits of split_rows rows of each, those of the shared prefix
+// first, then each sequence's own.
+constexpr int kWgtGroups = 64, kWgtRanks = 128;
+struct WeightGroup {
+  int32_t seq, lo, hi, row0, rows, item0, kb0;
+};
+struct WeightArgs {
+  int32_t n_group, block, split_rows, n_pre;  // n_pre: items of the prefix
+  WeightGroup pre, group[kWgtGroups];
+  WeightRank rank[kWgtRanks];
+};
+// args null: the plan in device memory (items, ranks); else by value.  block: 128 or
+// 256 keys; n_items < 65536.
+int launch_attend_weights(int dtype, const WeightCall& call, const WeightArgs* args, const WeightItem* items,
+                          const WeightRank* ranks, int n_items, int block, const CacheView& cv, hipStream_t s);
+
 // Merge split partials into out: part_o and out fp32 rows, or (mfma_part) both
 // bf16, part_o in the accumulator order of the MFMA prefill kernel.
 int launch_combine(const CombineArgs& args, const TokenMeta* meta, int Hq, int Hkv, int D,

@@ -44,11 +44,13 @@ EXPORTS = [
     "fcg_rope_create", "fcg_rope_frequencies", "fcg_rope_destroy", "fcg_rope_apply", "fcg_graft_rope", "fcg_append",
     "fcg_prefix_attend",
     "fcg_norm_rope_apply", "fcg_norm_rope_workspace", "fcg_norm_rope_backward", "fcg_append_norm",
+    "fcg_attend_weights",
 ]
 FCG_ROPE_HALF, FCG_ROPE_PAIRS = 0, 1
 FCG_ROPE_PLAIN, FCG_ROPE_LINEAR, FCG_ROPE_NTK, FCG_ROPE_PARTS, FCG_ROPE_GIVEN = range(5)
 FCG_ROPE_BACKWARD = 1
 FCG_REPLACE = 1
+FCG_ADD = 1
 FCG_TIME_GRAFT, FCG_TIME_PREFILL_ATTN, FCG_TIME_PREFILL, FCG_TIME_DECODE, FCG_TIME_DECODE_ATTN = range(5)
 
 
@@ -145,6 +147,7 @@ def _load():
         "fcg_norm_rope_apply": [P, I32, I32, I32, I32, P, I32, PN, PT, PT, I32, PN, PT, PT, P],
         "fcg_norm_rope_workspace": [I32, I32, I32, I32, I32, PI64],
         "fcg_norm_rope_backward": [P, I32, I32, I32, I32, P, PS, PS, P, I64, P],
+        "fcg_attend_weights": [P, I32, I32, I32, I32, P, P, PT, P, P, U32, P],
         "fcg_append_norm": [P, I32, I32, I32, P, P, P, PN, PN, PT, PT, PT, PT, U32, P],
     })
     for name, args in sig.items():
@@ -765,6 +768,32 @@ def fcg_append_norm(cache: Cache, layer: int, seq, pos, k, v, k_norm: Optional[N
     nk = _norm_ref(k_norm, layers, d.n_kv_heads, d.head_dim, td, dev, "k_norm")
     _check(_L.fcg_append_norm(cache.h, int(layer), layers, n, _p(s), _p(p), None if rope is None else rope.h, nq, nk,
                               _ref(vq), _ref(vqo), _ref(vk), _ref(vv), int(flags), _stream_of(stream, dev)))
+
+
+# ------------------------------------ what a cache keeps of its positions
+
+def _plain(t, shape: tuple, dtype, device, what: str, strict: bool = True):
+    """Address of a contiguous GPU tensor of a shape (None: not given, where strict is False)."""
+    if t is None and not strict:
+        return None
+    if t is None or t.dtype is not dtype or t.get_device() != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} tensor {shape} on GPU {device}")
+    return t.data_ptr()
+
+
+def fcg_attend_weights(cache: Cache, layer: int, prefix_seq: int, prefix_len: int, seq, pos, q, lse, weights,
+                       flags: int = 0, stream=None) -> None:
+    """Attention weight per cached position, summed over tokens and the heads of a kv head, of the tokens of a
+    ``fcg_prefix_attend`` (its arguments and its lse).  weights float32 [n_seqs][Hkv][max_tokens] of the layer."""
+    s, p = _i32(seq), _i32(pos)
+    if s.ndim != 1 or s.shape != p.shape:
+        raise ValueError("seq and pos differ in length")
+    d, n, dev = cache.desc, int(s.size), cache.device
+    vq = _view(q, (1, n, d.n_q_heads, d.head_dim), _DT_TORCH[d.dtype], dev, "q")
+    a = _plain(lse, (n, d.n_q_heads), torch.float32, dev, "lse")
+    w = _plain(weights, (cache.n_seqs, d.n_kv_heads, cache.max_tokens), torch.float32, dev, "weights")
+    _check(_L.fcg_attend_weights(cache.h, int(layer), int(prefix_seq), int(prefix_len), n, _p(s), _p(p), _ref(vq), a, w,
+                                 int(flags), _stream_of(stream, dev)))
 
 
 def fcg_status_string(status: int) -> str:
