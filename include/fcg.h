@@ -515,6 +515,38 @@ fcg_status fcg_attend_weights(fcg_cache* cache, int32_t layer, int32_t prefix_se
                               const int32_t* seq, const int32_t* pos, const fcg_tensor* q, const float* lse,
                               float* weights, uint32_t flags, void* stream);
 
+/* Squeeze sequences to the positions of most weight.  Item i keeps, of the n
+ * positions of sequence src[i], min(keep[i], n): in each layer and kv head by
+ * itself the first n_first ones, the last n_recent ones (where keep[i] is
+ * smaller, first ones go before last ones), and of the others those of the
+ * largest weight, the lower position where weights are equal (NaN counts as
+ * less than any number).  In order of position they become positions 0, 1, ..
+ * of sequence dst[i] in all layers: keys turned to their new position (by the
+ * distance moved, without the attention factor; unmoved keys and all values are
+ * copied bit for bit) in the form of `rope`, null the cache's own.
+ *   dst[i] = src[i]: in place; what is behind is forgotten and its pages return.
+ *   dst[i] another sequence: emptied first; src[i] stays as it is, and may be
+ *   the source of several items.
+ * weights: device fp32 [n_layers][n_seqs][Hkv][max_tokens], contiguous
+ * (fcg_attend_weights of each layer): read in row src[i]; row dst[i] receives
+ * the kept positions' weights in their new order and zeros after them, to
+ * max_tokens.  kept: device int32 [n_layers][n_items][Hkv][largest keep[i]],
+ * contiguous, may be null: receives the former positions; elements past an
+ * item's stay as they are.
+ * The kept positions (where kept is null) and a table of turns sit in the
+ * workspace of fcg_prefix_attend, with its rules for captures and overlapping calls;
+ * a call that maps no page can be captured, and replays move from the same
+ * positions to the same ones.
+ * Errors: EINVAL (null arrays, negative counts, rotary_dim above the head, a dst
+ * given twice or also the src of another item), ERANGE (sequences, keep outside [0,
+ * max_tokens]), ESTATE (layers of a src that differ in length; in place with
+ * values read from the library, FCG_ALIAS_V; a capture that would map pages or
+ * needs a larger workspace), EHOLE (an unwritten position below the length), ENOMEM
+ * (pages), EHIP (other dst are left empty). */
+fcg_status fcg_evict(fcg_cache* cache, int32_t n_items, const int32_t* src, const int32_t* dst, const int32_t* keep,
+                     int32_t n_first, int32_t n_recent, const fcg_rope* rope, float* weights, int32_t* kept,
+                     void* stream);
+
 /* ------------------------------------------------- code-cache management */
 
 /* Locality score of the cache entries (Sec. 4.1, Eq. 3; App. B.1, Eq. 8-10;

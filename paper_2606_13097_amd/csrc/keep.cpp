@@ -1,5 +1,5 @@
 // Entry points of what a cache keeps of its positions (include/fcg.h): the attention
-// weight they receive.
+// weight they receive, and eviction by it.
 #include <algorithm>
 
 #include "objects.hpp"
@@ -165,5 +165,124 @@ fcg_status fcg_attend_weights(fcg_cache* c, int32_t layer, int32_t prefix_seq, i
                                          std::min(kGridY, p.n_items - i0), p.block, c->view(), s))
         return hip_fail((hipError_t)rc, "attention weights launch");
     return p.by_value ? FCG_OK : c->ring.retire(s);
+  });
+}
+
+// -------------------------------------------------------------------- eviction
+
+fcg_status fcg_evict(fcg_cache* c, int32_t n_items, const int32_t* src, const int32_t* dst, const int32_t* keep,
+                     int32_t n_first, int32_t n_recent, const fcg_rope* rope, float* weights, int32_t* kept, void* stream) {
+  if (!c) return fail(FCG_EINVAL, "null cache");
+  if (n_items < 0 || n_first < 0 || n_recent < 0) return fail(FCG_EINVAL, "negative count");
+  if (n_items > 0 && (!src || !dst || !keep)) return fail(FCG_EINVAL, "null item array");
+  const fcg_model_desc& d = c->desc;
+  if (rope && rope->rot > d.head_dim) return fail(FCG_EINVAL, "rotary_dim exceeds head_dim");
+  if (n_items > 0 && !c->layout_only() && !weights) return fail(FCG_EINVAL, "null weights");
+  if ((int64_t)d.n_kv_heads * 2 > kGridY || d.n_layers > kGridY) return fail(FCG_EINVAL, "too many layers or kv heads");
+  return guarded([&]() -> fcg_status {
+    std::string msg;
+    std::vector<int32_t> len;
+    std::vector<std::pair<int32_t, int32_t>> new_pages;
+    if (fcg_status st = c->plan.check_evict(n_items, src, dst, keep, &len, &new_pages, &msg)) return fail(st, msg);
+    if (n_items == 0) return FCG_OK;
+    auto stays = [&](int32_t i) { return std::min(keep[i], len[i]); };
+    auto commit = [&]() {
+      for (int32_t i = 0; i < n_items; ++i)
+        if (src[i] == dst[i]) c->plan.truncate(dst[i], stays(i));
+        else c->plan.mark_all_layers(dst[i], 0, stays(i));
+      return FCG_OK;
+    };
+    auto empty_targets = [&]() {
+      for (int32_t i = 0; i < n_items; ++i)
+        if (src[i] != dst[i]) (void)fcg_cache_reset(c, dst[i]);
+    };
+    if (c->layout_only()) {
+      empty_targets();
+      c->plan.map_pages(new_pages);
+      return commit();
+    }
+    OnDevice dev(c->device);
+    HIP_TRY(dev.err, "hipSetDevice");
+    hipStream_t s = (hipStream_t)stream;
+    int32_t most = 0, far = 0;  // positions kept, the furthest that a row moves
+    for (int32_t i = 0; i < n_items; ++i) {
+      most = std::max(most, keep[i]);
+      far = std::max(far, len[i] - stays(i));
+    }
+    RopeArgs ra{};
+    if (rope) ra = rope->args();
+    else ra.rot = d.head_dim;
+    const int half = ra.rot / 2;
+    const size_t kept_bytes = kept ? 0 : ((size_t)d.n_layers * n_items * d.n_kv_heads * most * 4 + 255) & ~size_t(255);
+    const size_t turn_bytes = rope ? ((size_t)far + 1) * half * sizeof(float2) : 0;
+    const bool cap = capturing(s);
+    // what needs an upload cannot be captured: its staging memory is used again
+    if (cap && !new_pages.empty()) return fail(FCG_ESTATE, "this eviction maps pages: it cannot be captured into a graph");
+    if (kept_bytes + turn_bytes)
+      if (fcg_status st = prefix_workspace(c, kept_bytes + turn_bytes, cap, "fcg_evict")) return st;
+    EvictCall ec{};
+    ec.weights = weights;
+    ec.kept = kept ? kept : (int32_t*)c->xpart;
+    ec.turns = rope ? (float2*)((char*)c->xpart + kept_bytes) : c->d_rope;
+    ec.kept_stride = most;
+    ec.n_items = n_items;
+    ec.first = n_first;
+    ec.recent = n_recent;
+    // Everything that can fail for want of memory comes before the targets are emptied:
+    // the page rows are staged with room for the new entries, which are filled in after.
+    Blob blob;
+    std::vector<std::pair<int32_t, size_t>> rows;
+    if (!new_pages.empty()) {
+      stage_pages(c, new_pages, &blob, &rows);
+      if (fcg_status st = c->ring.reserve(blob.bytes.size() + 512)) return st;
+    }
+    empty_targets();
+    c->plan.map_pages(new_pages);
+    auto undo = [&](fcg_status st) {
+      empty_targets();
+      return st;
+    };
+    if (!rows.empty()) {
+      const size_t bytes = sizeof(int32_t) * c->plan.n_logical_pages();
+      for (const auto& r : rows) {
+        std::memcpy(blob.bytes.data() + r.second, c->plan.page_row(r.first), bytes);
+        std::memcpy(blob.bytes.data() + r.second + bytes, c->plan.alias_row(r.first), bytes);
+      }
+      char* at = nullptr;
+      if (fcg_status st = upload(c, blob, rows, s, &at, nullptr)) return undo(st);
+      if (fcg_status st = c->ring.retire(s)) return undo(st);
+    }
+    // launches of up to kEvictItems items, those into other sequences and those in place
+    bool table = rope != nullptr;
+    for (int in_place = 0; in_place < 2; ++in_place)
+      for (int32_t i = 0; i < n_items;) {
+        EvictArgs args;
+        args.n = 0;
+        int64_t chunks = 0, rows_of = 0;
+        ec.item0 = i;
+        for (; i < n_items && args.n < kEvictItems; ++i) {
+          // items of one launch are neighbours in the call: `kept` counts them on
+          if ((src[i] == dst[i]) != (in_place == 1)) {
+            if (args.n) break;
+            ec.item0 = i + 1;
+            continue;
+          }
+          const int64_t more = (stays(i) + kEvictRows - 1) / kEvictRows;
+          rows_of += (int64_t)d.n_kv_heads * d.n_layers;
+          if (args.n && (chunks + more > kGridX || rows_of > 1 << 20)) break;
+          args.item[args.n++] = EvictItem{src[i], dst[i], len[i], stays(i), (int32_t)chunks};
+          chunks += more;
+        }
+        if (!args.n) break;
+        if (int rc = launch_evict_select(ec, args, ra, d.n_layers, c->n_seqs, d.n_kv_heads, c->max_tokens,
+                                         table ? far + 1 : 0, s))
+          return undo(hip_fail((hipError_t)rc, "eviction launch"));
+        table = false;
+        if (!chunks) continue;
+        if (int rc = launch_evict_move(d.dtype, rope && rope->pairs(), in_place == 1, ec, args, (int)chunks, c->view(), half,
+                                       d.n_layers, s))
+          return undo(hip_fail((hipError_t)rc, "eviction launch"));
+      }
+    return commit();
   });
 }

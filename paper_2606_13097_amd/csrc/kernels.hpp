@@ -472,6 +472,32 @@ struct WeightArgs {
 int launch_attend_weights(int dtype, const WeightCall& call, const WeightArgs* args, const WeightItem* items,
                           const WeightRank* ranks, int n_items, int block, const CacheView& cv, hipStream_t s);
 
+// Eviction by weight: item by item, `keep` of a sequence's `len` positions, moved to
+// positions 0 .. keep - 1 of sequence dst.  Items of a launch go by value; chunk0: first
+// chunk of kEvictRows rows of the item.
+constexpr int kEvictItems = 64, kEvictRows = 64;
+struct EvictItem {
+  int32_t src, dst, len, keep, chunk0;
+};
+struct EvictArgs {
+  int32_t n;
+  EvictItem item[kEvictItems];
+};
+struct EvictCall {
+  float* weights;       // [L][n_seqs][Hkv][max_tokens]
+  int32_t* kept;        // [L][n_items][Hkv][kept_stride]
+  float2* turns;        // (cos, sin) of the pairs by distance [..][rot / 2]
+  int64_t kept_stride;
+  int32_t n_items, item0;  // of the call; the launch's first one
+  int32_t first, recent;
+};
+// Select; n_turn distances of the table are filled (0: it is there already).
+int launch_evict_select(const EvictCall& ec, const EvictArgs& args, const RopeArgs& ra, int n_layers, int n_seqs, int Hkv,
+                        int max_tokens, int n_turn, hipStream_t s);
+// Move what was selected, after it on the stream.  half: pairs of the table's rows.
+int launch_evict_move(int dtype, bool pairs, bool in_place, const EvictCall& ec, const EvictArgs& args, int n_chunks,
+                      const CacheView& cv, int half, int n_layers, hipStream_t s);
+
 // Merge split partials into out: part_o and out fp32 rows, or (mfma_part) both
 // bf16, part_o in the accumulator order of the MFMA prefill kernel.
 int launch_combine(const CombineArgs& args, const TokenMeta* meta, int Hq, int Hkv, int D,

@@ -242,6 +242,58 @@ fcg_status Planner::check_attend(int32_t layer, int32_t prefix_seq, int32_t pref
   return FCG_OK;
 }
 
+fcg_status Planner::check_evict(int32_t n, const int32_t* src, const int32_t* dst, const int32_t* keep,
+                                std::vector<int32_t>* len, std::vector<std::pair<int32_t, int32_t>>* new_pages,
+                                std::string* msg) const {
+  std::vector<int32_t> to(dst, dst + n);
+  std::sort(to.begin(), to.end());
+  for (int32_t i = 1; i < n; ++i)
+    if (to[i] == to[i - 1]) { *msg = fmt("sequence %lld is the target of two items", to[i]); return FCG_EINVAL; }
+  for (int32_t i = 0; i < n; ++i)
+    if (src[i] != dst[i] && std::binary_search(to.begin(), to.end(), src[i])) {
+      *msg = fmt("sequence %lld is the source of an item and the target of another", src[i]);
+      return FCG_EINVAL;
+    }
+  for (int32_t i = 0; i < n; ++i) {
+    for (int32_t s : {src[i], dst[i]})
+      if (s < 0 || s >= S_) { *msg = fmt("sequence %lld out of range", s); return FCG_ERANGE; }
+    if (keep[i] < 0 || keep[i] > T_) { *msg = fmt("%lld positions to keep: out of range", keep[i]); return FCG_ERANGE; }
+  }
+  for (int32_t i = 0; i < n; ++i) {
+    for (int32_t l = 1; l < L_; ++l)
+      if (seq_len(src[i], l) != seq_len(src[i], 0)) {
+        *msg = fmt("the layers of sequence %lld have different lengths", src[i]);
+        return FCG_ESTATE;
+      }
+    if (src[i] == dst[i] && P_)
+      for (int32_t lp = 0; lp < NLP_; ++lp)
+        if (alias_row(src[i])[lp] >= 0) {
+          *msg = fmt("sequence %lld reads values in the library: squeeze it into another sequence", src[i]);
+          return FCG_ESTATE;
+        }
+  }
+  len->clear();
+  new_pages->clear();
+  int64_t room = n_free_;
+  for (int32_t i = 0; i < n; ++i) {
+    for (int32_t l = 0; l < L_; ++l)
+      if (count(src[i], l) != seq_len(src[i], l)) {
+        *msg = fmt("sequence %lld has unwritten positions (layer %lld)", src[i], l);
+        return FCG_EHOLE;
+      }
+    len->push_back(seq_len(src[i], 0));
+    if (!P_ || src[i] == dst[i]) continue;
+    for (int32_t lp = 0; lp < NLP_; ++lp) room += page_row(dst[i])[lp] >= 0;
+    for (int32_t p = 0; p < std::min(keep[i], len->back()); p += P_) new_pages->push_back({dst[i], p / P_});
+  }
+  if ((int64_t)new_pages->size() > room) {
+    *msg = fmt("%lld new pages needed, %lld free", (long long)new_pages->size(), (long long)room);
+    return FCG_ENOMEM;
+  }
+  std::sort(new_pages->begin(), new_pages->end());
+  return FCG_OK;
+}
+
 fcg_status Planner::check_decode(int32_t layer, int32_t n, const int32_t* seq, std::vector<int32_t>* pos_out,
                                  std::vector<std::pair<int32_t, int32_t>>* new_pages, std::string* msg) const {
   std::vector<int32_t> s(seq, seq + n);

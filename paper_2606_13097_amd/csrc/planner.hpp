@@ -41,6 +41,7 @@ class Planner {
   int32_t max_tokens() const { return T_; }
   int32_t page_size() const { return P_; }
   int32_t n_pages() const { return NP_; }
+  int32_t free_pages() const { return n_free_; }
   int32_t n_logical_pages() const { return NLP_; }
   bool alias_v() const { return AV_; }
 
@@ -65,6 +66,13 @@ class Planner {
   // [prefix_len, pos] of their own sequence.
   fcg_status check_attend(int32_t layer, int32_t prefix_seq, int32_t prefix_len, int32_t n, const int32_t* seq,
                           const int32_t* pos, std::string* msg) const;
+
+  // Sequences src[i] squeezed to keep[i] positions (or all, where they have fewer) in
+  // dst[i], which may be src[i].  *len receives their lengths, *new_pages the pages of the
+  // other dst, which are emptied first.
+  fcg_status check_evict(int32_t n, const int32_t* src, const int32_t* dst, const int32_t* keep,
+                         std::vector<int32_t>* len, std::vector<std::pair<int32_t, int32_t>>* new_pages,
+                         std::string* msg) const;
 
   // Commits (after a successful check); nothing here allocates or fails.
   void map_pages(const std::vector<std::pair<int32_t, int32_t>>& new_pages);

@@ -44,7 +44,7 @@ EXPORTS = [
     "fcg_rope_create", "fcg_rope_frequencies", "fcg_rope_destroy", "fcg_rope_apply", "fcg_graft_rope", "fcg_append",
     "fcg_prefix_attend",
     "fcg_norm_rope_apply", "fcg_norm_rope_workspace", "fcg_norm_rope_backward", "fcg_append_norm",
-    "fcg_attend_weights",
+    "fcg_attend_weights", "fcg_evict",
 ]
 FCG_ROPE_HALF, FCG_ROPE_PAIRS = 0, 1
 FCG_ROPE_PLAIN, FCG_ROPE_LINEAR, FCG_ROPE_NTK, FCG_ROPE_PARTS, FCG_ROPE_GIVEN = range(5)
@@ -148,6 +148,7 @@ def _load():
         "fcg_norm_rope_workspace": [I32, I32, I32, I32, I32, PI64],
         "fcg_norm_rope_backward": [P, I32, I32, I32, I32, P, PS, PS, P, I64, P],
         "fcg_attend_weights": [P, I32, I32, I32, I32, P, P, PT, P, P, U32, P],
+        "fcg_evict": [P, I32, P, P, P, I32, I32, P, P, P, P],
         "fcg_append_norm": [P, I32, I32, I32, P, P, P, PN, PN, PT, PT, PT, PT, U32, P],
     })
     for name, args in sig.items():
@@ -794,6 +795,23 @@ def fcg_attend_weights(cache: Cache, layer: int, prefix_seq: int, prefix_len: in
     w = _plain(weights, (cache.n_seqs, d.n_kv_heads, cache.max_tokens), torch.float32, dev, "weights")
     _check(_L.fcg_attend_weights(cache.h, int(layer), int(prefix_seq), int(prefix_len), n, _p(s), _p(p), _ref(vq), a, w,
                                  int(flags), _stream_of(stream, dev)))
+
+
+def fcg_evict(cache: Cache, src, dst, keep, weights, first: int = 0, recent: int = 0, rope: Optional[Rope] = None,
+              kept=None, stream=None) -> None:
+    """Squeeze sequences ``src`` to ``keep`` positions each (the ``first``, the ``recent`` and those of most weight) as
+    sequences ``dst``, which may be ``src``.  weights float32 [n_layers][n_seqs][Hkv][max_tokens], rewritten with the
+    rows; kept int32 [n_layers][n_items][Hkv][max(keep)] or None receives the positions kept."""
+    a, b, k = _i32(src), _i32(dst), _i32(keep)
+    if a.ndim != 1 or a.shape != b.shape or a.shape != k.shape:
+        raise ValueError("src, dst and keep differ in length")
+    d, dev, n = cache.desc, cache.device, int(a.size)
+    pw = pk = None
+    if dev is not None:
+        pw = _plain(weights, (d.n_layers, cache.n_seqs, d.n_kv_heads, cache.max_tokens), torch.float32, dev, "weights")
+        pk = _plain(kept, (d.n_layers, n, d.n_kv_heads, int(k.max(initial=0))), torch.int32, dev, "kept", strict=False)
+    _check(_L.fcg_evict(cache.h, n, _p(a), _p(b), _p(k), int(first), int(recent), None if rope is None else rope.h, pw, pk,
+                        _stream_of(stream, dev)))
 
 
 def fcg_status_string(status: int) -> str:

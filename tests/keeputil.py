@@ -54,3 +54,16 @@ def weights64(q, keys, pre, P, seq, pos, T, hkv):
         attended[pre, :, :P] = True
         attended[s, :, P:P + own] = True
     return out, lse, n * g, reach, attended
+
+
+def kept64(w, n, keep, first, recent):
+    """Positions that stay of the n first of a weight row w (numpy float32), ascending."""
+    keep = min(keep, n)
+    if keep == n:
+        return np.arange(n)
+    f = min(keep, first)
+    r = min(keep - f, recent)
+    x = w[f:n - r].astype(np.float64)
+    order = sorted(range(len(x)), key=lambda i: (math.isnan(x[i]), -x[i] if not math.isnan(x[i]) else 0.0, i))
+    mid = sorted(f + i for i in order[:keep - f - r])
+    return np.concatenate([np.arange(f), mid, np.arange(n - r, n)]).astype(np.int64)
