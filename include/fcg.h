@@ -547,6 +547,46 @@ fcg_status fcg_evict(fcg_cache* cache, int32_t n_items, const int32_t* src, cons
                      int32_t n_first, int32_t n_recent, const fcg_rope* rope, float* weights, int32_t* kept,
                      void* stream);
 
+/* -------------------------------------------------- log probabilities */
+
+/* Of each row of logits [n_rows][vocab] (device, dtype, rows row_stride >= 0
+ * elements apart, starting anywhere), in fp32 and one pass over it, any of
+ *   lse[r]     = ln sum_j exp(x_j),
+ *   logprob[r] = x_t - lse with t = targets[r] (device int32 [n_rows]; a t outside
+ *                [0, vocab) is no target: 0),
+ *   entropy[r] = - sum_j p_j ln p_j, p_j = exp(x_j - lse),
+ *   top_id, top_logprob [n_rows][n_top]: the n_top <= 64 most likely tokens, the most likely
+ *                first, the lower id where logits are equal (NaN counts as less than any
+ *                number), and their x - lse.
+ * Outputs are device, fp32 (ids int32), contiguous; null: not wanted (top_id only
+ * with n_top = 0).  Logits of -inf are tokens ruled out; a row of nothing else has
+ * lse -inf, log probabilities -inf and entropy 0; a row with a NaN has NaN for all three.
+ * workspace: device, 16-byte aligned, fcg_token_logprobs_workspace bytes (0 for
+ * many rows), of any content, for this call alone until it is done.  Nothing is allocated or
+ * uploaded: the call can be captured.  Runs on the current device.
+ * Errors: EINVAL (dtype, negative counts or stride, vocab outside [1, 2^30], n_top
+ * outside [0, min(64, vocab)], null logits, logprob without targets, alternatives without
+ * top_id, a workspace that is too small or not aligned), EHIP. */
+fcg_status fcg_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, int64_t* bytes);
+fcg_status fcg_token_logprobs(int32_t dtype, int32_t n_rows, int32_t vocab, const void* logits, int64_t row_stride,
+                              const int32_t* targets, float* logprob, float* entropy, float* lse, int32_t n_top,
+                              int32_t* top_id, float* top_logprob, void* workspace, int64_t workspace_bytes,
+                              void* stream);
+
+/* The gradient of the logits from those of logprob, entropy and lse (device fp32
+ * [n_rows], each may be null: zero):
+ *   dx_j = p_j (g_lse - g_logprob - g_entropy (ln p_j + entropy)) + g_logprob [j = t],
+ * in fp32, rounded once to dtype; 0 where x_j is -inf (but at the target), and no
+ * g_logprob in rows without a target.  lse and, with g_entropy, entropy: what
+ * fcg_token_logprobs gave.  dlogits [n_rows][vocab], rows d_stride apart; may be the
+ * logits in place (the same stride), and must not overlap them otherwise.  Can be captured.
+ * Errors: EINVAL (dtype, negative counts or stride, vocab, null tensors, a gradient
+ * without targets or entropy, overlapping rows of dlogits), EHIP. */
+fcg_status fcg_token_logprobs_backward(int32_t dtype, int32_t n_rows, int32_t vocab, const void* logits,
+                                       int64_t row_stride, const int32_t* targets, const float* lse,
+                                       const float* entropy, const float* g_logprob, const float* g_entropy,
+                                       const float* g_lse, void* dlogits, int64_t d_stride, void* stream);
+
 /* ------------------------------------------------- code-cache management */
 
 /* Locality score of the cache entries (Sec. 4.1, Eq. 3; App. B.1, Eq. 8-10;
@@ -571,6 +611,14 @@ fcg_status fcg_locality_record(fcg_locality* loc, int32_t n, const int32_t* func
 /* Perplexity of function func's implementation (>= 0; 0 until set).
  * Errors: EINVAL (null handle, negative or NaN ppl), ERANGE (func). */
 fcg_status fcg_locality_set_ppl(fcg_locality* loc, int32_t func, double ppl);
+/* The same for n functions at once, measured: logprob (device fp32) holds the log
+ * probabilities of n_tok[i] >= 1 tokens of funcs[i] (host arrays), function after
+ * function, as fcg_token_logprobs gives them (every token with a target); PPL = exp(-their mean),
+ * summed in 64 bits.  Waits for the stream.  On an error no perplexity changes.
+ * Errors: EINVAL (null arguments, a negative count, a function without tokens, a perplexity
+ * that is not finite), ERANGE (a function), ENOMEM, EHIP. */
+fcg_status fcg_locality_measure_ppl(fcg_locality* loc, int32_t n, const int32_t* funcs, const int32_t* n_tok,
+                                    const float* logprob, void* stream);
 /* scores[n_funcs] (host) receives l(f), each in [0, 1].  Errors: EINVAL. */
 fcg_status fcg_locality_scores(const fcg_locality* loc, double* scores);
 /* Which entries stay in device memory under a budget: in descending score

@@ -1,0 +1,415 @@
+// Log probabilities of given tokens, entropy and the most likely tokens from rows of
+// logits, and the gradient of the logits, for gfx950.
+//
+//   lse = ln sum e^x,  logprob_t = x_t - lse,  H = -sum p ln p,  p = e^(x - lse).
+//
+// One pass over a row: with a reference r near the row's maximum, in base 2 (c = log2 e),
+//   S = sum 2^(c x - c r),  U = sum 2^(c x - c r) (c x - c r),
+//   lse = r + ln S,  H = ln 2 (log2 S - U / S).
+// A thread keeps its reference until an element is more than 2^40 above it, so nothing is
+// rescaled in nearly all steps; products with c r round once, and what that leaves (eta)
+// is taken out of S and U at the end, so large logits cost no digits.  Past 10^6 that
+// no longer holds (a row of nothing but the type's lowest value, say): parts of a row with such a
+// maximum are read once more with x - r formed first.
+//
+// The most likely tokens: order is (value, then lower index), as one 64-bit key.  A block
+// holds a chunk of its row in registers (4 vectors a thread); a lower bound on the k-th
+// largest key is the k-th largest of the maxima of 64 groups of 8 threads (later chunks:
+// the k-th found so far), and the few elements at or above it go to a list in LDS, of which
+// k are kept by counting.  If too many pass (a row of equal logits), the bound is taken
+// anew from the threads' own largest keys: at most (k - 1) 32 + 1 elements reach that.
+//
+// Few rows are cut into splits, whose partials a second launch joins.
+#include "fcg_device.hpp"
+#include "kernels.hpp"
+
+namespace fcg {
+
+namespace {
+
+constexpr int kThreads = 512, kWaves = kThreads / 64;
+constexpr int kListCap = kLogpTop + (kLogpTop - 1) * 32 + 1;  // keys kept, and those of one chunk
+constexpr float kC = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kFar = 1e6f;  // rows whose largest logit is past this take the second reading: c r is off by up to a tenth there
+
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  const uint32_t k = u >> 31 ? ~u : u | 0x80000000u;
+  return x != x ? 0u : k;
+}
+__device__ __forceinline__ float value_of(uint32_t k) {
+  return k ? __uint_as_float(k >> 31 ? k ^ 0x80000000u : ~k) : __uint_as_float(0x7FC00000u);
+}
+__device__ __forceinline__ uint64_t key_of(float x, int i) { return (uint64_t)order_of(x) << 32 | (uint32_t)~i; }
+
+// S and U about a reference
+struct Stat {
+  float r, s, u;
+};
+__device__ __forceinline__ Stat join(const Stat& a, const Stat& b) {
+  const float r = fmaxf(a.r, b.r);
+  const float da = fmaxf((a.r - r) * kC, -1e30f), db = fmaxf((b.r - r) * kC, -1e30f);
+  const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+  return Stat{r, fmaf(a.s, fa, b.s * fb), fmaf(fmaf(a.s, da, a.u), fa, fmaf(b.s, db, b.u) * fb)};
+}
+__device__ __forceinline__ Stat join_wave(Stat a) {
+#pragma unroll
+  for (int d = 32; d >= 1; d /= 2) a = join(a, Stat{__shfl_xor(a.r, d), __shfl_xor(a.s, d), __shfl_xor(a.u, d)});
+  return a;
+}
+
+// what a row's statistics give
+struct Row {
+  float r, ln_s, lse;
+  bool empty;
+  __device__ __forceinline__ explicit Row(const Stat& a) {
+    empty = a.s == 0.f;
+    r = a.r;
+    ln_s = empty ? 0.f : log2f(a.s) * kLn2;
+    lse = empty ? -INFINITY : r + ln_s;
+  }
+  __device__ __forceinline__ float logprob(float x) const { return empty ? -INFINITY : (x - r) - ln_s; }
+  __device__ __forceinline__ float entropy(const Stat& a) const {
+    return empty ? 0.f : (log2f(a.s) - a.u / a.s) * kLn2;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void finish(const LogpArgs& la, int row, const Stat& st) {
+  const Row rw(st);
+  if (la.lse) la.lse[row] = rw.lse;
+  if (la.entropy) la.entropy[row] = rw.entropy(st);
+  if (la.logprob) {
+    const int t = la.targets[row];
+    la.logprob[row] = t < 0 || t >= la.vocab
+                          ? 0.f
+                          : rw.logprob(Store<T>::load1(reinterpret_cast<const T*>(la.x) + (int64_t)row * la.stride + t));
+  }
+}
+__device__ __forceinline__ void put_top(const LogpArgs& la, int row, int j, uint64_t key, const Stat& st) {
+  const Row rw(st);
+  la.top_id[(int64_t)row * la.n_top + j] = (int)~(uint32_t)key;
+  if (la.top_logprob) la.top_logprob[(int64_t)row * la.n_top + j] = rw.logprob(value_of((uint32_t)(key >> 32)));
+}
+
+// A vector without its first n elements, -inf behind the others.
+template <typename T>
+__device__ __forceinline__ uint4 shifted(const uint4& v, int n) {
+  const uint64_t none = sizeof(T) == 2 ? 0xFF80FF80FF80FF80ull : 0xFF800000FF800000ull;
+  const uint64_t lo = (uint64_t)v.y << 32 | v.x, hi = (uint64_t)v.w << 32 | v.z;
+  const int bits = n * (int)sizeof(T) * 8;
+  uint64_t a, b;
+  if (bits >= 128) a = b = none;
+  else if (bits >= 64) {
+    a = bits == 64 ? hi : hi >> (bits - 64) | none << (128 - bits);
+    b = none;
+  } else {
+    a = bits ? lo >> bits | hi << (64 - bits) : lo;
+    b = bits ? hi >> bits | none << (64 - bits) : hi;
+  }
+  return make_uint4((uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32));
+}
+// elements i .. of a row shorter than a vector
+template <typename T>
+__device__ __forceinline__ uint4 few(const T* x, int i, int n) {
+  float f[Store<T>::VEC];
+#pragma unroll
+  for (int e = 0; e < Store<T>::VEC; ++e) f[e] = i + e < n ? Store<T>::load1(x + i + e) : -INFINITY;
+  return Store<T>::pack(f);
+}
+
+// The n keys in s: those of rank < k to out, largest first, by counting; threads of the block.
+__device__ __forceinline__ void rank_keys(const uint64_t* s, int n, uint64_t* out, int k, int threads) {
+  for (int i = threadIdx.x; i < n; i += threads) {
+    const uint64_t mine = s[i];
+    int above = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) above += s[j] > mine;
+    if (above < k) out[above] = mine;
+  }
+}
+
+}  // namespace
+
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
+  constexpr int kVecs = TOP ? 4 : 8;  // vectors of a thread in a chunk
+  constexpr int VEC = Store<T>::VEC, CHUNK = kThreads * kVecs * VEC;
+  __shared__ Stat s_stat[kWaves];
+  __shared__ float s_max[kWaves];
+  __shared__ uint64_t s_list[TOP ? kListCap : 1], s_top[TOP ? kLogpTop : 1], s_bound;
+  __shared__ uint64_t s_own[TOP ? kThreads : 1];
+  __shared__ float s_grp[64];
+  __shared__ int s_n;
+
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int row = blockIdx.x / la.splits, split = blockIdx.x - row * la.splits;
+  const int e0 = split * la.split_len, e1 = min(la.vocab, e0 + la.split_len);
+  const T* x = reinterpret_cast<const T*>(la.x) + (int64_t)row * la.stride;
+  const int k = la.n_top;
+
+  uint4 cur[kVecs], next[kVecs];
+  // (vectors that pass the part's end read its last elements: see fix)
+  auto load = [&](uint4* v, int chunk) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      const int i = e0 + chunk * CHUNK + (j * kThreads + t) * VEC;
+      if (e1 >= VEC) v[j] = ld16_any(x + min(i, e1 - VEC));
+      else v[j] = few<T>(x, i, e1);
+    }
+  };
+  // in the last chunk: the elements in their places, -inf past the end
+  auto fix = [&](uint4* v, int chunk) __attribute__((always_inline)) {
+    if (e1 < VEC) return;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      const int i = e0 + chunk * CHUNK + (j * kThreads + t) * VEC;
+      if (i + VEC > e1) v[j] = shifted<T>(v[j], min(i + VEC - e1, VEC));
+    }
+  };
+  float r = -kFar, rc = -kFar * kC, s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f, top = -INFINITY;
+  if (TOP && t == 0) {
+    s_n = 0;
+    s_bound = 0;
+  }
+  int have = 0;  // keys in s_list
+  const int n_chunk = (e1 - e0 + CHUNK - 1) / CHUNK;
+  load(cur, 0);
+  for (int ch = 0; ch < n_chunk; ++ch) {
+    if (ch + 1 < n_chunk) load(next, ch + 1);
+    else fix(cur, ch);
+    float vmax[kVecs];
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      float f[VEC];
+      Store<T>::unpack(cur[j], f);
+      float m = f[0];
+#pragma unroll
+      for (int e = 1; e < VEC; ++e) m = fmaxf(m, f[e]);
+      vmax[j] = m;
+      if (m * kC > rc + 40.f) {
+#pragma clang fp contract(off)  // the difference is that of the rounded products
+        r = fminf(m, kFar);
+        const float to = r * kC, d = rc - to, g = __builtin_amdgcn_exp2f(d);
+        u0 = fmaf(s0, d, u0) * g;
+        u1 = fmaf(s1, d, u1) * g;
+        s0 *= g;
+        s1 *= g;
+        rc = to;
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; e += 2) {
+        const float a = fmaf(f[e], kC, -rc), b = fmaf(f[e + 1], kC, -rc);
+        const float ea = __builtin_amdgcn_exp2f(a), eb = __builtin_amdgcn_exp2f(b);
+        s0 += ea;
+        s1 += eb;
+        u0 = fmaf(ea, fmaxf(a, -1e30f), u0);  // (0 times -inf is NaN)
+        u1 = fmaf(eb, fmaxf(b, -1e30f), u1);
+      }
+    }
+    float tmax = vmax[0];
+#pragma unroll
+    for (int j = 1; j < kVecs; ++j) tmax = fmaxf(tmax, vmax[j]);
+    top = fmaxf(top, tmax);
+
+    if constexpr (TOP) {
+      const int at = e0 + ch * CHUNK;
+      if (have < k) {  // a bound from the groups' maxima
+        float gm = fmaxf(tmax, dpp_f32<kDppXor1>(tmax));
+        gm = fmaxf(gm, dpp_f32<kDppXor2>(gm));
+        gm = fmaxf(gm, dpp_f32<kDppHalfMirror>(gm));
+        if (t % 8 == 0) s_grp[t / 8] = gm;
+        __syncthreads();
+        if (w == 0) {
+          const uint64_t mine = key_of(s_grp[lane], lane);
+          int above = 0;
+#pragma unroll 8
+          for (int j = 0; j < 64; ++j) above += key_of(s_grp[j], j) > mine;
+          // (below -inf there is NaN, which the maxima passed over)
+          if (above == k - 1) s_bound = s_grp[lane] > -INFINITY ? mine >> 32 << 32 : 0;
+        }
+      }
+      __syncthreads();
+      auto each = [&](uint64_t bound, auto&& f) __attribute__((always_inline)) {
+        const float least = bound >> 32 > 0x007FFFFFu ? value_of((uint32_t)(bound >> 32)) : -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kVecs; ++j) {
+          const int i = at + (j * kThreads + t) * VEC;
+          if (vmax[j] < least || i >= e1) continue;  // (NaN: not less)
+          float v[VEC];
+          Store<T>::unpack(cur[j], v);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            const uint64_t key = key_of(v[e], i + e);
+            if (i + e < e1 && key >= bound) f(key);
+          }
+        }
+      };
+      auto append = [&](uint64_t key) __attribute__((always_inline)) {
+        const int to = have + atomicAdd(&s_n, 1);
+        if (to < kListCap) s_list[to] = key;
+      };
+      each(s_bound, append);
+      __syncthreads();
+      int total = have + s_n;
+      if (total > kListCap) {  // (block-uniform) a bound from each thread's largest key
+        const uint64_t was = s_bound;
+        uint64_t best = 0;
+        each(was, [&](uint64_t key) __attribute__((always_inline)) { best = key > best ? key : best; });
+        s_own[t] = best;
+        __syncthreads();
+        if (t == 0) s_n = 0;
+        int above = 0;
+#pragma unroll 8
+        for (int j = 0; j < kThreads; ++j) above += s_own[j] > best;
+        if (best && above == k - 1) s_bound = best;
+        __syncthreads();
+        each(s_bound, append);
+        __syncthreads();
+        total = min(have + s_n, kListCap);
+      }
+      if (total > have) {
+        rank_keys(s_list, total, s_top, k, kThreads);
+        __syncthreads();
+        have = min(total, k);
+        if (t < have) s_list[t] = s_top[t];
+        if (t == 0) {
+          s_n = 0;
+          if (have == k) s_bound = s_top[k - 1];
+        }
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) cur[j] = next[j];
+  }
+
+  // the block's statistics; eta is what the product c r lost
+  const float eta = fmaf(r, kC, -rc), back = __builtin_amdgcn_exp2f(-eta);
+  Stat st{r, (s0 + s1) * back, fmaf(-eta, s0 + s1, u0 + u1) * back};
+  st = join_wave(st);
+  for (int d = 32; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane == 0) {
+    s_stat[w] = st;
+    s_max[w] = top;
+  }
+  __syncthreads();
+  top = s_max[0];
+#pragma unroll
+  for (int j = 1; j < kWaves; ++j) top = fmaxf(top, s_max[j]);
+  if (!(fabsf(top) < kFar)) {  // (block-uniform) far out, or nothing but -inf and NaN: once more, x - r first
+    __syncthreads();
+    st = Stat{fminf(fmaxf(top, -3.4028235e38f), 3.4028235e38f), 0.f, 0.f};
+    for (int i = e0 + t; i < e1; i += kThreads) {
+      const float a = (Store<T>::load1(x + i) - st.r) * kC, ea = __builtin_amdgcn_exp2f(a);
+      st.s += ea;
+      st.u = fmaf(ea, fmaxf(a, -1e30f), st.u);
+    }
+    st = join_wave(st);
+    if (lane == 0) s_stat[w] = st;
+    __syncthreads();
+  }
+  st = s_stat[0];
+#pragma unroll
+  for (int j = 1; j < kWaves; ++j) st = join(st, s_stat[j]);
+
+  if (la.splits > 1) {
+    if (t == 0) la.part[blockIdx.x] = make_float4(st.r, st.s, st.u, 0.f);
+    if (TOP && t < k) la.part_top[(int64_t)blockIdx.x * k + t] = t < have ? s_list[t] : 0;
+    return;
+  }
+  if (t == 0) finish<T>(la, row, st);
+  if (TOP && t < k) put_top(la, row, t, s_list[t], st);
+}
+
+// The splits of a row joined, in their order.
+template <typename T>
+__global__ void __launch_bounds__(256) logprob_merge_kernel(LogpArgs la) {
+  __shared__ uint64_t s_key[kLogpSplits * kLogpTop], s_top[kLogpTop];
+  const int row = blockIdx.x, t = threadIdx.x, k = la.n_top, n = la.splits * k;
+  const float4* p = la.part + (int64_t)row * la.splits;
+  for (int i = t; i < n; i += 256) s_key[i] = la.part_top[(int64_t)row * n + i];
+  Stat st{p[0].x, p[0].y, p[0].z};
+#pragma unroll 4
+  for (int j = 1; j < la.splits; ++j) st = join(st, Stat{p[j].x, p[j].y, p[j].z});
+  if (t == 0) finish<T>(la, row, st);
+  if (!k) return;
+  __syncthreads();
+  // (empty places, 0, lie below every key)
+  rank_keys(s_key, n, s_top, k, 256);
+  __syncthreads();
+  if (t < k) put_top(la, row, t, s_top[t], st);
+}
+
+// dx = p (g_lse - g_logprob - g_entropy (ln p + H)), and g_logprob more at the target
+template <typename T>
+__global__ void __launch_bounds__(256) logprob_grad_kernel(LogpGradArgs ga, int64_t block0) {
+  constexpr int VEC = Store<T>::VEC;
+  const int64_t b = block0 + blockIdx.x;
+  const int row = (int)(b / ga.chunks), chunk = (int)(b - (int64_t)row * ga.chunks);
+  const T* x = reinterpret_cast<const T*>(ga.x) + (int64_t)row * ga.stride;
+  T* dx = reinterpret_cast<T*>(ga.dx) + (int64_t)row * ga.d_stride;
+  uint4 v[kLogpGradVecs];
+  const int i0 = (chunk * kLogpGradVecs * 256 + (int)threadIdx.x) * VEC;
+#pragma unroll
+  for (int j = 0; j < kLogpGradVecs; ++j) {
+    const int i = i0 + j * 256 * VEC;
+    if (i + VEC <= ga.vocab) v[j] = ld16_any(x + i);
+  }
+  const int tgt = ga.targets ? ga.targets[row] : -1;
+  const float gl = ga.g_logprob && tgt >= 0 && tgt < ga.vocab ? ga.g_logprob[row] : 0.f;
+  const float gh = ga.g_entropy ? ga.g_entropy[row] : 0.f, gs = ga.g_lse ? ga.g_lse[row] : 0.f;
+  const float lse = ga.lse[row], ent = ga.g_entropy ? ga.entropy[row] : 0.f;
+  const float a = gs - gl - gh * ent;
+  auto grad = [&](float f, int i) __attribute__((always_inline)) -> float {
+    const float lp = f - lse, p = __builtin_amdgcn_exp2f(lp * kC);
+    float d = p * fmaf(-gh, lp, a);
+    d = f == -INFINITY || p == 0.f ? 0.f : d;  // (a row of nothing but -inf has no gradient)
+    return i == tgt ? d + gl : d;
+  };
+#pragma unroll
+  for (int j = 0; j < kLogpGradVecs; ++j) {
+    const int i = i0 + j * 256 * VEC;
+    if (i + VEC <= ga.vocab) {
+      float f[VEC];
+      Store<T>::unpack(v[j], f);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) f[e] = grad(f[e], i + e);
+      st16_any(dx + i, Store<T>::pack(f));
+    }
+  }
+  const int e = ga.vocab / VEC * VEC + (int)threadIdx.x;  // what is left of the row, an element a lane
+  if (chunk == ga.chunks - 1 && e < ga.vocab) Store<T>::store1(dx + e, grad(Store<T>::load1(x + e), e));
+}
+
+namespace {
+
+int check(hipError_t e) { return e == hipSuccess ? 0 : (int)e; }
+
+}  // namespace
+
+int launch_logprobs(int dtype, const LogpArgs& args, hipStream_t s) {
+  const dim3 grid(args.n * args.splits);
+#define LP(T, TOP) hipLaunchKernelGGL((logprob_kernel<T, TOP>), grid, dim3(kThreads), 0, s, args)
+  if (dtype == 0) { if (args.n_top) LP(float, true); else LP(float, false); }
+  else { if (args.n_top) LP(bf16_t, true); else LP(bf16_t, false); }
+#undef LP
+  if (int rc = check(hipGetLastError())) return rc;
+  if (args.splits == 1) return 0;
+  if (dtype == 0) hipLaunchKernelGGL((logprob_merge_kernel<float>), dim3(args.n), dim3(256), 0, s, args);
+  else hipLaunchKernelGGL((logprob_merge_kernel<bf16_t>), dim3(args.n), dim3(256), 0, s, args);
+  return check(hipGetLastError());
+}
+
+int launch_logprobs_grad(int dtype, const LogpGradArgs& args, hipStream_t s) {
+  const int64_t blocks = (int64_t)args.n * args.chunks;
+  for (int64_t b = 0; b < blocks; b += kGridX) {
+    const dim3 grid((uint32_t)(blocks - b < kGridX ? blocks - b : kGridX));
+    if (dtype == 0) hipLaunchKernelGGL((logprob_grad_kernel<float>), grid, dim3(256), 0, s, args, b);
+    else hipLaunchKernelGGL((logprob_grad_kernel<bf16_t>), grid, dim3(256), 0, s, args, b);
+    if (int rc = check(hipGetLastError())) return rc;
+  }
+  return 0;
+}
+
+}  // namespace fcg

@@ -498,6 +498,35 @@ int launch_evict_select(const EvictCall& ec, const EvictArgs& args, const RopeAr
 int launch_evict_move(int dtype, bool pairs, bool in_place, const EvictCall& ec, const EvictArgs& args, int n_chunks,
                       const CacheView& cv, int half, int n_layers, hipStream_t s);
 
+// Log probabilities of rows of logits [n][vocab], rows `stride` elements apart.  Each row
+// is cut into `splits` of split_len elements (the last one shorter), which leave (reference,
+// S, U) and their n_top largest keys.  n * splits < 2^23.
+constexpr int kLogpTop = 64, kLogpSplits = 32;
+struct LogpArgs {
+  const void* x;
+  int64_t stride;
+  const int32_t* targets;      // [n], null without logprob
+  float *logprob, *entropy, *lse;  // [n] or null
+  int32_t* top_id;             // [n][n_top]
+  float* top_logprob;          // [n][n_top] or null
+  float4* part;                // [n][splits]
+  uint64_t* part_top;          // [n][splits][n_top]
+  int32_t n, vocab, n_top, splits, split_len;
+};
+int launch_logprobs(int dtype, const LogpArgs& args, hipStream_t s);
+// The gradient of the logits; any g_ may be null.  chunks: blocks of a row, kLogpGradVecs
+// vectors a thread of 256.
+constexpr int kLogpGradVecs = 4;
+struct LogpGradArgs {
+  const void* x;
+  void* dx;
+  int64_t stride, d_stride;
+  const int32_t* targets;
+  const float *lse, *entropy, *g_logprob, *g_entropy, *g_lse;
+  int32_t n, vocab, chunks;
+};
+int launch_logprobs_grad(int dtype, const LogpGradArgs& args, hipStream_t s);
+
 // Merge split partials into out: part_o and out fp32 rows, or (mfma_part) both
 // bf16, part_o in the accumulator order of the MFMA prefill kernel.
 int launch_combine(const CombineArgs& args, const TokenMeta* meta, int Hq, int Hkv, int D,

@@ -45,6 +45,7 @@ EXPORTS = [
     "fcg_prefix_attend",
     "fcg_norm_rope_apply", "fcg_norm_rope_workspace", "fcg_norm_rope_backward", "fcg_append_norm",
     "fcg_attend_weights", "fcg_evict",
+    "fcg_token_logprobs_workspace", "fcg_token_logprobs", "fcg_token_logprobs_backward", "fcg_locality_measure_ppl",
 ]
 FCG_ROPE_HALF, FCG_ROPE_PAIRS = 0, 1
 FCG_ROPE_PLAIN, FCG_ROPE_LINEAR, FCG_ROPE_NTK, FCG_ROPE_PARTS, FCG_ROPE_GIVEN = range(5)
@@ -149,6 +150,10 @@ def _load():
         "fcg_norm_rope_backward": [P, I32, I32, I32, I32, P, PS, PS, P, I64, P],
         "fcg_attend_weights": [P, I32, I32, I32, I32, P, P, PT, P, P, U32, P],
         "fcg_evict": [P, I32, P, P, P, I32, I32, P, P, P, P],
+        "fcg_token_logprobs_workspace": [I32, I32, I32, PI64],
+        "fcg_token_logprobs": [I32, I32, I32, P, I64, P, P, P, P, I32, P, P, P, I64, P],
+        "fcg_token_logprobs_backward": [I32, I32, I32, P, I64, P, P, P, P, P, P, P, I64, P],
+        "fcg_locality_measure_ppl": [P, I32, P, P, P, P],
         "fcg_append_norm": [P, I32, I32, I32, P, P, P, PN, PN, PT, PT, PT, PT, U32, P],
     })
     for name, args in sig.items():
@@ -812,6 +817,75 @@ def fcg_evict(cache: Cache, src, dst, keep, weights, first: int = 0, recent: int
         pk = _plain(kept, (d.n_layers, n, d.n_kv_heads, int(k.max(initial=0))), torch.int32, dev, "kept", strict=False)
     _check(_L.fcg_evict(cache.h, n, _p(a), _p(b), _p(k), int(first), int(recent), None if rope is None else rope.h, pw, pk,
                         _stream_of(stream, dev)))
+
+
+# -------------------------------------------------- log probabilities
+
+def _logits(t, what: str):
+    """(dtype code, rows, vocab, row stride) of a tensor of logits [n][vocab]."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what}: requires a gradient, which these calls do not record")
+    if t.dim() != 2 or t.dtype not in _TORCH_DT or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1 and t.numel()):
+        raise ValueError(f"{what}: a float32 or bfloat16 GPU tensor [rows][vocab], the logits of a row adjacent")
+    return _TORCH_DT[t.dtype], t.shape[0], t.shape[1], t.stride(0)
+
+
+def fcg_token_logprobs_workspace(n_rows: int, vocab: int, n_top: int = 0) -> int:
+    """Bytes of workspace that ``fcg_token_logprobs`` needs (0 for many rows)."""
+    n = C.c_int64()
+    _check(_L.fcg_token_logprobs_workspace(int(n_rows), int(vocab), int(n_top), C.byref(n)))
+    return n.value
+
+
+def fcg_token_logprobs(logits, targets=None, logprob=None, entropy=None, lse=None, top_id=None, top_logprob=None,
+                       workspace=None, stream=None) -> None:
+    """Of each row of logits [n][vocab]: the log probability of its target (int32 [n]; outside the vocabulary: none), its
+    entropy, its log-sum-exp (float32 [n]) and the most likely tokens (top_id int32, top_logprob float32 [n][k], k <= 64);
+    None: not wanted.  Records no gradient: fcg_token_logprobs_backward is that of an autograd function."""
+    dt, n, vocab, step = _logits(logits, "logits")
+    dev, f32, k = logits.get_device(), torch.float32, 0 if top_id is None else top_id.shape[-1]
+    if top_id is None and top_logprob is not None:
+        raise ValueError("top_logprob without top_id")
+    if logprob is not None and targets is None:
+        raise ValueError("log probabilities without targets")
+    outs = [_plain(t, (n,), d, dev, what, strict=False) for t, d, what in
+            ((targets, torch.int32, "targets"), (logprob, f32, "logprob"), (entropy, f32, "entropy"), (lse, f32, "lse"))]
+    tops = [_plain(top_id, (n, k), torch.int32, dev, "top_id", strict=False),
+            _plain(top_logprob, (n, k), f32, dev, "top_logprob", strict=False)]
+    ws, nbytes, keep = _workspace(workspace, 0 if workspace is not None else fcg_token_logprobs_workspace(n, vocab, k), dev,
+                                  stream)
+    _on_device(dev, _L.fcg_token_logprobs, (dt, n, vocab, logits.data_ptr(), step, *outs, k, *tops, ws, nbytes,
+                                            _stream_of(stream, dev)))
+
+
+def fcg_token_logprobs_backward(logits, targets, lse, entropy, dlogits, g_logprob=None, g_entropy=None, g_lse=None,
+                                stream=None) -> None:
+    """Gradient of the logits from those of logprob, entropy and lse (float32 [n], None: zero), with the lse and entropy of
+    the forward pass.  dlogits may be the logits in place."""
+    dt, n, vocab, step = _logits(logits, "logits")
+    dev, f32 = logits.get_device(), torch.float32
+    if (dlogits.shape != logits.shape or dlogits.dtype != logits.dtype or dlogits.get_device() != dev or
+            (dlogits.shape[1] > 1 and dlogits.stride(1) != 1 and dlogits.numel())):
+        raise ValueError("dlogits: a tensor as the logits")
+    ins = [_plain(t, (n,), d, dev, what, strict=False) for t, d, what in
+           ((targets, torch.int32, "targets"), (lse, f32, "lse"), (entropy, f32, "entropy"), (g_logprob, f32, "g_logprob"),
+            (g_entropy, f32, "g_entropy"), (g_lse, f32, "g_lse"))]
+    _on_device(dev, _L.fcg_token_logprobs_backward, (dt, n, vocab, logits.data_ptr(), step, *ins, dlogits.data_ptr(),
+                                                     dlogits.stride(0), _stream_of(stream, dev)))
+
+
+def fcg_locality_measure_ppl(loc: Locality, funcs, lengths, logprob, stream=None) -> None:
+    """Set the perplexities of ``funcs`` from the log probabilities of their tokens (float32 GPU tensor, ``lengths[i]`` of
+    function i after those before it).  Waits for the stream."""
+    f, n = _i32(funcs), _i32(lengths)
+    if f.ndim != 1 or f.shape != n.shape:
+        raise ValueError("funcs and lengths differ in length")
+    if logprob.dtype != torch.float32 or not logprob.is_cuda or not logprob.is_contiguous() or \
+            logprob.numel() < int(n.sum(dtype=np.int64)):
+        raise ValueError("logprob: a contiguous float32 GPU tensor of every function's tokens")
+    dev = logprob.get_device()
+    _on_device(dev, _L.fcg_locality_measure_ppl, (loc.h, int(f.size), _p(f), _p(n), logprob.data_ptr(),
+                                                  _stream_of(stream, dev)))
 
 
 def fcg_status_string(status: int) -> str:
