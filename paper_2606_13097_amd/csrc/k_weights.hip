@@ -121,23 +121,36 @@ __global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightCall wc, P
   }
 
   const int n_tile = (it.n_row + kTileRows - 1) / kTileRows;
+  // Two tiles ahead the rows' tokens, one tile ahead the rows: neither load waits for the
+  // other inside a tile.  Rows past the item's repeat its last one and see no key.
   uint4 pf[PF];
+  int tok[PF], ltok = 0, lpos = -1, pp = -1;
   float pl = 0.f;
-  int pp = 0;
-  // rows past the item's repeat its last one and see no key
+  auto find = [&](int ti) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < PF; ++j) {
+      const int r = min(ti * kTileRows + (j * 256 + t) / NC, it.n_row - 1);
+      tok[j] = plan.rank((it.row0 + r) >> wc.g_shift).tok;
+    }
+    if (t < kTileRows) {
+      const int r = ti * kTileRows + t;
+      const WeightRank m = plan.rank((it.row0 + min(r, it.n_row - 1)) >> wc.g_shift);
+      ltok = m.tok;
+      lpos = r < it.n_row ? m.pos : -1;
+    }
+  };
   auto fetch = [&](int ti) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < PF; ++j) {
-      const int c = j * 256 + t, r = min(ti * kTileRows + c / NC, it.n_row - 1), row = it.row0 + r;
-      const int tok = plan.rank(row >> wc.g_shift).tok, head = (hk << wc.g_shift) + (row & (g - 1));
-      const T* src = reinterpret_cast<const T*>(wc.q.p) + (int64_t)tok * wc.q.token + (int64_t)head * wc.q.head;
+      const int c = j * 256 + t, row = it.row0 + min(ti * kTileRows + c / NC, it.n_row - 1);
+      const int head = (hk << wc.g_shift) + (row & (g - 1));
+      const T* src = reinterpret_cast<const T*>(wc.q.p) + (int64_t)tok[j] * wc.q.token + (int64_t)head * wc.q.head;
       pf[j] = ld16_any(reinterpret_cast<const char*>(src) + c % NC * 16);
     }
     if (t < kTileRows) {
-      const int r = ti * kTileRows + t, row = it.row0 + min(r, it.n_row - 1);
-      const WeightRank m = plan.rank(row >> wc.g_shift);
-      pl = wc.lse[(int64_t)m.tok * wc.n_q_heads + (hk << wc.g_shift) + (row & (g - 1))] * 1.4426950408889634f;
-      pp = r < it.n_row ? m.pos : -1;
+      const int row = it.row0 + min(ti * kTileRows + t, it.n_row - 1);
+      pl = wc.lse[(int64_t)ltok * wc.n_q_heads + (hk << wc.g_shift) + (row & (g - 1))];
+      pp = lpos;
     }
   };
   auto put = [&](int b) __attribute__((always_inline)) {
@@ -147,11 +160,13 @@ __global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightCall wc, P
       s_q[b][r * NC + ((c % NC) ^ (r % SW))] = pf[j];
     }
     if (t < kTileRows) {
-      s_l[b][t] = pl;
+      s_l[b][t] = pl * 1.4426950408889634f;
       s_pos[b][t] = pp;
     }
   };
+  find(0);
   fetch(0);
+  find(1);
   put(0);
   __syncthreads();
 
@@ -161,11 +176,14 @@ __global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightCall wc, P
   for (int i = 0; i < KN; ++i) sum[i] = 0.f;
   for (int ti = 0; ti < n_tile; ++ti) {
     const int b = ti & 1;
-    if (ti + 1 < n_tile) fetch(ti + 1);
+    if (ti + 1 < n_tile) {
+      fetch(ti + 1);
+      find(ti + 2);
+    }
     const int left = it.n_row - ti * kTileRows;
 #pragma unroll
     for (int sub = 0; sub < kTileRows / 32; ++sub) {
-      if (sub * 32 >= left) break;
+      if (sub * 32 >= left || key0 >= it.k1) break;  // (wave-uniform) no rows, or no keys of this wave
       const int r0 = sub * 32;
       wt_f32x16 st[KN];
 #pragma unroll
@@ -251,7 +269,7 @@ int launch(int dtype, const WeightCall& wc, const Plan<VALUE>& plan, int n_items
            hipStream_t s) {
   const dim3 grid(cv.n_kv_heads, n_items);
 #define WK(T, DD, PG, KN) hipLaunchKernelGGL((attend_weights_kernel<T, DD, PG, KN, VALUE>), grid, dim3(256), 0, s, wc, plan, cv)
-#define WKN(T, DD, PG) { if (block == 256) WK(T, DD, PG, 2); else WK(T, DD, PG, 1); }
+#define WKN(T, DD, PG) { if (block == 256) WK(T, DD, PG, (weights_most_keys(sizeof(T), DD) / 128)); else WK(T, DD, PG, 1); }
 #define WKP(T, DD) { if (cv.page_size) WKN(T, DD, true) else WKN(T, DD, false) }
   if (dtype == 0) { if (cv.head_dim == 64) WKP(float, 64) else WKP(float, 128) }
   else { if (cv.head_dim == 64) WKP(bf16_t, 64) else WKP(bf16_t, 128) }

@@ -21,12 +21,13 @@ struct WeightPlan {
   bool by_value = false;
 };
 
-// Blocks of 256 keys (the rows are read half as often from LDS) where that leaves two
-// blocks of threads for each of 256 compute units, else of 128; the rows cut into splits
-// of at least 256 where even those are too few.
+// Blocks of 256 keys (the rows are read half as often from LDS) where the work is enough
+// for four times the blocks that are resident at once, else of 128.  The rows of a block
+// of keys are cut into splits where that makes twice the resident blocks of like work, of
+// 4 tiles of 64 rows at least: a split costs a partial, and a call with any a second launch.
 void plan_weights(const fcg_model_desc& d, int32_t prefix_seq, int32_t P, int32_t n, const int32_t* seq,
                   const int32_t* pos, WeightPlan* p) {
-  constexpr int64_t kBlocks = 512;
+  constexpr int64_t kResident = 512;
   const int g = d.n_q_heads / d.n_kv_heads;
   std::vector<int32_t> order(n);
   for (int32_t t = 0; t < n; ++t) order[t] = t;
@@ -42,17 +43,15 @@ void plan_weights(const fcg_model_desc& d, int32_t prefix_seq, int32_t P, int32_
     if (end > P) groups.push_back(WeightGroup{seq[order[i]], P, end, i * g, (j - i) * g, 0, 0});
     i = j;
   }
-  auto blocks = [&](int64_t len) {
-    int64_t b = 0;
-    for (const WeightGroup& x : groups) b += (x.hi - x.lo + len - 1) / len;
-    return b * d.n_kv_heads;
+  // tiles of 64 rows past a block of keys, over all kv heads
+  auto work = [&](int64_t len) {
+    int64_t tiles = 0;
+    for (const WeightGroup& x : groups) tiles += (x.hi - x.lo + len - 1) / len * ((x.rows + 63) / 64);
+    return tiles * d.n_kv_heads;
   };
-  p->block = blocks(256) >= kBlocks ? 256 : 128;
-  const int64_t have = std::max<int64_t>(1, blocks(p->block));
-  int32_t rows = 1;
-  for (const WeightGroup& x : groups) rows = std::max(rows, x.rows);
-  const int64_t want = (kBlocks + have - 1) / have;
-  int32_t split_rows = (int32_t)std::max<int64_t>(256, (rows / want + 63) / 64 * 64);
+  p->block = weights_most_keys(esize(d.dtype), d.head_dim);
+  if (work(p->block) < 8 * kResident) p->block = 128;
+  const int32_t split_rows = (int32_t)std::max<int64_t>(4, (work(p->block) + 2 * kResident - 1) / (2 * kResident)) * 64;
   const int pre = P && n ? 1 : 0;  // the first group is the prefix
   int64_t all = 0;
   for (const WeightGroup& x : groups)
