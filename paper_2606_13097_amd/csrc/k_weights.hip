@@ -98,7 +98,10 @@ __global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightCall wc, P
   constexpr int NC = D * (int)sizeof(T) / 16;  // 16-byte chunks of a row
   constexpr int KS = NC / 2;                   // a pair of lanes takes two chunks a step
   constexpr int SW = NC < 16 ? NC : 16;        // rows' chunks are XORed with the row modulo this
-  constexpr int PF = kTileRows * NC / 256;     // chunks of a tile that a thread brings in
+  constexpr int PF = NC / 4;                   // chunks of a tile that a thread brings in
+  // whole tiles' products beside exponentials: fp32 products leave these room anyway, and small
+  // calls gain more from a third block on a compute unit
+  constexpr bool PIPE = sizeof(T) == 2 && KN == 2;
   __shared__ __align__(16) uint4 s_q[2][kTileRows * NC];
   __shared__ __align__(16) float s_l[2][kTileRows];
   __shared__ __align__(16) int s_pos[2][kTileRows];
@@ -121,47 +124,33 @@ __global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightCall wc, P
   }
 
   const int n_tile = (it.n_row + kTileRows - 1) / kTileRows;
-  // Two tiles ahead the rows' tokens, one tile ahead the rows: neither load waits for the
-  // other inside a tile.  Rows past the item's repeat its last one and see no key.
+  // Four threads bring in a row, each every fourth chunk.  Two tiles ahead the rows' tokens,
+  // one tile ahead the rows: neither load waits for the other inside a tile.  Rows past the
+  // item's repeat its last one and see no key.
+  const int tr = t >> 2, tc = t & 3;
   uint4 pf[PF];
-  int tok[PF], ltok = 0, lpos = -1, pp = -1;
+  WeightRank rank, at;
   float pl = 0.f;
   auto find = [&](int ti) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < PF; ++j) {
-      const int r = min(ti * kTileRows + (j * 256 + t) / NC, it.n_row - 1);
-      tok[j] = plan.rank((it.row0 + r) >> wc.g_shift).tok;
-    }
-    if (t < kTileRows) {
-      const int r = ti * kTileRows + t;
-      const WeightRank m = plan.rank((it.row0 + min(r, it.n_row - 1)) >> wc.g_shift);
-      ltok = m.tok;
-      lpos = r < it.n_row ? m.pos : -1;
-    }
+    rank = plan.rank((it.row0 + min(ti * kTileRows + tr, it.n_row - 1)) >> wc.g_shift);
   };
   auto fetch = [&](int ti) __attribute__((always_inline)) {
+    const int r = ti * kTileRows + tr, row = it.row0 + min(r, it.n_row - 1);
+    const int head = (hk << wc.g_shift) + (row & (g - 1));
+    at = WeightRank{rank.tok, r < it.n_row ? rank.pos : -1};
+    const char* src = reinterpret_cast<const char*>(reinterpret_cast<const T*>(wc.q.p) + (int64_t)at.tok * wc.q.token +
+                                                    (int64_t)head * wc.q.head) + tc * 16;
 #pragma unroll
-    for (int j = 0; j < PF; ++j) {
-      const int c = j * 256 + t, row = it.row0 + min(ti * kTileRows + c / NC, it.n_row - 1);
-      const int head = (hk << wc.g_shift) + (row & (g - 1));
-      const T* src = reinterpret_cast<const T*>(wc.q.p) + (int64_t)tok[j] * wc.q.token + (int64_t)head * wc.q.head;
-      pf[j] = ld16_any(reinterpret_cast<const char*>(src) + c % NC * 16);
-    }
-    if (t < kTileRows) {
-      const int row = it.row0 + min(ti * kTileRows + t, it.n_row - 1);
-      pl = wc.lse[(int64_t)ltok * wc.n_q_heads + (hk << wc.g_shift) + (row & (g - 1))];
-      pp = lpos;
-    }
+    for (int j = 0; j < PF; ++j) pf[j] = ld16_any(src + j * 64);
+    if (tc == 0) pl = wc.lse[(int64_t)at.tok * wc.n_q_heads + head];
   };
+  const int qoff = tr * NC + (tc ^ (tr % SW));  // chunk 4 j + tc of the row lies at qoff ^ 4 j
   auto put = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < PF; ++j) {
-      const int c = j * 256 + t, r = c / NC;
-      s_q[b][r * NC + ((c % NC) ^ (r % SW))] = pf[j];
-    }
-    if (t < kTileRows) {
-      s_l[b][t] = pl * 1.4426950408889634f;
-      s_pos[b][t] = pp;
+    for (int j = 0; j < PF; ++j) s_q[b][qoff ^ (4 * j)] = pf[j];
+    if (tc == 0) {
+      s_l[b][tr] = pl * 1.4426950408889634f;
+      s_pos[b][tr] = at.pos;
     }
   };
   find(0);
@@ -171,16 +160,11 @@ __global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightCall wc, P
   __syncthreads();
 
   const float scale = 1.4426950408889634f / sqrtf((float)D);
-  float sum[KN];
+  float sum[KN][4];
 #pragma unroll
-  for (int i = 0; i < KN; ++i) sum[i] = 0.f;
-  for (int ti = 0; ti < n_tile; ++ti) {
-    const int b = ti & 1;
-    if (ti + 1 < n_tile) {
-      fetch(ti + 1);
-      find(ti + 2);
-    }
-    const int left = it.n_row - ti * kTileRows;
+  for (int i = 0; i < KN; ++i) sum[i][0] = sum[i][1] = sum[i][2] = sum[i][3] = 0.f;
+  // A tile of which some row is missing or does not see some key of this wave.
+  auto parts = [&](int b, int left) __attribute__((always_inline)) {
 #pragma unroll
     for (int sub = 0; sub < kTileRows / 32; ++sub) {
       if (sub * 32 >= left || key0 >= it.k1) break;  // (wave-uniform) no rows, or no keys of this wave
@@ -224,15 +208,75 @@ __global__ void __launch_bounds__(256, 2) attend_weights_kernel(WeightCall wc, P
         for (int n = 8; n >= 1; n /= 2)
 #pragma unroll
           for (int e = 0; e < n; ++e) p[e] += p[e + n];
-        sum[i] += p[0];
+        sum[i][0] += p[0];
       }
     }
+  };
+  // A whole tile that sees all of this wave's keys: a product's steps beside the
+  // exponentials of the one before (the matrix unit works while the others are issued), row
+  // operands and log-sum-exps of the next 32 rows read in the place of those just used.
+  constexpr int UN = kTileRows / 32 * KN;  // products
+  auto whole = [&](int b) __attribute__((always_inline)) {
+    if constexpr (PIPE) {
+    uint4 qf[KS];
+    float l[16];
+    wt_f32x16 st[2];
+    auto row_frag = [&](int sub, int s) __attribute__((always_inline)) {
+      return s_q[b][(sub * 32 + lc) * NC + ((2 * s + lh) ^ (lc % SW))];
+    };
+    auto row_lse = [&](int sub, int q) __attribute__((always_inline)) {
+      const float4 x = *reinterpret_cast<const float4*>(&s_l[b][sub * 32 + 8 * q + 4 * lh]);
+      l[4 * q] = x.x;
+      l[4 * q + 1] = x.y;
+      l[4 * q + 2] = x.z;
+      l[4 * q + 3] = x.w;
+    };
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = row_frag(0, s);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) row_lse(0, q);
+#pragma unroll
+    for (int u = 0; u <= UN; ++u) {  // product u (32 rows u / KN, keys u % KN) and the exponentials of u - 1
+      const int sub = u / KN, i = u % KN, before = (u + KN - 1) % KN;
+      float p[16];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        if (u < UN) {
+          st[u & 1] = mma<T>(qf[s], kf[i][s], s ? st[u & 1] : wt_f32x16{});
+          if (i == KN - 1 && sub + 1 < kTileRows / 32) qf[s] = row_frag(sub + 1, s);
+        }
+        if (u) {
+#pragma unroll
+          for (int e = s * 16 / KS; e < (s + 1) * 16 / KS; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(fmaf(st[(u & 1) ^ 1][e], scale, -l[e]));
+            if (e % 4 == 3) {
+              sum[before][e / 4] += (p[e - 3] + p[e - 2]) + (p[e - 1] + p[e]);
+              if (before == KN - 1 && u < UN) row_lse(sub, e / 4);
+            }
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    }
+  };
+  for (int ti = 0; ti < n_tile; ++ti) {
+    const int b = ti & 1;
+    if (ti + 1 < n_tile) {
+      fetch(ti + 1);
+      find(ti + 2);
+    }
+    const int left = it.n_row - ti * kTileRows;
+    const bool full = PIPE && left >= kTileRows && key0 < it.k1 && s_pos[b][0] >= key0 + 32 * KN - 1;
+    if (__builtin_amdgcn_readfirstlane(full)) whole(b);
+    else parts(b, left);
     if (ti + 1 < n_tile) put(b ^ 1);
     __syncthreads();
   }
 #pragma unroll
   for (int i = 0; i < KN; ++i) {
-    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[i]), __float_as_uint(sum[i]), false, false);
+    const uint32_t mine = __float_as_uint((sum[i][0] + sum[i][1]) + (sum[i][2] + sum[i][3]));
+    const auto x = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
     const float total = __uint_as_float(x[0]) + __uint_as_float(x[1]);
     const int key = key0 + 32 * i + lc;
     if (lh || key >= it.k1) continue;
