@@ -33,14 +33,19 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 }
 constexpr uint32_t kAlways = 0xFFFFFFFFu;
 
-// inclusive sum over the lanes of a wave up to this one
-__device__ __forceinline__ int scan_wave(int v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int x = __shfl_up(v, d);
-    if (lane >= d) v += x;
-  }
-  return v;
+// inclusive sum over the lanes of a wave up to this one: within rows of 16 lanes by DPP
+// shifts, then the sums of the rows before by its broadcasts of lanes 15, 47 and 31
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int scan_wave(int v) {
+  v = dpp_add<0x111, 0xF>(v);  // row_shr:1
+  v = dpp_add<0x112, 0xF>(v);
+  v = dpp_add<0x114, 0xF>(v);
+  v = dpp_add<0x118, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);     // row_bcast:15 to rows 1 and 3
+  return dpp_add<0x143, 0xC>(v);  // row_bcast:31 to rows 2 and 3
 }
 
 // The item of chunk (or block) b: the last one whose first chunk is at most b.
@@ -60,7 +65,7 @@ __device__ __forceinline__ int32_t* kept_row(const EvictCall& ec, int item, int 
 __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(EvictCall ec, EvictArgs a, RopeArgs ra, int n_rows,
                                                                    int n_seqs, int Hkv, int max_tokens, int n_turn) {
   __shared__ int s_hist[kBins];
-  __shared__ int s_wave[kSelWaves];
+  __shared__ __align__(16) int s_wave[kSelWaves];
   __shared__ int s_gt[kSelKeys * kSelWaves], s_eq[kSelKeys * kSelWaves];
   __shared__ int s_bin, s_above;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
@@ -85,16 +90,20 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(EvictCall ec,
   const int first = min(keep, ec.first), recent = min(keep - first, ec.recent);
 
   float v[kSelKeys];
+  uint32_t key[kSelKeys];
+  // (uniform) some thread's element e of the segment is in the row
+  auto used = [&](int seg, int e) __attribute__((always_inline)) { return seg * kSelSeg + e * kSelThreads < n; };
   auto load = [&](int seg) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < kSelKeys; ++e) {
       const int i = seg * kSelSeg + e * kSelThreads + t;
-      v[e] = i < n ? src[i] : 0.f;
+      if (used(seg, e)) v[e] = i < n ? src[i] : 0.f;
     }
-  };
-  auto key_of = [&](int seg, int e) __attribute__((always_inline)) -> uint32_t {
-    const int i = seg * kSelSeg + e * kSelThreads + t;
-    return i < first || i >= n - recent ? kAlways : order_of(v[e]);
+#pragma unroll
+    for (int e = 0; e < kSelKeys; ++e) {
+      const int i = seg * kSelSeg + e * kSelThreads + t;
+      if (used(seg, e)) key[e] = i < first || i >= n - recent ? kAlways : order_of(v[e]);
+    }
   };
   const int n_seg = keep ? (n + kSelSeg - 1) / kSelSeg : 0;
   // threshold: the keep-th largest key; `equal` of those equal to it stay
@@ -110,19 +119,21 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(EvictCall ec,
         if (n_seg > 1) load(seg);
 #pragma unroll
         for (int e = 0; e < kSelKeys; ++e) {
+          if (!used(seg, e)) break;
           const int i = seg * kSelSeg + e * kSelThreads + t;
-          const uint32_t k = key_of(seg, e);
+          const uint32_t k = key[e];
           if (i < n && (k & mask) == top) atomicAdd(&s_hist[k >> shift & ((1u << bits) - 1)], 1);
         }
       }
       __syncthreads();
       // bins from the highest down, two a thread: the one in which the count passes `equal`
       const int b1 = kBins - 1 - 2 * t, h1 = s_hist[b1], h0 = s_hist[b1 - 1];
-      const int up = scan_wave(h1 + h0, lane);
+      const int up = scan_wave(h1 + h0);
       if (lane == 63) s_wave[w] = up;
       __syncthreads();
       int above = up - h1 - h0;
-      for (int j = 0; j < w; ++j) above += s_wave[j];
+#pragma unroll
+      for (int j = 0; j < kSelWaves; ++j) above += j < w ? s_wave[j] : 0;
       if (above < equal && above + h1 >= equal) {
         s_bin = b1;
         s_above = above;
@@ -144,8 +155,12 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(EvictCall ec,
     uint32_t is_gt = 0, is_eq = 0;
 #pragma unroll
     for (int e = 0; e < kSelKeys; ++e) {
+      if (!used(seg, e)) {  // (counts of the places past the row)
+        if (t < kSelWaves) s_gt[e * kSelWaves + t] = s_eq[e * kSelWaves + t] = 0;
+        continue;
+      }
       const int i = seg * kSelSeg + e * kSelThreads + t;
-      const uint32_t k = key_of(seg, e);
+      const uint32_t k = key[e];
       const bool all = keep >= n;
       const bool gt = i < n && (all || k > top), eq = i < n && !all && k == top;
       is_gt |= (uint32_t)gt << e;
@@ -162,15 +177,16 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(EvictCall ec,
       int base = w ? eq0 : gt0;
 #pragma unroll
       for (int j = 0; j < kSelKeys * kSelWaves; j += 64) {
-        const int c = s[j + lane], up = scan_wave(c, lane);
+        const int c = s[j + lane], up = scan_wave(c);
         s[j + lane] = base + up - c;
-        base += __shfl(up, 63);
+        base += __builtin_amdgcn_readlane(up, 63);
       }
       if (lane == 0) s_wave[w] = base;
     }
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < kSelKeys; ++e) {
+      if (!used(seg, e)) break;
       const bool gt = is_gt >> e & 1, eq = is_eq >> e & 1;
       const uint64_t bg = __builtin_amdgcn_ballot_w64(gt), be = __builtin_amdgcn_ballot_w64(eq);
       const int g = s_gt[e * kSelWaves + w] + __builtin_amdgcn_mbcnt_hi(bg >> 32, __builtin_amdgcn_mbcnt_lo((uint32_t)bg, 0));
@@ -276,10 +292,10 @@ __global__ void __launch_bounds__(256) evict_copy_kernel(EvictCall ec, EvictArgs
     const int j = min(j0 + p * RP + row, it.keep - 1);
     const T* k = reinterpret_cast<const T*>(cv.k) + kv_offset<PAGED>(cv, layer, it.src, hk, from[p]);
     const T* v = v_row<PAGED, T>(cv, layer, it.src, hk, from[p]);
-    ka[p] = ld16(k + ln.lo);
-    kb[p] = ld16(k + ln.hi);
-    va[p] = ld16(v + ln.lo);
-    vb[p] = ld16(v + ln.hi);
+    ka[p] = ld16_nt(k + ln.lo);
+    kb[p] = ld16_nt(k + ln.hi);
+    va[p] = ld16_nt(v + ln.lo);
+    vb[p] = ld16_nt(v + ln.hi);
     ln.load(ec.turns + (int64_t)(from[p] - j) * half, cs[p]);
   }
 #pragma unroll
@@ -290,10 +306,10 @@ __global__ void __launch_bounds__(256) evict_copy_kernel(EvictCall ec, EvictArgs
     T* k = reinterpret_cast<T*>(cv.k) + at;
     T* v = reinterpret_cast<T*>(cv.v) + at;
     if (from[p] != j) ln.turn(&ka[p], &kb[p], cs[p]);
-    st16(k + ln.lo, ka[p]);
-    st16(k + ln.hi, kb[p]);
-    st16(v + ln.lo, va[p]);
-    st16(v + ln.hi, vb[p]);
+    st16_nt(k + ln.lo, ka[p]);
+    st16_nt(k + ln.hi, kb[p]);
+    st16_nt(v + ln.lo, va[p]);
+    st16_nt(v + ln.hi, vb[p]);
   }
 }
 
@@ -360,7 +376,7 @@ int launch_evict_select(const EvictCall& ec, const EvictArgs& args, const RopeAr
                         int max_tokens, int n_turn, hipStream_t s) {
   const int n_rows = args.n * Hkv * n_layers;
   const int64_t entries = (int64_t)n_turn * (ra.rot / 2);
-  const int64_t want = (entries + 4 * kSelThreads - 1) / (4 * kSelThreads);
+  const int64_t want = (entries + kSelThreads - 1) / kSelThreads;
   const int n_tab = (int)(want < 1024 ? want : 1024);
   hipLaunchKernelGGL(evict_select_kernel, dim3(n_rows + n_tab), dim3(kSelThreads), 0, s, ec, args, ra, n_rows, n_seqs, Hkv,
                      max_tokens, n_turn);
