@@ -14,12 +14,14 @@
 //
 // The most likely tokens: order is (value, then lower index), as one 64-bit key.  A block
 // holds a chunk of its row in registers (4 vectors a thread); a lower bound on the k-th
-// largest key is the k-th largest of the maxima of 64 groups of 8 threads (later chunks:
+// largest key is the k-th largest of the maxima of 64 groups of 4 threads (later chunks:
 // the k-th found so far), and the few elements at or above it go to a list in LDS, of which
 // k are kept by counting.  If too many pass (a row of equal logits), the bound is taken
 // anew from the threads' own largest keys: at most (k - 1) 32 + 1 elements reach that.
 //
 // Few rows are cut into splits, whose partials a second launch joins.
+#include <type_traits>
+
 #include "fcg_device.hpp"
 #include "kernels.hpp"
 
@@ -27,7 +29,7 @@ namespace fcg {
 
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kListCap = kLogpTop + (kLogpTop - 1) * 32 + 1;  // keys kept, and those of one chunk
 constexpr float kC = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kFar = 1e6f;  // rows whose largest logit is past this take the second reading: c r is off by up to a tenth there
@@ -42,6 +44,8 @@ __device__ __forceinline__ float value_of(uint32_t k) {
 }
 __device__ __forceinline__ uint64_t key_of(float x, int i) { return (uint64_t)order_of(x) << 32 | (uint32_t)~i; }
 
+constexpr uint32_t kLowest = 0x007FFFFFu;  // order_of(-inf)
+
 // S and U about a reference
 struct Stat {
   float r, s, u;
@@ -52,10 +56,20 @@ __device__ __forceinline__ Stat join(const Stat& a, const Stat& b) {
   const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
   return Stat{r, fmaf(a.s, fa, b.s * fb), fmaf(fmaf(a.s, da, a.u), fa, fmaf(b.s, db, b.u) * fb)};
 }
-__device__ __forceinline__ Stat join_wave(Stat a) {
-#pragma unroll
-  for (int d = 32; d >= 1; d /= 2) a = join(a, Stat{__shfl_xor(a.r, d), __shfl_xor(a.s, d), __shfl_xor(a.u, d)});
-  return a;
+__device__ __forceinline__ float max_wave(float v) {
+  v = max_lanes32(v);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_wave(float v) {
+  v = sum_lanes32(v);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+// over the lanes of a wave: every lane's brought to the largest reference, then added
+__device__ __forceinline__ Stat join_wave(const Stat& a) {
+  const float r = max_wave(a.r), d = fmaxf((a.r - r) * kC, -1e30f), f = __builtin_amdgcn_exp2f(d);
+  return Stat{r, sum_wave(a.s * f), sum_wave(fmaf(a.s, d, a.u) * f)};
 }
 
 // what a row's statistics give
@@ -74,17 +88,23 @@ struct Row {
   }
 };
 
+// A row's target and its logit, asked for early: two memory round trips.
 template <typename T>
-__device__ __forceinline__ void finish(const LogpArgs& la, int row, const Stat& st) {
+struct Target {
+  int t;
+  float x;
+  __device__ __forceinline__ Target(const LogpArgs& la, int row) : t(la.logprob ? la.targets[row] : -1), x(0.f) {}
+  __device__ __forceinline__ void load(const LogpArgs& la, int row) {
+    if (t >= la.vocab) t = -1;
+    if (t >= 0) x = Store<T>::load1(reinterpret_cast<const T*>(la.x) + (int64_t)row * la.stride + t);
+  }
+};
+template <typename T>
+__device__ __forceinline__ void finish(const LogpArgs& la, int row, const Stat& st, const Target<T>& tg) {
   const Row rw(st);
   if (la.lse) la.lse[row] = rw.lse;
   if (la.entropy) la.entropy[row] = rw.entropy(st);
-  if (la.logprob) {
-    const int t = la.targets[row];
-    la.logprob[row] = t < 0 || t >= la.vocab
-                          ? 0.f
-                          : rw.logprob(Store<T>::load1(reinterpret_cast<const T*>(la.x) + (int64_t)row * la.stride + t));
-  }
+  if (la.logprob) la.logprob[row] = tg.t < 0 ? 0.f : rw.logprob(tg.x);
 }
 __device__ __forceinline__ void put_top(const LogpArgs& la, int row, int j, uint64_t key, const Stat& st) {
   const Row rw(st);
@@ -139,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
   __shared__ float s_max[kWaves];
   __shared__ uint64_t s_list[TOP ? kListCap : 1], s_top[TOP ? kLogpTop : 1], s_bound;
   __shared__ uint64_t s_own[TOP ? kThreads : 1];
-  __shared__ float s_grp[64];
+  __shared__ uint64_t s_grp[64];
   __shared__ int s_n;
 
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
@@ -149,13 +169,17 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
   const int k = la.n_top;
 
   uint4 cur[kVecs], next[kVecs];
-  // (vectors that pass the part's end read its last elements: see fix)
+  // (uniform) some thread's vector j of the chunk is in the part
+  auto used = [&](int chunk, int j) __attribute__((always_inline)) {
+    return e0 + chunk * CHUNK + j * kThreads * VEC < e1;
+  };
+  // (vectors that pass the part's end read its last elements: see fix; no branches, so that
+  // the compiler can count which loads it waits for)
   auto load = [&](uint4* v, int chunk) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
       const int i = e0 + chunk * CHUNK + (j * kThreads + t) * VEC;
-      if (e1 >= VEC) v[j] = ld16_any(x + min(i, e1 - VEC));
-      else v[j] = few<T>(x, i, e1);
+      v[j] = ld16_any(x + min(i, e1 - VEC));
     }
   };
   // in the last chunk: the elements in their places, -inf past the end
@@ -163,6 +187,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
     if (e1 < VEC) return;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
+      if (!used(chunk, j)) break;
       const int i = e0 + chunk * CHUNK + (j * kThreads + t) * VEC;
       if (i + VEC > e1) v[j] = shifted<T>(v[j], min(i + VEC - e1, VEC));
     }
@@ -174,19 +199,28 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
   }
   int have = 0;  // keys in s_list
   const int n_chunk = (e1 - e0 + CHUNK - 1) / CHUNK;
-  load(cur, 0);
-  for (int ch = 0; ch < n_chunk; ++ch) {
-    if (ch + 1 < n_chunk) load(next, ch + 1);
-    else fix(cur, ch);
-    float vmax[kVecs];
+  Target<T> target(la, row);
+  if (e1 >= VEC) {
+    load(cur, 0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) cur[j] = few<T>(x, (j * kThreads + t) * VEC, e1);
+  }
+  if (la.splits == 1) target.load(la, row);
+  auto take = [&](int ch, auto last) __attribute__((always_inline)) {
+    auto in_use = [&](int j) __attribute__((always_inline)) { return !decltype(last)::value || used(ch, j); };
+    float vmax[kVecs], tmax = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
+      vmax[j] = -INFINITY;
+      if (!in_use(j)) continue;
       float f[VEC];
       Store<T>::unpack(cur[j], f);
       float m = f[0];
 #pragma unroll
       for (int e = 1; e < VEC; ++e) m = fmaxf(m, f[e]);
       vmax[j] = m;
+      tmax = fmaxf(tmax, m);
       if (m * kC > rc + 40.f) {
 #pragma clang fp contract(off)  // the difference is that of the rounded products
         r = fminf(m, kFar);
@@ -207,9 +241,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
         u1 = fmaf(eb, fmaxf(b, -1e30f), u1);
       }
     }
-    float tmax = vmax[0];
-#pragma unroll
-    for (int j = 1; j < kVecs; ++j) tmax = fmaxf(tmax, vmax[j]);
+
     top = fmaxf(top, tmax);
 
     if constexpr (TOP) {
@@ -217,24 +249,24 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
       if (have < k) {  // a bound from the groups' maxima
         float gm = fmaxf(tmax, dpp_f32<kDppXor1>(tmax));
         gm = fmaxf(gm, dpp_f32<kDppXor2>(gm));
-        gm = fmaxf(gm, dpp_f32<kDppHalfMirror>(gm));
-        if (t % 8 == 0) s_grp[t / 8] = gm;
+        if (t % 4 == 0) s_grp[t / 4] = key_of(gm, t / 4);
         __syncthreads();
         if (w == 0) {
-          const uint64_t mine = key_of(s_grp[lane], lane);
+          const uint64_t mine = s_grp[lane];
           int above = 0;
-#pragma unroll 8
-          for (int j = 0; j < 64; ++j) above += key_of(s_grp[j], j) > mine;
+#pragma unroll 16
+          for (int j = 0; j < 64; ++j) above += s_grp[j] > mine;
           // (below -inf there is NaN, which the maxima passed over)
-          if (above == k - 1) s_bound = s_grp[lane] > -INFINITY ? mine >> 32 << 32 : 0;
+          if (above == k - 1) s_bound = mine >> 32 > kLowest ? mine >> 32 << 32 : 0;
         }
       }
       __syncthreads();
       auto each = [&](uint64_t bound, auto&& f) __attribute__((always_inline)) {
-        const float least = bound >> 32 > 0x007FFFFFu ? value_of((uint32_t)(bound >> 32)) : -INFINITY;
+        const float least = bound >> 32 > kLowest ? value_of((uint32_t)(bound >> 32)) : -INFINITY;
 #pragma unroll
         for (int j = 0; j < kVecs; ++j) {
           const int i = at + (j * kThreads + t) * VEC;
+          if (!in_use(j)) break;
           if (vmax[j] < least || i >= e1) continue;  // (NaN: not less)
           float v[VEC];
           Store<T>::unpack(cur[j], v);
@@ -280,15 +312,21 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
       }
       __syncthreads();
     }
+  };
+  for (int ch = 0; ch + 1 < n_chunk; ++ch) {
+    load(next, ch + 1);
+    take(ch, std::false_type{});
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) cur[j] = next[j];
   }
+  fix(cur, n_chunk - 1);
+  take(n_chunk - 1, std::true_type{});
 
   // the block's statistics; eta is what the product c r lost
   const float eta = fmaf(r, kC, -rc), back = __builtin_amdgcn_exp2f(-eta);
   Stat st{r, (s0 + s1) * back, fmaf(-eta, s0 + s1, u0 + u1) * back};
   st = join_wave(st);
-  for (int d = 32; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+  top = max_wave(top);
   if (lane == 0) {
     s_stat[w] = st;
     s_max[w] = top;
@@ -318,25 +356,57 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
     if (TOP && t < k) la.part_top[(int64_t)blockIdx.x * k + t] = t < have ? s_list[t] : 0;
     return;
   }
-  if (t == 0) finish<T>(la, row, st);
+  if (t == 0) finish<T>(la, row, st, target);
   if (TOP && t < k) put_top(la, row, t, s_list[t], st);
 }
 
 // The splits of a row joined, in their order.
 template <typename T>
 __global__ void __launch_bounds__(256) logprob_merge_kernel(LogpArgs la) {
-  __shared__ uint64_t s_key[kLogpSplits * kLogpTop], s_top[kLogpTop];
-  const int row = blockIdx.x, t = threadIdx.x, k = la.n_top, n = la.splits * k;
-  const float4* p = la.part + (int64_t)row * la.splits;
-  for (int i = t; i < n; i += 256) s_key[i] = la.part_top[(int64_t)row * n + i];
-  Stat st{p[0].x, p[0].y, p[0].z};
-#pragma unroll 4
-  for (int j = 1; j < la.splits; ++j) st = join(st, Stat{p[j].x, p[j].y, p[j].z});
-  if (t == 0) finish<T>(la, row, st);
+  constexpr int KEYS = kLogpSplits * kLogpTop;
+  __shared__ uint64_t s_first[2 * kLogpTop], s_list[KEYS], s_top[kLogpTop], s_bound;
+  __shared__ int s_n;
+  const int row = blockIdx.x, t = threadIdx.x, lane = t & 63, k = la.n_top, n = la.splits * k;
+  static_assert(kLogpSplits <= 64, "a split a lane");
+  const uint64_t* keys = la.part_top + (int64_t)row * n;
+  Target<T> target(la, row);
+  Stat st{-3.4028235e38f, 0.f, 0.f};
+  if (lane < la.splits) {
+    const float4 p = la.part[(int64_t)row * la.splits + lane];
+    st = Stat{p.x, p.y, p.z};
+  }
+  uint64_t mine[KEYS / 256];  // (empty places, 0, lie below every key)
+#pragma unroll
+  for (int j = 0; j < KEYS / 256; ++j)
+    if (j * 256 < n) mine[j] = j * 256 + t < n ? keys[j * 256 + t] : 0;
+  target.load(la, row);
+  st = join_wave(st);
+  if (t == 0) finish<T>(la, row, st, target);
   if (!k) return;
+  // A lower bound on the row's k-th key: the k-th of the splits' first few, k in all or a
+  // few more (a split's own k-th lies far below where there are many splits).
+  const int m = (k + la.splits - 1) / la.splits, q = m * la.splits;
+  static_assert(kLogpSplits <= kLogpTop, "q < 2 kLogpTop");
+#pragma unroll
+  for (int j = 0; j < KEYS / 256; ++j) {
+    const int i = j * 256 + t, split = i / k, at = i - split * k;
+    if (j * 256 < n && i < n && at < m) s_first[split * m + at] = mine[j];
+  }
+  if (t == 0) s_n = 0;
   __syncthreads();
-  // (empty places, 0, lie below every key)
-  rank_keys(s_key, n, s_top, k, 256);
+  if (t < q) {
+    const uint64_t own = s_first[t];
+    int above = 0;
+#pragma unroll 8
+    for (int j = 0; j < q; ++j) above += s_first[j] > own || (s_first[j] == own && j < t);  // (several empty places)
+    if (above == k - 1) s_bound = own;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < KEYS / 256; ++j)
+    if (j * 256 < n && j * 256 + t < n && mine[j] >= s_bound && mine[j]) s_list[atomicAdd(&s_n, 1)] = mine[j];
+  __syncthreads();
+  rank_keys(s_list, s_n, s_top, k, 256);
   __syncthreads();
   if (t < k) put_top(la, row, t, s_top[t], st);
 }

@@ -11,8 +11,8 @@ using namespace fcg;
 
 namespace {
 
-constexpr int64_t kBlocks = 512;          // that few rows are cut into
-constexpr int32_t kSplitElements = 8192;  // and the least of one
+constexpr int64_t kBlocks = 1024;         // that few rows are cut into
+constexpr int32_t kSplitElements = 4096;  // and the least of one
 
 struct Cut {
   int32_t splits, split_len;

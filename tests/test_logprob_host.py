@@ -43,9 +43,9 @@ def test_backward_refusals_reach_no_kernel():
 
 def test_workspace():
     w = fcg.fcg_token_logprobs_workspace
-    assert w(0, 1000) == 0 and w(1, 8192, 64) == 0 and w(512, 200000, 64) == 0
-    assert w(1, 131072, 20) == 16 * (16 + 8 * 20)
-    for n in (1, 3, 100, 511):
+    assert w(0, 1000) == 0 and w(1, 4096, 64) == 0 and w(1024, 200000, 64) == 0
+    assert w(1, 131072, 20) == 32 * (16 + 8 * 20)
+    for n in (1, 3, 100, 1023):
         for vocab in (8193, 50021, 1 << 30):
             for k in (0, 64):
                 assert 0 < w(n, vocab, k) <= n * 32 * (16 + 8 * k)
