@@ -151,7 +151,8 @@ __device__ __forceinline__ void rank_keys(const uint64_t* s, int n, uint64_t* ou
 
 }  // namespace
 
-template <typename T, bool TOP>
+// STREAM: more than the last-level cache holds, read past it.
+template <typename T, bool TOP, bool STREAM>
 __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
   constexpr int kVecs = TOP ? 4 : 8;  // vectors of a thread in a chunk
   constexpr int VEC = Store<T>::VEC, CHUNK = kThreads * kVecs * VEC;
@@ -179,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
       const int i = e0 + chunk * CHUNK + (j * kThreads + t) * VEC;
-      v[j] = ld16_any(x + min(i, e1 - VEC));
+      v[j] = STREAM ? ld16_nt_any(x + min(i, e1 - VEC)) : ld16_any(x + min(i, e1 - VEC));
     }
   };
   // in the last chunk: the elements in their places, -inf past the end
@@ -460,9 +461,11 @@ int check(hipError_t e) { return e == hipSuccess ? 0 : (int)e; }
 
 int launch_logprobs(int dtype, const LogpArgs& args, hipStream_t s) {
   const dim3 grid(args.n * args.splits);
-#define LP(T, TOP) hipLaunchKernelGGL((logprob_kernel<T, TOP>), grid, dim3(kThreads), 0, s, args)
-  if (dtype == 0) { if (args.n_top) LP(float, true); else LP(float, false); }
-  else { if (args.n_top) LP(bf16_t, true); else LP(bf16_t, false); }
+#define LP(T, TOP, ST) hipLaunchKernelGGL((logprob_kernel<T, TOP, ST>), grid, dim3(kThreads), 0, s, args)
+#define LPS(T, TOP) { if (args.stream) LP(T, TOP, true); else LP(T, TOP, false); }
+  if (dtype == 0) { if (args.n_top) LPS(float, true) else LPS(float, false) }
+  else { if (args.n_top) LPS(bf16_t, true) else LPS(bf16_t, false) }
+#undef LPS
 #undef LP
   if (int rc = check(hipGetLastError())) return rc;
   if (args.splits == 1) return 0;

@@ -514,6 +514,7 @@ struct LogpArgs {
   float4* part;                // [n][splits]
   uint64_t* part_top;          // [n][splits][n_top]
   int32_t n, vocab, n_top, splits, split_len;
+  int32_t stream;  // 1: read past the caches
 };
 int launch_logprobs(int dtype, const LogpArgs& args, hipStream_t s);
 // The gradient of the logits; any g_ may be null.  chunks: blocks of a row, kLogpGradVecs

@@ -77,6 +77,9 @@ fcg_status fcg_token_logprobs(int32_t dtype, int32_t n_rows, int32_t vocab, cons
     a.n_top = n_top;
     a.splits = c.splits;
     a.split_len = c.split_len;
+    // more than the last-level cache holds (256 MB): nothing of it lies there (3001 fp32 rows of
+    // 50021, 0.6 GB, read through the caches 102 us, past them 94)
+    a.stream = (int64_t)n_rows * vocab * (int64_t)esize(dtype) > (int64_t)256 << 20;
     a.part = (float4*)workspace;
     a.part_top = (uint64_t*)((char*)workspace + (need ? (int64_t)n_rows * c.splits * 16 : 0));
     if (int rc = launch_logprobs(dtype, a, (hipStream_t)stream)) return hip_fail((hipError_t)rc, "log probability launch");
