@@ -47,12 +47,17 @@ struct NormLane<T, true> {
   bool on;
   uint4 wa, wb;
   __device__ __forceinline__ NormLane(const NormArgs<true>& n, int kind, int head, int lo_, int hi_) : lo(lo_), hi(hi_) {
-    const NormView& v = kind == 0 ? n.q : n.k;
-    on = kind != 2 && v.on;
-    w = on && v.w ? reinterpret_cast<const T*>(v.w) + head * v.head : nullptr;
-    layer = v.layer;
-    eps = v.eps;
-    offset = w ? v.offset : 1.f;
+    // (fields chosen from scalar registers: a view chosen by address is loaded lane by lane,
+    // field after field, before the first row)
+    const NormView q = n.q, k = n.k;
+    const bool is_q = kind == 0;
+    on = kind != 2 && (is_q ? q.on : k.on);
+    const int64_t step = is_q ? q.head : k.head;
+    const T* first = reinterpret_cast<const T*>(is_q ? q.w : k.w);
+    w = on && first ? first + head * step : nullptr;
+    layer = is_q ? q.layer : k.layer;
+    eps = is_q ? q.eps : k.eps;
+    offset = w ? is_q ? q.offset : k.offset : 1.f;
     wa = wb = make_uint4(0, 0, 0, 0);
   }
   __device__ __forceinline__ void load(int l) {
@@ -203,7 +208,6 @@ __device__ __forceinline__ void rope_rows(const Where<MODE>& where, const RopeRo
   uint4 a, b;
   NormLane<T, NORM> nl(norm, kind, head, lo, hi);
   auto load = [&](int layer) __attribute__((always_inline)) {
-    nl.load(layer);
     const T* p = src + layer * src_layer;
     if (rows.stream) {  // (uniform) more than the last-level cache holds
       a = ld16_nt_any(p + lo);
@@ -212,6 +216,7 @@ __device__ __forceinline__ void rope_rows(const Where<MODE>& where, const RopeRo
       a = ld16_any(p + lo);
       b = ld16_any(p + hi);
     }
+    nl.load(layer);
   };
   load(blockIdx.z);
 
