@@ -12,11 +12,11 @@
 // Forward: the blocks of rope_rows.hpp; the D / (2 VEC) lanes that hold a row add up its
 // squares by DPP, so the norm costs no memory round trip and no LDS beside the turn.
 //
-// Backward: a block takes chunks of 32 or 64 tokens, whose (cos, sin) are computed
-// once into LDS, and up to kNormHeads heads of them; a lane holds the same two vectors of
-// every row it takes, so it adds up its part of dw in registers.  With one weight vector
-// for all heads the lanes' parts are joined once, at the block's end, else after each
-// head, in LDS.  The blocks' partials are added by a second launch in a fixed order: no
+// Backward: a block takes chunks of 16 to 64 tokens, as many as it holds a row of each, whose
+// (cos, sin) are computed once into LDS, and up to kNormHeads heads of them; a lane holds the same two vectors of
+// every row it takes, so it adds up its part of dw in registers; the lanes of a wave that
+// hold the same vectors join theirs by lane exchanges, after each head (or, with one weight
+// vector for all, once), into the wave's own sums in LDS: no barrier.  The blocks' partials are added by a second launch in a fixed order: no
 // atomics, so the same call gives the same bits.
 #include "rope_rows.hpp"
 
@@ -29,19 +29,24 @@ __global__ void __launch_bounds__(256) norm_rope_kernel(Where<MODE> where, RopeR
   rope_rows<T, D, PAIRS, MODE, PAGED, true>(where, rows, cv, layer0, ra, tab, norm);
 }
 
+// sum over the lanes of a wave that are equal modulo N (4, 8 or 16)
+template <int N>
+__device__ __forceinline__ float sum_same(float v) {
+  if (N <= 8) v += dpp_f32<0x128>(v);  // row_ror:8
+  if (N <= 4) v += dpp_f32<0x124>(v);  // row_ror:4
+  return sum_rows4(v);
+}
+
 template <typename T, int D, bool PAIRS>
 __global__ void __launch_bounds__(256) norm_rope_grad_kernel(NormGradArgs args, RopeArgs ra) {
   constexpr int VEC = Store<T>::VEC;
   constexpr int NCH = D / (2 * VEC);  // lanes of a row
-  constexpr int RP = 256 / NCH;       // rows of a pass
-  constexpr int TK = norm_tokens(D);  // tokens of a chunk
-  constexpr int PASSES = TK / RP;     // passes over them
-  static_assert(TK % RP == 0, "whole passes");
+  constexpr int TK = 256 / NCH;       // tokens of a chunk, a row of each at a time
+  static_assert(TK == norm_tokens(D, sizeof(T)), "as the host counts them");
   __shared__ __align__(16) float2 s_cs[TK * D / 2];
-  __shared__ __align__(16) float s_part[RP * D];      // the lanes' parts of dw
-  __shared__ __align__(16) float s_dw[kNormHeads * D];  // (weights for each head) the block's dw
+  __shared__ __align__(16) float s_dw[4][kNormHeads * D];  // each wave's dw
 
-  const int t = threadIdx.x, c = t % NCH, tr = t / NCH;
+  const int t = threadIdx.x, c = t % NCH, tr = t / NCH, lane = t & 63, w = t >> 6;
   const int bs = blockIdx.x < args.blocks_q ? 0 : 1, b = blockIdx.x - (bs ? args.blocks_q : 0);
   const NormSide& sd = args.side[bs];
   const int layer = blockIdx.y;
@@ -58,37 +63,31 @@ __global__ void __launch_bounds__(256) norm_rope_grad_kernel(NormGradArgs args, 
   float dwa[VEC], dwb[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) dwa[e] = dwb[e] = 0.f;
-  if (has_dw && own_w)
-    for (int j = t; j < nh * D; j += 256) s_dw[j] = 0.f;
+  if (has_dw)
+    for (int j = lane; j < (own_w ? nh : 1) * D; j += 64) s_dw[w][j] = 0.f;
 
-  // the lanes' parts of dw, one row of D floats for each row of a pass, added into dst by
-  // the thread of each column, in the order of the rows
-  auto join = [&](float* dst, bool add) __attribute__((always_inline)) {
-    __syncthreads();  // the readers before are done
+  // the lanes' parts of dw into the wave's sums of a weight vector
+  auto join = [&](float* dst) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      s_part[tr * D + lo + e] = dwa[e];
-      s_part[tr * D + hi + e] = dwb[e];
+      const float a = sum_same<NCH>(dwa[e]), b = sum_same<NCH>(dwb[e]);
+      if (lane < NCH) {
+        dst[lo + e] += a;
+        dst[hi + e] += b;
+      }
       dwa[e] = dwb[e] = 0.f;
-    }
-    __syncthreads();
-    for (int j = t; j < D; j += 256) {
-      float sum = add ? dst[j] : 0.f;
-#pragma unroll 8
-      for (int r = 0; r < RP; ++r) sum += s_part[r * D + j];
-      dst[j] = sum;
     }
   };
 
   const int n_chunk = (args.n_tok + TK - 1) / TK;
   for (int ch = tc; ch < n_chunk; ch += sd.spread) {
     const int tok0 = ch * TK, n = min(TK, args.n_tok - tok0);
-    const int steps = nh * PASSES;
-    uint4 xa, xb, ga, gb;
+    const bool mine = tr < n;
+    uint4 xa, xb, ga, gb, wa = make_uint4(0, 0, 0, 0), wb = wa;
     auto row_of = [&](const RowView& v, int step) __attribute__((always_inline)) {
-      const int tok = tok0 + min(step % PASSES * RP + tr, n - 1);
+      const int tok = tok0 + min(tr, n - 1);
       return reinterpret_cast<const T*>(v.p) + (int64_t)layer * v.layer + (int64_t)tok * v.token +
-             (int64_t)(h0 + step / PASSES) * v.head;
+             (int64_t)(h0 + step) * v.head;
     };
     auto load = [&](int step) __attribute__((always_inline)) {
       const T *x = row_of(sd.x, step), *g = row_of(sd.gy, step);
@@ -96,6 +95,13 @@ __global__ void __launch_bounds__(256) norm_rope_grad_kernel(NormGradArgs args, 
       xb = ld16_any(x + hi);
       ga = ld16_any(g + lo);
       gb = ld16_any(g + hi);
+      // (beside the rows: a load asked for later is waited for with all before it)
+      if (sd.norm.w && (step == 0 || own_w)) {
+        const T* wt = reinterpret_cast<const T*>(sd.norm.w) + layer * sd.norm.layer +
+                      (int64_t)(h0 + step) * sd.norm.head;
+        wa = ld16_any(wt + lo);
+        wb = ld16_any(wt + hi);
+      }
     };
     load(0);
     __syncthreads();  // the chunk before has been read
@@ -105,17 +111,17 @@ __global__ void __launch_bounds__(256) norm_rope_grad_kernel(NormGradArgs args, 
       s_cs[j] = make_float2(cs * ra.m, sn * ra.m);
     }
     __syncthreads();
-    for (int step = 0; step < steps; ++step) {
-      const int tl = step % PASSES * RP + tr, head = h0 + step / PASSES;
-      const bool mine = tl < n;
-      float x[2 * VEC], g[2 * VEC];
+    for (int step = 0; step < nh; ++step) {  // a head
+      float x[2 * VEC], g[2 * VEC], f[2 * VEC];
       Store<T>::unpack(xa, x);
       Store<T>::unpack(xb, x + VEC);
       Store<T>::unpack(ga, g);
       Store<T>::unpack(gb, g + VEC);
-      if (step + 1 < steps) load(step + 1);
+      Store<T>::unpack(wa, f);
+      Store<T>::unpack(wb, f + VEC);
+      if (step + 1 < nh) load(step + 1);
       // dn = R^T g
-      const float2* cs = s_cs + min(tl, n - 1) * half + c * (PAIRS ? VEC / 2 : VEC);
+      const float2* cs = s_cs + min(tr, n - 1) * half + c * (PAIRS ? VEC / 2 : VEC);
       if constexpr (PAIRS) {
         constexpr int P = VEC / 2;
         if (turn_a) {
@@ -158,10 +164,6 @@ __global__ void __launch_bounds__(256) norm_rope_grad_kernel(NormGradArgs args, 
           }
         }
         if (sd.norm.w) {
-          const T* w = reinterpret_cast<const T*>(sd.norm.w) + layer * sd.norm.layer + head * sd.norm.head;
-          float f[2 * VEC];
-          Store<T>::unpack(ld16_any(w + lo), f);
-          Store<T>::unpack(ld16_any(w + hi), f + VEC);
 #pragma unroll
           for (int e = 0; e < 2 * VEC; ++e) g[e] *= sd.norm.offset + f[e];
         }
@@ -177,19 +179,16 @@ __global__ void __launch_bounds__(256) norm_rope_grad_kernel(NormGradArgs args, 
         st16_any(p + lo, Store<T>::pack(g));
         st16_any(p + hi, Store<T>::pack(g + VEC));
       }
-      if (has_dw && own_w && (step + 1) % PASSES == 0) join(s_dw + (head - h0) * D, true);
+      if (has_dw && own_w) join(s_dw[w] + step * D);
     }
   }
   if (!has_dw) return;
   float* part = args.part + sd.part0;
-  if (!own_w) {
-    join(part + ((int64_t)layer * sd.parts + b) * D, false);
-  } else {
-    __syncthreads();
-    for (int j = t; j < nh * D; j += 256) {
-      const int64_t group = (int64_t)layer * sd.w_heads + h0 + j / D;
-      part[(group * sd.parts + tc) * D + j % D] = s_dw[j];
-    }
+  if (!own_w) join(s_dw[w]);
+  __syncthreads();
+  for (int j = t; j < (own_w ? nh : 1) * D; j += 256) {
+    const int64_t group = (int64_t)layer * sd.w_heads + (own_w ? h0 + j / D : 0);
+    part[(group * sd.parts + (own_w ? tc : b)) * D + j % D] = (s_dw[0][j] + s_dw[1][j]) + (s_dw[2][j] + s_dw[3][j]);
   }
 }
 

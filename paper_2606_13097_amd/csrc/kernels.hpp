@@ -366,10 +366,10 @@ int launch_append_norm(int dtype, bool pairs, const RopeRows& rows, const Append
 
 // The gradient of norm and turn.  A side is the queries or the keys; its blocks take
 // head_blocks ranges of `heads_per` heads, `spread` of them beside each other every
-// `spread`-th chunk of norm_tokens(D) tokens.  Weight gradients: a partial [D] for each
+// `spread`-th chunk of norm_tokens tokens.  Weight gradients: a partial [D] for each
 // (layer, weight head, partial of `parts`), summed by a second launch.
 constexpr int kNormHeads = 8;
-constexpr int norm_tokens(int D) { return D == 64 ? 64 : 32; }
+constexpr int norm_tokens(int D, size_t esize) { return 8192 / (D * (int)esize); }  // a row for each D / (32 / esize) lanes of 256
 struct NormSide {
   RowView x, gy, dx;
   NormView norm;
