@@ -4,9 +4,10 @@
 //
 // Selection (evict_select_kernel, one block for each item, kv head and layer): the
 // weights as ordered 32-bit keys (the ends that always stay above all others), the
-// threshold found 11, 11 and 10 bits at a time by histograms in LDS, then the positions
+// threshold found 8 to 11 bits at a time by histograms in LDS, then the positions
 // above it, and as many equal to it as are left, lowest first, written in order by counts
-// over waves.  A row of up to 16K positions stays in registers over all of it.  More blocks of the
+// over waves.  A row of up to 16K positions stays in registers over all of it (block sizes:
+// see the launch).  More blocks of the
 // launch fill the table of turns: (cos, sin) of every distance, so that the rows that move
 // the same distance, in whatever layer and head, share them (one sincos for each row and
 // pair took as long as the memory).
@@ -22,8 +23,7 @@ namespace fcg {
 
 namespace {
 
-constexpr int kSelThreads = 1024, kSelKeys = 16;  // keys of a thread in registers
-constexpr int kSelSeg = kSelThreads * kSelKeys, kSelWaves = kSelThreads / 64, kBins = 2048;
+constexpr int kSelKeys = 16;  // keys of a thread in registers
 
 // order of a weight: larger ones above, -0 as 0, NaN below everything
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -62,8 +62,13 @@ __device__ __forceinline__ int32_t* kept_row(const EvictCall& ec, int item, int 
 
 }  // namespace
 
+// BITS of the keys a pass
+template <int kSelThreads, int BITS>
 __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(EvictCall ec, EvictArgs a, RopeArgs ra, int n_rows,
                                                                    int n_seqs, int Hkv, int max_tokens, int n_turn) {
+  constexpr int kSelSeg = kSelThreads * kSelKeys, kSelWaves = kSelThreads / 64, kBins = 1 << BITS;
+  constexpr int PASSES = (32 + BITS - 1) / BITS, PER = kBins / kSelThreads;  // bins of a thread
+  static_assert(PER >= 1 && PER <= 2, "one or two bins a thread");
   __shared__ int s_hist[kBins];
   __shared__ __align__(16) int s_wave[kSelWaves];
   __shared__ int s_gt[kSelKeys * kSelWaves], s_eq[kSelKeys * kSelWaves];
@@ -111,8 +116,8 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(EvictCall ec,
   int equal = keep;
   if (n_seg) load(0);
   if (n_seg && keep < n) {
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+    for (int pass = 0; pass < PASSES; ++pass) {
+      const int hi = 32 - pass * BITS, shift = max(hi - BITS, 0), bits = hi - shift;
       for (int j = t; j < kBins; j += kSelThreads) s_hist[j] = 0;
       __syncthreads();
       for (int seg = 0; seg < n_seg; ++seg) {
@@ -126,8 +131,8 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(EvictCall ec,
         }
       }
       __syncthreads();
-      // bins from the highest down, two a thread: the one in which the count passes `equal`
-      const int b1 = kBins - 1 - 2 * t, h1 = s_hist[b1], h0 = s_hist[b1 - 1];
+      // bins from the highest down, one or two a thread: the one in which the count passes `equal`
+      const int b1 = kBins - 1 - PER * t, h1 = s_hist[b1], h0 = PER == 2 ? s_hist[b1 - 1] : 0;
       const int up = scan_wave(h1 + h0);
       if (lane == 63) s_wave[w] = up;
       __syncthreads();
@@ -375,11 +380,24 @@ int check(hipError_t e) { return e == hipSuccess ? 0 : (int)e; }
 int launch_evict_select(const EvictCall& ec, const EvictArgs& args, const RopeArgs& ra, int n_layers, int n_seqs, int Hkv,
                         int max_tokens, int n_turn, hipStream_t s) {
   const int n_rows = args.n * Hkv * n_layers;
+  int longest = 0;
+  for (int i = 0; i < args.n; ++i) longest = args.item[i].len > longest ? args.item[i].len : longest;
+  // The smallest block that holds the longest row in its registers, of 256 threads for short
+  // rows only (us a call with blocks of 256, 512 and 1024 threads: 14 sequences of up to 317
+  // positions, 28 layers of 4 kv heads, 25, 32, 62; 4 of 1000, 16 layers of 8, 35, 35, 44; 1
+  // of 2000, 32 layers, 25.3, 24.5, 26.3; 8 of 4000, 16 layers, 73, 74, 92; 1 of 8000, 32 layers,
+  // 65, 33.0, 33.4; 1 of 15000, 104, 67, 41).
+  const int threads = longest <= 1024 ? 256 : longest <= 512 * kSelKeys ? 512 : 1024;
   const int64_t entries = (int64_t)n_turn * (ra.rot / 2);
-  const int64_t want = (entries + kSelThreads - 1) / kSelThreads;
-  const int n_tab = (int)(want < 1024 ? want : 1024);
-  hipLaunchKernelGGL(evict_select_kernel, dim3(n_rows + n_tab), dim3(kSelThreads), 0, s, ec, args, ra, n_rows, n_seqs, Hkv,
-                     max_tokens, n_turn);
+  const int64_t want = (entries + threads - 1) / threads;
+  const int n_tab = (int)(want < 4096 ? want : 4096);
+#define SEL(TH, BITS)                                                                                              \
+  hipLaunchKernelGGL((evict_select_kernel<TH, BITS>), dim3(n_rows + n_tab), dim3(TH), 0, s, ec, args, ra, n_rows, n_seqs, \
+                     Hkv, max_tokens, n_turn)
+  if (threads == 256) SEL(256, 8);
+  else if (threads == 512) SEL(512, 9);
+  else SEL(1024, 11);
+#undef SEL
   return check(hipGetLastError());
 }
 

@@ -14,7 +14,7 @@
 //
 // The most likely tokens: order is (value, then lower index), as one 64-bit key.  A block
 // holds a chunk of its row in registers (4 vectors a thread); a lower bound on the k-th
-// largest key is the k-th largest of the maxima of 64 groups of 4 threads (later chunks:
+// largest key is the k-th largest of the maxima of 64 or 128 groups of threads (later chunks:
 // the k-th found so far), and the few elements at or above it go to a list in LDS, of which
 // k are kept by counting.  If too many pass (a row of equal logits), the bound is taken
 // anew from the threads' own largest keys: at most (k - 1) 32 + 1 elements reach that.
@@ -160,7 +160,6 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
   __shared__ float s_max[kWaves];
   __shared__ uint64_t s_list[TOP ? kListCap : 1], s_top[TOP ? kLogpTop : 1], s_bound;
   __shared__ uint64_t s_own[TOP ? kThreads : 1];
-  __shared__ uint64_t s_grp[64];
   __shared__ int s_n;
 
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
@@ -247,16 +246,19 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
 
     if constexpr (TOP) {
       const int at = e0 + ch * CHUNK;
-      if (have < k) {  // a bound from the groups' maxima
+      if (have < k) {  // a bound from the groups' maxima: of 4 threads, of 2 where 64 groups leave too low a one
+        const bool fine = k > 32;
+        const int groups = fine ? kThreads / 2 : kThreads / 4;
         float gm = fmaxf(tmax, dpp_f32<kDppXor1>(tmax));
-        gm = fmaxf(gm, dpp_f32<kDppXor2>(gm));
-        if (t % 4 == 0) s_grp[t / 4] = key_of(gm, t / 4);
+        if (!fine) gm = fmaxf(gm, dpp_f32<kDppXor2>(gm));
+        const int gi = fine ? t / 2 : t / 4;
+        if (gi * (kThreads / groups) == t) s_own[gi] = key_of(gm, gi);
         __syncthreads();
-        if (w == 0) {
-          const uint64_t mine = s_grp[lane];
+        if (t < groups) {
+          const uint64_t mine = s_own[t];
           int above = 0;
 #pragma unroll 16
-          for (int j = 0; j < 64; ++j) above += s_grp[j] > mine;
+          for (int j = 0; j < groups; ++j) above += s_own[j] > mine;
           // (below -inf there is NaN, which the maxima passed over)
           if (above == k - 1) s_bound = mine >> 32 > kLowest ? mine >> 32 << 32 : 0;
         }

@@ -166,6 +166,21 @@ def test_rows_longer_than_the_registers_hold(dst):
     c.close()
 
 
+@pytest.mark.parametrize("n", [1024, 1025, 4096, 8192, 8193, 16384, 16385])
+@pytest.mark.parametrize("dst", [0, 1])
+def test_rows_at_the_sizes_of_the_blocks(n, dst):
+    """The longest rows that a block of each size holds, and one position more; weights that share their upper bits."""
+    c, mem, rows = make("f32", 2, 64, 0, [n], L=1, spare=1, extra=3)
+    w = 1.0 + weights_of(c, 1, n) * 2.0 ** -12
+    w0 = w.clone()
+    keep = n // 3
+    kept = torch.full((1, 1, 2, keep), -7, dtype=torch.int32, device="cuda")
+    fcg.fcg_evict(c, [0], [dst], [keep], w, first=1, recent=5, kept=kept)
+    torch.cuda.synchronize()
+    check(c, mem, rows, w0, w, kept, [0], [dst], [keep], 1, 5, freqs64(64, 1e4), False, "f32", [n])
+    c.close()
+
+
 def test_more_items_than_a_launch_takes_and_no_list_of_positions():
     lens = [50 + 3 * i for i in range(150)]
     c, mem, rows = make("bf16", 2, 64, 16, lens, L=1)
