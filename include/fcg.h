@@ -542,7 +542,7 @@ fcg_status fcg_attend_weights(fcg_cache* cache, int32_t layer, int32_t prefix_se
  * max_tokens]), ESTATE (layers of a src that differ in length; in place with
  * values read from the library, FCG_ALIAS_V; a capture that would map pages or
  * needs a larger workspace), EHOLE (an unwritten position below the length), ENOMEM
- * (pages), EHIP (other dst are left empty). */
+ * (pages), ENOMEM of host memory and EHIP (other dst may be left empty). */
 fcg_status fcg_evict(fcg_cache* cache, int32_t n_items, const int32_t* src, const int32_t* dst, const int32_t* keep,
                      int32_t n_first, int32_t n_recent, const fcg_rope* rope, float* weights, int32_t* kept,
                      void* stream);
@@ -616,7 +616,8 @@ fcg_status fcg_locality_set_ppl(fcg_locality* loc, int32_t func, double ppl);
  * function, as fcg_token_logprobs gives them (every token with a target); PPL = exp(-their mean),
  * summed in 64 bits.  Waits for the stream.  On an error no perplexity changes.
  * Errors: EINVAL (null arguments, a negative count, a function without tokens, a perplexity
- * that is not finite), ERANGE (a function), ENOMEM, EHIP. */
+ * that is not finite), ERANGE (a function), ESTATE (the stream is being captured), ENOMEM,
+ * EHIP. */
 fcg_status fcg_locality_measure_ppl(fcg_locality* loc, int32_t n, const int32_t* funcs, const int32_t* n_tok,
                                     const float* logprob, void* stream);
 /* scores[n_funcs] (host) receives l(f), each in [0, 1].  Errors: EINVAL. */

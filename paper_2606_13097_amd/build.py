@@ -38,10 +38,10 @@ COMMON = [
 LIBS = {
     os.path.join(PKG, "libfcg.so"): [
         os.path.join(CSRC, f) for f in
-        ("api.cpp", "ops.cpp", "norm.cpp", "keep.cpp", "logprob.cpp", "planner.cpp", "locality.cpp", "k_graft.hip", "k_append.hip", "k_rope.hip",
-         "k_norm_rope.hip", "k_prefix.hip", "k_weights.hip", "k_evict.hip", "k_logprob.hip",
-         "k_attn_rows.hip", "k_attn_mfma.hip", "k_decode.hip",
-         "k_decode_mfma.hip", "noalloc.hip")
+        ("api.cpp", "ops.cpp", "norm.cpp", "keep.cpp", "logprob.cpp", "planner.cpp", "locality.cpp",
+         "k_graft.hip", "k_append.hip", "k_rope.hip", "k_norm_rope.hip", "k_prefix.hip",
+         "k_weights.hip", "k_evict.hip", "k_logprob.hip", "k_attn_rows.hip", "k_attn_mfma.hip",
+         "k_decode.hip", "k_decode_mfma.hip", "noalloc.hip")
     ],
     os.path.join(PKG, "synth", "libfcg_synth.so"): [os.path.join(PKG, "synth", "synth.hip")],
     os.path.join(PKG, "measure", "libfcg_measure.so"): [os.path.join(PKG, "measure", "peak.hip")],

@@ -7,15 +7,22 @@
 // threshold found 8 to 11 bits at a time by histograms in LDS, then the positions
 // above it, and as many equal to it as are left, lowest first, written in order by counts
 // over waves.  A row of up to 16K positions stays in registers over all of it (block sizes:
-// see the launch).  More blocks of the
-// launch fill the table of turns: (cos, sin) of every distance, so that the rows that move
-// the same distance, in whatever layer and head, share them (one sincos for each row and
-// pair took as long as the memory).
+// see the launch).  Bound by its chain of passes, not by the weights it reads (256 rows of 4321:
+// 12 us, 0.4 TB/s).  More blocks of the launch fill the table of turns: (cos, sin) of every
+// distance, so that the rows that move the same distance, in whatever layer and head, share
+// them (one sincos for each row and pair took as long as the memory).
 //
 // Moving: into another sequence, 64 rows of a layer and head a block, keys and values
-// together, every load before the first store.  In place a row only moves down, so a later row never
-// reads what an earlier one wrote; a block takes a layer's and head's keys or values in
-// order, 128 rows a step, and stores a step's rows once all its waves have read theirs.
+// together, every load before the first store.  Bound by the memory: 1111 of 4321 bf16 rows
+// of 32 layers and 8 heads 60 us, 5 TB/s; 16 sequences of 4 layers, half of their rows or so,
+// 142 us.  The rows go past the caches: the calls took 81 us and 187 us through them, 78 and
+// 180 with the stores past them, 76.5 and 173.5 with the loads too.  (Data asked for before the
+// turns, and five blocks a compute unit by register count: no difference.  Turns computed by
+// the copy for calls of few rows: 5.5 us against 3.9, for one launch's table less.)
+//
+// In place a row only moves down, so a later row never reads what an earlier one wrote; a
+// block takes a layer's and head's keys or values in order, 128 rows a step, and stores a
+// step's rows once all its waves have read theirs.
 #include "fcg_device.hpp"
 #include "kernels.hpp"
 

@@ -25,6 +25,8 @@ struct WeightPlan {
 // for four times the blocks that are resident at once, else of 128.  The rows of a block
 // of keys are cut into splits where that makes twice the resident blocks of like work, of
 // 4 tiles of 64 rows at least: a split costs a partial, and a call with any a second launch.
+// (us a call: 32 sequences of 64 tokens past a prefix of 6007, 256 keys 139, 128 keys 152; one
+// token each of 64 sequences, prefix 4321, 128 keys 12.0, 256 keys 13.9.)
 void plan_weights(const fcg_model_desc& d, int32_t prefix_seq, int32_t P, int32_t n, const int32_t* seq,
                   const int32_t* pos, WeightPlan* p) {
   constexpr int64_t kResident = 512;
@@ -177,7 +179,9 @@ fcg_status fcg_evict(fcg_cache* c, int32_t n_items, const int32_t* src, const in
   const fcg_model_desc& d = c->desc;
   if (rope && rope->rot > d.head_dim) return fail(FCG_EINVAL, "rotary_dim exceeds head_dim");
   if (n_items > 0 && !c->layout_only() && !weights) return fail(FCG_EINVAL, "null weights");
-  if ((int64_t)d.n_kv_heads * 2 > kGridY || d.n_layers > kGridY) return fail(FCG_EINVAL, "too many layers or kv heads");
+  // (a selection block for each layer and kv head of an item, of at most 1024 threads)
+  if ((int64_t)d.n_kv_heads * 2 > kGridY || (int64_t)d.n_kv_heads * d.n_layers > 1 << 20)
+    return fail(FCG_EINVAL, "too many layers or kv heads");
   return guarded([&]() -> fcg_status {
     std::string msg;
     std::vector<int32_t> len;
@@ -227,8 +231,8 @@ fcg_status fcg_evict(fcg_cache* c, int32_t n_items, const int32_t* src, const in
     ec.n_items = n_items;
     ec.first = n_first;
     ec.recent = n_recent;
-    // Everything that can fail for want of memory comes before the targets are emptied:
-    // the page rows are staged with room for the new entries, which are filled in after.
+    // What takes much memory comes before the targets are emptied: the page rows are staged
+    // with room for the new entries, which are filled in after.
     Blob blob;
     std::vector<std::pair<int32_t, size_t>> rows;
     if (!new_pages.empty()) {
@@ -248,8 +252,15 @@ fcg_status fcg_evict(fcg_cache* c, int32_t n_items, const int32_t* src, const in
         std::memcpy(blob.bytes.data() + r.second + bytes, c->plan.alias_row(r.first), bytes);
       }
       char* at = nullptr;
-      if (fcg_status st = upload(c, blob, rows, s, &at, nullptr)) return undo(st);
-      if (fcg_status st = c->ring.retire(s)) return undo(st);
+      fcg_status st;
+      try {
+        st = upload(c, blob, rows, s, &at, nullptr);
+        if (!st) st = c->ring.retire(s);
+      } catch (...) {  // (the list of staged regions grows)
+        empty_targets();
+        throw;
+      }
+      if (st) return undo(st);
     }
     // launches of up to kEvictItems items, those into other sequences and those in place
     bool table = rope != nullptr;

@@ -41,7 +41,6 @@ class Planner {
   int32_t max_tokens() const { return T_; }
   int32_t page_size() const { return P_; }
   int32_t n_pages() const { return NP_; }
-  int32_t free_pages() const { return n_free_; }
   int32_t n_logical_pages() const { return NLP_; }
   bool alias_v() const { return AV_; }
 

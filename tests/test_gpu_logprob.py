@@ -374,3 +374,21 @@ def test_perplexities_reach_the_locality_score():
     with pytest.raises(fcg.FcgError):
         fcg.fcg_locality_measure_ppl(loc, [0, 1], [2, 2], lp)
     assert np.array_equal(before, fcg.fcg_locality_scores(loc))
+
+
+def test_perplexities_are_not_measured_while_capturing():
+    loc = fcg.Locality(2)
+    lp, x = torch.zeros(2, device="cuda"), torch.zeros(1, device="cuda")
+    status, graph = fcg.FCG_OK, torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        try:
+            fcg.fcg_locality_measure_ppl(loc, [0], [2], lp)
+        except fcg.FcgError as e:
+            status = e.status
+        x += 1.0
+    assert status == fcg.FCG_ESTATE
+    for n in range(1, 4):                    # the capture went on
+        graph.replay()
+        torch.cuda.synchronize()
+        assert float(x) == n
+    fcg.fcg_locality_measure_ppl(loc, [0], [2], lp)
