@@ -231,12 +231,16 @@ fcg_status fcg_evict(fcg_cache* c, int32_t n_items, const int32_t* src, const in
     ec.n_items = n_items;
     ec.first = n_first;
     ec.recent = n_recent;
-    // What takes much memory comes before the targets are emptied: the page rows are staged
-    // with room for the new entries, which are filled in after.
+    // What takes much memory comes before the targets are emptied: room for their page rows,
+    // which are filled in once the pages are mapped.
     Blob blob;
     std::vector<std::pair<int32_t, size_t>> rows;
-    if (!new_pages.empty()) {
-      stage_pages(c, new_pages, &blob, &rows);
+    const size_t row_bytes = 2 * sizeof(int32_t) * c->plan.n_logical_pages();
+    for (const auto& page : new_pages)  // (in order of the targets)
+      if (rows.empty() || rows.back().first != page.first)
+        rows.push_back({page.first, rows.size() * ((row_bytes + 255) & ~size_t(255))});
+    if (!rows.empty()) {
+      blob.bytes.resize(rows.back().second + row_bytes);
       if (fcg_status st = c->ring.reserve(blob.bytes.size() + 512)) return st;
     }
     empty_targets();
@@ -246,10 +250,9 @@ fcg_status fcg_evict(fcg_cache* c, int32_t n_items, const int32_t* src, const in
       return st;
     };
     if (!rows.empty()) {
-      const size_t bytes = sizeof(int32_t) * c->plan.n_logical_pages();
       for (const auto& r : rows) {
-        std::memcpy(blob.bytes.data() + r.second, c->plan.page_row(r.first), bytes);
-        std::memcpy(blob.bytes.data() + r.second + bytes, c->plan.alias_row(r.first), bytes);
+        std::memcpy(blob.bytes.data() + r.second, c->plan.page_row(r.first), row_bytes / 2);
+        std::memcpy(blob.bytes.data() + r.second + row_bytes / 2, c->plan.alias_row(r.first), row_bytes / 2);
       }
       char* at = nullptr;
       fcg_status st;
