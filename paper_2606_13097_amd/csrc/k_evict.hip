@@ -7,8 +7,9 @@
 // threshold found 8 to 11 bits at a time by histograms in LDS, then the positions
 // above it, and as many equal to it as are left, lowest first, written in order by counts
 // over waves.  A row of up to 16K positions stays in registers over all of it (block sizes:
-// see the launch).  Bound by its chain of passes, not by the weights it reads (256 rows of 4321:
-// 12 us, 0.4 TB/s).  More blocks of the launch fill the table of turns: (cos, sin) of every
+// see the launch); a longer one is read anew in each pass (56 rows of up to 20K: 38 us).  Bound by
+// its chain of passes, not by the weights it reads (256 rows of 4321: 12 us, 0.4 TB/s; eight
+// copies of each bin, so that adds meet less often: no difference).  More blocks of the launch fill the table of turns: (cos, sin) of every
 // distance, so that the rows that move the same distance, in whatever layer and head, share
 // them (one sincos for each row and pair took as long as the memory).
 //
