@@ -538,8 +538,8 @@ fcg_status fcg_attend_weights(fcg_cache* cache, int32_t layer, int32_t prefix_se
  * a call that maps no page can be captured, and replays move from the same
  * positions to the same ones.
  * Errors: EINVAL (null arrays, negative counts, rotary_dim above the head, a dst
- * given twice or also the src of another item), ERANGE (sequences, keep outside [0,
- * max_tokens]), ESTATE (layers of a src that differ in length; in place with
+ * given twice or also the src of another item, more than 32767 kv heads or 2^20
+ * over all layers), ERANGE (sequences, keep outside [0, max_tokens]), ESTATE (layers of a src that differ in length; in place with
  * values read from the library, FCG_ALIAS_V; a capture that would map pages or
  * needs a larger workspace), EHOLE (an unwritten position below the length), ENOMEM
  * (pages), ENOMEM of host memory and EHIP (other dst may be left empty). */

@@ -137,3 +137,15 @@ def test_evict_in_place_refuses_values_in_the_library():
     fcg.fcg_graft(c, lib, [1], [0], [16])
     evict(c, dst=[1], keep=[10])                                         # emptied: its values leave the library
     assert fcg.fcg_cache_export_v_alias(c, 1).tolist() == [-1] * 4
+
+
+@pytest.mark.parametrize("layers,heads,status", [(255, 4096, 0), (255, 8192, E.FCG_EINVAL), (1, 32768, E.FCG_EINVAL)])
+def test_evict_refuses_more_heads_than_a_launch_takes(layers, heads, status):
+    c = fcg.Cache(fcg.model_desc(layers, heads, heads, 64, 1e4, "bf16"), 1, 8, flags=fcg.FCG_LAYOUT_ONLY)
+    fcg.fcg_append(c, 0, [0] * 3, [0, 1, 2], n_layers=layers)
+    if status:
+        refuses(status, fcg.fcg_evict, c, [0], [0], [2], None)
+        assert fcg.fcg_cache_export_layout(c, 0, 0)[1] == 3
+    else:
+        fcg.fcg_evict(c, [0], [0], [2], None)
+        assert fcg.fcg_cache_export_layout(c, 0, layers - 1)[1] == 2
