@@ -539,10 +539,11 @@ fcg_status fcg_attend_weights(fcg_cache* cache, int32_t layer, int32_t prefix_se
  * positions to the same ones.
  * Errors: EINVAL (null arrays, negative counts, rotary_dim above the head, a dst
  * given twice or also the src of another item, more than 32767 kv heads or 2^20
- * over all layers), ERANGE (sequences, keep outside [0, max_tokens]), ESTATE (layers of a src that differ in length; in place with
- * values read from the library, FCG_ALIAS_V; a capture that would map pages or
- * needs a larger workspace), EHOLE (an unwritten position below the length), ENOMEM
- * (pages), ENOMEM of host memory and EHIP (other dst may be left empty). */
+ * over all layers), ERANGE (sequences, keep outside [0, max_tokens]), ESTATE
+ * (layers of a src that differ in length; in place with values read from the
+ * library, FCG_ALIAS_V; a capture that would map pages or needs a larger
+ * workspace), EHOLE (an unwritten position below the length), ENOMEM (pages),
+ * ENOMEM of host memory and EHIP (other dst may be left empty). */
 fcg_status fcg_evict(fcg_cache* cache, int32_t n_items, const int32_t* src, const int32_t* dst, const int32_t* keep,
                      int32_t n_first, int32_t n_recent, const fcg_rope* rope, float* weights, int32_t* kept,
                      void* stream);

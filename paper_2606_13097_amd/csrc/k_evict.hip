@@ -9,9 +9,10 @@
 // over waves.  A row of up to 16K positions stays in registers over all of it (block sizes:
 // see the launch); a longer one is read anew in each pass (56 rows of up to 20K: 38 us).  Bound by
 // its chain of passes, not by the weights it reads (256 rows of 4321: 12 us, 0.4 TB/s; eight
-// copies of each bin, so that adds meet less often: no difference).  More blocks of the launch fill the table of turns: (cos, sin) of every
-// distance, so that the rows that move the same distance, in whatever layer and head, share
-// them (one sincos for each row and pair took as long as the memory).
+// copies of each bin, so that adds meet less often: no difference).  More blocks of the launch
+// fill the table of turns: (cos, sin) of every distance, so that the rows that move the same
+// distance, in whatever layer and head, share them (one sincos for each row and pair took as
+// long as the memory).
 //
 // Moving: into another sequence, 64 rows of a layer and head a block, keys and values
 // together, every load before the first store.  Bound by the memory: 1111 of 4321 bf16 rows
