@@ -27,9 +27,9 @@ struct WeightPlan {
 // 4 tiles of 64 rows at least: a split costs a partial, and a call with any a second launch.
 // (us a call: 32 sequences of 64 tokens past a prefix of 6007, 256 keys 139, 128 keys 152; one
 // token each of 64 sequences, prefix 4321, 128 keys 12.0, 256 keys 13.9.)
+constexpr int64_t kResident = 512;
 void plan_weights(const fcg_model_desc& d, int32_t prefix_seq, int32_t P, int32_t n, const int32_t* seq,
                   const int32_t* pos, WeightPlan* p) {
-  constexpr int64_t kResident = 512;
   const int g = d.n_q_heads / d.n_kv_heads;
   std::vector<int32_t> order(n);
   for (int32_t t = 0; t < n; ++t) order[t] = t;
@@ -161,10 +161,17 @@ fcg_status fcg_attend_weights(fcg_cache* c, int32_t layer, int32_t prefix_seq, i
       items = (const WeightItem*)(dplan + o_items);
       ranks = (const WeightRank*)(dplan + o_ranks);
     }
-    for (int i0 = 0; i0 < p.n_items; i0 += kGridY)
+    for (int i0 = 0; i0 < p.n_items;) {
+      int i1 = std::min(kGridY, p.n_items - i0) + i0;
+      // each launch adds up the splits of its blocks of keys: it ends between two blocks
+      // (which have at most 2 kResident splits; a plan by value is one launch)
+      if (i1 < p.n_items)
+        while (p.items[i1].split) --i1;
       if (int rc = launch_attend_weights(d.dtype, wc, p.by_value ? &p.args : nullptr, items ? items + i0 : nullptr, ranks,
-                                         std::min(kGridY, p.n_items - i0), p.block, c->view(), s))
+                                         i1 - i0, p.block, c->view(), s))
         return hip_fail((hipError_t)rc, "attention weights launch");
+      i0 = i1;
+    }
     return p.by_value ? FCG_OK : c->ring.retire(s);
   });
 }

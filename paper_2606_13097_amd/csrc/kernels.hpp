@@ -470,7 +470,7 @@ struct WeightArgs {
 // Keys of a block at most: 512-byte rows of 256 would not fit the registers.
 constexpr int weights_most_keys(size_t esize, int D) { return esize * D > 256 ? 128 : 256; }
 // args null: the plan in device memory (items, ranks); else by value.  block: 128 or
-// weights_most_keys; n_items < 65536.
+// weights_most_keys; n_items < 65536, of every block of keys all splits (they are added up).
 int launch_attend_weights(int dtype, const WeightCall& call, const WeightArgs* args, const WeightItem* items,
                           const WeightRank* ranks, int n_items, int block, const CacheView& cv, hipStream_t s);
 

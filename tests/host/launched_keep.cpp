@@ -1,0 +1,74 @@
+// What sums of attention weight launch, on a machine without a GPU: see the checks of each.
+#include "keep_runtime.hpp"
+
+#include <numeric>
+#include <set>
+
+namespace {
+
+int failures = 0;
+#define CHECK(cond, ...)                                   \
+  do {                                                     \
+    if (!(cond)) {                                         \
+      std::printf("FAILED %s:%d: ", __FILE__, __LINE__);   \
+      std::printf(__VA_ARGS__);                            \
+      std::printf(" (%s)\n", #cond);                       \
+      ++failures;                                          \
+    }                                                      \
+  } while (0)
+
+fcg_cache* cache_of(int32_t dtype, int hq, int hkv, int d, int seqs, int tokens, int page, int pages) {
+  const fcg_model_desc m{1, hq, hkv, d, 1e4, dtype, 0};
+  fcg_cache* c = nullptr;
+  if (fcg_cache_create(&m, seqs, tokens, page, pages, 0, &c)) std::abort();
+  return c;
+}
+
+// Each launch adds up the splits of the blocks of keys whose first split is in it: all splits
+// of a block have to be in that launch, and every block is in one.
+void splits_meet_in_one_launch() {
+  struct {
+    int hq, tokens;  // tokens of the last sequence
+  } cases[] = {{16, 2000}, {1, 8192}, {16, 8192}, {2, 1}};
+  for (const auto& x : cases) {
+    const int singles = 65530, n = singles + x.tokens;
+    fcg_cache* c = cache_of(FCG_BF16, x.hq, 1, 64, singles + 1, 8192, 16, singles + 512);
+    std::vector<int32_t> seq(n, singles), pos(n, 0);
+    std::iota(seq.begin(), seq.begin() + singles, 0);
+    std::iota(pos.begin() + singles, pos.end(), 0);
+    CHECK(fcg_append(c, 0, 1, n, seq.data(), pos.data(), nullptr, nullptr, nullptr, nullptr, nullptr, 0, nullptr) == FCG_OK,
+          "%s", fcg_last_error());
+    std::vector<host::Weights> seen;
+    host::weights = &seen;
+    float y[4] = {};
+    const fcg_tensor q{y, 0, 0, 0};
+    CHECK(fcg_attend_weights(c, 0, -1, 0, n, seq.data(), pos.data(), &q, y, y, 0, nullptr) == FCG_OK, "%s", fcg_last_error());
+    host::weights = nullptr;
+    std::set<int> blocks;
+    int most = 0;
+    for (const auto& l : seen) {
+      CHECK(!l.by_value && l.n_items > 0 && l.n_items <= 65535, "a launch of %d items", l.n_items);
+      for (size_t i = 0; i < l.items.size() && failures < 20; ++i) {
+        const fcg::WeightItem& it = l.items[i];
+        most = std::max(most, it.n_split);
+        if (it.split == 0) CHECK(blocks.insert(it.kb).second, "block %d of keys twice", it.kb);
+        else CHECK(i && l.items[i - 1].kb == it.kb && l.items[i - 1].split == it.split - 1,
+                   "split %d of %d of block %d of keys does not follow the one before in its launch", it.split, it.n_split, it.kb);
+        if (i + 1 == l.items.size()) CHECK(it.split == it.n_split - 1, "a launch ends at split %d of %d", it.split, it.n_split);
+        if (it.n_split > 1) CHECK(l.call.part, "splits without a workspace");
+      }
+    }
+    CHECK((int)blocks.size() == singles + (x.tokens + seen[0].block - 1) / seen[0].block, "%zu blocks of keys", blocks.size());
+    std::printf("%d query heads, %d tokens: %zu launches, up to %d splits\n", x.hq, x.tokens, seen.size(), most);
+    fcg_cache_destroy(c);
+  }
+}
+
+}  // namespace
+
+int main() {
+  std::setvbuf(stdout, nullptr, _IOLBF, 0);
+  splits_meet_in_one_launch();
+  if (!failures) std::printf("ok\n");
+  return failures ? 1 : 0;
+}
