@@ -628,18 +628,34 @@ def fcg_prefix_attend(cache: Cache, layer: int, prefix_seq: int, prefix_len: int
 
 class Norm:
     """A norm of rows (``fcg_norm``): (offset + weight) x / sqrt(mean(x^2) + eps) over each head.  weight: [head_dim],
-    [heads][head_dim] or [layers][heads][head_dim] (a dimension of 1 is shared), or None for ones."""
+    [heads][head_dim] or [layers][heads][head_dim] (a dimension of 1 is shared), or None for ones.  A call takes the
+    weight's storage as it is then: a parameter may be moved or replaced between calls."""
 
     def __init__(self, weight=None, eps: float = 1e-6, offset: float = 0.0):
-        if weight is not None:
-            if weight.dim() not in (1, 2, 3) or (weight.numel() and weight.stride(-1) != 1):
-                raise ValueError("norm weight: one to three dimensions, the elements of a head adjacent")
         self.weight = weight
-        step = [0, 0]
-        if weight is not None:
-            for i, (n, st) in enumerate(zip(weight.shape[-2::-1], weight.stride()[-2::-1])):   # heads, then layers
-                step[i] = st if n > 1 else 0
-        self.desc = NormDesc(None if weight is None else weight.data_ptr(), step[1], step[0], float(eps), float(offset))
+        # one structure, brought up to date by each call (a new one is a visible part of a small step)
+        self._desc = NormDesc(None, 0, 0, float(eps), float(offset))
+        self._ref = C.byref(self._desc)
+        self._lay_out()
+
+    def _lay_out(self) -> None:
+        w, d = self.weight, self._desc
+        self._shape, self._strides = (None, None) if w is None else (w.shape, w.stride())
+        d.weight, d.layer, d.head = None, 0, 0
+        if w is not None:
+            sh, st = self._shape, self._strides
+            if not 1 <= len(sh) <= 3 or (st[-1] != 1 and w.numel()):
+                self._strides = None          # (looked at again in the next call)
+                raise ValueError("norm weight: one to three dimensions, the elements of a head adjacent")
+            d.weight = w.data_ptr()
+            d.layer = st[0] if len(sh) == 3 and sh[0] > 1 else 0
+            d.head = st[-2] if len(sh) > 1 and sh[-2] > 1 else 0
+
+    @property
+    def desc(self) -> NormDesc:
+        """The description of the present weight."""
+        self._lay_out()
+        return self._desc
 
     def dweight_shape(self, layers: int, heads: int) -> tuple:
         """Shape of the weights' gradient: [layers][heads or 1][head_dim]."""
@@ -650,15 +666,21 @@ def _norm_ref(norm: Optional[Norm], layers: int, heads: int, d: int, dtype, devi
     if norm is None:
         return None
     w = norm.weight
-    if w is not None:
-        if w.requires_grad and torch.is_grad_enabled():
-            raise ValueError(f"{what}: the weights require a gradient, which these calls do not record")
-        if w.dtype is not dtype or w.get_device() != device:
-            raise ValueError(f"{what}: weights of {w.dtype} on {w.device}, expected {dtype} on GPU {device}")
-        sh = w.shape
-        if sh[-1] != d or (len(sh) > 1 and sh[-2] not in (1, heads)) or (len(sh) > 2 and sh[0] not in (1, layers)):
-            raise ValueError(f"{what}: weights of shape {tuple(sh)} for {layers} layers of {heads} heads of {d}")
-    return C.byref(norm.desc)
+    if w is None:
+        if norm._shape is not None:
+            norm._lay_out()
+        return norm._ref
+    if w.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what}: the weights require a gradient, which these calls do not record")
+    if w.dtype is not dtype or w.get_device() != device:
+        raise ValueError(f"{what}: weights of {w.dtype} on {w.device}, expected {dtype} on GPU {device}")
+    sh = w.shape
+    if w.stride() != norm._strides or sh != norm._shape:
+        norm._lay_out()
+    norm._desc.weight = w.data_ptr()
+    if sh[-1] != d or (len(sh) > 1 and sh[-2] not in (1, heads)) or (len(sh) > 2 and sh[0] not in (1, layers)):
+        raise ValueError(f"{what}: weights of shape {tuple(sh)} for {layers} layers of {heads} heads of {d}")
+    return norm._ref
 
 
 def _rows_of(pos, q, k):
@@ -734,7 +756,7 @@ def _norm_side(x, norm, grad, dx, dw, shape, td, dev, what: str):
                 dw.numel() != want[0] * want[1] * want[2]):
             raise ValueError(f"{what}: weight gradient, a contiguous float32 GPU tensor {want}")
     empty = TensorView(None, 0, 0, 0)
-    return NormSide(shape[2], None if ref is None else C.pointer(norm.desc), _view(x, shape, td, dev, what) or empty,
+    return NormSide(shape[2], None if ref is None else C.pointer(norm._desc), _view(x, shape, td, dev, what) or empty,
                     _view(grad, shape, td, dev, what + "_grad"), _view(dx, shape, td, dev, "d" + what), _dptr(dw))
 
 

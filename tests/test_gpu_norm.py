@@ -288,3 +288,30 @@ def test_calls_larger_than_the_caches_equal_their_layers():
     for l in range(L):
         fcg.fcg_norm_rope_apply(rope, pos, q[l], fcg.Norm(nm.weight[l, 0]), one)
         assert torch.equal(bits(one), bits(qo[l]))
+
+
+def test_a_norm_built_before_its_module_moves():
+    """Weights made on the host, the norm with them, then moved to the GPU and replaced: each call takes the present ones."""
+    d, hq, n = 64, 4, 33
+    rope, w = make_rope(64, False)
+    x, pos = randn(gen(1), 1, n, hq, d), np.arange(n)
+    module = torch.nn.Module()
+    module.weight = torch.nn.Parameter(torch.ones(d, dtype=torch.bfloat16), requires_grad=False)
+    norm, y = fcg.Norm(module.weight), torch.empty_like(x)
+    with pytest.raises(ValueError):
+        fcg.fcg_norm_rope_apply(rope, dpos(pos), x, norm, y)
+    module.cuda()
+    for seed in (2, 3):
+        fcg.fcg_norm_rope_apply(rope, dpos(pos), x, norm, y)
+        torch.cuda.synchronize()
+        check_normed(y, x, weights64(module.weight.data, 0.0, 1, hq, d), 1e-6, pos, w, False, 1.0, "bf16", f"weights {seed}")
+        wide = randn(gen(seed), hq, 2 * d)
+        module.weight.data = wide[:, d:] if seed == 2 else wide[0, :d].clone()
+    fcg.fcg_norm_rope_apply(rope, dpos(pos), x, norm, y)
+    dx, dw = torch.empty_like(x), torch.empty(norm.dweight_shape(1, hq), device="cuda")
+    gy = randn(gen(5), 1, n, hq, d)
+    fcg.fcg_norm_rope_backward(rope, dpos(pos), x, norm, gy, dx, dw)
+    torch.cuda.synchronize()
+    w64 = weights64(module.weight.data, 0.0, 1, hq, d)
+    check_normed(y, x, w64, 1e-6, pos, w, False, 1.0, "bf16", "the last weights")
+    check_grad(dx, dw, x, w64, gy, 1e-6, pos, w, False, 1.0, "bf16", "the last weights")

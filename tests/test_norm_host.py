@@ -153,3 +153,22 @@ def test_gradient_formula_against_differences():
         e[i] = h
         e = e.view(w.shape)
         assert abs((loss(x, w + e) - loss(x, w - e)) / (2 * h) - float(dw.sum(1, keepdim=True).view(-1)[i])) < 1e-7
+
+
+def test_a_norm_goes_by_the_weights_of_the_call():
+    """A parameter's storage moves under it (Module.to, an optimiser's swap): address and strides are the present ones."""
+    w = torch.nn.Parameter(torch.zeros(4, 64), requires_grad=False)
+    norm = fcg.Norm(w, eps=1e-5, offset=1.0)
+    old = w.data                                  # keeps the first storage, so that no other takes its address
+    w.data = torch.ones(4, 128)[:, 64:]
+    assert norm.desc.weight == w.data_ptr() != old.data_ptr() and (norm.desc.layer, norm.desc.head) == (0, 128)
+    desc = fcg._norm_ref(norm, 1, 4, 64, torch.float32, w.get_device(), "q_norm")._obj
+    assert (desc.weight, desc.layer, desc.head, desc.eps, desc.offset) == (w.data_ptr(), 0, 128, 1e-5, 1.0)
+    x = torch.zeros(2, 4, 64)
+    side = fcg._norm_side(x, norm, x, x.clone(), None, (1, 2, 4, 64), torch.float32, w.get_device(), "q")
+    assert (side.norm.contents.weight, side.norm.contents.head) == (w.data_ptr(), 128)
+    w.data = torch.ones(4, 64)[:1]
+    assert norm.desc.head == 0 and norm.dweight_shape(2, 4) == (2, 1, 64)
+    w.data = torch.zeros(64, 4).T
+    with pytest.raises(ValueError):               # elements of a head that are no longer adjacent
+        fcg._norm_ref(norm, 1, 4, 64, torch.float32, w.get_device(), "q_norm")
