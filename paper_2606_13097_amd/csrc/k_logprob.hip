@@ -3,14 +3,15 @@
 //
 //   lse = ln sum e^x,  logprob_t = x_t - lse,  H = -sum p ln p,  p = e^(x - lse).
 //
-// One pass over a row: with a reference r near the row's maximum, in base 2 (c = log2 e),
-//   S = sum 2^(c x - c r),  U = sum 2^(c x - c r) (c x - c r),
-//   lse = r + ln S,  H = ln 2 (log2 S - U / S).
-// A thread keeps its reference until an element is more than 2^40 above it, so nothing is
-// rescaled in nearly all steps; products with c r round once, and what that leaves (eta)
-// is taken out of S and U at the end, so large logits cost no digits.  Past 10^6 that
-// no longer holds (a row of nothing but the type's lowest value, say): parts of a row with such a
-// maximum are read once more with x - r formed first.
+// One pass over a row: with a reference r near the row's maximum,
+//   S = sum e^(x - r),  U = sum e^(x - r) (x - r),  lse = r + ln S,  H = ln S - U / S.
+// x - r is formed first, so large logits cost no digits.  A thread keeps its reference until
+// an element's e^(x - r) passes 8, so few steps rescale, and yet a token that has nearly all of
+// the probability is the reference itself: its term is 1, S is at least 1 and U at most 0, so
+// that no log probability is above 0 and no entropy below.  (A reference that trails by d costs
+// ln S and U / S d units of 2^-24: a reference moved at 2^40 had entropies of such rows off
+// by 2e-6, of any sign.)  A vector's terms are added to each other before they meet the sum,
+// so that fewer and larger addends are rounded against a peak.
 //
 // The most likely tokens: order is (value, then lower index), as one 64-bit key.  A block
 // holds a chunk of its row in registers (4 vectors a thread); a lower bound on the k-th
@@ -21,7 +22,7 @@
 //
 // Few rows are cut into splits, whose partials a second launch joins.
 //
-// What bounds it: many rows the memory (3001 fp32 rows of 50021: 94 us, 6.4 TB/s; each logit is
+// What bounds it: many rows the memory (3001 fp32 rows of 50021: 95 us, 6.3 TB/s; each logit is
 // read once, with 8 vectors a thread in flight where no alternatives are kept); blocks of 256
 // threads, several to a compute unit, so that one's exponentials (8 cycles each) run beside
 // another's loads (141 us with blocks of 1024).  Few rows the chain of a row: load,
@@ -42,8 +43,9 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kListCap = kLogpTop + (kLogpTop - 1) * 32 + 1;  // keys kept, and those of one chunk
 constexpr float kC = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// Rows whose largest logit is past this take the second reading: c r is off by up to a tenth there.
-constexpr float kFar = 1e6f;
+constexpr float kMove = 3 * kLn2;  // a reference moves when an element is further above it
+constexpr float kLeast = -3.4028235e38f;  // the reference of nothing
+constexpr float kBound = -1e20f;  // a difference in a product: 0 times -inf is NaN
 
 __device__ __forceinline__ uint32_t order_of(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
@@ -63,8 +65,8 @@ struct Stat {
 };
 __device__ __forceinline__ Stat join(const Stat& a, const Stat& b) {
   const float r = fmaxf(a.r, b.r);
-  const float da = fmaxf((a.r - r) * kC, -1e30f), db = fmaxf((b.r - r) * kC, -1e30f);
-  const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+  const float da = fmaxf(a.r - r, kBound), db = fmaxf(b.r - r, kBound);
+  const float fa = __builtin_amdgcn_exp2f(da * kC), fb = __builtin_amdgcn_exp2f(db * kC);
   return Stat{r, fmaf(a.s, fa, b.s * fb), fmaf(fmaf(a.s, da, a.u), fa, fmaf(b.s, db, b.u) * fb)};
 }
 __device__ __forceinline__ float max_wave(float v) {
@@ -79,7 +81,7 @@ __device__ __forceinline__ float sum_wave(float v) {
 }
 // over the lanes of a wave: every lane's brought to the largest reference, then added
 __device__ __forceinline__ Stat join_wave(const Stat& a) {
-  const float r = max_wave(a.r), d = fmaxf((a.r - r) * kC, -1e30f), f = __builtin_amdgcn_exp2f(d);
+  const float r = max_wave(a.r), d = fmaxf(a.r - r, kBound), f = __builtin_amdgcn_exp2f(d * kC);
   return Stat{r, sum_wave(a.s * f), sum_wave(fmaf(a.s, d, a.u) * f)};
 }
 
@@ -95,7 +97,7 @@ struct Row {
   }
   __device__ __forceinline__ float logprob(float x) const { return empty ? -INFINITY : (x - r) - ln_s; }
   __device__ __forceinline__ float entropy(const Stat& a) const {
-    return empty ? 0.f : (log2f(a.s) - a.u / a.s) * kLn2;
+    return empty ? 0.f : ln_s - a.u / a.s;
   }
 };
 
@@ -168,7 +170,6 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
   constexpr int kVecs = TOP ? 4 : 8;  // vectors of a thread in a chunk
   constexpr int VEC = Store<T>::VEC, CHUNK = kThreads * kVecs * VEC;
   __shared__ Stat s_stat[kWaves];
-  __shared__ float s_max[kWaves];
   __shared__ uint64_t s_list[TOP ? kListCap : 1], s_top[TOP ? kLogpTop : 1], s_bound;
   __shared__ uint64_t s_own[TOP ? kThreads : 1];
   __shared__ int s_n;
@@ -203,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
       if (i + VEC > e1) v[j] = shifted<T>(v[j], min(i + VEC - e1, VEC));
     }
   };
-  float r = -kFar, rc = -kFar * kC, s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f, top = -INFINITY;
+  float r = kLeast, s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
   if (TOP && t == 0) {
     s_n = 0;
     s_bound = 0;
@@ -232,28 +233,27 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
       for (int e = 1; e < VEC; ++e) m = fmaxf(m, f[e]);
       vmax[j] = m;
       tmax = fmaxf(tmax, m);
-      if (m * kC > rc + 40.f) {
-#pragma clang fp contract(off)  // the difference is that of the rounded products
-        r = fminf(m, kFar);
-        const float to = r * kC, d = rc - to, g = __builtin_amdgcn_exp2f(d);
+      if (m > r + kMove) {
+        const float to = fminf(m, -kLeast), d = fmaxf(r - to, kBound), g = __builtin_amdgcn_exp2f(d * kC);
         u0 = fmaf(s0, d, u0) * g;
         u1 = fmaf(s1, d, u1) * g;
         s0 *= g;
         s1 *= g;
-        rc = to;
+        r = to;
+      }
+      float sum[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float d = f[e] - r, p = __builtin_amdgcn_exp2f(d * kC);
+        sum[e] = p;
+        (e & 1 ? u1 : u0) = fmaf(p, fmaxf(d, kBound), e & 1 ? u1 : u0);
       }
 #pragma unroll
-      for (int e = 0; e < VEC; e += 2) {
-        const float a = fmaf(f[e], kC, -rc), b = fmaf(f[e + 1], kC, -rc);
-        const float ea = __builtin_amdgcn_exp2f(a), eb = __builtin_amdgcn_exp2f(b);
-        s0 += ea;
-        s1 += eb;
-        u0 = fmaf(ea, fmaxf(a, -1e30f), u0);  // (0 times -inf is NaN)
-        u1 = fmaf(eb, fmaxf(b, -1e30f), u1);
-      }
+      for (int n = VEC / 2; n; n /= 2)
+#pragma unroll
+        for (int e = 0; e < n; ++e) sum[e] += sum[e + n];
+      (j & 1 ? s1 : s0) += sum[0];
     }
-
-    top = fmaxf(top, tmax);
 
     if constexpr (TOP) {
       const int at = e0 + ch * CHUNK;
@@ -336,31 +336,10 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_kernel(LogpArgs la) {
   fix(cur, n_chunk - 1);
   take(n_chunk - 1, std::true_type{});
 
-  // the block's statistics; eta is what the product c r lost
-  const float eta = fmaf(r, kC, -rc), back = __builtin_amdgcn_exp2f(-eta);
-  Stat st{r, (s0 + s1) * back, fmaf(-eta, s0 + s1, u0 + u1) * back};
-  st = join_wave(st);
-  top = max_wave(top);
-  if (lane == 0) {
-    s_stat[w] = st;
-    s_max[w] = top;
-  }
+  // the block's statistics
+  Stat st = join_wave(Stat{r, s0 + s1, u0 + u1});
+  if (lane == 0) s_stat[w] = st;
   __syncthreads();
-  top = s_max[0];
-#pragma unroll
-  for (int j = 1; j < kWaves; ++j) top = fmaxf(top, s_max[j]);
-  if (!(fabsf(top) < kFar)) {  // (block-uniform) far out, or nothing but -inf and NaN: once more, x - r first
-    __syncthreads();
-    st = Stat{fminf(fmaxf(top, -3.4028235e38f), 3.4028235e38f), 0.f, 0.f};
-    for (int i = e0 + t; i < e1; i += kThreads) {
-      const float a = (Store<T>::load1(x + i) - st.r) * kC, ea = __builtin_amdgcn_exp2f(a);
-      st.s += ea;
-      st.u = fmaf(ea, fmaxf(a, -1e30f), st.u);
-    }
-    st = join_wave(st);
-    if (lane == 0) s_stat[w] = st;
-    __syncthreads();
-  }
   st = s_stat[0];
 #pragma unroll
   for (int j = 1; j < kWaves; ++j) st = join(st, s_stat[j]);
@@ -384,7 +363,7 @@ __global__ void __launch_bounds__(256) logprob_merge_kernel(LogpArgs la) {
   static_assert(kLogpSplits <= 64, "a split a lane");
   const uint64_t* keys = la.part_top + (int64_t)row * n;
   Target<T> target(la, row);
-  Stat st{-3.4028235e38f, 0.f, 0.f};
+  Stat st{kLeast, 0.f, 0.f};
   if (lane < la.splits) {
     const float4 p = la.part[(int64_t)row * la.splits + lane];
     st = Stat{p.x, p.y, p.z};
