@@ -221,7 +221,9 @@ fcg_status fcg_append_norm(fcg_cache* c, int32_t layer, int32_t n_layers, int32_
                            uint32_t flags, void* stream) {
   if (fcg_status st = check_norm(q_norm, "q")) return st;
   if (fcg_status st = check_norm(k_norm, "k")) return st;
-  if ((q_norm && !(q && q->data)) || (k_norm && !(k && k->data))) return fail(FCG_EINVAL, "a norm without its rows");
+  const bool rows = n_layers > 0 && n_tok > 0;  // (tensors of none may have no address)
+  if (rows && ((q_norm && !(q && q->data)) || (k_norm && !(k && k->data))))
+    return fail(FCG_EINVAL, "a norm without its rows");
   const NormArgs<true> norm{::view_of(q_norm), ::view_of(k_norm)};
   auto launch = [](const void* context, int dtype, bool pairs, const RopeRows& rows, const AppendArgs& args, int n_runs,
                    const AppendGroup* groups, int n_groups, const CacheView& cv, int layer0, const RopeArgs& ra,

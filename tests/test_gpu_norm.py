@@ -315,3 +315,11 @@ def test_a_norm_built_before_its_module_moves():
     w64 = weights64(module.weight.data, 0.0, 1, hq, d)
     check_normed(y, x, w64, 1e-6, pos, w, False, 1.0, "bf16", "the last weights")
     check_grad(dx, dw, x, w64, gy, 1e-6, pos, w, False, 1.0, "bf16", "the last weights")
+
+
+def test_a_step_of_no_tokens():
+    c = fcg.Cache(fcg.model_desc(1, 4, 2, 64, 1e4, "bf16"), 1, 32, 16, 2)
+    q, kv = (torch.empty(0, h, 64, dtype=torch.bfloat16, device="cuda") for h in (4, 2))
+    norm = fcg.Norm(randn(gen(1), 64))
+    fcg.fcg_append_norm(c, 0, [], [], kv, kv, norm, q=q, q_norm=norm, q_out=torch.empty_like(q))
+    assert fcg.fcg_cache_export_layout(c, 0, 0)[1] == 0

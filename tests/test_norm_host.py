@@ -172,3 +172,17 @@ def test_a_norm_goes_by_the_weights_of_the_call():
     w.data = torch.zeros(64, 4).T
     with pytest.raises(ValueError):               # elements of a head that are no longer adjacent
         fcg._norm_ref(norm, 1, 4, 64, torch.float32, w.get_device(), "q_norm")
+
+
+def test_append_norm_of_no_tokens_is_no_error():
+    """As fcg_append of none: an empty tensor has no address."""
+    c = fcg.Cache(fcg.model_desc(2, 4, 2, 64, 1e4, "bf16"), 1, 32, flags=fcg.FCG_LAYOUT_ONLY)
+    none = np.zeros(0, dtype=np.int32)
+    for layers, n in ((1, 0), (2, 0), (0, 0), (0, 1)):
+        i = np.zeros(n, dtype=np.int32)
+        for q, k in ((None, None), (V(None), V(None))):
+            args = (c.h, 0, layers, n, fcg._p(i), fcg._p(i), None)
+            fcg._check(fcg._L.fcg_append_norm(*args, ref(N()), ref(N()), ref(q), ref(q), ref(k), ref(k), 0, None))
+    assert fcg.fcg_cache_export_layout(c, 0, 0)[1] == 0
+    refuses(E.FCG_EINVAL, lambda: fcg._check(fcg._L.fcg_append_norm(
+        c.h, 0, 1, 0, fcg._p(none), fcg._p(none), None, ref(N(eps=0.0)), None, None, None, None, None, 0, None)))
