@@ -543,7 +543,9 @@ fcg_status fcg_attend_weights(fcg_cache* cache, int32_t layer, int32_t prefix_se
  * (layers of a src that differ in length; in place with values read from the
  * library, FCG_ALIAS_V; a capture that would map pages or needs a larger
  * workspace), EHOLE (an unwritten position below the length), ENOMEM (pages),
- * ENOMEM of host memory and EHIP (other dst may be left empty). */
+ * ENOMEM of host memory and EHIP (other dst may be left empty; a sequence in
+ * place is squeezed or has the rows and the length that it had, but its weights
+ * may be rewritten then). */
 fcg_status fcg_evict(fcg_cache* cache, int32_t n_items, const int32_t* src, const int32_t* dst, const int32_t* keep,
                      int32_t n_first, int32_t n_recent, const fcg_rope* rope, float* weights, int32_t* kept,
                      void* stream);

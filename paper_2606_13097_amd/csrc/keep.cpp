@@ -196,10 +196,13 @@ fcg_status fcg_evict(fcg_cache* c, int32_t n_items, const int32_t* src, const in
     if (fcg_status st = c->plan.check_evict(n_items, src, dst, keep, &len, &new_pages, &msg)) return fail(st, msg);
     if (n_items == 0) return FCG_OK;
     auto stays = [&](int32_t i) { return std::min(keep[i], len[i]); };
-    auto commit = [&]() {
-      for (int32_t i = 0; i < n_items; ++i)
+    auto cut = [&](int32_t i0, int32_t i1) {  // in place
+      for (int32_t i = i0; i < i1; ++i)
         if (src[i] == dst[i]) c->plan.truncate(dst[i], stays(i));
-        else c->plan.mark_all_layers(dst[i], 0, stays(i));
+    };
+    auto fill_targets = [&]() {
+      for (int32_t i = 0; i < n_items; ++i)
+        if (src[i] != dst[i]) c->plan.mark_all_layers(dst[i], 0, stays(i));
       return FCG_OK;
     };
     auto empty_targets = [&]() {
@@ -209,7 +212,8 @@ fcg_status fcg_evict(fcg_cache* c, int32_t n_items, const int32_t* src, const in
     if (c->layout_only()) {
       empty_targets();
       c->plan.map_pages(new_pages);
-      return commit();
+      cut(0, n_items);
+      return fill_targets();
     }
     OnDevice dev(c->device);
     HIP_TRY(dev.err, "hipSetDevice");
@@ -298,11 +302,13 @@ fcg_status fcg_evict(fcg_cache* c, int32_t n_items, const int32_t* src, const in
                                          table ? far + 1 : 0, s))
           return undo(hip_fail((hipError_t)rc, "eviction launch"));
         table = false;
-        if (!chunks) continue;
-        if (int rc = launch_evict_move(d.dtype, rope && rope->pairs(), in_place == 1, ec, args, (int)chunks, c->view(), half,
-                                       d.n_layers, s))
-          return undo(hip_fail((hipError_t)rc, "eviction launch"));
+        if (chunks)
+          if (int rc = launch_evict_move(d.dtype, rope && rope->pairs(), in_place == 1, ec, args, (int)chunks, c->view(),
+                                         half, d.n_layers, s))
+            return undo(hip_fail((hipError_t)rc, "eviction launch"));
+        // (at once: should a later launch fail, the length goes with the rows)
+        if (in_place) cut(ec.item0, ec.item0 + args.n);
       }
-    return commit();
+    return fill_targets();
   });
 }

@@ -13,6 +13,7 @@ struct Weights {
   int n_items, block;
 };
 inline std::vector<Weights>* weights = nullptr;
+inline std::vector<fcg::EvictItem>* moved = nullptr;  // items whose move was launched
 
 }  // namespace host
 
@@ -39,8 +40,10 @@ int launch_attend_weights(int, const WeightCall& call, const WeightArgs* args, c
 int launch_evict_select(const EvictCall&, const EvictArgs&, const RopeArgs&, int, int, int, int, int, hipStream_t) {
   return host::launch();
 }
-int launch_evict_move(int, bool, bool, const EvictCall&, const EvictArgs&, int, const CacheView&, int, int, hipStream_t) {
-  return host::launch();
+int launch_evict_move(int, bool, bool, const EvictCall&, const EvictArgs& a, int, const CacheView&, int, int, hipStream_t) {
+  if (int rc = host::launch()) return rc;
+  if (host::moved) host::moved->insert(host::moved->end(), a.item, a.item + a.n);
+  return 0;
 }
 int launch_logprobs(int, const LogpArgs&, hipStream_t) { return host::launch(); }
 int launch_logprobs_grad(int, const LogpGradArgs&, hipStream_t) { return host::launch(); }

@@ -1,4 +1,4 @@
-// What sums of attention weight launch, on a machine without a GPU: see the checks of each.
+// What sums of attention weight and evictions launch, on a machine without a GPU: see the checks of each.
 #include "keep_runtime.hpp"
 
 #include <numeric>
@@ -64,11 +64,48 @@ void splits_meet_in_one_launch() {
   }
 }
 
+// An eviction in place of more sequences than a launch takes, each of its HIP calls made to fail
+// in turn: a sequence has its new length if its rows were moved, and its old one if not.
+void failures_in_place() {
+  const int seqs = 150, tokens = 40;
+  for (int n = 0;; ++n) {
+    fcg_cache* c = cache_of(FCG_BF16, 4, 2, 64, seqs, 64, 16, seqs * 4);
+    std::vector<int32_t> seq, pos, all(seqs), keep(seqs);
+    for (int s = 0; s < seqs; ++s) {
+      for (int t = 0; t < tokens; ++t) seq.push_back(s), pos.push_back(t);
+      all[s] = s;
+      keep[s] = s % 7 * 5;  // (0: nothing to move)
+    }
+    CHECK(fcg_append(c, 0, 1, (int)seq.size(), seq.data(), pos.data(), nullptr, nullptr, nullptr, nullptr, nullptr, 0,
+                     nullptr) == FCG_OK, "%s", fcg_last_error());
+    std::vector<float> w((size_t)seqs * 2 * 64);
+    std::vector<fcg::EvictItem> moved;
+    host::moved = &moved;
+    host::fail_hip = n;
+    const fcg_status st = fcg_evict(c, seqs, all.data(), all.data(), keep.data(), 0, 0, nullptr, w.data(), nullptr, nullptr);
+    const bool reached = host::fail_hip < 0;
+    host::fail_hip = -1;
+    host::moved = nullptr;
+    CHECK((st == FCG_OK) == !reached, "call %d: status %d", n, st);
+    std::vector<int> want(seqs, tokens);
+    for (const auto& it : moved) want[it.src] = it.keep;
+    for (int s = 0; s < seqs && failures < 20; ++s)
+      CHECK(c->plan.seq_len(s, 0) == want[s], "call %d: sequence %d of length %d, not %d", n, s, c->plan.seq_len(s, 0), want[s]);
+    fcg_cache_destroy(c);
+    if (!reached) {
+      CHECK((int)moved.size() == seqs, "%zu sequences moved", moved.size());
+      std::printf("eviction in place: %d HIP calls\n", n);
+      return;
+    }
+  }
+}
+
 }  // namespace
 
 int main() {
   std::setvbuf(stdout, nullptr, _IOLBF, 0);
   splits_meet_in_one_launch();
+  failures_in_place();
   if (!failures) std::printf("ok\n");
   return failures ? 1 : 0;
 }
