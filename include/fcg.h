@@ -527,6 +527,10 @@ fcg_status fcg_attend_weights(fcg_cache* cache, int32_t layer, int32_t prefix_se
  *   dst[i] = src[i]: in place; what is behind is forgotten and its pages return.
  *   dst[i] another sequence: emptied first; src[i] stays as it is, and may be
  *   the source of several items.
+ * A prefix that sequences share (fcg_prefix_attend): squeeze it into another
+ * sequence, over which others start.  Those that have positions behind it attend to
+ * it as it was; after an eviction in place they cannot (EHOLE), nor are they whole
+ * sequences that could be squeezed themselves.
  * weights: device fp32 [n_layers][n_seqs][Hkv][max_tokens], contiguous
  * (fcg_attend_weights of each layer): read in row src[i]; row dst[i] receives
  * the kept positions' weights in their new order and zeros after them, to

@@ -149,3 +149,26 @@ def test_evict_refuses_more_heads_than_a_launch_takes(layers, heads, status):
     else:
         fcg.fcg_evict(c, [0], [0], [2], None)
         assert fcg.fcg_cache_export_layout(c, 0, layers - 1)[1] == 2
+
+
+@pytest.mark.parametrize("page", [0, 16])
+def test_a_prefix_squeezed_beside_itself_serves_others(page):
+    """Sequences that run over a prefix go on with it; others start over its squeezed copy.  One with positions behind a
+    prefix is no whole sequence and is refused, and so are those left by a prefix that was squeezed in place."""
+    c = fcg.Cache(fcg.model_desc(2, 4, 2, 64, 1e4, "bf16"), 4, 200, page, 40 if page else 0, fcg.FCG_LAYOUT_ONLY)
+    fcg.fcg_append(c, 0, [0] * 100, range(100), n_layers=2)
+    fcg.fcg_append(c, 0, [1] * 40, range(100, 140), n_layers=2)
+
+    def attend(pre, P, s, p):
+        i = np.array([s, p], dtype=np.int32)
+        fcg._check(fcg._L.fcg_prefix_attend(c.h, 0, pre, P, 1, fcg._p(i[:1]), fcg._p(i[1:]), None, None, None, None))
+
+    attend(0, 100, 1, 139)
+    evict(c, src=[0], dst=[2], keep=[50])
+    attend(0, 100, 1, 139)
+    fcg.fcg_append(c, 0, [3], [50], n_layers=2)
+    attend(2, 50, 3, 50)
+    refuses(E.FCG_EHOLE, evict, c, src=[1], dst=[1], keep=[10])
+    evict(c, src=[0], dst=[0], keep=[50])
+    refuses(E.FCG_EHOLE, attend, 0, 100, 1, 139)
+    refuses(E.FCG_EHOLE, attend, 0, 50, 1, 139)
