@@ -1,6 +1,7 @@
 // What sums of attention weight and evictions launch, on a machine without a GPU: see the checks of each.
 #include "keep_runtime.hpp"
 
+#include <fstream>
 #include <numeric>
 #include <set>
 
@@ -100,10 +101,42 @@ void failures_in_place() {
   }
 }
 
+// The calls of a file, a line each: dtype, query heads, kv heads, head dim, page size, prefix, the own
+// positions of each sequence and the tokens: prints block size, whether the plan goes by value, whether rows are split.
+void plans(const char* file) {
+  std::ifstream in(file);
+  int dtype, hq, hkv, d, page, P, n_own, n;
+  while (in >> dtype >> hq >> hkv >> d >> page >> P >> n_own >> n) {
+    std::vector<int32_t> own(n_own), seq(n), pos(n), rs, rp;
+    for (auto* v : {&own, &seq, &pos})
+      for (int32_t& x : *v) in >> x;
+    int tokens = std::max(P, 1);
+    for (int s = 0; s < n_own; ++s)
+      for (int t = 0; t < own[s]; ++t) rs.push_back(s), rp.push_back(P + t), tokens = std::max(tokens, P + t + 1);
+    for (int t = 0; t < P; ++t) rs.push_back(n_own), rp.push_back(t);
+    fcg_cache* c = cache_of(dtype, hq, hkv, d, n_own + 1, tokens, page, page ? (n_own + 1) * (tokens / 16 + 1) : 0);
+    CHECK(fcg_append(c, 0, 1, (int)rs.size(), rs.data(), rp.data(), nullptr, nullptr, nullptr, nullptr, nullptr, 0,
+                     nullptr) == FCG_OK, "%s", fcg_last_error());
+    std::vector<host::Weights> seen;
+    host::weights = &seen;
+    float y[4] = {};
+    const fcg_tensor q{y, 0, 0, 0};
+    CHECK(fcg_attend_weights(c, 0, n_own, P, n, seq.data(), pos.data(), &q, y, y, 0, nullptr) == FCG_OK, "%s", fcg_last_error());
+    host::weights = nullptr;
+    CHECK(seen.size() == 1, "%zu launches", seen.size());
+    std::printf("plan %d %d %d\n", seen[0].block, (int)seen[0].by_value, seen[0].call.part != nullptr);
+    fcg_cache_destroy(c);
+  }
+}
+
 }  // namespace
 
-int main() {
+int main(int argc, char** argv) {
   std::setvbuf(stdout, nullptr, _IOLBF, 0);
+  if (argc > 1) {
+    plans(argv[1]);
+    return failures ? 1 : 0;
+  }
   splits_meet_in_one_launch();
   failures_in_place();
   if (!failures) std::printf("ok\n");

@@ -1,15 +1,31 @@
-"""Attention weight per cached position on the GPU, for plans that take several launches."""
+"""Attention weight per cached position on the GPU, for plans that take several launches and for blocks of 256 keys."""
 import math
 
 import numpy as np
 import pytest
 import torch
 
+from keeputil import fill_sequence
 from opsutil import cache_memory, randn
 from paper_2606_13097_amd import fcg
-from test_gpu_weights import check
+from test_gpu_weights import check, run_case
 
 pytestmark = pytest.mark.gpu
+
+
+# Calls with blocks of 256 keys (the prefix's positions, own positions and tokens' positions behind the prefix of each
+# sequence; whether the plan goes by value): test_launched_keep.py holds them to that.
+BLOCKS_OF_256 = {
+    # an uploaded plan; a last block of keys of 208, a last tile of 16 rows, own blocks of few keys
+    "list": (2000, [33] + [32] * 15, [list(range(33))] + [list(range(32))] * 15, False),
+    # by value; a last block of 208 keys, tiles that see the prefix and a mask on the own keys
+    "value": (8400, [2, 40] * 30, [[0, 1], [39, 5]] * 30, True),
+    # one sequence, no prefix: tiles before, on and past the edge of each block
+    "causal": (0, [1030], [list(range(1030))], False),
+    # positions twice, tokens that see the prefix only, in any order
+    "mixed": (1999, [300, 7], [list(range(0, 300, 2)) * 3, [-1] * 60 + [6, 3, 3]], False),
+}
+SHAPES_OF_256 = [("bf16", 64, 4, 128), ("bf16", 64, 4, 64), ("f32", 64, 4, 64)]
 
 
 def gen(seed):
@@ -62,4 +78,35 @@ def test_splits_in_more_than_one_launch():
         ref[:singles, 0, 0], ref[singles, 0, :own] = one, long
         attended[:singles, 0, 0] = attended[singles, 0, :own] = True
         check(got, before, ref, own * hq, reach, attended, d, f"queries {seed}")
+    c.close()
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d", SHAPES_OF_256)
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("case", list(BLOCKS_OF_256))
+def test_blocks_of_256_keys_and_full_tiles(dtype, hq, hkv, d, page, case):
+    print(f"[gpu] blocks of 256 keys, {case} {dtype} {d} page {page}", flush=True)
+    P, lens, toks, _ = BLOCKS_OF_256[case]
+    run_case(dtype, hq, hkv, d, page, P, lens, toks, flags=fcg.FCG_ADD if case == "value" else 0, shuffle=case == "mixed")
+
+
+def test_weights_past_32_bits():
+    """Weights of more than 2^31 bytes and a page table of many sequences: the last positions of the last sequence."""
+    print("[gpu] weights past 2^31 bytes", flush=True)
+    hq, hkv, d, T, S = 2, 2, 64, 1 << 20, 258
+    c = fcg.Cache(fcg.model_desc(1, hq, hkv, d, 1e4, "bf16"), S, T, 16, T // 16 + 1)
+    mem = cache_memory(c, "bf16")[0]
+    x = randn(gen(1), T, hkv, d)
+    fill_sequence(c, mem, 0, S - 1, 0, x)
+    q = randn(gen(2), 1, hq, d)
+    z = torch.stack([x[:, h].double() @ q[0, h].double() / math.sqrt(d) for h in range(hkv)])
+    lse = torch.logsumexp(z, -1)
+    w = torch.zeros(S, hkv, T, device="cuda")
+    assert w.numel() * 4 > 1 << 31
+    fcg.fcg_attend_weights(c, 0, 0, 0, [S - 1], [T - 1], q, lse.float()[None], w)
+    torch.cuda.synchronize()
+    reach = max(float((x[:, h].double().abs() @ q[0, h].double().abs()).max()) / math.sqrt(d) for h in range(hkv))
+    attended = torch.ones(1, hkv, T, dtype=torch.bool, device="cuda")
+    check(w[S - 1:], torch.zeros(1, hkv, T, device="cuda"), torch.exp(z - lse[:, None])[None], 1, reach, attended, d, "far weights")
+    assert not bool(w[:S - 1].any())
     c.close()
