@@ -83,3 +83,19 @@ def test_two_tokens_share_a_row(n):
     assert bool(((lp.double() - ref[:, 0]).abs() <= 24 * 2.0 ** -24 * (1 + ref[:, 0].abs())).all())
     assert bool(((ent.double() - H).abs() <= 48 * 2.0 ** -24).all()) and bool((lp <= 0).all())
     assert math.isclose(float(ent[0]), math.log(2), rel_tol=1e-6)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(1, 5), (3, 4099), (2, 131075), (1100, 20011)])
+def test_alternatives_change_no_statistics(dtype, n, V):
+    """A call with alternatives reads a row in other pieces: sums of V / 1024 + 32 terms in another order, each within
+    2^-22 and 3 roundings of differences of at most 64, so ln S within (V / 1024 + 90) 2^-24 of the 64-bit one (the entropy 64
+    times that) on both sides, and roundings of the results."""
+    print(f"[gpu] with and without alternatives {dtype} {n} x {V}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = randn(g, n, V, dtype=dtype, scale=3.0)
+    target = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    a, b = call(x, target, 0), call(x, target, min(20, V))
+    rel = 2 * (V / 1024 + 90) * 2.0 ** -24
+    for i, (p, q) in enumerate(zip(a[:3], b[:3])):
+        assert bool(((p.double() - q.double()).abs() <= rel * (64 if i == 1 else 1) + 2.0 ** -22 * p.abs()).all())
