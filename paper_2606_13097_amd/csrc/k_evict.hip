@@ -7,7 +7,8 @@
 // threshold found 8 to 11 bits at a time by histograms in LDS, then the positions
 // above it, and as many equal to it as are left, lowest first, written in order by counts
 // over waves.  A row of up to 16K positions stays in registers over all of it (block sizes:
-// see the launch); a longer one is read anew in each pass (56 rows of up to 20K: 38 us).  Bound by
+// see the launch); a longer one is read anew in each pass (56 rows of up to 20K: 40 us; twice the
+// weights a thread would still fit the registers, of which 68 are in use).  Bound by
 // its chain of passes, not by the weights it reads (256 rows of 4321: 12 us, 0.4 TB/s; eight
 // copies of each bin, so that adds meet less often: no difference).  More blocks of the launch
 // fill the table of turns: (cos, sin) of every distance, so that the rows that move the same
@@ -24,7 +25,8 @@
 //
 // In place a row only moves down, so a later row never reads what an earlier one wrote; a
 // block takes a layer's and head's keys or values in order, 128 rows a step, and stores a
-// step's rows once all its waves have read theirs.
+// step's rows once all its waves have read theirs: 1111 of 4321 bf16 rows of 32 layers and 8
+// heads 66 us, 4.6 TB/s, bound by that chain of steps, with accesses through the caches.
 #include "fcg_device.hpp"
 #include "kernels.hpp"
 

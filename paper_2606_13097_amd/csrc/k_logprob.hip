@@ -26,11 +26,14 @@
 // read once, with 8 vectors a thread in flight where no alternatives are kept); blocks of 256
 // threads, several to a compute unit, so that one's exponentials (8 cycles each) run beside
 // another's loads (141 us with blocks of 1024).  Few rows the chain of a row: load,
-// reduce, bound, list, partial, second launch (1 row of 128K bf16 with 20 alternatives 7.6 + 4.7
-// us; 64 rows 12.1 + 4.8).
+// reduce, bound, list, partial, second launch (1 row of 128K bf16 with 20 alternatives 7.3 + 4.7
+// us; 64 rows, one chunk a block, 11.9 + 4.8).  Many bf16 rows lie between: as many
+// exponentials in half the bytes (3001 rows of 50021 70 us, 4.3 TB/s; 1501 of 100003 with 20
+// alternatives 95 us, 3.1 TB/s).
 //
 // The gradient reads and writes each logit once and is bound by that: 1501 bf16 rows of 100003,
-// 108 us, 5.6 TB/s (a copy of such a size: 4.9).
+// 108 us, 5.5 TB/s (the fastest copies 6.2).  Times of many rows are of calls one after the other;
+// a profiler's kernel times of the two are 115 and 114 us.
 #include <type_traits>
 
 #include "fcg_device.hpp"

@@ -11,7 +11,7 @@
 //
 // Forward: the blocks of rope_rows.hpp; the D / (2 VEC) lanes that hold a row add up its
 // squares by DPP, so the norm costs no memory round trip and no LDS beside the turn.  Bound by
-// the memory: 4.4K tokens of 32 + 8 bf16 heads of 128, 18.6 us, 4.9 TB/s, as fast as a copy;
+// the memory: 4.4K tokens of 32 + 8 bf16 heads of 128, 18.7 us, 5.1 TB/s (the fastest copies 6.2);
 // one token appended 4.4 us, a launch.
 //
 // Backward: a block takes chunks of 16 to 64 tokens, as many as it holds a row of each, whose
@@ -20,8 +20,9 @@
 // of a wave that hold the same vectors join theirs by lane exchanges, after each head (or, with
 // one weight vector for all, once), into the wave's own sums in LDS: no barrier.  The blocks'
 // partials are added by a second launch in a fixed order: no atomics, so the same call gives
-// the same bits.  4.4K tokens of 16 + 4 fp32 heads: 30 + 4 us, 4.4 TB/s in the first; bound by
-// the memory and, for a quarter of the time, the angles and the joins.
+// the same bits.  4.4K tokens of 16 + 4 fp32 heads: 30 + 4 us, 4.7 TB/s in the first; bound by
+// the memory and, for a quarter of the time, the angles and the joins.  In bf16 every range of
+// heads computes as many angles for half the bytes: 32 + 8 heads 44 + 5 us, 3.1 TB/s.
 #include "rope_rows.hpp"
 
 namespace fcg {

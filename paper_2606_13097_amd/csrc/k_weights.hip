@@ -17,10 +17,11 @@
 // What bounds it: with many rows the issue of instructions.  Of 234K cycles a SIMD, 2048
 // tokens of 32 heads past 6007 shared keys take 99K in the matrix unit and 126K in the
 // others (an exponential for each pair of row and key is 8 cycles, its sum and
-// scale more), and the two hardly overlap though nothing waits between them: 125 us, 825
+// scale more), and the two hardly overlap though nothing waits between them: 127 us a call, 810
 // TFLOP/s of the products.  More keys a block share a row's reads from LDS (KN = 1: 158 us); a
 // third or fourth wave a SIMD does not fit the registers.  With few rows the latency of a block: its
-// keys, two tiles of rows (one token each of 64 sequences past 4321 keys 11.8 us).
+// keys, then its tiles of rows one after the other (one token each of 64 sequences past 4321
+// keys, four tiles in a block of the prefix, one of four rows in a block of own keys: 11.9 us).
 //
 // fp32 caches: the same on 32x32x2 products, four for each 16-byte vector (elements e of
 // the two lanes' vectors together make a product's depth of two; the order of the head's
