@@ -638,6 +638,9 @@ class Norm:
         self._ref = C.byref(self._desc)
         self._lay_out()
 
+    def __reduce__(self):                     # (a copy has a structure of its own)
+        return Norm, (self.weight, self._desc.eps, self._desc.offset)
+
     def _lay_out(self) -> None:
         w, d = self.weight, self._desc
         self._shape, self._strides = (None, None) if w is None else (w.shape, w.stride())

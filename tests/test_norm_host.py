@@ -1,5 +1,7 @@
 """Norms with a rotary turn without a GPU: refusals, workspace sizes, the gradient's formula against differences."""
+import copy
 import ctypes
+import pickle
 
 import numpy as np
 import pytest
@@ -186,3 +188,14 @@ def test_append_norm_of_no_tokens_is_no_error():
     assert fcg.fcg_cache_export_layout(c, 0, 0)[1] == 0
     refuses(E.FCG_EINVAL, lambda: fcg._check(fcg._L.fcg_append_norm(
         c.h, 0, 1, 0, fcg._p(none), fcg._p(none), None, ref(N(eps=0.0)), None, None, None, None, None, 0, None)))
+
+
+def test_copies_of_a_norm_stand_alone():
+    """A model that holds norms can be copied; a copy with other weights leaves the first one's description as it is."""
+    norm = fcg.Norm(torch.zeros(4, 64), 1e-5, 1.0)
+    for twin in (copy.copy(norm), copy.deepcopy(norm), pickle.loads(pickle.dumps(norm))):
+        first = fcg._norm_ref(norm, 1, 4, 64, torch.float32, -1, "q")._obj
+        twin.weight = torch.ones(4, 128)[:, :64]
+        other = fcg._norm_ref(twin, 1, 4, 64, torch.float32, -1, "q")._obj
+        assert (first.weight, first.head) == (norm.weight.data_ptr(), 64)
+        assert (other.weight, other.head, other.eps, other.offset) == (twin.weight.data_ptr(), 128, 1e-5, 1.0)
