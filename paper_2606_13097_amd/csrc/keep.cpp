@@ -53,7 +53,9 @@ void plan_weights(const fcg_model_desc& d, int32_t prefix_seq, int32_t P, int32_
   };
   p->block = weights_most_keys(esize(d.dtype), d.head_dim);
   if (work(p->block) < 8 * kResident) p->block = 128;
-  const int32_t split_rows = (int32_t)std::max<int64_t>(4, (work(p->block) + 2 * kResident - 1) / (2 * kResident)) * 64;
+  // (at most the 2^30 rows that a call has)
+  const int64_t split_tiles = std::max<int64_t>(4, (work(p->block) + 2 * kResident - 1) / (2 * kResident));
+  const int32_t split_rows = (int32_t)std::min<int64_t>(split_tiles, 1 << 24) * 64;
   const int pre = P && n ? 1 : 0;  // the first group is the prefix
   int64_t all = 0;
   for (const WeightGroup& x : groups)

@@ -65,6 +65,36 @@ void splits_meet_in_one_launch() {
   }
 }
 
+// The longest cache and many rows: tiles past blocks of keys are more than 32 bits count.
+void largest_plans() {
+  const int tokens = (1 << 25) - 16, n = 1 << 21;
+  fcg_cache* c = cache_of(FCG_BF16, 16, 1, 64, 2, tokens, 0, 0);
+  std::vector<int32_t> seq(tokens), pos(tokens);
+  std::iota(pos.begin(), pos.end(), 0);
+  CHECK(fcg_append(c, 0, 1, tokens, seq.data(), pos.data(), nullptr, nullptr, nullptr, nullptr, nullptr, 0, nullptr) == FCG_OK,
+        "%s", fcg_last_error());
+  seq.assign(n, 1);  // rows that see the prefix only
+  pos.assign(n, tokens - 1);
+  std::vector<host::Weights> seen;
+  host::weights = &seen;
+  float y[4] = {};
+  const fcg_tensor q{y, 0, 0, 0};
+  CHECK(fcg_attend_weights(c, 0, 0, tokens, n, seq.data(), pos.data(), &q, y, y, 0, nullptr) == FCG_OK, "%s", fcg_last_error());
+  host::weights = nullptr;
+  int64_t rows = 0, keys = 0;
+  for (const auto& l : seen)
+    for (const fcg::WeightItem& it : l.items) {
+      if (failures > 20) break;
+      CHECK(it.n_row > 0 && it.row0 >= 0 && (int64_t)it.row0 + it.n_row <= (int64_t)n * 16, "rows %d + %d", it.row0, it.n_row);
+      CHECK(it.split >= 0 && it.split < it.n_split, "split %d of %d", it.split, it.n_split);
+      rows += it.n_row;
+      if (it.split == 0) keys += it.k1 - it.k0;
+    }
+  const int64_t blocks = seen.empty() ? 0 : (tokens + seen[0].block - 1) / seen[0].block;
+  CHECK(keys == tokens && rows == blocks * n * 16, "%lld keys, %lld rows", (long long)keys, (long long)rows);
+  fcg_cache_destroy(c);
+}
+
 // An eviction in place of more sequences than a launch takes, each of its HIP calls made to fail
 // in turn: a sequence has its new length if its rows were moved, and its old one if not.
 void failures_in_place() {
@@ -138,6 +168,7 @@ int main(int argc, char** argv) {
     return failures ? 1 : 0;
   }
   splits_meet_in_one_launch();
+  largest_plans();
   failures_in_place();
   if (!failures) std::printf("ok\n");
   return failures ? 1 : 0;

@@ -27,7 +27,7 @@ def exe(tmp_path_factory):
 
 
 def run(*command):
-    r = subprocess.run(command, capture_output=True, text=True, timeout=120)
+    r = subprocess.run(command, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "FAILED" not in r.stdout, r.stdout[-4000:] + r.stderr[-1000:]
     return r.stdout
 
